@@ -333,6 +333,91 @@ int sp_stencil2d(const void* in, void* out, int64_t M, int64_t N, float c_center
 int sp_softmax(const void* in, void* out, int64_t M, int64_t N, int32_t mode, int scheme, const sp_params* params,
                void* stream);
 
+/* ---- the linear layers of a language model ----
+ *
+ * Two further forms of "x times the transpose of a weight matrix", beside sp_gemm's bf16 product: in 8-bit integers with a scale
+ * per token and per output channel, and the last layer's product with its softmax cross entropy, whose scores are never
+ * stored.  (The paper has no counterpart; the tile orders and the pipeline are the same.) */
+#define SP_BF16 0
+#define SP_FP32 1
+#define SP_FP16 2
+
+/* Order argument of sp_gemm_i8 and sp_linear_i8: the library chooses the order, and the tile too when tile_m = tile_n = 0. */
+#define SP_ORDER_AUTO (-1)
+
+/* Longest k axis of an 8-bit product: 128 * 128 * K stays below 2^31, so its 32-bit sums are exact. */
+#define SP_I8_MAX_K 131056
+
+/* Rows to 8 bits, one scale per row (symmetric):  scale[m] = max_k |x[m][k]| / 127, rounded to fp32;  q[m][k] = the integer
+ * nearest to x[m][k] / scale[m] (of the exact quotient, halves to even), so that x ~ scale * q.  A row of zeros gets scale 0 and q = 0.
+ * A row that holds an infinity or a NaN gets scale NaN and q = 0: every product with it is NaN.
+ *   x     : DEVICE, M x K row-major, x_dtype SP_BF16, SP_FP32 or SP_FP16, read-only.  Any K.
+ *   q     : DEVICE, M x ceil(K / 16) * 16 int8 row-major; the columns beyond K are written as zeros (they add nothing to a product).
+ *   scale : DEVICE, M fp32.
+ * Asynchronous on `stream`; allocates nothing.  Errors: SP_ERR_INVALID_ARG, SP_ERR_UNSUPPORTED (sizes of 2^31 and beyond),
+ * SP_ERR_ALIGNMENT (q not 16-byte aligned, x or scale not aligned to their elements), SP_ERR_DEVICE, SP_ERR_CUDA. */
+int sp_quantize_i8(const void* x, int32_t x_dtype, int64_t M, int64_t K, int8_t* q, float* scale, void* stream);
+
+/* C[m][n] = a_scale[m] * b_scale[n] * sum_k A[m][k] * B[n][k] under a tile order.  The sum is exact (32-bit integers); it is rounded to fp32,
+ * multiplied by a_scale, then by b_scale, and rounded to C's type.
+ *   A : DEVICE, M x K int8 row-major (tokens; -128 is allowed).   a_scale : DEVICE, M fp32.
+ *   B : DEVICE, N x K int8 row-major (weights, one row per output channel).   b_scale : DEVICE, N fp32.
+ *   C : DEVICE, M x N row-major, params->out_dtype SP_BF16, SP_FP32 or SP_FP16 (params NULL: SP_BF16); must not overlap an input.
+ *   scheme, params : the order of the tile grid, exactly as for sp_tile_map(M, N, tile_m, tile_n, ...), or SP_ORDER_AUTO.  Tiles
+ *       128x128, 128x256, 256x256, or 0,0: the one with the least estimated time.  Of the flags only SP_FLAG_SERPENTINE applies;
+ *       b_layout must be 1.  With SP_ORDER_AUTO, tile 0,0 and at most 128 tokens the call is bound by reading B and takes
+ *       another form: 128 rows of B per block, the k axis split over a cluster of blocks, partial sums joined through distributed
+ *       shared memory.  Every order and form gives the same bits.
+ * K must be a multiple of 16 (pad rows with zeros, as sp_quantize_i8 does) and at most SP_I8_MAX_K; M and N are free (rows of C that do not
+ * start on 16-byte boundaries are written with plain stores).
+ * Caching, first call, stream capture and the status word: as sp_gemm.  Errors: as sp_gemm; SP_ERR_UNSUPPORTED also for
+ * b_layout 0. */
+int sp_gemm_i8(const int8_t* A, const float* a_scale, const int8_t* B, const float* b_scale, void* C, int64_t M, int64_t N, int64_t K,
+               int scheme, const sp_params* params, void* stream);
+
+/* A linear layer on 8-bit weights in one call: x is quantised (sp_quantize_i8) into q and q_scale, which stay with the caller, and
+ * y = sp_gemm_i8(q, q_scale, W, w_scale).  Same results as the two calls; with few tokens the weights are fetched while x is
+ * being quantised.  K is x's own number of columns; q and W have rows of ceil(K / 16) * 16.  Errors: those of the two calls. */
+int sp_linear_i8(const void* x, int32_t x_dtype, int8_t* q, float* q_scale, const int8_t* W, const float* w_scale, void* y, int64_t M, int64_t N,
+                 int64_t K, int scheme, const sp_params* params, void* stream);
+
+/* Softmax cross entropy of a vocabulary product:  z = h . W^T in fp32,  lse[t] = log sum_v exp z[t][v],
+ *   loss[t] = lse[t] - z[t][target[t]],  0 where target[t] = ignore_index.
+ * The T x V scores are never stored: each tile of them is reduced on chip to a maximum and a sum per row.
+ *   h      : DEVICE, T x D row-major, SP_BF16 or SP_FP16 (`dtype`), read-only.
+ *   W      : DEVICE, V x D row-major, same type, read-only.
+ *   target : DEVICE, T int64.  A value that is neither ignore_index nor in [0, V) makes that token's loss NaN.
+ *   lse    : DEVICE, T fp32, written for every token (the gradient call reads it).
+ *   loss   : DEVICE, fp32: T values (SP_REDUCE_NONE), or one: their sum (SP_REDUCE_SUM) or the sum over the number of tokens that are
+ *            not ignored (SP_REDUCE_MEAN; 0 / 0 = NaN when every token is).
+ *   workspace : DEVICE, 16-byte aligned, sp_linear_ce_workspace(T, V, D, 0) bytes, the caller's, free again when the
+ *            call's work on `stream` is done; calls that may overlap need one each.
+ * Scores that are not finite give NaN (minus infinity: probability 0).  D must be a multiple of 8; T and V are free.  Sums are
+ * taken in a fixed order: the same bits every time.  Asynchronous on `stream`; apart from the library's first call on a device it allocates and synchronises
+ * nothing and can be captured.  Errors: SP_ERR_INVALID_ARG (NULL, sizes, reduction, workspace too small),
+ * SP_ERR_UNSUPPORTED (dtype, sizes), SP_ERR_ALIGNMENT, SP_ERR_DEVICE, SP_ERR_CUDA. */
+#define SP_REDUCE_NONE 0
+#define SP_REDUCE_MEAN 1
+#define SP_REDUCE_SUM 2
+int sp_linear_ce(const void* h, const void* W, const int64_t* target, float* lse, float* loss, int64_t T, int64_t V, int64_t D, int32_t dtype,
+                 int64_t ignore_index, int32_t reduction, void* workspace, int64_t workspace_bytes, void* stream);
+
+/* Its gradients:  g[t][v] = c[t] * (exp(z[t][v] - lse[t]) - [v = target[t]]),  dh = g . W,  dW = g^T . h,  with c[t] = 0 where ignored, else
+ * grad_loss[t] (SP_REDUCE_NONE), grad_loss[0] (SP_REDUCE_SUM) or grad_loss[0] / number of tokens not ignored (SP_REDUCE_MEAN).
+ * The scores are made again, the vocabulary in pieces; g is held in h's type (fp16: scaled by a power of two in between), sums in fp32.
+ *   lse       : DEVICE, T fp32, as sp_linear_ce left it.
+ *   grad_loss : DEVICE, fp32, T values or one; NULL: 1.
+ *   dh, dW    : DEVICE, T x D and V x D, same type as h and W, fully overwritten, or NULL: not wanted (at most one of them).
+ *   workspace : DEVICE, sp_linear_ce_workspace(T, V, D, 1) bytes, as above.
+ * A token that is ignored adds exactly nothing, and its row of dh is zero; its row of h must still be finite where dW is wanted.  A target
+ * outside the vocabulary makes the gradients NaN.  Errors as sp_linear_ce. */
+int sp_linear_ce_grad(const void* h, const void* W, const int64_t* target, const float* lse, const float* grad_loss, void* dh, void* dW, int64_t T,
+                      int64_t V, int64_t D, int32_t dtype, int64_t ignore_index, int32_t reduction, void* workspace, int64_t workspace_bytes,
+                      void* stream);
+
+/* Bytes of workspace sp_linear_ce (grad = 0) or sp_linear_ce_grad (grad != 0) needs; -1 on sizes that those refuse.  Host only. */
+int64_t sp_linear_ce_workspace(int64_t T, int64_t V, int64_t D, int32_t grad);
+
 /* A starting configuration for sp_gemm on this hardware: tile shape, order and its parameters for a given problem.
  * The paper arrives at a remap by searching with measurements in the loop; this is the short table that this
  * library's own sweeps on B200 distil to (no counterpart in the paper, and no substitute for measuring: the search

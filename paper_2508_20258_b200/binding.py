@@ -22,6 +22,7 @@ LIB_PATH = os.path.join(_HERE, "libswizzleperf.so")
 OK, ERR_INVALID_ARG, ERR_NOT_BIJECTIVE, ERR_UNSUPPORTED, ERR_ALIGNMENT, ERR_CUDA, ERR_TIMEOUT, ERR_DEVICE = range(8)
 # sp_scheme
 ROW_MAJOR, COL_MAJOR, GROUP_M, GROUP_N, MORTON, HILBERT, XCD, DIE_SPLIT, CUSTOM, HILBERT_RECT = range(10)
+ORDER_AUTO = -1     # gemm_i8, linear_i8: the library chooses
 SCHEME_NAMES = ["row_major", "col_major", "group_m", "group_n", "morton", "hilbert", "xcd", "die_split", "custom", "hilbert_rect"]
 
 
@@ -57,7 +58,8 @@ TRACE_DTYPE = np.dtype([("slot", "<i4"), ("tile", "<i4"), ("smid", "<i4"), ("uni
                         ("mma_wait_acc", "<u4"), ("load_wait_stage", "<u4"), ("epi_wait_acc", "<u4")])
 
 EXPORTS = ["sp_tile_count", "sp_tile_map", "sp_tile_map_device", "sp_gemm", "sp_gemm_trace", "sp_gemm_host",
-           "sp_gemm_noalloc", "sp_transpose", "sp_stencil2d", "sp_softmax", "sp_gemm_units", "sp_streamk_plan", "sp_recommend",
+           "sp_gemm_noalloc", "sp_quantize_i8", "sp_gemm_i8", "sp_linear_i8", "sp_linear_ce", "sp_linear_ce_grad", "sp_linear_ce_workspace",
+           "sp_transpose", "sp_stencil2d", "sp_softmax", "sp_gemm_units", "sp_streamk_plan", "sp_recommend",
            "sp_probe_dispatch", "sp_probe_topology", "sp_probe_l2_capacity", "sp_selftest_timeout", "sp_selftest_pinned_tickets", "sp_get_status", "sp_last_error", "sp_shutdown"]
 
 
@@ -99,6 +101,18 @@ def lib() -> ctypes.CDLL:
         L.sp_stencil2d.argtypes = [vp, vp, i64, i64, ctypes.c_float, ctypes.c_float, ctypes.c_int, pp, vp]
         L.sp_softmax.restype = ctypes.c_int
         L.sp_softmax.argtypes = [vp, vp, i64, i64, i32, ctypes.c_int, pp, vp]
+        L.sp_quantize_i8.restype = ctypes.c_int
+        L.sp_quantize_i8.argtypes = [vp, i32, i64, i64, vp, vp, vp]
+        L.sp_gemm_i8.restype = ctypes.c_int
+        L.sp_gemm_i8.argtypes = [vp, vp, vp, vp, vp, i64, i64, i64, ctypes.c_int, pp, vp]
+        L.sp_linear_i8.restype = ctypes.c_int
+        L.sp_linear_i8.argtypes = [vp, i32, vp, vp, vp, vp, vp, i64, i64, i64, ctypes.c_int, pp, vp]
+        L.sp_linear_ce.restype = ctypes.c_int
+        L.sp_linear_ce.argtypes = [vp, vp, vp, vp, vp, i64, i64, i64, i32, i64, i32, vp, i64, vp]
+        L.sp_linear_ce_grad.restype = ctypes.c_int
+        L.sp_linear_ce_grad.argtypes = [vp, vp, vp, vp, vp, vp, vp, i64, i64, i64, i32, i64, i32, vp, i64, vp]
+        L.sp_linear_ce_workspace.restype = i64
+        L.sp_linear_ce_workspace.argtypes = [i64, i64, i64, i32]
         L.sp_gemm_units.restype = ctypes.c_int
         L.sp_gemm_units.argtypes = [i32, i32, i64]
         L.sp_recommend.restype = ctypes.c_int
@@ -304,6 +318,168 @@ def softmax(x, out, mode: int = SOFTMAX_SINGLE_PASS, scheme: int = ROW_MAJOR, pa
         if not t.is_cuda or not t.is_contiguous():
             raise ValueError("x and out must be contiguous CUDA tensors")
     _check(lib().sp_softmax(x.data_ptr(), out.data_ptr(), M, N, mode, scheme, _pp(params), _stream_handle(stream)))
+
+
+# ---- the linear layers of a language model
+BF16, FP32, FP16 = 0, 1, 2                       # types of sp_quantize_i8, sp_gemm_i8, sp_linear_ce
+REDUCE_NONE, REDUCE_MEAN, REDUCE_SUM = 0, 1, 2
+I8_MAX_K = 131056
+_REDUCE = {"none": REDUCE_NONE, "mean": REDUCE_MEAN, "sum": REDUCE_SUM}
+
+
+def _dtype_code(t, allowed):
+    import torch
+    code = {torch.bfloat16: BF16, torch.float32: FP32, torch.float16: FP16}.get(t.dtype)
+    if code not in allowed:
+        raise ValueError(f"unsupported element type {t.dtype}")
+    return code
+
+
+def _device_tensors(*tensors) -> None:
+    """Contiguous CUDA tensors on the current device: the library launches there."""
+    import torch
+    if not all(t.is_cuda and t.is_contiguous() for t in tensors):
+        raise ValueError("tensors must be contiguous CUDA tensors")
+    here = torch.cuda.current_device()
+    for t in tensors:
+        if t.device.index != here:
+            raise ValueError(f"tensor on {t.device}, but the current device is cuda:{here}")
+
+
+def _vector(t, n: int, dtype, what: str) -> None:
+    if t.dtype != dtype or t.dim() != 1 or t.shape[0] != n:
+        raise ValueError(f"{what} must be a {dtype} vector of {n}")
+
+
+def _matrix_i8(t, rows, cols: int, what: str) -> None:
+    import torch
+    if t.dtype != torch.int8 or t.dim() != 2 or (rows is not None and t.shape[0] != rows) or t.shape[1] != cols:
+        raise ValueError(f"{what} must be an int8 matrix with rows of {cols}")
+
+
+def _i8_params(y, params: Optional[SpParams]) -> SpParams:
+    code = _dtype_code(y, (BF16, FP32, FP16))
+    if params is None:
+        return make_params(out_dtype=code, b_layout=1)
+    if params.out_dtype != code:
+        raise ValueError("params.out_dtype does not say the output's element type")
+    return params
+
+
+def quantize_i8(x, q, scale, stream=None) -> None:
+    """q [M, ceil(K / 16) * 16] int8 and scale [M] fp32 such that x [M, K] ~ scale * q, row by row (asynchronous)."""
+    import torch
+    M, K = x.shape
+    _matrix_i8(q, M, (K + 15) // 16 * 16, "q")
+    _vector(scale, M, torch.float32, "scale")
+    _device_tensors(x, q, scale)
+    _check(lib().sp_quantize_i8(x.data_ptr(), _dtype_code(x, (BF16, FP32, FP16)), M, K, q.data_ptr(), scale.data_ptr(), _stream_handle(stream)))
+
+
+def gemm_i8(A, a_scale, B, b_scale, C, scheme: int = ORDER_AUTO, params: Optional[SpParams] = None, stream=None) -> None:
+    """C [M, N] = a_scale[:, None] * b_scale * (A [M, K] . B [N, K]^T) with exact integer sums (asynchronous).
+    C's element type (bf16, fp16, fp32) is taken from the tensor; ``params`` must agree with it and have b_layout = 1."""
+    import torch
+    M, K = A.shape
+    N = B.shape[0]
+    _matrix_i8(A, M, K, "A")
+    _matrix_i8(B, N, K, "B")
+    _vector(a_scale, M, torch.float32, "a_scale")
+    _vector(b_scale, N, torch.float32, "b_scale")
+    if tuple(C.shape) != (M, N):
+        raise ValueError("shape mismatch")
+    _device_tensors(A, a_scale, B, b_scale, C)
+    p = _i8_params(C, params)
+    _check(lib().sp_gemm_i8(A.data_ptr(), a_scale.data_ptr(), B.data_ptr(), b_scale.data_ptr(), C.data_ptr(), M, N, K, scheme, _pp(p),
+                            _stream_handle(stream)))
+
+
+def linear_i8(x, q, q_scale, W, w_scale, y, scheme: int = ORDER_AUTO, params: Optional[SpParams] = None, stream=None) -> None:
+    """y [M, N] = x [M, K] . (w_scale[:, None] * W [N, ceil(K / 16) * 16])^T with x quantised on the way (asynchronous): what
+    quantize_i8(x, q, q_scale) and gemm_i8(q, q_scale, W, w_scale, y) compute, in one call.  q and q_scale are left filled."""
+    import torch
+    M, K = x.shape
+    N, kp = W.shape[0], (K + 15) // 16 * 16
+    _matrix_i8(q, M, kp, "q")
+    _matrix_i8(W, N, kp, "W")
+    _vector(q_scale, M, torch.float32, "q_scale")
+    _vector(w_scale, N, torch.float32, "w_scale")
+    if tuple(y.shape) != (M, N):
+        raise ValueError("shape mismatch")
+    _device_tensors(x, q, q_scale, W, w_scale, y)
+    p = _i8_params(y, params)
+    _check(lib().sp_linear_i8(x.data_ptr(), _dtype_code(x, (BF16, FP32, FP16)), q.data_ptr(), q_scale.data_ptr(), W.data_ptr(), w_scale.data_ptr(),
+                              y.data_ptr(), M, N, K, scheme, _pp(p), _stream_handle(stream)))
+
+
+def linear_ce_workspace(T: int, V: int, D: int, grad: bool = False) -> int:
+    """Bytes of workspace linear_ce (or, with ``grad``, linear_ce_grad) needs."""
+    n = int(lib().sp_linear_ce_workspace(T, V, D, int(grad)))
+    if n < 0:
+        raise SpError(ERR_INVALID_ARG, "sizes must be positive and below 2^31")
+    return n
+
+
+def _ce_workspace(workspace, need: int, device, stream):
+    """The caller's workspace, or one of torch's allocator's that outlives the work on the stream it is used on."""
+    import torch
+    if workspace is not None:
+        _device_tensors(workspace)
+        return workspace, workspace.numel() * workspace.element_size()
+    buf = torch.empty(need, dtype=torch.uint8, device=device)
+    if stream is not None:
+        handle = _stream_handle(stream)
+        if handle != int(torch.cuda.current_stream().cuda_stream):
+            buf.record_stream(torch.cuda.ExternalStream(handle) if isinstance(stream, int) else stream)
+    return buf, need
+
+
+def _ce_shapes(h, W, target, lse, reduction: str):
+    import torch
+    if h.dim() != 2 or W.dim() != 2 or h.shape[1] != W.shape[1]:
+        raise ValueError("h must be [T, D] and W [V, D]")
+    if h.dtype != W.dtype:
+        raise ValueError("h and W must have the same element type")
+    if reduction not in _REDUCE:
+        raise ValueError(f"unknown reduction {reduction!r}")
+    T, D = h.shape
+    _vector(target, T, torch.int64, "target")
+    _vector(lse, T, torch.float32, "lse")
+    return T, W.shape[0], D, _dtype_code(h, (BF16, FP16))
+
+
+def linear_ce(h, W, target, lse, loss, reduction: str = "mean", ignore_index: int = -100, workspace=None, stream=None) -> None:
+    """Softmax cross entropy of the scores h [T, D] . W [V, D]^T against target [T] (int64), without storing the scores (asynchronous).
+    Fills lse [T] (kept for linear_ce_grad) and loss: [T] for reduction "none", [1] for "mean" (over the tokens that are not
+    ignored) and "sum".  ``workspace``: a CUDA tensor of linear_ce_workspace(T, V, D) bytes, allocated here when not given."""
+    import torch
+    T, V, D, code = _ce_shapes(h, W, target, lse, reduction)
+    _vector(loss, T if reduction == "none" else 1, torch.float32, "loss")
+    _device_tensors(h, W, target, lse, loss)
+    ws, n = _ce_workspace(workspace, linear_ce_workspace(T, V, D), h.device, stream)
+    _check(lib().sp_linear_ce(h.data_ptr(), W.data_ptr(), target.data_ptr(), lse.data_ptr(), loss.data_ptr(), T, V, D, code, ignore_index,
+                              _REDUCE[reduction], ws.data_ptr(), n, _stream_handle(stream)))
+
+
+def linear_ce_grad(h, W, target, lse, grad_loss, dh, dW, reduction: str = "mean", ignore_index: int = -100, workspace=None, stream=None) -> None:
+    """Gradients of linear_ce: dh [T, D] and dW [V, D] (either may be None) for the gradient ``grad_loss`` of the loss ([T] or [1]
+    fp32; None: ones).  ``lse`` as linear_ce left it; ``workspace``: linear_ce_workspace(T, V, D, grad=True) bytes (asynchronous)."""
+    import torch
+    T, V, D, code = _ce_shapes(h, W, target, lse, reduction)
+    tensors = [h, W, target, lse]
+    if grad_loss is not None:
+        _vector(grad_loss, T if reduction == "none" else 1, torch.float32, "grad_loss")
+        tensors.append(grad_loss)
+    for g, like in ((dh, h), (dW, W)):
+        if g is not None:
+            if g.shape != like.shape or g.dtype != like.dtype:
+                raise ValueError("a gradient must have its input's shape and element type")
+            tensors.append(g)
+    _device_tensors(*tensors)
+    ws, n = _ce_workspace(workspace, linear_ce_workspace(T, V, D, True), h.device, stream)
+    ptr = lambda t: None if t is None else t.data_ptr()  # noqa: E731
+    _check(lib().sp_linear_ce_grad(h.data_ptr(), W.data_ptr(), target.data_ptr(), lse.data_ptr(), ptr(grad_loss), ptr(dh), ptr(dW), T, V, D, code,
+                                   ignore_index, _REDUCE[reduction], ws.data_ptr(), n, _stream_handle(stream)))
 
 
 def gemm_units(tile_m: int, tile_n: int, T: int) -> int:

@@ -9,7 +9,8 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libswizzleperf.so")
-SOURCES = ["api.cu", "remap_device.cu", "gemm_sm100.cu", "gemm_noalloc.cu", "probes.cu", "transpose_sm100.cu", "stencil_sm100.cu", "softmax_sm100.cu"]
+SOURCES = ["api.cu", "remap_device.cu", "gemm_sm100.cu", "gemm_noalloc.cu", "probes.cu", "transpose_sm100.cu", "stencil_sm100.cu", "softmax_sm100.cu",
+           "linear_i8_sm100.cu", "linear_ce_sm100.cu"]
 
 
 def _nvcc() -> str:
@@ -34,7 +35,7 @@ def build(force: bool = False, verbose: bool = False) -> str:
     out = LIB
     tmp = out + f".tmp{os.getpid()}"
     cmd = [_nvcc(), "-std=c++17", "-O3", "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo",
-           "-Xcompiler", "-fPIC", "-shared", "-cudart", "static", "-o", tmp]
+           "-Xcompiler", "-fPIC", "-shared", "-cudart", "static", "--threads", "0", "-o", tmp]   # sources in parallel
     if verbose:
         cmd += ["-Xptxas", "-v"]
     cmd += [os.path.join(CSRC, s) for s in SOURCES]

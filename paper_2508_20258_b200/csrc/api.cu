@@ -307,6 +307,20 @@ static int get_table(DeviceState* ds, const Sched& c, const std::vector<int32_t>
   return SP_OK;
 }
 
+int library_state(const Sched* sched, const std::vector<int32_t>& host_perm, cudaStream_t stream, LibraryState* out) {
+  int dev = 0;
+  int rc = current_device(&dev);
+  if (rc != SP_OK) return rc;
+  std::lock_guard<std::mutex> lock(g_mu);
+  DeviceState* ds = device_state(dev);
+  rc = get_status_word(ds);
+  if (rc != SP_OK) return rc;
+  out->status = ds->status;
+  out->perm = nullptr;
+  if (sched != nullptr && sched->use_table) return get_table(ds, *sched, host_perm, sched->scheme == kCustom, stream, &out->perm);
+  return SP_OK;
+}
+
 // Argument checks shared by every GEMM entry point; fills the resolved shape options.
 int validate_gemm_args(const void* A, const void* B, const void* C, int64_t M, int64_t N, int64_t K, const sp_params* params,
                        int* tile_m_out, int* tile_n_out, int* out_f32_out, int* b_nk_out) {

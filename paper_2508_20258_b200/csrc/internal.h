@@ -97,6 +97,19 @@ int launch_gemm(const GemmCall& call);
 // box_rows x 128 bytes and the 128-byte shared-memory swizzle.  `m` is a CUtensorMap.
 int make_map(struct CUtensorMap_st* m, const void* base, int64_t rows, int64_t cols, int box_rows, bool f32);
 int make_map_plain(struct CUtensorMap_st* m, const void* base, int64_t rows, int64_t cols, int box_rows, int box_cols);
+// General forms.  2-D: row-major [rows, cols] of 1-, 2- or 4-byte elements with a row pitch of `ld` elements (a multiple of 16
+// bytes).  3-D: `slices` row-major fp32 matrices one after the other.  Inner extent of a box 128 bytes, 128-byte swizzle.
+int make_map_any(struct CUtensorMap_st* m, const void* base, int elt_bytes, int64_t rows, int64_t cols, int64_t ld, int box_rows, int box_cols);
+int make_map_3d_f32(struct CUtensorMap_st* m, const void* base, int64_t slices, int64_t rows, int64_t cols, int box_rows, int box_cols);
+
+// What the linear-layer entry points need of the library's per-device state: the status word of the bounded waits and, for
+// an order that is read from a table, the device table (sched != nullptr).  Same caching and first-call rules as sp_gemm.
+struct LibraryState {
+  int32_t* status;
+  const int32_t* perm;
+};
+int library_state(const Sched* sched, const std::vector<int32_t>& host_perm, cudaStream_t stream, LibraryState* out);
+
 int launch_stencil(const void* in, void* out, int64_t M, int64_t N, float c_center, float c_neighbor, const Sched& sched,
                    const int32_t* perm_dev, int32_t* status_dev, cudaStream_t stream);
 int launch_transpose(const void* in, void* out, int64_t M, int64_t N, const Sched& sched, const int32_t* perm_dev,

@@ -1,0 +1,627 @@
+// Softmax cross entropy of a vocabulary product without keeping the scores, and its gradients.
+//
+//   z = h . W^T  (T x V),   lse_t = log sum_v exp z_tv,   loss_t = lse_t - z_t,target(t)
+//   g_tv = c_t (exp(z_tv - lse_t) - [v = target(t)]),     dh = g . W,   dW = g^T . h
+//
+// Forward: the product runs tile by tile on the tensor cores; the epilogue reduces each tile's 256 columns of a row to a
+// (maximum, sum of exponentials) pair, so T x V scores become T x V / 256 pairs, which a second kernel joins.
+// Gradient: the vocabulary is walked in pieces.  A piece's scores are made again, turned into g in the epilogue and written as 16 bits;
+// two more products read them: dh += g . W_piece (k = the vocabulary) and dW_piece = g^T . h (k = the tokens).
+#include <math_constants.h>
+
+#include <mutex>
+#include <new>
+#include <vector>
+
+#include "product.cuh"
+
+namespace sp {
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
+constexpr int kCeTile = 256;     // vocabulary columns of one tile
+constexpr int kMaxSplits = 64;   // slices of the vocabulary in the product for dh
+
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+__device__ __forceinline__ void tma_store_3d(const CUtensorMap* map, uint32_t src, int x, int y, int z) {
+  asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.tile.bulk_group [%0, {%1, %2, %3}], [%4];"
+               ::"l"(map), "r"(x), "r"(y), "r"(z), "r"(src) : "memory");
+}
+__device__ __forceinline__ void tma_add_3d(const CUtensorMap* map, uint32_t src, int x, int y, int z) {
+  asm volatile("cp.reduce.async.bulk.tensor.3d.global.shared::cta.add.tile.bulk_group [%0, {%1, %2, %3}], [%4];"
+               ::"l"(map), "r"(x), "r"(y), "r"(z), "r"(src) : "memory");
+}
+
+// ------------------------------------------------------------------ forward: statistics of a tile's rows
+// Per row the running maximum m (in powers of two: m = max z * log2 e, rounded once) and s = sum 2^(z log2 e - m).  Any m serves as
+// long as the joined result uses the same one, so its rounding costs nothing.  64 columns at a time: one rescaling of
+// s per 64 exponentials.
+struct EpiStats {
+  static constexpr uint32_t kBytes = 0;
+  struct Args {
+    float2* stats;            // [tile column][row]
+    float* picked;            // score of the row's target
+    const int64_t* target;
+  };
+  const Args& a;
+  int lane;
+  int rel;                    // the row's target, as a column of this tile; -1: not here
+  __device__ EpiStats(const Args& args, const CUtensorMap*, uint32_t, int, int l) : a(args), lane(l) {}
+  __device__ __forceinline__ void before(const EpiTile& e, int M, int N) {
+    const int row = e.row0 + lane;
+    const int64_t t = row < M ? __ldg(a.target + row) : -1;
+    rel = t >= e.col0 && t < N && t < (int64_t)e.col0 + kCeTile ? (int)(t - e.col0) : -1;
+  }
+  template <int BN>
+  __device__ __forceinline__ void tile(const EpiTile& e, int M, int N) {
+    static_assert(BN == kCeTile, "");
+    float m = -CUDART_INF_F, s = 0.f, hit = 0.f;
+#pragma unroll 1
+    for (int q = 0; q < BN / 64; ++q) {
+      uint32_t v[32], w[32];
+      tmem_ld_32x32b_x32(e.taddr + (uint32_t)(q * 64), v);
+      tmem_ld_32x32b_x32(e.taddr + (uint32_t)(q * 64 + 32), w);
+      tmem_ld_wait();
+      const int col = e.col0 + q * 64;
+      if (col + 64 > N) {     // columns beyond the vocabulary
+#pragma unroll
+        for (int j = 0; j < 32; ++j) {
+          if (col + j >= N) v[j] = 0xff800000u;
+          if (col + 32 + j >= N) w[j] = 0xff800000u;
+        }
+      }
+      if (rel >= q * 64 && rel < q * 64 + 64) {
+#pragma unroll
+        for (int j = 0; j < 32; ++j) {
+          if (rel == q * 64 + j) hit = __uint_as_float(v[j]);
+          if (rel == q * 64 + 32 + j) hit = __uint_as_float(w[j]);
+        }
+      }
+      float top = __uint_as_float(v[0]);
+#pragma unroll
+      for (int j = 0; j < 32; ++j) top = fmaxf(fmaxf(top, __uint_as_float(v[j])), __uint_as_float(w[j]));
+      const float mn = fmaxf(m, top * kLog2e);
+      const float ref = mn == -CUDART_INF_F ? 0.f : mn;    // nothing finite yet: every term is exp2(-inf) = 0
+      float s0 = 0.f, s1 = 0.f, s2 = 0.f, s3 = 0.f;
+#pragma unroll
+      for (int j = 0; j < 32; j += 2) {
+        s0 += ex2(fmaf(__uint_as_float(v[j]), kLog2e, -ref));
+        s1 += ex2(fmaf(__uint_as_float(w[j]), kLog2e, -ref));
+        s2 += ex2(fmaf(__uint_as_float(v[j + 1]), kLog2e, -ref));
+        s3 += ex2(fmaf(__uint_as_float(w[j + 1]), kLog2e, -ref));
+      }
+      s = fmaf(s, ex2(m - ref), (s0 + s1) + (s2 + s3));
+      m = mn;
+    }
+    const int row = e.row0 + lane;
+    if (row < M) {
+      a.stats[(int64_t)e.tn * M + row] = make_float2(m, s);
+      if (rel >= 0) a.picked[row] = hit;
+    }
+  }
+};
+
+struct CeJoin {
+  const float2* stats;
+  const float* picked;
+  const int64_t* target;
+  float* lse;
+  float* each;        // loss per token
+  float* loss;        // the reduced loss (mean, sum), else nullptr
+  int T, V, tiles;
+  int64_t ignore;
+  int mean;
+};
+
+// Mean or sum of the per-token losses in a fixed order, in fp64.  One block.
+__device__ void reduce_losses(const CeJoin& a) {
+  __shared__ double part_s[32];
+  __shared__ int part_n[32];
+  double s = 0;
+  int n = 0;
+  for (int t = threadIdx.x; t < a.T; t += blockDim.x) {
+    s += a.each[t];
+    n += a.target[t] != a.ignore;
+  }
+  for (int o = 16; o; o >>= 1) {
+    s += __shfl_xor_sync(0xffffffffu, s, o);
+    n += __shfl_xor_sync(0xffffffffu, n, o);
+  }
+  if ((threadIdx.x & 31) == 0) { part_s[threadIdx.x >> 5] = s; part_n[threadIdx.x >> 5] = n; }
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    for (int i = 1; i < (int)blockDim.x / 32; ++i) { s += part_s[i]; n += part_n[i]; }
+    a.loss[0] = (float)(a.mean ? s / n : s);     // no token left by the mask: 0 / 0
+  }
+}
+
+// 32 rows per block; eight threads share a row's pairs, then join theirs.
+__global__ void __launch_bounds__(256) ce_join_kernel(const CeJoin a) {
+  pdl_launch_dependents();
+  pdl_wait();
+  __shared__ float2 part[8][33];
+  const int r = threadIdx.x & 31, g = threadIdx.x >> 5, row = blockIdx.x * 32 + r;
+  float m = -CUDART_INF_F, s = 0.f;
+  auto join = [&](float2 p) {
+    const float mn = fmaxf(m, p.x), ref = mn == -CUDART_INF_F ? 0.f : mn;
+    s = s * ex2(m - ref) + p.y * ex2(p.x - ref);
+    m = mn;
+  };
+  if (row < a.T) {
+#pragma unroll 4
+    for (int i = g; i < a.tiles; i += 8) join(__ldg(a.stats + (int64_t)i * a.T + row));
+  }
+  part[g][r] = make_float2(m, s);
+  __syncthreads();
+  if (g == 0 && row < a.T) {
+    for (int i = 1; i < 8; ++i) join(part[i][r]);
+    const float lse = (m + log2f(s)) * kLn2;
+    const int64_t t = a.target[row];
+    a.lse[row] = lse;
+    a.each[row] = t == a.ignore ? 0.f : t >= 0 && t < a.V ? lse - a.picked[row] : CUDART_NAN_F;
+  }
+  if (a.loss != nullptr && gridDim.x == 1) {
+    __syncthreads();
+    reduce_losses(a);
+  }
+}
+
+__global__ void __launch_bounds__(1024) ce_reduce_kernel(const CeJoin a) {
+  pdl_launch_dependents();
+  pdl_wait();
+  reduce_losses(a);
+}
+
+// ------------------------------------------------------------------ gradient
+struct CeCoef {
+  const int64_t* target;
+  const float* grad;     // per token (none) or one number; nullptr: 1
+  float* coef;           // per token
+  float* factor;         // one number
+  int T, V;
+  int64_t ignore;
+  int reduction, fp16;
+};
+
+// What the loss's gradient puts on each token, c_t = factor * coef_t: g is made with coef_t and rounded to 16 bits, the two products
+// multiply by `factor` in fp32.
+//   One number for all tokens (mean, sum): it all goes to `factor`, so that its own rounding does not repeat in every token's
+//   largest entry, p - 1 ~ -1, which 16 bits hold well.
+//   A weight per token (none): coef_t.
+// fp16 reaches down to 2^-24 only, and p ranges down to 1 / V and below: there coef is scaled by a power of two that brings
+// its largest value to [2^14, 2^15] (|g| <= coef stays below 65504), and `factor` by the inverse.  One block.
+__global__ void __launch_bounds__(1024) ce_coef_kernel(const CeCoef a) {
+  pdl_launch_dependents();
+  pdl_wait();
+  __shared__ int part_n[32];
+  __shared__ float part_m[32];
+  int n = 0;
+  float top = 0.f;
+  for (int t = threadIdx.x; t < a.T; t += 1024) {
+    const bool kept = a.target[t] != a.ignore;
+    n += kept;
+    if (kept && a.reduction == SP_REDUCE_NONE && a.grad) top = fmaxf(top, fabsf(a.grad[t]));
+  }
+  for (int o = 16; o; o >>= 1) {
+    n += __shfl_xor_sync(0xffffffffu, n, o);
+    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+  }
+  if ((threadIdx.x & 31) == 0) { part_n[threadIdx.x >> 5] = n; part_m[threadIdx.x >> 5] = top; }
+  __syncthreads();
+  n = 0; top = 0.f;
+  for (int i = 0; i < 32; ++i) { n += part_n[i]; top = fmaxf(top, part_m[i]); }
+  const bool each = a.reduction == SP_REDUCE_NONE && a.grad;
+  float factor = 1.f;
+  if (!each) {
+    factor = a.grad ? a.grad[0] : 1.f;
+    if (a.reduction == SP_REDUCE_MEAN) factor = n > 0 ? factor / (float)n : 0.f;
+    top = 1.f;
+  }
+  // not finite (an overflowed loss scale): onto the tokens that count, so that it does not meet the zeros of the ignored ones
+  const float wild = fabsf(factor) < CUDART_INF_F ? 1.f : factor;
+  if (wild != 1.f) factor = 1.f;
+  int up = 0;
+  if (a.fp16 && top > 0.f && top < CUDART_INF_F) {
+    int e;
+    frexpf(top, &e);                     // top in [2^(e-1), 2^e)
+    up = max(-100, min(100, each ? 15 - e : 15));
+  }
+  const float scale = exp2f((float)up);
+  for (int t = threadIdx.x; t < a.T; t += 1024) {
+    const int64_t y = a.target[t];
+    float c = 0.f;
+    if (y != a.ignore) c = y < 0 || y >= a.V ? CUDART_NAN_F : (each ? a.grad[t] : wild) * scale;
+    a.coef[t] = c;
+  }
+  if (threadIdx.x == 0) *a.factor = factor * exp2f((float)-up);
+}
+
+// g of a tile, to 16 bits: its rounding (half a step, 2^-9 of bf16 or 2^-12 of fp16 relative) is independent from entry to entry and
+// enters sums over the vocabulary or the tokens, so it moves a gradient by less than the gradient's own rounding to the same type.
+struct EpiG {
+  static constexpr uint32_t kBytes = 4 * 2 * 4096;
+  struct Args {
+    const float* lse;
+    const float* coef;
+    const int64_t* target;
+    int64_t v0;              // first column of the piece
+    int bf16;
+  };
+  const Args& a;
+  const CUtensorMap* map;
+  EpiStage stage;
+  int lane, rel;
+  float lse2, c;
+  __device__ EpiG(const Args& args, const CUtensorMap* m, uint32_t base, int w, int l)
+      : a(args), map(m), stage{base + (uint32_t)w * 8192u, 0}, lane(l) {}
+  __device__ __forceinline__ void before(const EpiTile& e, int M, int) {
+    const int row = e.row0 + lane;
+    const bool in = row < M;
+    c = in ? __ldg(a.coef + row) : 0.f;
+    lse2 = in ? __ldg(a.lse + row) * kLog2e : 0.f;
+    const int64_t t = in ? __ldg(a.target + row) - a.v0 - e.col0 : -1;
+    rel = t >= 0 && t < kCeTile ? (int)t : -1;
+  }
+  template <int BN>
+  __device__ __forceinline__ void tile(const EpiTile& e, int M, int N) {
+#pragma unroll 1
+    for (int q = 0; q < BN / 64; ++q) {
+      uint32_t v[32], w[32], p[32];
+      tmem_ld_32x32b_x32(e.taddr + (uint32_t)(q * 64), v);
+      tmem_ld_32x32b_x32(e.taddr + (uint32_t)(q * 64 + 32), w);
+      tmem_ld_wait();
+#pragma unroll
+      for (int j = 0; j < 32; ++j) {
+        v[j] = __float_as_uint(ex2(fmaf(__uint_as_float(v[j]), kLog2e, -lse2)));
+        w[j] = __float_as_uint(ex2(fmaf(__uint_as_float(w[j]), kLog2e, -lse2)));
+      }
+      if (rel >= q * 64 && rel < q * 64 + 64) {
+#pragma unroll
+        for (int j = 0; j < 32; ++j) {
+          if (rel == q * 64 + j) v[j] = __float_as_uint(__uint_as_float(v[j]) - 1.f);
+          if (rel == q * 64 + 32 + j) w[j] = __float_as_uint(__uint_as_float(w[j]) - 1.f);
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < 16; ++j) {
+        p[j] = pack_16(__uint_as_float(v[2 * j]) * c, __uint_as_float(v[2 * j + 1]) * c, a.bf16);
+        p[16 + j] = pack_16(__uint_as_float(w[2 * j]) * c, __uint_as_float(w[2 * j + 1]) * c, a.bf16);
+      }
+      if (c == 0.f) {          // a token that does not count: exactly nothing, whatever its scores are
+#pragma unroll
+        for (int j = 0; j < 32; ++j) p[j] = 0;
+      }
+      const uint32_t slice = stage.next(lane);
+      stage_row(slice, lane, p);
+      fence_async_smem();
+      __syncwarp();
+      if (lane == 0) {
+        const int col = e.col0 + q * 64;
+        if (e.row0 < M && col < N) tma_store_2d(map, slice, col, e.row0);
+        bulk_commit();
+      }
+    }
+  }
+};
+
+// fp32 sums of a slice of the vocabulary: stored by the first piece, added to by the later ones (each element once per piece,
+// in stream order: the same bits every time).
+struct EpiSum {
+  static constexpr uint32_t kBytes = 4 * 2 * 4096;
+  struct Args { int add; };
+  const Args& a;
+  const CUtensorMap* map;
+  EpiStage stage;
+  int lane;
+  __device__ EpiSum(const Args& args, const CUtensorMap* m, uint32_t base, int w, int l)
+      : a(args), map(m), stage{base + (uint32_t)w * 8192u, 0}, lane(l) {}
+  __device__ __forceinline__ void before(const EpiTile&, int, int) {}
+  template <int BN>
+  __device__ __forceinline__ void tile(const EpiTile& e, int M, int N) {
+#pragma unroll 1
+    for (int q = 0; q < BN / 32; ++q) {
+      uint32_t v[32];
+      tmem_ld_32x32b_x32(e.taddr + (uint32_t)(q * 32), v);
+      tmem_ld_wait();
+      const uint32_t slice = stage.next(lane);
+      stage_row(slice, lane, v);
+      fence_async_smem();
+      __syncwarp();
+      if (lane == 0) {
+        const int col = e.col0 + q * 32;
+        if (e.row0 < M && col < N) {
+          if (a.add) tma_add_3d(map, slice, col, e.row0, e.z);
+          else tma_store_3d(map, slice, col, e.row0, e.z);
+        }
+        bulk_commit();
+      }
+    }
+  }
+};
+
+// A finished gradient, to its 16-bit type.
+struct EpiOut16 {
+  static constexpr uint32_t kBytes = 4 * 2 * 4096;
+  struct Args {
+    const float* factor;
+    int bf16;
+  };
+  const Args& a;
+  const CUtensorMap* map;
+  EpiStage stage;
+  int lane;
+  float factor;
+  __device__ EpiOut16(const Args& args, const CUtensorMap* m, uint32_t base, int w, int l)
+      : a(args), map(m), stage{base + (uint32_t)w * 8192u, 0}, lane(l), factor(__ldg(args.factor)) {}
+  __device__ __forceinline__ void before(const EpiTile&, int, int) {}
+  template <int BN>
+  __device__ __forceinline__ void tile(const EpiTile& e, int M, int N) {
+#pragma unroll 1
+    for (int q = 0; q < BN / 64; ++q) {
+      uint32_t v[32], w[32];
+      tmem_ld_32x32b_x32(e.taddr + (uint32_t)(q * 64), v);
+      tmem_ld_32x32b_x32(e.taddr + (uint32_t)(q * 64 + 32), w);
+      tmem_ld_wait();
+#pragma unroll
+      for (int j = 0; j < 16; ++j) v[j] = pack_16(__uint_as_float(v[2 * j]) * factor, __uint_as_float(v[2 * j + 1]) * factor, a.bf16);
+#pragma unroll
+      for (int j = 0; j < 16; ++j) v[16 + j] = pack_16(__uint_as_float(w[2 * j]) * factor, __uint_as_float(w[2 * j + 1]) * factor, a.bf16);
+      const uint32_t slice = stage.next(lane);
+      stage_row(slice, lane, v);
+      fence_async_smem();
+      __syncwarp();
+      if (lane == 0) {
+        const int col = e.col0 + q * 64;
+        if (e.row0 < M && col < N) tma_store_2d(map, slice, col, e.row0);
+        bulk_commit();
+      }
+    }
+  }
+};
+
+// dh from the fp32 sums of its slices, added in slice order.  Four elements per thread (T x D is a multiple of 8).
+__global__ void __launch_bounds__(256) ce_finish_kernel(const float4* acc, int64_t n4, int slices, const float* factor, int bf16, uint2* out) {
+  pdl_launch_dependents();
+  pdl_wait();
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (i >= n4) return;
+  float4 s = __ldcs(acc + i);
+  for (int z = 1; z < slices; ++z) {
+    const float4 p = __ldcs(acc + (int64_t)z * n4 + i);
+    s.x += p.x; s.y += p.y; s.z += p.z; s.w += p.w;
+  }
+  const float f = __ldg(factor);
+  out[i] = make_uint2(pack_16(s.x * f, s.y * f, bf16), pack_16(s.z * f, s.w * f, bf16));
+}
+
+// ------------------------------------------------------------------ host side
+static std::mutex g_ce_mu;   // per-kernel set-up is done under it
+
+static int64_t up256(int64_t b) { return (b + 255) & ~255ll; }
+static int64_t div_up(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+// Everything that follows from the sizes alone.
+struct CePlan {
+  int64_t T, V, D;
+  int tile_m;                 // rows of a token tile: a CTA pair's 256, or 128 where no more tokens are there
+  int64_t tiles;              // vocabulary tiles of the forward product
+  int64_t piece, ld_g;        // gradient: vocabulary rows of a piece, row pitch of g
+  int pieces, slices;         // slices of the vocabulary in the product for dh
+  int64_t off_picked, off_each, forward_bytes;
+  int64_t off_factor, off_g, off_acc, grad_bytes;
+};
+
+static CePlan ce_plan(int64_t T, int64_t V, int64_t D) {
+  CePlan p = {};
+  p.T = T; p.V = V; p.D = D;
+  p.tile_m = T <= 128 ? 128 : 256;
+  p.tiles = div_up(V, kCeTile);
+  p.off_picked = up256(p.tiles * T * 8);
+  p.off_each = p.off_picked + up256(T * 4);
+  p.forward_bytes = p.off_each + up256(T * 4);
+  // g of one piece takes at most 256 MiB: 27 waves of tiles on the whole device, whatever T is
+  constexpr int64_t kEntries = 128ll << 20;
+  p.piece = V;
+  if (T * V > kEntries) {
+    p.piece = kEntries / T / kCeTile * kCeTile;
+    if (p.piece < 4 * kCeTile) p.piece = 4 * kCeTile;
+    if (p.piece > V) p.piece = V;
+  }
+  p.pieces = (int)div_up(V, p.piece);
+  p.ld_g = (p.piece + 7) / 8 * 8;
+  // Few tiles of dh and a long k axis: the vocabulary is cut into slices until every SM has one, each at least 16 stages long.
+  const int64_t out_tiles = div_up(T, p.tile_m) * div_up(D, 256), units = p.tile_m == 256 ? 74 : 148, kb = div_up(p.piece, 64);
+  int64_t s = out_tiles < units ? units / out_tiles : 1;
+  if (s > kb / 16) s = kb / 16;
+  if (s > kMaxSplits) s = kMaxSplits;
+  if (s < 1) s = 1;
+  p.slices = (int)div_up(kb, div_up(kb, s));
+  p.off_factor = up256(T * 4);
+  p.off_g = p.off_factor + 256;
+  p.off_acc = p.off_g + up256(T * p.ld_g * 2);
+  p.grad_bytes = p.off_acc + ((p.pieces > 1 || p.slices > 1) ? up256(p.slices * T * D * 4) : 0);
+  return p;
+}
+
+static int check_ce(const void* h, const void* W, const void* target, const void* lse, int64_t T, int64_t V, int64_t D, int32_t dtype, int32_t reduction,
+                    const void* workspace) {
+  if (!h || !W || !target || !lse || !workspace) { set_error("h, W, target, lse and workspace must not be NULL"); return SP_ERR_INVALID_ARG; }
+  if (T <= 0 || V <= 0 || D <= 0) { set_error("T, V, D must be positive"); return SP_ERR_INVALID_ARG; }
+  if (T >= (1ll << 31) - 512 || V >= (1ll << 31) - 512 || D >= (1ll << 31) - 512) { set_error("dimension too large"); return SP_ERR_UNSUPPORTED; }
+  if (dtype != SP_BF16 && dtype != SP_FP16) { set_error("h and W must both be bf16 or both fp16"); return SP_ERR_UNSUPPORTED; }
+  if (reduction != SP_REDUCE_NONE && reduction != SP_REDUCE_MEAN && reduction != SP_REDUCE_SUM) { set_error("unknown reduction %d", reduction); return SP_ERR_INVALID_ARG; }
+  if ((D % 8) != 0) { set_error("D must be a multiple of 8 (16-byte row pitch)"); return SP_ERR_ALIGNMENT; }
+  if ((((uintptr_t)h | (uintptr_t)W | (uintptr_t)workspace) & 15u) || ((uintptr_t)target & 7u) || ((uintptr_t)lse & 3u)) {
+    set_error("h, W and workspace must be 16-byte aligned, target and lse aligned to their elements");
+    return SP_ERR_ALIGNMENT;
+  }
+  return SP_OK;
+}
+
+// The tile grid of one product in bands of eight tile rows, walked serpentine-wise: a wave of tiles is then about as
+// tall as it is wide, so it needs few operand panels, and a band starts on the panels the last one used last.
+static int ce_sched(int64_t M, int64_t N, int tile_m, Sched* out) {
+  sp_params p = {};
+  p.struct_size = sizeof p;
+  p.group = 8;
+  p.flags = SP_FLAG_SERPENTINE;
+  return resolve_sched(M, N, tile_m, 256, SP_GROUP_M, &p, out);
+}
+
+static ProdArgs ce_args(const Sched& sched, int32_t* status, int64_t M, int64_t N, int64_t K, int slices) {
+  ProdArgs a = {};
+  a.status = status;
+  a.M = (int)M; a.N = (int)N;
+  a.kblocks = (int)div_up(K, 64);
+  a.kb_split = (int)div_up(a.kblocks, slices);
+  a.splits = (int)div_up(a.kblocks, a.kb_split);
+  a.sched = sched;
+  return a;
+}
+
+// h . W_piece^T with an epilogue of scores.
+template <class Epi>
+static int ce_scores(const char* what, const CePlan& p, const void* h, const void* W, int64_t cols, int32_t* status, bool bf16, const CUtensorMap* tmC,
+                     const typename Epi::Args& ea, cudaStream_t stream) {
+  CUtensorMap tmA, tmB;
+  Sched sched;
+  int rc = ce_sched(p.T, cols, p.tile_m, &sched);
+  if (rc == SP_OK) rc = make_map_any(&tmA, h, 2, p.T, p.D, p.D, 128, 64);
+  if (rc == SP_OK) rc = make_map_any(&tmB, W, 2, cols, p.D, p.D, p.tile_m == 256 ? 128 : 256, 64);
+  if (rc != SP_OK) return rc;
+  const ProdArgs a = ce_args(sched, status, p.T, cols, p.D, 1);
+  if (p.tile_m == 256) return launch_product<2, 256, kElem16, false, false, Epi>(what, tmA, tmB, tmC ? *tmC : tmA, a, bf16, ea, stream);
+  return launch_product<1, 256, kElem16, false, false, Epi>(what, tmA, tmB, tmC ? *tmC : tmA, a, bf16, ea, stream);
+}
+
+}  // namespace sp
+
+using namespace sp;
+
+extern "C" {
+
+int64_t sp_linear_ce_workspace(int64_t T, int64_t V, int64_t D, int32_t grad) {
+  if (T <= 0 || V <= 0 || D <= 0 || T >= (1ll << 31) - 512 || V >= (1ll << 31) - 512 || D >= (1ll << 31) - 512) return -1;
+  const CePlan p = ce_plan(T, V, D);
+  return grad ? p.grad_bytes : p.forward_bytes;
+}
+
+int sp_linear_ce(const void* h, const void* W, const int64_t* target, float* lse, float* loss, int64_t T, int64_t V, int64_t D, int32_t dtype,
+                 int64_t ignore_index, int32_t reduction, void* workspace, int64_t workspace_bytes, void* stream) try {
+  int rc = check_ce(h, W, target, lse, T, V, D, dtype, reduction, workspace);
+  if (rc != SP_OK) return rc;
+  if (!loss) { set_error("loss must not be NULL"); return SP_ERR_INVALID_ARG; }
+  if ((uintptr_t)loss & 3u) { set_error("loss must be aligned to its elements"); return SP_ERR_ALIGNMENT; }
+  const CePlan p = ce_plan(T, V, D);
+  if (workspace_bytes < p.forward_bytes) { set_error("workspace of %lld bytes, %lld needed", (long long)workspace_bytes, (long long)p.forward_bytes); return SP_ERR_INVALID_ARG; }
+  int dev = 0;
+  rc = current_device(&dev);
+  if (rc != SP_OK) return rc;
+  std::lock_guard<std::mutex> lock(g_ce_mu);
+  LibraryState st;
+  rc = library_state(nullptr, {}, (cudaStream_t)stream, &st);
+  if (rc != SP_OK) return rc;
+  char* ws = (char*)workspace;
+  const EpiStats::Args ea = {(float2*)ws, (float*)(ws + p.off_picked), target};
+  rc = ce_scores<EpiStats>("vocabulary product", p, h, W, V, st.status, dtype == SP_BF16, nullptr, ea, (cudaStream_t)stream);
+  if (rc != SP_OK) return rc;
+  CeJoin j = {};
+  j.stats = ea.stats; j.picked = ea.picked; j.target = target; j.lse = lse;
+  j.each = reduction == SP_REDUCE_NONE ? loss : (float*)(ws + p.off_each);
+  j.loss = reduction == SP_REDUCE_NONE ? nullptr : loss;
+  j.T = (int)T; j.V = (int)V; j.tiles = (int)p.tiles; j.ignore = ignore_index; j.mean = reduction == SP_REDUCE_MEAN;
+  rc = launch_pdl("join of the row statistics", ce_join_kernel, dim3((unsigned)div_up(T, 32)), 256, 0, 1, (cudaStream_t)stream, j);
+  if (rc == SP_OK && j.loss && T > 32) rc = launch_pdl("sum of the losses", ce_reduce_kernel, dim3(1), 1024, 0, 1, (cudaStream_t)stream, j);
+  return rc;
+} catch (const std::exception& e) {
+  set_error("sp_linear_ce: %s", e.what());
+  return SP_ERR_CUDA;
+}
+
+int sp_linear_ce_grad(const void* h, const void* W, const int64_t* target, const float* lse, const float* grad_loss, void* dh, void* dW, int64_t T,
+                      int64_t V, int64_t D, int32_t dtype, int64_t ignore_index, int32_t reduction, void* workspace, int64_t workspace_bytes,
+                      void* stream_) try {
+  int rc = check_ce(h, W, target, lse, T, V, D, dtype, reduction, workspace);
+  if (rc != SP_OK) return rc;
+  if (!dh && !dW) { set_error("dh and dW must not both be NULL"); return SP_ERR_INVALID_ARG; }
+  if (dh == h || dW == W) { set_error("a gradient must not overlap an input"); return SP_ERR_INVALID_ARG; }
+  if ((((uintptr_t)dh | (uintptr_t)dW) & 15u) || ((uintptr_t)grad_loss & 3u)) { set_error("dh and dW must be 16-byte aligned, grad_loss aligned to its elements"); return SP_ERR_ALIGNMENT; }
+  const CePlan p = ce_plan(T, V, D);
+  if (workspace_bytes < p.grad_bytes) { set_error("workspace of %lld bytes, %lld needed", (long long)workspace_bytes, (long long)p.grad_bytes); return SP_ERR_INVALID_ARG; }
+  int dev = 0;
+  rc = current_device(&dev);
+  if (rc != SP_OK) return rc;
+  cudaStream_t stream = (cudaStream_t)stream_;
+  std::lock_guard<std::mutex> lock(g_ce_mu);
+  LibraryState st;
+  rc = library_state(nullptr, {}, stream, &st);
+  if (rc != SP_OK) return rc;
+  const bool bf16 = dtype == SP_BF16;
+  char* ws = (char*)workspace;
+  float *coef = (float*)ws, *factor = (float*)(ws + p.off_factor), *acc = (float*)(ws + p.off_acc);
+  char* g = ws + p.off_g;
+  const CeCoef cc = {target, grad_loss, coef, factor, (int)T, (int)V, ignore_index, reduction, !bf16};
+  rc = launch_pdl("token coefficients", ce_coef_kernel, dim3(1), 1024, 0, 1, stream, cc);
+  if (rc != SP_OK) return rc;
+  const bool summed = p.pieces > 1 || p.slices > 1;     // dh passes through fp32 sums
+  for (int i = 0; i < p.pieces; ++i) {
+    const int64_t v0 = i * p.piece, cols = V - v0 < p.piece ? V - v0 : p.piece;
+    const char* Wp = (const char*)W + v0 * D * 2;
+    CUtensorMap tmG, tmA, tmB, tmC;
+    rc = make_map_any(&tmG, g, 2, T, cols, p.ld_g, 32, 64);
+    if (rc != SP_OK) return rc;
+    const EpiG::Args ea = {lse, coef, target, v0, bf16};
+    rc = ce_scores<EpiG>("gradient of the scores", p, h, Wp, cols, st.status, bf16, &tmG, ea, stream);
+    if (rc != SP_OK) return rc;
+    if (dh) {
+      Sched sched;
+      rc = ce_sched(T, D, p.tile_m, &sched);
+      if (rc == SP_OK) rc = make_map_any(&tmA, g, 2, T, cols, p.ld_g, 128, 64);
+      if (rc == SP_OK) rc = make_map_any(&tmB, Wp, 2, cols, D, D, 64, 64);
+      if (rc != SP_OK) return rc;
+      const ProdArgs a = ce_args(sched, st.status, T, D, cols, p.slices);
+      if (summed) {
+        rc = make_map_3d_f32(&tmC, acc, p.slices, T, D, 32, 32);
+        if (rc != SP_OK) return rc;
+        const EpiSum::Args es = {i > 0};
+        rc = p.tile_m == 256 ? launch_product<2, 256, kElem16, false, true, EpiSum>("gradient of h", tmA, tmB, tmC, a, bf16, es, stream)
+                             : launch_product<1, 256, kElem16, false, true, EpiSum>("gradient of h", tmA, tmB, tmC, a, bf16, es, stream);
+      } else {
+        rc = make_map_any(&tmC, dh, 2, T, D, D, 32, 64);
+        if (rc != SP_OK) return rc;
+        const EpiOut16::Args eo = {factor, bf16};
+        rc = p.tile_m == 256 ? launch_product<2, 256, kElem16, false, true, EpiOut16>("gradient of h", tmA, tmB, tmC, a, bf16, eo, stream)
+                             : launch_product<1, 256, kElem16, false, true, EpiOut16>("gradient of h", tmA, tmB, tmC, a, bf16, eo, stream);
+      }
+      if (rc != SP_OK) return rc;
+    }
+    if (dW) {
+      Sched sched;
+      rc = ce_sched(cols, D, 256, &sched);
+      if (rc == SP_OK) rc = make_map_any(&tmA, g, 2, T, cols, p.ld_g, 64, 64);
+      if (rc == SP_OK) rc = make_map_any(&tmB, h, 2, T, D, D, 64, 64);
+      if (rc == SP_OK) rc = make_map_any(&tmC, (char*)dW + v0 * D * 2, 2, cols, D, D, 32, 64);
+      if (rc != SP_OK) return rc;
+      const ProdArgs a = ce_args(sched, st.status, cols, D, T, 1);
+      const EpiOut16::Args eo = {factor, bf16};
+      rc = launch_product<2, 256, kElem16, true, true, EpiOut16>("gradient of W", tmA, tmB, tmC, a, bf16, eo, stream);
+      if (rc != SP_OK) return rc;
+    }
+  }
+  if (dh && summed) {
+    const int64_t n4 = T * D / 4;
+    rc = launch_pdl("sum of the slices", ce_finish_kernel, dim3((unsigned)div_up(n4, 256)), 256, 0, 1, stream, (const float4*)acc, n4, p.slices,
+                    (const float*)factor, (int)bf16, (uint2*)dh);
+  }
+  return rc;
+} catch (const std::exception& e) {
+  set_error("sp_linear_ce_grad: %s", e.what());
+  return SP_ERR_CUDA;
+}
+
+}  // extern "C"

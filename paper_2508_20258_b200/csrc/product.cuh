@@ -1,0 +1,374 @@
+// The persistent tcgen05 pipeline of the linear-layer operators: D = A . B^T on tiles of 128*CG x BN, an epilogue of the
+// operator's own on the accumulator while the next tile's products run.
+//
+// Same machine as the bf16 GEMM (TMA producer warp, MMA issuer warp, four epilogue warps, two accumulator buffers in
+// TMEM, mbarriers only, every wait bounded), cut down to what these operators need: a fixed stride through the slots
+// of a tile order, optionally repeated for `splits` slices of the k axis, and an `Epi` type that is handed 32 rows of
+// the accumulator at a time.  Operands are 8-bit integers (kind::i8, exact 32-bit integer sums) or 16-bit floats
+// (kind::f16, fp32 sums); either may be stored with k or with its other axis contiguous (16-bit types only).
+//
+// One stage holds 128 bytes of k per row (one swizzle row): 128 int8 or 64 16-bit elements.  CTA pairs (CG = 2) compute
+// 256 rows per tile; each CTA supplies half of the B columns.
+#pragma once
+#include <cuda.h>
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+
+#include "internal.h"
+#include "ptx.cuh"
+
+namespace sp {
+
+constexpr uint32_t kProdSmemLimit = 232448;  // 227 KiB opt-in maximum per CTA
+constexpr uint32_t kProdBarrierBytes = 1024;
+
+// status word: (role << 8) | which wait
+enum : int { kProdProducer = 0x11, kProdMma = 0x12, kProdEpilogue = 0x13 };
+
+enum : int { kElemI8 = 0, kElem16 = 1 };
+
+template <int CG, int BN, int ELEM, bool A_MN, bool B_MN, uint32_t EPI_BYTES>
+struct ProdCfg {
+  static constexpr int kBK = ELEM == kElemI8 ? 128 : 64;        // elements of k per stage
+  static constexpr int kUmmaK = ELEM == kElemI8 ? 32 : 16;      // elements of k per MMA: 32 bytes
+  static constexpr int kBCols = BN / CG;                        // columns of B one CTA supplies
+  static constexpr uint32_t kABytes = 128 * 128;
+  static constexpr uint32_t kBBytes = kBCols * 128;
+  static constexpr uint32_t kStageBytes = kABytes + kBBytes;
+  static constexpr int kFit = (kProdSmemLimit - kProdBarrierBytes - 1024 - EPI_BYTES) / kStageBytes;
+  static constexpr int kStages = kFit > 8 ? 8 : kFit;
+  static constexpr uint32_t kSmemBytes = kStages * kStageBytes + EPI_BYTES + kProdBarrierBytes + 1024;  // + alignment slack
+  static constexpr int kTmemCols = 2 * BN;                      // two accumulator buffers (a power of two)
+  static constexpr int kThreads = 192;
+};
+
+struct ProdArgs {
+  const int32_t* perm;   // tile table (orders that are not arithmetic), else nullptr
+  int32_t* status;
+  int M, N;              // rows of A, rows of B
+  int kblocks;           // stages that cover k
+  int splits, kb_split;  // slices of k, stages per slice (slice z: [z * kb_split, min(kblocks, (z + 1) * kb_split)))
+  int k_last_first;      // 1: slices are walked from the last to the first (see launch_product's callers)
+  int units;             // CTAs or CTA pairs launched
+  uint32_t idesc;        // instruction descriptor
+  Sched sched;
+};
+
+// Shared-memory operand descriptor: start address, leading / stride byte offsets in 16-byte units, version 1, 128-byte swizzle.
+__device__ __forceinline__ uint64_t prod_desc(uint32_t lbo_bytes, uint32_t sbo_bytes) {
+  return ((uint64_t)((lbo_bytes >> 4) & 0x3FFFu) << 16) | ((uint64_t)((sbo_bytes >> 4) & 0x3FFFu) << 32) | (1ull << 46) | (2ull << 61);
+}
+__device__ __forceinline__ uint64_t prod_desc_at(uint64_t base, uint32_t addr) { return base + (uint64_t)((addr & 0x3FFFFu) >> 4); }
+
+// Instruction descriptors.  kind::i8: D s32, A and B signed 8-bit.  kind::f16: D fp32, A and B both fp16 or both bf16,
+// each k-major or (bit 15 / 16) contiguous along its other axis.
+inline uint32_t idesc_i8(int m, int n) {
+  return (2u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(m >> 4) << 24);
+}
+inline uint32_t idesc_16(int m, int n, bool bf16, bool a_mn, bool b_mn) {
+  const uint32_t t = bf16 ? 1u : 0u;
+  return (1u << 4) | (t << 7) | (t << 10) | ((a_mn ? 1u : 0u) << 15) | ((b_mn ? 1u : 0u) << 16) | ((uint32_t)(n >> 3) << 17) |
+         ((uint32_t)(m >> 4) << 24);
+}
+
+template <int CG, int ELEM>
+__device__ __forceinline__ void prod_mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+  if constexpr (ELEM == kElem16) {
+    umma_bf16<CG>(d, a, b, idesc, accumulate);   // kind::f16: fp16 or bf16 by the instruction descriptor
+  } else if constexpr (CG == 1) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::i8 [%0], %1, %2, %3, p;\n\t}"
+        ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+  } else {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::2.kind::i8 [%0], %1, %2, %3, p;\n\t}"
+        ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+  }
+}
+
+__device__ __forceinline__ void pdl_launch_dependents() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+__device__ __forceinline__ void pdl_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+
+__device__ __forceinline__ uint32_t pack_16(float lo, float hi, bool bf16) {
+  if (bf16) {
+    const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&v);
+  }
+  const __half2 v = __floats2half2_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&v);
+}
+
+// What an epilogue is given: 32 rows of one tile's accumulator.
+struct EpiTile {
+  uint32_t taddr;    // TMEM address of (first of the 32 lanes, first column of the tile)
+  int row0, col0;    // row of lane 0, first column of the tile
+  int tn;            // tile column
+  int z;             // slice of k
+};
+
+// Staging of one epilogue warp: two slices of 32 rows x 128 bytes, used in turn; a slice may be overwritten once the
+// bulk store before last has read it.
+struct EpiStage {
+  uint32_t base;
+  int chunk;
+  __device__ __forceinline__ uint32_t next(int lane) {   // whole warp
+    if (chunk >= 2) {
+      if (lane == 0) bulk_wait_read_1();
+      __syncwarp();
+    }
+    return base + (uint32_t)(chunk++ & 1) * 4096u;
+  }
+};
+
+// 128 bytes of this lane's row into a slice, 128-byte swizzle (16-byte unit j of row r at j ^ (r % 8)): conflict-free,
+// and what a bulk tensor store with that swizzle reads back.
+__device__ __forceinline__ void stage_row(uint32_t slice, int lane, const uint32_t (&v)[32]) {
+  const uint32_t row = slice + (uint32_t)lane * 128u, sw = (uint32_t)lane & 7u;
+#pragma unroll
+  for (uint32_t j = 0; j < 8; ++j) st_shared_16(row + ((j ^ sw) << 4), v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
+}
+
+__device__ __forceinline__ uint32_t ld_shared_32(uint32_t addr) {
+  uint32_t v;
+  asm volatile("ld.shared.b32 %0, [%1];" : "=r"(v) : "r"(addr) : "memory");
+  return v;
+}
+
+// A staged slice to a matrix whose rows a bulk store cannot take (row pitch or address not a multiple of 16 bytes, but whole elements):
+// row by row, each store instruction of the warp on consecutive addresses.
+template <int ELT>
+__device__ __forceinline__ void store_slice_plain(uint32_t slice, int lane, char* out, int64_t ld_bytes, int row0, int col, int M, int N) {
+  __syncwarp();
+  const int rows = min(32, M - row0);
+  for (int r = 0; r < rows; ++r) {
+    const uint32_t w = ld_shared_32(slice + (uint32_t)r * 128u + (((((uint32_t)lane >> 2) ^ ((uint32_t)r & 7u)) << 4) | (((uint32_t)lane & 3u) << 2)));
+    char* p = out + (int64_t)(row0 + r) * ld_bytes;
+    if constexpr (ELT == 4) {
+      if (col + lane < N) *reinterpret_cast<uint32_t*>(p + (int64_t)(col + lane) * 4) = w;
+    } else {
+      const int c = col + 2 * lane;
+      if (c < N) *reinterpret_cast<uint16_t*>(p + (int64_t)c * 2) = (uint16_t)(w & 0xffffu);
+      if (c + 1 < N) *reinterpret_cast<uint16_t*>(p + (int64_t)(c + 1) * 2) = (uint16_t)(w >> 16);
+    }
+  }
+  __syncwarp();
+}
+
+template <int CG, int BN, int ELEM, bool A_MN, bool B_MN, class Epi>
+__global__ void __launch_bounds__(192, 1)
+product_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const __grid_constant__ CUtensorMap tmC,
+               const ProdArgs args, const typename Epi::Args eargs) {
+  using C = ProdCfg<CG, BN, ELEM, A_MN, B_MN, Epi::kBytes>;
+  constexpr int S = C::kStages;
+  static_assert(ELEM == kElem16 || (!A_MN && !B_MN), "8-bit operands are k-major");
+
+  extern __shared__ uint8_t smem_raw[];
+  const uint32_t smem_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+  const uint32_t epi_base = smem_base + S * C::kStageBytes;      // 1024-byte aligned
+  const uint32_t bar_base = epi_base + Epi::kBytes;
+  const uint32_t bar_full = bar_base, bar_empty = bar_base + 8 * S, bar_tfull = bar_base + 16 * S, bar_tempty = bar_tfull + 16;
+  const uint32_t tmem_slot = bar_tempty + 16;
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t rank = CG == 1 ? 0u : cluster_ctarank();
+  const int unit = blockIdx.x / CG;
+  const int T = args.sched.T, Tn = args.sched.Tn, total = T * args.splits;
+
+  pdl_launch_dependents();
+  if (threadIdx.x == 32) { prefetch_tensormap(&tmA); prefetch_tensormap(&tmB); }
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < S; ++i) { mbar_init(bar_full + 8 * i, 1); mbar_init(bar_empty + 8 * i, 1); }
+    for (int i = 0; i < 2; ++i) { mbar_init(bar_tfull + 8 * i, 1); mbar_init(bar_tempty + 8 * i, 4 * CG); }
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 1) {
+    tmem_alloc<CG>(tmem_slot, C::kTmemCols);
+    tmem_relinquish<CG>();
+  }
+  tcgen05_fence_before();
+  unit_sync<CG>();
+  tcgen05_fence_after();
+  const uint32_t tmem_base = ld_shared_32(tmem_slot);
+  pdl_wait();   // set-up may overlap the kernel before this one; global memory is touched only from here on
+
+  auto tile_at = [&](int s, int& tm, int& tn, int& z) {
+    z = s / T;
+    const int o = s - z * T;
+    const int t = args.sched.use_table ? __ldg(args.perm + o) : slot_to_tile(args.sched, o);
+    tm = t / Tn; tn = t - tm * Tn;
+    if (args.k_last_first) z = args.splits - 1 - z;
+  };
+  auto k_range = [&](int z, int& k0, int& k1) {
+    k0 = z * args.kb_split;
+    k1 = min(args.kblocks, k0 + args.kb_split);
+  };
+
+  if (warp == 0) {
+    // ---------------------------------------------------------------- TMA producer
+    int stage = 0;
+    uint32_t phase = 0;
+    bool ok = true;
+    for (int s = unit; s < total && ok; s += args.units) {
+      int tm, tn, z, k0, k1;
+      tile_at(s, tm, tn, z);
+      k_range(z, k0, k1);
+      const int row0 = tm * 128 * CG + (int)rank * 128, col0 = tn * BN + (int)rank * C::kBCols;
+      for (int kb = k0; kb < k1; ++kb) {
+        ok = mbar_wait(bar_empty + 8 * stage, phase ^ 1u, args.status, (kProdProducer << 8) | 1);
+        ok = __all_sync(0xffffffffu, ok);
+        if (!ok) break;
+        const uint32_t full_local = bar_full + 8 * stage;
+        const uint32_t full_leader = CG == 1 ? full_local : mapa(full_local, 0);
+        const uint32_t sa = smem_base + stage * C::kStageBytes, sb = sa + C::kABytes;
+        const int k = kb * C::kBK;
+        if (elect_one()) {
+          if (rank == 0) mbar_arrive_expect_tx(full_local, CG * C::kStageBytes);
+          if constexpr (A_MN) {
+#pragma unroll
+            for (int j = 0; j < 2; ++j) tma_load_2d<CG>(sa + j * 8192, &tmA, row0 + j * 64, k, full_leader);   // boxes of 64 k x 64 rows
+          } else {
+            tma_load_2d<CG>(sa, &tmA, k, row0, full_leader);
+          }
+          if constexpr (B_MN) {
+#pragma unroll
+            for (int j = 0; j < C::kBCols / 64; ++j) tma_load_2d<CG>(sb + j * 8192, &tmB, col0 + j * 64, k, full_leader);
+          } else {
+            tma_load_2d<CG>(sb, &tmB, k, col0, full_leader);
+          }
+        }
+        __syncwarp();
+        if (++stage == S) { stage = 0; phase ^= 1u; }
+      }
+    }
+    // every stage handed out must have been released before this CTA may exit: no commit arrival (or, after a failure,
+    // no copy) is still in flight towards its shared memory
+    for (int i = 0; i < S && ok; ++i) {
+      ok = mbar_wait(bar_empty + 8 * stage, phase ^ 1u, args.status, (kProdProducer << 8) | 2);
+      ok = __all_sync(0xffffffffu, ok);
+      if (++stage == S) { stage = 0; phase ^= 1u; }
+    }
+    if (!ok) {
+      const unsigned long long t0 = globaltimer();
+      while (globaltimer() - t0 < 1000000ull) __nanosleep(1000);   // let copies in flight land
+    }
+    __syncwarp();
+  } else if (warp == 1) {
+    // ---------------------------------------------------------------- MMA issuer (leader CTA only)
+    if (rank == 0) {
+      // k-major: rows of 128 bytes, groups of 8 rows 1024 bytes apart, k advances 32 bytes inside the swizzle row.
+      // Other axis contiguous: a box is 64 k-rows of 128 bytes; groups of 8 k-rows 1024 bytes apart (stride offset), the
+      // next 64 rows of the operand in the next box, 8192 bytes on (leading offset); 16 k are 2048 bytes.
+      const uint64_t da0 = A_MN ? prod_desc(8192, 1024) : prod_desc(16, 1024);
+      const uint64_t db0 = B_MN ? prod_desc(8192, 1024) : prod_desc(16, 1024);
+      constexpr uint32_t ka = A_MN ? 2048 : 32, kb_ = B_MN ? 2048 : 32;
+      int stage = 0;
+      uint32_t phase = 0;
+      int it = 0;
+      bool ok = true;
+      for (int s = unit; s < total && ok; s += args.units, ++it) {
+        int tm, tn, z, k0, k1;
+        tile_at(s, tm, tn, z);
+        k_range(z, k0, k1);
+        const int buf = it & 1;
+        const uint32_t use = (uint32_t)(it >> 1) & 1u;
+        ok = mbar_wait(bar_tempty + 8 * buf, use ^ 1u, args.status, (kProdMma << 8) | 1);
+        ok = __all_sync(0xffffffffu, ok);
+        if (!ok) break;
+        tcgen05_fence_after();
+        const uint32_t d = tmem_base + (uint32_t)(buf * BN);
+        for (int kb = k0; kb < k1; ++kb) {
+          ok = mbar_wait(bar_full + 8 * stage, phase, args.status, (kProdMma << 8) | 2);
+          ok = __all_sync(0xffffffffu, ok);
+          if (!ok) break;
+          tcgen05_fence_after();
+          if (elect_one()) {
+            const uint32_t sa = smem_base + stage * C::kStageBytes, sb = sa + C::kABytes;
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+              prod_mma<CG, ELEM>(d, prod_desc_at(da0, sa + k * ka), prod_desc_at(db0, sb + k * kb_), args.idesc, (uint32_t)(kb > k0 || k != 0));
+            umma_commit<CG>(bar_empty + 8 * stage);
+            if (kb == k1 - 1) umma_commit<CG>(bar_tfull + 8 * buf);
+          }
+          __syncwarp();
+          if (++stage == S) { stage = 0; phase ^= 1u; }
+        }
+      }
+    }
+    __syncwarp();
+  } else {
+    // ---------------------------------------------------------------- epilogue
+    const int quarter = warp & 3;   // TMEM lanes [32 * quarter, 32 * quarter + 32)
+    Epi epi(eargs, &tmC, epi_base, warp - 2, lane);
+    int it = 0;
+    bool ok = true;
+    for (int s = unit; s < total && ok; s += args.units, ++it) {
+      EpiTile e;
+      int tm;
+      tile_at(s, tm, e.tn, e.z);
+      const int buf = it & 1;
+      const uint32_t use = (uint32_t)(it >> 1) & 1u;
+      e.row0 = tm * 128 * CG + (int)rank * 128 + quarter * 32;
+      e.col0 = e.tn * BN;
+      e.taddr = tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(buf * BN);
+      epi.before(e, args.M, args.N);
+      ok = mbar_wait(bar_tfull + 8 * buf, use, args.status, (kProdEpilogue << 8) | 1);
+      ok = __all_sync(0xffffffffu, ok);
+      if (!ok) break;
+      tcgen05_fence_after();
+      epi.template tile<BN>(e, args.M, args.N);
+      tcgen05_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive_cluster(CG == 1 ? bar_tempty + 8 * buf : mapa(bar_tempty + 8 * buf, 0));
+    }
+    if (lane == 0) bulk_wait_all();   // every store of this warp has reached global memory
+    __syncwarp();
+  }
+
+  tcgen05_fence_before();
+  unit_sync<CG>();
+  if (warp == 1) tmem_dealloc<CG>(tmem_base, C::kTmemCols);
+}
+
+// Launch with programmatic stream serialisation: the next kernel's set-up overlaps this one's tail.
+template <class... KArgs, class... Args>
+inline int launch_pdl(const char* what, void (*kern)(KArgs...), dim3 grid, int threads, size_t smem, int cluster, cudaStream_t stream, Args... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3((unsigned)threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = stream;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = (unsigned)cluster; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = cluster > 1 ? 2 : 1;
+  const cudaError_t e = cudaLaunchKernelEx(&cfg, kern, static_cast<KArgs>(args)...);
+  if (e != cudaSuccess) { set_error("launching %s failed: %s", what, cudaGetErrorString(e)); return SP_ERR_CUDA; }
+  return SP_OK;
+}
+
+// Fills args.idesc, args.units and launches one product.  The caller has set M, N, kblocks, splits, kb_split, sched, perm, status.
+template <int CG, int BN, int ELEM, bool A_MN, bool B_MN, class Epi>
+int launch_product(const char* what, const CUtensorMap& tmA, const CUtensorMap& tmB, const CUtensorMap& tmC, ProdArgs args, bool bf16,
+                   const typename Epi::Args& eargs, cudaStream_t stream) {
+  using C = ProdCfg<CG, BN, ELEM, A_MN, B_MN, Epi::kBytes>;
+  auto kern = product_kernel<CG, BN, ELEM, A_MN, B_MN, Epi>;
+  static uint64_t configured = 0;   // per instantiation, one bit per device
+  if (first_use_on_this_device(configured)) {
+    const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)C::kSmemBytes);
+    if (e != cudaSuccess) { configured = 0; set_error("cudaFuncSetAttribute(smem=%u) failed: %s", C::kSmemBytes, cudaGetErrorString(e)); return SP_ERR_CUDA; }
+  }
+  const int64_t work = (int64_t)args.sched.T * args.splits;
+  if (work > 0x3fffffff) { set_error("%s: too many tiles", what); return SP_ERR_UNSUPPORTED; }
+  args.units = gemm_units(128 * CG, BN, work);   // one CTA per SM, or as many CTA pairs as fit: same as sp_gemm's tiles of this shape
+  if (args.units <= 0) { set_error("could not size the grid"); return SP_ERR_CUDA; }
+  args.idesc = ELEM == kElemI8 ? idesc_i8(128 * CG, BN) : idesc_16(128 * CG, BN, bf16, A_MN, B_MN);
+  return launch_pdl(what, kern, dim3((unsigned)(args.units * CG)), C::kThreads, C::kSmemBytes, CG, stream, tmA, tmB, tmC, args, eargs);
+}
+
+}  // namespace sp

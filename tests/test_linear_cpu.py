@@ -1,0 +1,179 @@
+"""The linear-layer operators without a GPU: pins of their oracle, refusals on the host, workspace sizes, argument checks of the binding."""
+
+import ctypes
+import re
+import os
+
+import numpy as np
+import pytest
+
+import paper_2508_20258_b200 as sp
+from paper_2508_20258_b200 import binding
+from oracle import linear as LN
+
+A, B = 0x100000, 0x200000     # never dereferenced: every check below fails on the host first
+
+
+def test_oracle_quantiser_on_values_worked_by_hand():
+    x = np.array([[127.0, -127.0, 0.5, 1.5, 2.5, -0.5, 0.49], [0.0] * 7, [1.0, np.inf, 0, 0, 0, 0, 0], [np.nan, 1.0, 0, 0, 0, 0, 0]])
+    q, s = LN.quantize_i8(x)
+    assert q.shape == (4, 16)
+    assert list(q[0, :7]) == [127, -127, 0, 2, 2, 0, 0] and (q[0, 7:] == 0).all() and s[0] == 1.0      # halves to even
+    assert (q[1:] == 0).all() and s[1] == 0 and np.isnan(s[2]) and np.isnan(s[3])
+
+
+def test_oracle_quantiser_is_within_half_a_step():
+    x = np.random.default_rng(0).standard_normal((50, 33))
+    q, s = LN.quantize_i8(x)
+    assert (np.abs(q[:, :33] * s[:, None].astype(np.float64) - x) <= 0.5 * s[:, None] * (1 + 1e-6)).all()
+    assert (np.abs(q).max(axis=1) == 127).all()
+
+
+def test_oracle_cross_entropy_against_direct_formulas_and_differences():
+    rng = np.random.default_rng(1)
+    h, W = rng.standard_normal((6, 5)), rng.standard_normal((9, 5))
+    t = np.array([0, 8, -100, 3, 3, 1])
+    for red in ("none", "mean", "sum"):
+        grad = rng.uniform(0.5, 2.0, 6) if red == "none" else np.array([1.7])
+        loss, lse, each, kept = LN.linear_ce(h, W, t, red)
+        z = h @ W.T
+        assert np.allclose(lse, np.log(np.exp(z).sum(axis=1)), rtol=1e-13)
+        assert each[2] == 0 and kept.sum() == 5
+        dh, dW, *_ = LN.linear_ce_grad(h, W, t, grad, red)
+        f = lambda hh, ww: float(np.sum(LN.linear_ce(hh, ww, t, red)[0] * grad)) if red == "none" else float(LN.linear_ce(hh, ww, t, red)[0] * grad[0])  # noqa: E731
+        for x, d, first in ((h, dh, True), (W, dW, False)):
+            for i in np.ndindex(x.shape):
+                e = np.zeros_like(x)
+                e[i] = 1e-5
+                num = (f(h + e, W) - f(h - e, W) if first else f(h, W + e) - f(h, W - e)) / 2e-5
+                assert abs(num - d[i]) < 1e-8
+        assert (dh[2] == 0).all()
+
+
+def test_quantize_refusals():
+    q = sp.lib().sp_quantize_i8
+    assert q(None, sp.BF16, 4, 4, B, B, None) == sp.ERR_INVALID_ARG
+    assert q(A, sp.BF16, 4, 4, None, B, None) == sp.ERR_INVALID_ARG
+    assert q(A, sp.BF16, 4, 4, B, None, None) == sp.ERR_INVALID_ARG
+    assert q(A, sp.BF16, 0, 4, B, B, None) == sp.ERR_INVALID_ARG
+    assert q(A, sp.BF16, 4, -1, B, B, None) == sp.ERR_INVALID_ARG
+    assert q(A, 3, 4, 4, B, B, None) == sp.ERR_INVALID_ARG
+    assert q(A, sp.BF16, 1 << 31, 4, B, B, None) == sp.ERR_UNSUPPORTED
+    assert q(A, sp.BF16, 4, 4, B + 8, B, None) == sp.ERR_ALIGNMENT
+    assert q(A + 1, sp.BF16, 4, 4, B, B, None) == sp.ERR_ALIGNMENT
+    assert q(A + 2, sp.FP32, 4, 4, B, B, None) == sp.ERR_ALIGNMENT
+    assert q(A, sp.BF16, 4, 4, B, B + 2, None) == sp.ERR_ALIGNMENT
+    assert sp.last_error() != ""
+
+
+def _gemm(a=A, sa=A, b=A, sb=A, c=B, M=256, N=256, K=256, scheme=sp.ORDER_AUTO, **kw):
+    p = sp.make_params(**{"b_layout": 1, **kw})
+    return sp.lib().sp_gemm_i8(a, sa, b, sb, c, M, N, K, scheme, ctypes.byref(p), None)
+
+
+def test_gemm_i8_refusals():
+    for name in ("a", "sa", "b", "sb", "c"):
+        assert _gemm(**{name: None}) == sp.ERR_INVALID_ARG
+    for name in ("M", "N", "K"):
+        assert _gemm(**{name: 0}) == sp.ERR_INVALID_ARG
+    assert _gemm(K=264) == sp.ERR_ALIGNMENT
+    assert _gemm(a=A + 8) == sp.ERR_ALIGNMENT and _gemm(b=A + 1) == sp.ERR_ALIGNMENT
+    assert _gemm(sa=A + 1) == sp.ERR_ALIGNMENT and _gemm(c=B + 1) == sp.ERR_ALIGNMENT
+    assert _gemm(c=B + 2, out_dtype=sp.FP32) == sp.ERR_ALIGNMENT
+    assert _gemm(K=sp.I8_MAX_K + 16) == sp.ERR_UNSUPPORTED
+    assert _gemm(M=1 << 31) == sp.ERR_UNSUPPORTED
+    assert _gemm(b_layout=0) == sp.ERR_UNSUPPORTED
+    assert _gemm(out_dtype=3) == sp.ERR_INVALID_ARG
+    assert _gemm(tile_m=256, tile_n=512) == sp.ERR_UNSUPPORTED
+    assert _gemm(tile_m=256, tile_n=0) == sp.ERR_UNSUPPORTED
+    assert _gemm(flags=sp.FLAG_STREAM_K) == sp.ERR_INVALID_ARG
+    assert _gemm(scheme=-2) == sp.ERR_INVALID_ARG and _gemm(scheme=sp.GROUP_M, group=0) == sp.ERR_INVALID_ARG
+    assert _gemm(M=256, N=512, scheme=sp.CUSTOM, tile_m=256, tile_n=256, custom_perm=[1, 1]) == sp.ERR_NOT_BIJECTIVE
+    assert _gemm(M=1280, N=512, scheme=sp.XCD, tile_m=256, tile_n=256, num_xcds=4) == sp.ERR_NOT_BIJECTIVE
+    p = sp.make_params(b_layout=1)
+    p.struct_size = 4
+    assert sp.lib().sp_gemm_i8(A, A, A, A, B, 256, 256, 256, 0, ctypes.byref(p), None) == sp.ERR_INVALID_ARG
+
+
+def test_linear_i8_refuses_what_its_two_calls_refuse():
+    f = sp.lib().sp_linear_i8
+    p = sp.make_params(b_layout=1)
+    assert f(None, sp.BF16, A, A, A, A, B, 4, 4, 4, -1, ctypes.byref(p), None) == sp.ERR_INVALID_ARG
+    assert f(A, 7, A, A, A, A, B, 4, 4, 4, -1, ctypes.byref(p), None) == sp.ERR_INVALID_ARG
+    assert f(A, sp.BF16, A, A, None, A, B, 4, 4, 4, -1, ctypes.byref(p), None) == sp.ERR_INVALID_ARG
+    assert f(A, sp.BF16, A, A, A, A, B, 4, 0, 4, -1, ctypes.byref(p), None) == sp.ERR_INVALID_ARG
+    assert f(A, sp.BF16, A, A, A, A, B, 4, 4, sp.I8_MAX_K + 1, -1, ctypes.byref(p), None) == sp.ERR_UNSUPPORTED
+    assert f(A, sp.BF16, A + 4, A, A, A, B, 4, 4, 4, -1, ctypes.byref(p), None) == sp.ERR_ALIGNMENT
+
+
+def _ce(h=A, W=A, t=A, lse=A, loss=B, T=8, V=100, D=64, dtype=sp.BF16, red=1, ws=B, n=1 << 40):
+    return sp.lib().sp_linear_ce(h, W, t, lse, loss, T, V, D, dtype, -100, red, ws, n, None)
+
+
+def _ce_grad(h=A, W=A, t=A, lse=A, g=A, dh=B, dW=B, T=8, V=100, D=64, dtype=sp.BF16, red=1, ws=B, n=1 << 40):
+    return sp.lib().sp_linear_ce_grad(h, W, t, lse, g, dh, dW, T, V, D, dtype, -100, red, ws, n, None)
+
+
+@pytest.mark.parametrize("f", [_ce, _ce_grad])
+def test_linear_ce_refusals(f):
+    for name in ("h", "W", "t", "lse", "ws"):
+        assert f(**{name: None}) == sp.ERR_INVALID_ARG
+    for name in ("T", "V", "D"):
+        assert f(**{name: 0}) == sp.ERR_INVALID_ARG
+        assert f(**{name: (1 << 31)}) == sp.ERR_UNSUPPORTED
+    assert f(D=60) == sp.ERR_ALIGNMENT
+    for name in ("h", "W", "ws"):
+        assert f(**{name: A + 8}) == sp.ERR_ALIGNMENT
+    assert f(t=A + 4) == sp.ERR_ALIGNMENT and f(lse=A + 2) == sp.ERR_ALIGNMENT
+    assert f(dtype=sp.FP32) == sp.ERR_UNSUPPORTED
+    assert f(red=3) == sp.ERR_INVALID_ARG
+    assert f(n=sp.linear_ce_workspace(8, 100, 64, f is _ce_grad) - 1) == sp.ERR_INVALID_ARG
+
+
+def test_linear_ce_refusals_of_one_call():
+    assert _ce(loss=None) == sp.ERR_INVALID_ARG and _ce(loss=B + 2) == sp.ERR_ALIGNMENT
+    assert _ce_grad(dh=None, dW=None) == sp.ERR_INVALID_ARG
+    assert _ce_grad(dh=A) == sp.ERR_INVALID_ARG and _ce_grad(dW=A) == sp.ERR_INVALID_ARG      # in place
+    assert _ce_grad(dh=B + 8) == sp.ERR_ALIGNMENT and _ce_grad(dW=B + 8) == sp.ERR_ALIGNMENT and _ce_grad(g=A + 2) == sp.ERR_ALIGNMENT
+
+
+def test_workspace_is_in_pieces_and_never_holds_the_scores():
+    for T, V, D in [(1, 2, 8), (16, 65536, 4096), (8192, 131072, 4096), (65536, 262144, 1024), (1 << 20, 1000, 64), (100, 1 << 24, 8)]:
+        fwd, grad = sp.linear_ce_workspace(T, V, D), sp.linear_ce_workspace(T, V, D, True)
+        assert 0 < fwd <= T * ((V + 255) // 256 * 8 + 8) + 4096                # a pair per 256 scores
+        sums = 64 * T * D * 4                                                   # at most 64 slices of dh
+        assert 0 < grad <= max(256 << 20, T * 1024 * 2) + T * 20 + sums + 4096
+    L = sp.lib()
+    for bad in [(0, 8, 8), (8, -1, 8), (8, 8, 0), (1 << 31, 8, 8)]:
+        assert L.sp_linear_ce_workspace(*bad, 0) == -1
+        with pytest.raises(sp.SpError):
+            sp.linear_ce_workspace(*bad)
+
+
+def test_binding_checks_its_tensors():
+    torch = pytest.importorskip("torch")
+    x, q, s = torch.zeros(4, 20), torch.zeros(4, 32, dtype=torch.int8), torch.zeros(4)
+    w, y = torch.zeros(8, 32, dtype=torch.int8), torch.zeros(4, 8)
+    ws = torch.zeros(8)
+    for bad in [lambda: sp.quantize_i8(x, q[:, :16].contiguous(), s), lambda: sp.quantize_i8(x, q.int(), s), lambda: sp.quantize_i8(x, q, s.double()),
+                lambda: sp.quantize_i8(x, q, s),                                                   # not on a GPU
+                lambda: sp.linear_i8(x, q, s, w[:, :16].contiguous(), ws, y), lambda: sp.linear_i8(x, q, s, w, s, y),
+                lambda: sp.linear_i8(x, q, s, w, ws, y.t().contiguous()), lambda: sp.linear_i8(x, q, s, w, ws, y),
+                lambda: sp.gemm_i8(q, s, w[:, :16].contiguous(), ws, y), lambda: sp.gemm_i8(q, ws, w, ws, y), lambda: sp.gemm_i8(q, s, w, ws, y)]:
+        with pytest.raises(ValueError):
+            bad()
+    h, W, t, lse, one = torch.zeros(4, 16).bfloat16(), torch.zeros(9, 16).bfloat16(), torch.zeros(4, dtype=torch.int64), torch.zeros(4), torch.zeros(1)
+    for bad in [lambda: sp.linear_ce(h, W.half(), t, lse, one), lambda: sp.linear_ce(h, W[:, :8], t, lse, one), lambda: sp.linear_ce(h, W, t.int(), lse, one),
+                lambda: sp.linear_ce(h, W, t, lse, lse), lambda: sp.linear_ce(h, W, t, lse, one, reduction="none"), lambda: sp.linear_ce(h, W, t, lse, one, reduction="avg"),
+                lambda: sp.linear_ce(h.float(), W.float(), t, lse, one), lambda: sp.linear_ce(h, W, t, lse, one),
+                lambda: sp.linear_ce_grad(h, W, t, lse, lse, h.clone(), None), lambda: sp.linear_ce_grad(h, W, t, lse, one, W, None),
+                lambda: sp.linear_ce_grad(h, W, t, lse, one, h.clone(), W.clone())]:
+        with pytest.raises(ValueError):
+            bad()
+
+
+def test_constants_match_the_header():
+    text = open(os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "include", "swizzleperf.h")).read()
+    defs = {m.group(1): int(m.group(2)) for m in re.finditer(r"#define\s+SP_([A-Z_0-9]+)\s+\(?(-?\d+)\)?", text)}
+    for name in ("BF16", "FP32", "FP16", "ORDER_AUTO", "I8_MAX_K", "REDUCE_NONE", "REDUCE_MEAN", "REDUCE_SUM"):
+        assert defs[name] == getattr(binding, name), name

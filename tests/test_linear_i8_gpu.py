@@ -1,0 +1,271 @@
+"""The 8-bit linear layer against its oracle (quotients in float64, exact integer sums, float32 steps): every result is
+determined to the bit, so every comparison is for equality; a 16-bit output is the float32 result rounded once."""
+
+import numpy as np
+import pytest
+
+import paper_2508_20258_b200 as sp
+from oracle import linear as LN
+
+pytestmark = pytest.mark.gpu
+torch = pytest.importorskip("torch")
+
+BITS = {"bf16": torch.bfloat16, "fp16": torch.float16, "fp32": torch.float32}
+GUARD = 97
+
+
+def quantize(x):
+    """sp.quantize_i8 of a CUDA tensor, its neighbours checked."""
+    M, K = x.shape
+    kp = (K + 15) // 16 * 16
+    qb = torch.full((M * kp + 64,), GUARD, dtype=torch.int8, device="cuda")
+    sb = torch.full((M + 8,), float(GUARD), device="cuda")
+    q, s = qb[:M * kp].view(M, kp), sb[:M]
+    sp.quantize_i8(x, q, s)
+    assert sp.get_status() == 0
+    assert (qb[M * kp:] == GUARD).all() and (sb[M:] == GUARD).all()      # what lies behind is left as it was
+    return q.cpu().numpy(), s.cpu().numpy()
+
+
+def same(a, b):
+    return np.array_equal(np.asarray(a), np.asarray(b), equal_nan=True)
+
+
+def product(q, s, w, ws, out, **kw):
+    M, N = q.shape[0], w.shape[0]
+    buf = torch.full((M * N + 64,), float(GUARD), dtype=BITS[out], device="cuda")
+    y = buf[:M * N].view(M, N)
+    sp.gemm_i8(q, s, w, ws, y, **kw)
+    assert sp.get_status() == 0
+    assert (buf[M * N:] == GUARD).all()
+    return y
+
+
+def operands(M, N, K, seed, low=-128):
+    rng = np.random.default_rng(seed)
+    q, w = rng.integers(low, 128, (M, K), dtype=np.int8), rng.integers(low, 128, (N, K), dtype=np.int8)
+    s, ws = rng.uniform(0.01, 0.1, M).astype(np.float32), rng.uniform(0.001, 0.01, N).astype(np.float32)
+    return q, s, w, ws, [torch.from_numpy(v).cuda() for v in (q, s, w, ws)]
+
+
+def rounded(y32, out):
+    return torch.from_numpy(np.ascontiguousarray(y32)).to(BITS[out]).float().numpy()
+
+
+# one element, one vector, rows of one warp and of one block, both re-reading limits and just beyond, odd row pitches
+@pytest.mark.parametrize("M,K", [(1, 1), (1, 8), (3, 15), (9, 17), (5, 1000), (8, 1024), (7, 1025), (3, 2035), (2, 8192), (2, 8193), (1, 20011), (70, 64), (1, 40000)])
+@pytest.mark.parametrize("dtype", ["bf16", "fp16", "fp32"])
+def test_quantizer(M, K, dtype):
+    rng = np.random.default_rng(M * 31 + K)
+    x = torch.from_numpy((rng.standard_normal((M, K)) * 3).astype(np.float32)).to(BITS[dtype])
+    q, s = quantize(x.cuda())
+    rq, rs = LN.quantize_i8(x.double().numpy())
+    assert same(s, rs) and same(q, rq)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16", "fp32"])
+def test_quantizer_decides_halves_by_the_exact_quotient(dtype):
+    # rows whose scale is a power of two (quotients that are exact halves), and rows whose scale is not, with values laid as near to
+    # a half of it as the type allows
+    rows = []
+    for top in (127.0, 254.0, 63.5, 100.0, 77.0, 1.0, 3.140625):
+        scale = float(np.float32(top / 127))
+        halves = (np.arange(-126, 127) + 0.5) * scale
+        near = torch.tensor(halves).to(BITS[dtype])
+        up, down = (torch.nextafter(near, torch.tensor(sign * 1e30 if dtype != "fp16" else sign * 6e4).to(BITS[dtype])) for sign in (1, -1))
+        v = torch.cat([near, up, down]).double()
+        v[v.abs() > top] = 0
+        rows.append(torch.cat([v, torch.tensor([top], dtype=torch.float64)]))
+    x = torch.stack(rows).to(BITS[dtype])
+    q, s = quantize(x.cuda())
+    rq, rs = LN.quantize_i8(x.double().numpy())
+    assert same(s, rs) and same(q, rq)
+    assert (np.abs(np.mod(x.double().numpy() / rs[:, None].astype(np.float64), 1.0) - 0.5) == 0).any()     # there were exact halves
+
+
+@pytest.mark.parametrize("M,K", [(12, 40), (12, 9000)])
+def test_quantizer_on_rows_of_zeros_extremes_and_what_is_not_finite(M, K):
+    x = torch.randn(M, K, generator=torch.Generator().manual_seed(3))
+    x[0] = 0
+    x[1] = -0.0
+    x[2, 5] = float("inf")
+    x[3, K - 1] = float("nan")
+    x[4] *= 3e38 / x[4].abs().max()
+    x[5] *= 1e-39                                    # the row's maximum and its scale are denormal numbers
+    x[6] = 0
+    x[6, 7] = 1e-45                                  # smallest number of all: the scale rounds to zero
+    x[7] = 1e-43
+    x[8, 0] = -float("inf")
+    x[9] *= 1e-36
+    x[10] = 0
+    x[10, 3] = -5.0
+    q, s = quantize(x.cuda())
+    rq, rs = LN.quantize_i8(x.double().numpy())
+    assert same(s, rs) and same(q, rq)
+    assert np.isnan(s[[2, 3, 8]]).all() and (q[[2, 3, 8]] == 0).all() and (q[[0, 1, 6]] == 0).all()
+
+
+def test_quantizer_reads_rows_at_any_address():
+    base = torch.randn(8 * 72 + 8, generator=torch.Generator().manual_seed(1)).bfloat16().cuda()
+    for shift in (1, 3, 8):
+        x = base[shift:shift + 8 * 72].view(8, 72)
+        q, s = quantize(x)
+        rq, rs = LN.quantize_i8(x.double().cpu().numpy())
+        assert same(s, rs) and same(q, rq)
+
+
+# tokens: both sides of each few-token width; N: one channel, edges of 128-row blocks, odd; K: one stage, edges, several slices
+@pytest.mark.parametrize("M,N,K", [(1, 1, 16), (1, 128, 128), (1, 129, 2048), (2, 4096, 4096), (16, 200, 1040), (17, 1000, 528), (33, 77, 4096), (64, 640, 4112),
+                                   (65, 300, 1024), (128, 257, 8192), (128, 20000, 256)])
+@pytest.mark.parametrize("out", ["bf16", "fp16", "fp32"])
+def test_few_tokens(M, N, K, out):
+    q, s, w, ws, dev = operands(M, N, K, M + N + K)
+    assert same(product(*dev, out).float().cpu().numpy(), rounded(LN.gemm_i8(q, s, w, ws), out))
+
+
+# ragged both ways; rows of C that no bulk store can take (odd N); K of less than a stage; more tiles than units
+@pytest.mark.parametrize("M,N,K", [(129, 128, 128), (130, 1, 16), (256, 256, 272), (300, 301, 1040), (1000, 504, 96), (513, 2050, 400), (2600, 3001, 128)])
+@pytest.mark.parametrize("out", ["bf16", "fp16", "fp32"])
+@pytest.mark.parametrize("tile", [(0, 0), (128, 128), (128, 256), (256, 256)])
+def test_tiles(M, N, K, out, tile):
+    q, s, w, ws, dev = operands(M, N, K, M + N + K)
+    code = {"bf16": sp.BF16, "fp16": sp.FP16, "fp32": sp.FP32}[out]
+    p = sp.make_params(tile_m=tile[0], tile_n=tile[1], out_dtype=code, b_layout=1)
+    assert same(product(*dev, out, params=p).float().cpu().numpy(), rounded(LN.gemm_i8(q, s, w, ws), out))
+
+
+def test_every_order_gives_the_same_bits():
+    M, N, K = 700, 1300, 320
+    q, s, w, ws, dev = operands(M, N, K, 5)
+    ref = rounded(LN.gemm_i8(q, s, w, ws), "bf16")
+    perm = np.random.default_rng(1).permutation(3 * 6).astype(np.int32)
+    for scheme, kw in [(sp.ROW_MAJOR, {}), (sp.COL_MAJOR, {}), (sp.GROUP_M, dict(group=2)), (sp.GROUP_N, dict(group=3, flags=sp.FLAG_SERPENTINE)), (sp.MORTON, {}),
+                       (sp.HILBERT, {}), (sp.HILBERT_RECT, {}), (sp.XCD, dict(num_xcds=8, xcd_balanced=1)), (sp.DIE_SPLIT, dict(inner_scheme=sp.ROW_MAJOR)),
+                       (sp.CUSTOM, dict(custom_perm=perm))]:
+        p = sp.make_params(tile_m=256, tile_n=256, b_layout=1, **kw)
+        assert same(product(*dev, "bf16", scheme=scheme, params=p).float().cpu().numpy(), ref), scheme
+    # few tokens under an explicit order take the tiled form: the same bits as the few-token form
+    few = [dev[0][:50].contiguous(), dev[1][:50].contiguous(), dev[2], dev[3]]
+    assert torch.equal(product(*few, "fp32"), product(*few, "fp32", scheme=sp.ROW_MAJOR))
+
+
+def test_longest_sum_is_exact():
+    K = sp.I8_MAX_K
+    q, w = torch.full((130, K), -128, dtype=torch.int8, device="cuda"), torch.full((3, K), -128, dtype=torch.int8, device="cuda")
+    w[1] = 127
+    one = torch.ones(130, device="cuda")
+    want = torch.tensor([16384.0 * K, -16256.0 * K, 16384.0 * K], dtype=torch.float64).float().cuda()
+    for rows in (130, 5):      # tiles, few tokens
+        y = product(q[:rows].contiguous(), one[:rows].contiguous(), w, one[:3].contiguous(), "fp32")
+        assert (y == want).all()
+
+
+def test_scales_that_would_leave_the_range_together():
+    q, s, w, ws, dev = operands(140, 140, 64, 9)
+    s[:], ws[:] = 1e-30, 1e-12          # 1e-42 is a denormal number: the factors go on one after the other
+    s[3], ws[4] = np.nan, 0.0
+    dev[1], dev[3] = torch.from_numpy(s).cuda(), torch.from_numpy(ws).cuda()
+    ref = LN.gemm_i8(q, s, w, ws)
+    assert same(product(*dev, "fp32").cpu().numpy(), ref)
+    assert same(product(dev[0][:9].contiguous(), dev[1][:9].contiguous(), dev[2], dev[3], "fp32").cpu().numpy(), ref[:9])
+
+
+@pytest.mark.parametrize("M", [1, 40, 200])
+@pytest.mark.parametrize("dtype,out", [("bf16", "bf16"), ("fp16", "fp32"), ("fp32", "fp16")])
+def test_linear_is_its_two_calls(M, dtype, out):
+    N, K = 333, 1003
+    rng = np.random.default_rng(M)
+    x = torch.from_numpy(rng.standard_normal((M, K)).astype(np.float32)).to(BITS[dtype]).cuda()
+    x[M // 2, 3] = float("nan") if M > 1 else 1.0
+    w = np.zeros((N, 1008), np.int8)
+    w[:, :K] = rng.integers(-127, 128, (N, K))
+    ws = rng.uniform(0.001, 0.01, N).astype(np.float32)
+    q, s = torch.empty(M, 1008, dtype=torch.int8, device="cuda"), torch.empty(M, device="cuda")
+    y = torch.empty(M, N, dtype=BITS[out], device="cuda")
+    sp.linear_i8(x, q, s, torch.from_numpy(w).cuda(), torch.from_numpy(ws).cuda(), y)
+    assert sp.get_status() == 0
+    rq, rs = LN.quantize_i8(x.double().cpu().numpy())
+    assert same(q.cpu().numpy(), rq) and same(s.cpu().numpy(), rs)
+    ref = rounded(LN.gemm_i8(rq, rs, w, ws), out)
+    assert same(y.float().cpu().numpy(), ref)
+    assert np.isnan(ref[M // 2]).all() == (M > 1) and np.isfinite(np.delete(ref, M // 2, 0)).all()
+
+
+def test_weights_written_just_before_the_call_are_the_ones_used():
+    # the few-token form fetches weights while x is being quantised: they may still have been written by the kernel before the call
+    M, N, K = 4, 8192, 4096
+    g = torch.Generator(device="cuda").manual_seed(0)
+    x = torch.randn(M, K, device="cuda", generator=g).bfloat16()
+    ws = torch.ones(N, device="cuda")
+    q, s, w = torch.empty(M, K, dtype=torch.int8, device="cuda"), torch.empty(M, device="cuda"), torch.empty(N, K, dtype=torch.int8, device="cuda")
+    sources = [torch.randint(-127, 128, (N, K), device="cuda", generator=g, dtype=torch.int32).to(torch.int8) for _ in range(4)]
+    ys = [torch.empty(M, N, device="cuda") for _ in range(16)]
+    for i, y in enumerate(ys):
+        w.copy_(sources[i % 4])
+        sp.linear_i8(x, q, s, w, ws, y)
+    assert sp.get_status() == 0
+    for i, y in enumerate(ys):
+        ref = (q.double() @ sources[i % 4].double().t()).float() * s[:, None]
+        assert torch.equal(y, ref)
+
+
+@pytest.mark.parametrize("M", [3, 300])
+def test_captured_and_replayed_on_new_inputs(M):
+    N, K = 512, 1024
+    g = torch.Generator(device="cuda").manual_seed(1)
+    w = torch.randint(-127, 128, (N, K), device="cuda", generator=g, dtype=torch.int32).to(torch.int8)
+    ws = torch.ones(N, device="cuda")
+    x = torch.randn(M, K, device="cuda", generator=g).bfloat16()
+    q, s, y = torch.empty(M, K, dtype=torch.int8, device="cuda"), torch.empty(M, device="cuda"), torch.empty(M, N, device="cuda")
+    sp.linear_i8(x, q, s, w, ws, y)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        sp.linear_i8(x, q, s, w, ws, y)
+    for seed in range(3):
+        x.copy_(torch.randn(M, K, generator=torch.Generator().manual_seed(seed)).bfloat16())
+        y.fill_(float("nan"))
+        graph.replay()
+        torch.cuda.synchronize()
+        q2, s2, y2 = torch.empty_like(q), torch.empty_like(s), torch.empty_like(y)
+        sp.linear_i8(x, q2, s2, w, ws, y2)
+        assert torch.equal(y, y2) and torch.equal(q, q2)
+    assert sp.get_status() == 0
+
+
+def test_calls_on_two_streams_at_once():
+    a, b = operands(5, 3000, 2048, 1), operands(600, 700, 512, 2)
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    torch.cuda.synchronize()
+    ys = [torch.empty(5, 3000, device="cuda"), torch.empty(600, 700, device="cuda")]
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for (_, _, _, _, dev), y, st in zip((a, b), ys, streams):
+            sp.gemm_i8(*dev, y, stream=st)
+    for st in streams:
+        assert sp.get_status(st) == 0
+    for (q, s, w, ws, _), y in zip((a, b), ys):
+        assert same(y.cpu().numpy(), LN.gemm_i8(q, s, w, ws))
+
+
+def test_offsets_beyond_32_bits():
+    # quantiser: 2.2e9 elements; product: 2.2e9 results, once through bulk stores and once row by row (odd N)
+    M, K = 70000, 32000
+    x = torch.ones(M, K, dtype=torch.bfloat16, device="cuda")
+    x[-1] = torch.arange(K, device="cuda") % 120
+    q, s = torch.empty(M, K, dtype=torch.int8, device="cuda"), torch.empty(M, device="cuda")
+    sp.quantize_i8(x, q, s)
+    assert sp.get_status() == 0
+    rq, rs = LN.quantize_i8(x[-2:].double().cpu().numpy())
+    assert same(q[-2:].cpu().numpy(), rq) and same(s[-2:].cpu().numpy(), rs) and bool((q[:-1] == 127).all())
+    del x, q
+    for N in (32768, 32767):
+        M = 66000
+        rng = np.random.default_rng(N)
+        a, w = rng.integers(-9, 10, (M, 16), dtype=np.int8), rng.integers(-9, 10, (N, 16), dtype=np.int8)
+        one = torch.ones(M, device="cuda")
+        y = torch.empty(M, N, dtype=torch.bfloat16, device="cuda")
+        sp.gemm_i8(torch.from_numpy(a).cuda(), one, torch.from_numpy(w).cuda(), one[:N].contiguous(), y)
+        assert sp.get_status() == 0
+        rows = np.r_[0:3, M // 2, M - 300:M]
+        assert same(y[torch.from_numpy(rows).cuda()].float().cpu().numpy(), rounded(LN.gemm_i8(a[rows], np.ones(len(rows)), w, np.ones(N)), "bf16"))
+        del y
