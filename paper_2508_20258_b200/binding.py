@@ -171,7 +171,7 @@ def _pp(params: Optional[SpParams]):
 def _stream_handle(stream) -> int:
     if stream is None:
         import torch
-        return int(torch.cuda.current_stream().cuda_stream)
+        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())   # the current stream's handle, without building a Stream
     if isinstance(stream, int):
         return stream
     return int(stream.cuda_stream)
@@ -338,11 +338,12 @@ def _dtype_code(t, allowed):
 def _device_tensors(*tensors) -> None:
     """Contiguous CUDA tensors on the current device: the library launches there."""
     import torch
-    if not all(t.is_cuda and t.is_contiguous() for t in tensors):
-        raise ValueError("tensors must be contiguous CUDA tensors")
+    for t in tensors:
+        if not t.is_cuda or not t.is_contiguous():
+            raise ValueError("tensors must be contiguous CUDA tensors")
     here = torch.cuda.current_device()
     for t in tensors:
-        if t.device.index != here:
+        if t.get_device() != here:
             raise ValueError(f"tensor on {t.device}, but the current device is cuda:{here}")
 
 
@@ -357,10 +358,15 @@ def _matrix_i8(t, rows, cols: int, what: str) -> None:
         raise ValueError(f"{what} must be an int8 matrix with rows of {cols}")
 
 
+_I8_DEFAULTS: dict = {}      # the parameters of a call that leaves tile and order to the library, per output type
+
+
 def _i8_params(y, params: Optional[SpParams]) -> SpParams:
     code = _dtype_code(y, (BF16, FP32, FP16))
     if params is None:
-        return make_params(out_dtype=code, b_layout=1)
+        if code not in _I8_DEFAULTS:
+            _I8_DEFAULTS[code] = make_params(out_dtype=code, b_layout=1)
+        return _I8_DEFAULTS[code]
     if params.out_dtype != code:
         raise ValueError("params.out_dtype does not say the output's element type")
     return params
@@ -429,7 +435,7 @@ def _ce_workspace(workspace, need: int, device, stream):
     buf = torch.empty(need, dtype=torch.uint8, device=device)
     if stream is not None:
         handle = _stream_handle(stream)
-        if handle != int(torch.cuda.current_stream().cuda_stream):
+        if handle != _stream_handle(None):
             buf.record_stream(torch.cuda.ExternalStream(handle) if isinstance(stream, int) else stream)
     return buf, need
 

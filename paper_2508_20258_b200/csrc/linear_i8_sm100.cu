@@ -2,6 +2,7 @@
 // 32-bit integer sums on the tensor cores, scaled per row (token) and per column (output channel) on the way out.
 #include <new>
 #include <mutex>
+#include <type_traits>
 #include <vector>
 
 #include "product.cuh"
@@ -11,112 +12,184 @@ namespace sp {
 // ------------------------------------------------------------------ quantiser
 // scale = max|x| / 127 (rounded once to fp32), q = the integer nearest to x / scale, halves to even.
 //
-// A quotient taken in fp32 can land on the wrong side of a half.  So the cheap product with 1 / scale decides only where
-// it is clear (its error is below 2^-16 for |q| <= 127); within 2^-12 of a half the remainder x - q * scale decides.  That
-// remainder is exact in fp32: near a half, x and q * scale are multiples of ulp(scale) / 2 and differ by about scale / 2.
+// A quotient taken in fp32 can land on the wrong side of a half.  So the product with 1 / scale decides only where it is clear; next to a
+// half the remainder x - q * scale decides, which is exact in fp32 there: x and q * scale are multiples of ulp(scale) / 2
+// and differ by about scale / 2.
 //
-// Bound: one read of x, one write of q; each thread keeps its vectors of the row in registers between the two passes.
+// Bound: one read of x, one write of q; each thread keeps its vectors of the row in registers, as they were read, between the two
+// passes.  What it has to be careful with is instructions: 67 million elements at 18 each take longer than their bytes.
 constexpr int kQuantThreads = 256;
 constexpr int kQuantVecs = 4;        // vectors of 8 elements a thread holds
 
-template <class T> __device__ __forceinline__ float quant_to_float(T v);
-template <> __device__ __forceinline__ float quant_to_float(__nv_bfloat16 v) { return __bfloat162float(v); }
-template <> __device__ __forceinline__ float quant_to_float(__half v) { return __half2float(v); }
-template <> __device__ __forceinline__ float quant_to_float(float v) { return v; }
-
-// Elements [c, c + 8) of a row; columns at or beyond `cols` read as zero.  `vec`: rows start on 16-byte boundaries.
+// Eight elements of a row as they lie in memory, their largest |x| as bits, and their values.
 template <class T>
-__device__ __forceinline__ void quant_load(const T* row, int64_t c, int64_t cols, bool vec, float (&v)[8]) {
-  if (vec && c + 8 <= cols) {
-    constexpr int kWords = (int)sizeof(T) * 8 / 16;
-    __align__(16) T e[8];
+struct Vec8 {
+  uint4 w[sizeof(T) / 2];
+  __device__ __forceinline__ void load(const T* p) {      // 16-byte aligned
 #pragma unroll
-    for (int i = 0; i < kWords; ++i) reinterpret_cast<uint4*>(e)[i] = __ldg(reinterpret_cast<const uint4*>(row + c) + i);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = quant_to_float(e[i]);
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = c + i < cols ? quant_to_float(row[c + i]) : 0.f;
+    for (int i = 0; i < (int)sizeof(T) / 2; ++i) w[i] = __ldg(reinterpret_cast<const uint4*>(p) + i);
   }
+  __device__ __forceinline__ void load_some(const T* p, int n) {      // any address; elements from n on are zero
+    uint32_t* u = reinterpret_cast<uint32_t*>(w);
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) u[i] = i < n ? __ldg(reinterpret_cast<const uint32_t*>(p) + i) : 0u;
+    } else {
+      const uint16_t* h = reinterpret_cast<const uint16_t*>(p);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) u[i] = (2 * i < n ? (uint32_t)__ldg(h + 2 * i) : 0u) | (2 * i + 1 < n ? (uint32_t)__ldg(h + 2 * i + 1) << 16 : 0u);
+    }
+  }
+  // Bits of |x| order like the values, infinities and NaN above all; 16-bit elements are compared in pairs.
+  __device__ __forceinline__ uint32_t larger(uint32_t top) const {
+    const uint32_t* u = reinterpret_cast<const uint32_t*>(w);
+#pragma unroll
+    for (int i = 0; i < (int)sizeof(T) * 2; i += 2) {
+      if constexpr (sizeof(T) == 4) top = __vimax3_u32(top, u[i] & 0x7fffffffu, u[i + 1] & 0x7fffffffu);
+      else top = __vimax3_u16x2(top, u[i] & 0x7fff7fffu, u[i + 1] & 0x7fff7fffu);
+    }
+    return top;
+  }
+  __device__ __forceinline__ void values(float (&v)[8]) const {
+    const uint32_t* u = reinterpret_cast<const uint32_t*>(w);
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(u[i]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if constexpr (std::is_same<T, __half>::value) {
+          const float2 f = __half22float2(*reinterpret_cast<const __half2*>(u + i));
+          v[2 * i] = f.x; v[2 * i + 1] = f.y;
+        } else {
+          v[2 * i] = __uint_as_float(u[i] << 16); v[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u);
+        }
+      }
+    }
+  }
+};
+
+// The row's largest |x| as a float from the bits above.
+template <class T>
+__device__ __forceinline__ float quant_top(uint32_t bits) {
+  if constexpr (sizeof(T) == 4) return __uint_as_float(bits);
+  const uint32_t b = max(bits & 0xffffu, bits >> 16);
+  if constexpr (std::is_same<T, __half>::value) return __half2float(__ushort_as_half((unsigned short)b));
+  return __uint_as_float(b << 16);
 }
 
-__device__ __forceinline__ int quant_one(float x, float s, float inv, bool divide) {
-  const float y = divide ? __fdiv_rn(x, s) : x * inv;
-  float q = rintf(y);
-  const float f = fabsf(y - q);
-  if (f > 0.5f - 0x1p-12f) {
-    const float r = fmaf(-q, s, x), two = 2.f * fabsf(r);
-    if (two > s || (two == s && (((int)q) & 1))) q += r > 0.f ? 1.f : -1.f;
+struct QuantScale {
+  float s, inv;
+  bool zero;      // all q are zero: a row of zeros, or one that is not finite
+  __device__ __forceinline__ explicit QuantScale(float top) {
+    const bool bad = !(top <= 3.402823466e38f);
+    s = bad ? __uint_as_float(0x7fffffffu) : __fdiv_rn(top, 127.f);
+    zero = bad || s == 0.f;
+    inv = s > 0x1p-100f && s < 0x1p100f ? 1.f / s : 0.f;    // 0: 1 / s may not be a normal number
   }
-  return (int)fminf(fmaxf(q, -127.f), 127.f);
+};
+
+// Eight elements to 8 bits.  z = x / s + 384.5 lies in [257, 512), where fp32 has 15 bits behind the point: bits 15 to 22 of z are
+// floor(x / s + 1/2) + 128, and z is off by less than its last bit, so that floor is right unless all 15 bits are zero.  Those
+// elements (exact halves among them, which coarse types meet often: 0.7 % of bf16 normal numbers) are decided by the
+// remainder.  No conversion instruction, of which an SM does few per clock.
+__device__ __forceinline__ uint2 quant_pack(const float (&v)[8], const QuantScale& k) {
+  uint32_t z[8], low = 0xffffffffu;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) z[e] = __float_as_uint(fmaf(v[e], k.inv, 384.5f)) << 1;      // integer in byte 2, fraction in the low half
+#pragma unroll
+  for (int e = 0; e < 8; e += 4) low = __vimin3_u16x2(low, __byte_perm(z[e], z[e + 1], 0x5410), __byte_perm(z[e + 2], z[e + 3], 0x5410));
+  if ((low & 0xffffu) == 0 || (low >> 16) == 0) {
+    const float h = 0.5f * k.s;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      // x / s is within 2^-15 of n - 1/2: n, or n - 1 where the remainder says so, or on a tie where n is odd
+      const float n = __uint_as_float((z[e] >> 1) & 0xffff8000u | 0x43800000u) - 384.f;
+      const float r = fmaf(-n, k.s, v[e]);
+      if ((z[e] & 0xffffu) == 0 && (r < -h || (r == -h && (z[e] & 0x10000u)))) z[e] -= 0x10000u;
+    }
+  }
+  return make_uint2(__byte_perm(__byte_perm(z[0], z[1], 0x0062), __byte_perm(z[2], z[3], 0x0062), 0x5410) ^ 0x80808080u,
+                    __byte_perm(__byte_perm(z[4], z[5], 0x0062), __byte_perm(z[6], z[7], 0x0062), 0x5410) ^ 0x80808080u);
+}
+
+// One element of a row whose scale has no normal inverse.
+static __device__ __noinline__ int8_t quant_by_remainder(float x, float s) {
+  float n = fminf(fmaxf(rintf(__fdiv_rn(x, s)), -127.f), 127.f);
+  const float r = fmaf(-n, s, x), two = 2.f * fabsf(r);
+  if (two > s || (two == s && ((int)n & 1))) n += r > 0.f ? 1.f : -1.f;
+  return (int8_t)(int)fminf(fmaxf(n, -127.f), 127.f);
+}
+
+// Elements [c, c + 8) of such a row.
+template <class T>
+__device__ __forceinline__ void quant_extreme(const T* row, int64_t c, int64_t cols, float s, int8_t* q) {
+#pragma unroll 1
+  for (int e = 0; e < 8; ++e, ++c) q[c] = c < cols ? quant_by_remainder((float)row[c], s) : (int8_t)0;
 }
 
 // TPR threads share a row (32: eight rows per block; 256: one).
 template <class T, int TPR>
-__global__ void __launch_bounds__(kQuantThreads) quantize_kernel(const T* x, int rows, int64_t cols, int64_t kp, int8_t* q, float* scale) {
+__global__ void __launch_bounds__(kQuantThreads, sizeof(T) == 2 ? 5 : 4) quantize_kernel(const T* x, int rows, int64_t cols, int64_t kp, int8_t* q, float* scale) {
   pdl_wait();
   // Only now may the next kernel start: one that reads nothing of this kernel before its own wait then finds everything
   // before this kernel complete (the few-token product fetches weights that early).
   pdl_launch_dependents();
   constexpr int kRows = kQuantThreads / TPR;
   const int t = threadIdx.x % TPR;
-  const int row = blockIdx.x * kRows + threadIdx.x / TPR;
+  const int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / TPR;
   const bool live = row < rows;
-  const T* xr = x + (int64_t)(live ? row : 0) * cols;
-  const bool vec = (((uintptr_t)x | (uintptr_t)(cols * (int64_t)sizeof(T))) & 15u) == 0;
-  const int64_t nvec = kp / 8;
-  float v[kQuantVecs][8];
-  uint32_t top = 0;      // |x| as bits: orders like the values, infinities and NaN above all
+  const T* xr = x + (live ? row : 0) * cols;
+  const int nvec = live ? (int)(kp / 8) : 0;
+  const int nfull = (((uintptr_t)x | (uintptr_t)(cols * (int64_t)sizeof(T))) & 15u) == 0 ? (int)(cols / 8) : 0;   // vectors read whole
+  auto load = [&](int j, Vec8<T>& w) {
+    if (j < nfull) w.load(xr + (int64_t)j * 8);
+    else w.load_some(xr + (int64_t)j * 8, (int)min((int64_t)8, max((int64_t)0, cols - (int64_t)j * 8)));
+  };
+  Vec8<T> v[kQuantVecs];
+  uint32_t top = 0;
 #pragma unroll
-  for (int i = 0; i < kQuantVecs; ++i) {
-    const int64_t j = t + (int64_t)i * TPR;
-    if (j < nvec) {
-      quant_load(xr, j * 8, cols, vec, v[i]);
+  for (int i = 0; i < kQuantVecs; ++i)
+    if (t + i * TPR < nvec) load(t + i * TPR, v[i]);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(v[i][e]) & 0x7fffffffu);
-    }
+  for (int i = 0; i < kQuantVecs; ++i)
+    if (t + i * TPR < nvec) top = v[i].larger(top);
+  for (int j = t + kQuantVecs * TPR; j < nvec; j += TPR) {   // long rows: read again below
+    Vec8<T> w;
+    load(j, w);
+    top = w.larger(top);
   }
-  for (int64_t j = t + (int64_t)kQuantVecs * TPR; j < nvec; j += TPR) {   // long rows: read again below
-    float w[8];
-    quant_load(xr, j * 8, cols, vec, w);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(w[e]) & 0x7fffffffu);
-  }
-  top = __reduce_max_sync(0xffffffffu, top);
+  uint32_t big = __reduce_max_sync(0xffffffffu, __float_as_uint(quant_top<T>(top)));
   if constexpr (TPR > 32) {
     __shared__ uint32_t part[kQuantThreads / 32];
-    if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = top;
+    if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = big;
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < kQuantThreads / 32; ++i) top = max(top, part[i]);
+    for (int i = 0; i < kQuantThreads / 32; ++i) big = max(big, part[i]);
   }
   if (!live) return;
-  const bool bad = top >= 0x7f800000u;
-  const float s = bad ? __uint_as_float(0x7fffffffu) : __fdiv_rn(__uint_as_float(top), 127.f);
-  if (t == 0) scale[row] = s;
-  const bool zero = bad || s == 0.f;
-  const bool divide = !(s > 0x1p-100f && s < 0x1p100f);   // 1 / scale must be a normal number
-  const float inv = divide ? 0.f : 1.f / s;
-  int8_t* qr = q + (int64_t)row * kp;
-  auto store = [&](int64_t j, const float (&w)[8]) {
-    uint32_t lo = 0, hi = 0;
-    if (!zero) {
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        lo |= (uint32_t)(quant_one(w[e], s, inv, divide) & 0xff) << (8 * e);
-        hi |= (uint32_t)(quant_one(w[e + 4], s, inv, divide) & 0xff) << (8 * e);
-      }
-    }
-    *reinterpret_cast<uint2*>(qr + j * 8) = make_uint2(lo, hi);
+  const QuantScale k(__uint_as_float(big));
+  if (t == 0) scale[row] = k.s;
+  int8_t* qr = q + row * kp;
+  if (k.zero) {
+    for (int j = t; j < nvec; j += TPR) *reinterpret_cast<uint2*>(qr + (int64_t)j * 8) = make_uint2(0u, 0u);
+    return;
+  }
+  if (k.inv == 0.f) {
+    for (int j = t; j < nvec; j += TPR) quant_extreme(xr, (int64_t)j * 8, cols, k.s, qr);
+    return;
+  }
+  auto store = [&](int j, const Vec8<T>& w) {
+    float f[8];
+    w.values(f);
+    *reinterpret_cast<uint2*>(qr + (int64_t)j * 8) = quant_pack(f, k);
   };
 #pragma unroll
-  for (int i = 0; i < kQuantVecs; ++i) {
-    const int64_t j = t + (int64_t)i * TPR;
-    if (j < nvec) store(j, v[i]);
-  }
-  for (int64_t j = t + (int64_t)kQuantVecs * TPR; j < nvec; j += TPR) {
-    float w[8];
-    quant_load(xr, j * 8, cols, vec, w);
+  for (int i = 0; i < kQuantVecs; ++i)
+    if (t + i * TPR < nvec) store(t + i * TPR, v[i]);
+  for (int j = t + kQuantVecs * TPR; j < nvec; j += TPR) {
+    Vec8<T> w;
+    load(j, w);
     store(j, w);
   }
 }
@@ -141,28 +214,29 @@ struct EpiI8 {
   uint32_t scales;
   int lane;
   float rs;
-  float bs[8];
+  float b0, b1;      // column scales of the chunk to come, a column (two for 16-bit results) per lane
   __device__ EpiI8(const Args& args, const CUtensorMap* m, uint32_t base, int w, int l)
       : a(args), map(m), stage{base + (uint32_t)w * 8192u, 0}, scales(base + 32768u + (uint32_t)w * 256u), lane(l) {}
+  __device__ __forceinline__ void fetch(int col, int N) {
+    b0 = col + lane < N ? __ldg(a.b_scale + col + lane) : 0.f;
+    if constexpr (!OUT_F32) b1 = col + 32 + lane < N ? __ldg(a.b_scale + col + 32 + lane) : 0.f;
+  }
   __device__ __forceinline__ void before(const EpiTile& e, int M, int N) {
     rs = e.row0 + lane < M ? __ldg(a.a_scale + e.row0 + lane) : 0.f;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const int c = e.col0 + i * 32 + lane;
-      bs[i] = c < N ? __ldg(a.b_scale + c) : 0.f;   // beyond the tile's own columns: loaded, never used
-    }
+    fetch(e.col0, N);
   }
   template <int BN>
   __device__ __forceinline__ void tile(const EpiTile& e, int M, int N) {
     constexpr int kCols = OUT_F32 ? 32 : 64;
-#pragma unroll
+    // a loop, not unrolled: both ways of storing make it long, and four warps with one instruction stream each live on the instruction cache
+#pragma unroll 1
     for (int q = 0; q < BN / kCols; ++q) {
       uint32_t v[32], w[32];
       tmem_ld_32x32b_x32(e.taddr + (uint32_t)(q * kCols), v);
       if constexpr (!OUT_F32) tmem_ld_32x32b_x32(e.taddr + (uint32_t)(q * kCols + 32), w);
-      const float b0 = bs[OUT_F32 ? q : 2 * q], b1 = OUT_F32 ? 0.f : bs[2 * q + (OUT_F32 ? 0 : 1)];
       asm volatile("st.shared.f32 [%0], %1;" ::"r"(scales + lane * 4), "f"(b0) : "memory");
       if constexpr (!OUT_F32) asm volatile("st.shared.f32 [%0], %1;" ::"r"(scales + 128 + lane * 4), "f"(b1) : "memory");
+      if (q + 1 < BN / kCols) fetch(e.col0 + (q + 1) * kCols, N);
       __syncwarp();
       tmem_ld_wait();
       auto scaled = [&](uint32_t (&r)[32], uint32_t at) {
@@ -189,7 +263,9 @@ struct EpiI8 {
       const int col = e.col0 + q * kCols;
       const bool inside = e.row0 < M && col < N;
       if (a.plain) {
-        if (inside) store_slice_plain<OUT_F32 ? 4 : 2>(slice, lane, a.C, a.ld_bytes, e.row0, col, M, N);
+        constexpr int kElt = OUT_F32 ? 4 : 2;
+        if (inside) store_slice_plain<kElt>(stage.last(), slice, lane, a.C, a.ld_bytes, e.row0, col, M, min(128, (N - col) * kElt), q == 0,
+                                            q == BN / kCols - 1 || col + kCols >= N);
         else __syncwarp();
       } else {
         fence_async_smem();
@@ -202,6 +278,165 @@ struct EpiI8 {
     }
   }
 };
+
+// One result, rounded to the output's type.
+__device__ __forceinline__ void store_y(char* C, int out, int64_t at, float y) {
+  if (out == SP_FP32) reinterpret_cast<float*>(C)[at] = y;
+  else if (out == SP_BF16) reinterpret_cast<__nv_bfloat16*>(C)[at] = __float2bfloat16_rn(y);
+  else reinterpret_cast<__half*>(C)[at] = __float2half_rn(y);
+}
+
+// ------------------------------------------------------------------ a handful of tokens
+// Up to 8 tokens whose 8-bit rows fit 64 KiB of shared memory: what counts is the time from launch to the first weight and from the last
+// weight to the result.  So no tensor memory, barriers or clusters: a warp takes two weight rows, asks for 4 KiB of each at
+// once (16 bytes per lane and load, straight to registers), multiplies them with the tokens in shared memory four bytes at a
+// time, and sums over the warp.  The weights are asked for before the tokens are read, and, where the tokens are small, each
+// block quantises them itself while the weights are on their way (a launch less).
+// Two blocks per SM walk the rows with a fixed stride.  FILLDOT
+constexpr int kDotThreads = 256, kDotUnroll = 8, kDotTokens = 8;
+constexpr int64_t kDotBytes = 65536;        // tokens x K that a block holds
+constexpr int64_t kDotQuantize = 8192;      // tokens x K up to which a block quantises for itself: at most 4 vectors per thread
+
+struct DotArgs {
+  const int8_t* W;
+  const float* w_scale;
+  const int8_t* q;        // tokens, already 8 bits ...
+  const float* q_scale;
+  const void* x;          // ... or not (nullptr: they are): quantised here, into q_out and scale_out as well
+  int x_dtype;
+  int64_t cols;           // of x
+  int8_t* q_out;
+  float* scale_out;
+  char* C;
+  int M, N, K;
+  int out;
+  int early;              // as FewArgs
+};
+
+// Eight elements of x as floats; elements from n on are zero.
+__device__ __forceinline__ void dot_load(const void* x, int dtype, int64_t at, int n, bool aligned, float (&f)[8]) {
+  auto as = [&](auto v, auto* p) {
+    if (n == 8 && aligned) v.load(p + at);
+    else v.load_some(p + at, n);
+    v.values(f);
+  };
+  if (dtype == SP_BF16) as(Vec8<__nv_bfloat16>(), static_cast<const __nv_bfloat16*>(x));
+  else if (dtype == SP_FP16) as(Vec8<__half>(), static_cast<const __half*>(x));
+  else as(Vec8<float>(), static_cast<const float*>(x));
+}
+
+// The tokens to 8 bits, by the whole block.  x is read twice, the second time from the nearest cache: held in registers between the
+// passes it would push out the weights that are on their way, and the block would wait for those first.
+__device__ __forceinline__ void dot_quantize(const DotArgs& a, int8_t* tokens, float* scales, uint32_t* tops) {
+  const int nvec = a.K / 8, total = a.M * nvec, lane = threadIdx.x & 31;
+  const bool aligned = (((uintptr_t)a.x | (uintptr_t)(a.cols * (a.x_dtype == SP_FP32 ? 4 : 2))) & 15u) == 0;
+  auto load = [&](int at, int& m, int& j, float (&f)[8]) {
+    m = at / nvec; j = at - m * nvec;
+    dot_load(a.x, a.x_dtype, (int64_t)m * a.cols + (int64_t)j * 8, (int)min((int64_t)8, max((int64_t)0, a.cols - (int64_t)j * 8)), aligned, f);
+  };
+#pragma unroll 2
+  for (int first = (int)threadIdx.x - lane; first < total; first += kDotThreads) {      // of this warp
+    float f[8];
+    int m = 0, j;
+    uint32_t top = 0;
+    if (first + lane < total) {
+      load(first + lane, m, j, f);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(f[e]) & 0x7fffffffu);
+    }
+    if (first / nvec == (first + 31) / nvec) {       // the warp is inside one row
+      top = __reduce_max_sync(0xffffffffu, top);
+      if (lane == 0) atomicMax(tops + m, top);
+    } else if (first + lane < total) {
+      atomicMax(tops + m, top);
+    }
+  }
+  __syncthreads();
+#pragma unroll 2
+  for (int at = threadIdx.x; at < total; at += kDotThreads) {
+    float f[8];
+    int m, j;
+    load(at, m, j, f);
+    const QuantScale k(__uint_as_float(tops[m]));
+    uint2 b = make_uint2(0u, 0u);
+    if (!k.zero && k.inv != 0.f) b = quant_pack(f, k);
+    if (!k.zero && k.inv == 0.f) {
+      uint64_t bytes = 0;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) bytes |= (uint64_t)(uint8_t)quant_by_remainder(f[e], k.s) << (8 * e);
+      b = make_uint2((uint32_t)bytes, (uint32_t)(bytes >> 32));
+    }
+    *reinterpret_cast<uint2*>(tokens + (int64_t)m * a.K + (int64_t)j * 8) = b;
+    if (j == 0) scales[m] = k.s;
+    if (blockIdx.x == 0) {
+      *reinterpret_cast<uint2*>(a.q_out + (int64_t)m * a.K + (int64_t)j * 8) = b;
+      if (j == 0) a.scale_out[m] = k.s;
+    }
+  }
+}
+
+template <int MT>
+__global__ void __launch_bounds__(kDotThreads, 2) dot_tokens_kernel(const DotArgs a) {
+  extern __shared__ __align__(16) int8_t dot_tokens[];     // MT rows of K bytes; rows beyond M are read and not used
+  __shared__ float scales[kDotTokens];
+  __shared__ uint32_t tops[kDotTokens];
+  const int lane = threadIdx.x & 31, warp = blockIdx.x * (kDotThreads / 32) + (threadIdx.x >> 5);
+  const int step = gridDim.x * (kDotThreads / 32) * 2;
+  pdl_launch_dependents();
+  int4 w[2][kDotUnroll];
+  auto fetch = [&](int n, int k) {     // bytes [k, k + 4096) of rows n and n + 1
+#pragma unroll
+    for (int u = 0; u < kDotUnroll; ++u)
+#pragma unroll
+      for (int r = 0; r < 2; ++r) {
+        const int c = k + u * 512 + lane * 16;
+        w[r][u] = n + r < a.N && c < a.K ? __ldcs(reinterpret_cast<const int4*>(a.W + (int64_t)(n + r) * a.K + c)) : make_int4(0, 0, 0, 0);
+      }
+  };
+  if (!a.early) pdl_wait();
+  fetch(warp * 2, 0);
+  if (a.early) pdl_wait();
+  if (a.x != nullptr) {
+    if (threadIdx.x < kDotTokens) tops[threadIdx.x] = 0;
+    __syncthreads();
+    dot_quantize(a, dot_tokens, scales, tops);
+  } else {
+    for (int i = threadIdx.x; i < a.M * (a.K / 16); i += kDotThreads)
+      reinterpret_cast<int4*>(dot_tokens)[i] = __ldg(reinterpret_cast<const int4*>(a.q) + i);
+    if (threadIdx.x < a.M) scales[threadIdx.x] = __ldg(a.q_scale + threadIdx.x);
+  }
+  __syncthreads();
+  for (int n = warp * 2; n < a.N; n += step) {
+    int acc[2][MT] = {};
+    for (int k = 0; k < a.K; k += kDotUnroll * 512) {
+#pragma unroll
+      for (int u = 0; u < kDotUnroll; ++u) {
+        const int c = k + u * 512 + lane * 16;
+        if (c < a.K) {
+#pragma unroll
+          for (int m = 0; m < MT; ++m) {
+            const int4 x = *reinterpret_cast<const int4*>(dot_tokens + m * a.K + c);
+#pragma unroll
+            for (int r = 0; r < 2; ++r)
+              acc[r][m] = __dp4a(w[r][u].x, x.x, __dp4a(w[r][u].y, x.y, __dp4a(w[r][u].z, x.z, __dp4a(w[r][u].w, x.w, acc[r][m]))));
+          }
+        }
+      }
+      if (k + kDotUnroll * 512 < a.K) fetch(n, k + kDotUnroll * 512);
+      else if (n + step < a.N) fetch(n + step, 0);
+    }
+    int mine = 0;
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+      for (int r = 0; r < 2; ++r) {
+        const int sum = __reduce_add_sync(0xffffffffu, acc[r][m]);
+        if (lane == 2 * m + r) mine = sum;
+      }
+    const int m = lane >> 1, col = n + (lane & 1);
+    if (m < a.M && col < a.N) store_y(a.C, a.out, (int64_t)m * a.N + col, (float)mine * scales[m] * __ldg(a.w_scale + col));
+  }
+}
 
 // ------------------------------------------------------------------ few tokens
 // At most NT rows of A: the call is bound by reading the weights once, so the weights take the 128-row side of the MMA and the
@@ -229,13 +464,6 @@ struct FewArgs {
   uint32_t idesc;
 };
 
-__device__ __forceinline__ void few_store(const FewArgs& a, int tok, int n, int acc) {
-  const float y = (float)acc * __ldg(a.a_scale + tok) * __ldg(a.b_scale + n);
-  const int64_t at = (int64_t)tok * a.N + n;
-  if (a.out == SP_FP32) reinterpret_cast<float*>(a.C)[at] = y;
-  else if (a.out == SP_BF16) reinterpret_cast<__nv_bfloat16*>(a.C)[at] = __float2bfloat16_rn(y);
-  else reinterpret_cast<__half*>(a.C)[at] = __float2half_rn(y);
-}
 
 template <int NT>
 __global__ void __launch_bounds__(192, 2)
@@ -329,6 +557,7 @@ few_tokens_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant
   } else {
     pdl_wait();
     const int quarter = warp & 3, row = quarter * 32 + lane, n = n0 + row;
+    const float bs = nranks == 1 && n < args.N ? __ldg(args.b_scale + n) : 0.f;
     bool ok = mbar_wait(bar_done, 0, args.status, (kProdEpilogue << 8) | 3);
     ok = __all_sync(0xffffffffu, ok);
     tcgen05_fence_after();
@@ -343,7 +572,7 @@ few_tokens_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant
           const int tok = q * 32 + j;
           if (tok >= args.M) break;
           if (nranks == 1) {
-            if (n < args.N) few_store(args, tok, n, (int)v[j]);
+            if (n < args.N) store_y(args.C, args.out, (int64_t)tok * args.N + n, (float)(int)v[j] * __ldg(args.a_scale + tok) * bs);
           } else {
             asm volatile("st.shared.b32 [%0], %1;" ::"r"(smem_base + (uint32_t)(tok * 128 + row) * 4u), "r"(v[j]) : "memory");
           }
@@ -357,15 +586,31 @@ few_tokens_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant
     asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
     asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
     if (warp >= 2) {
-      const int row = (int)threadIdx.x - 64, n = n0 + row;
-      for (int tok = (int)rank; tok < args.M; tok += (int)nranks) {
-        int acc = 0;
-        for (uint32_t r = 0; r < nranks; ++r) {
-          int p;
-          asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(p) : "r"(mapa(smem_base + (uint32_t)(tok * 128 + row) * 4u, r)) : "memory");
-          acc += p;
+      // Each CTA of the cluster finishes every S-th token.  Four tokens at a time, their remote reads in flight together: one after
+      // the other they cost a trip between SMs each (24 tokens, 16384 x 8192: 36 us that way).
+      const int quarter = warp & 3, row = quarter * 32 + lane, n = n0 + row;
+      const float bs = n < args.N ? __ldg(args.b_scale + n) : 0.f;
+      for (int tok = (int)rank; tok < args.M; tok += 4 * (int)nranks) {
+        int acc[4] = {0, 0, 0, 0};
+        float as[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) as[i] = tok + i * (int)nranks < args.M ? __ldg(args.a_scale + tok + i * (int)nranks) : 0.f;
+#pragma unroll
+        for (uint32_t r = 0; r < 8; ++r) {
+          if (r < nranks) {
+            const uint32_t peer = mapa(smem_base, r) + (uint32_t)row * 4u;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              int p = 0;
+              if (tok + i * (int)nranks < args.M)
+                asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(p) : "r"(peer + (uint32_t)(tok + i * (int)nranks) * 512u));
+              acc[i] += p;
+            }
+          }
         }
-        if (n < args.N) few_store(args, tok, n, acc);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (tok + i * (int)nranks < args.M && n < args.N) store_y(args.C, args.out, (int64_t)(tok + i * (int)nranks) * args.N + n, (float)acc[i] * as[i] * bs);
       }
     }
     __syncwarp();
@@ -487,6 +732,36 @@ static int check_i8(const void* A, const void* a_scale, const void* B, const voi
   return SP_OK;
 }
 
+template <int MT>
+static int launch_dot(const DotArgs& a, cudaStream_t stream) {
+  auto kern = dot_tokens_kernel<MT>;
+  static uint64_t configured = 0;
+  if (first_use_on_this_device(configured)) {
+    const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kDotBytes);
+    if (e != cudaSuccess) { configured = 0; set_error("cudaFuncSetAttribute failed: %s", cudaGetErrorString(e)); return SP_ERR_CUDA; }
+  }
+  const int64_t blocks = (a.N + 15) / 16;
+  return launch_pdl("dot products", kern, dim3((unsigned)(blocks < 2 * 148 ? blocks : 2 * 148)), kDotThreads, (size_t)MT * a.K, 1, stream, a);
+}
+
+// The tokens come quantised (x == nullptr) or are quantised by every block.
+static int run_dot(const I8Call& c, const void* x, int x_dtype, int64_t cols, bool early, cudaStream_t stream) {
+  DotArgs a = {};
+  a.W = (const int8_t*)c.B; a.w_scale = c.b_scale; a.q = (const int8_t*)c.A; a.q_scale = c.a_scale;
+  a.x = x; a.x_dtype = x_dtype; a.cols = cols; a.q_out = (int8_t*)const_cast<void*>(c.A); a.scale_out = const_cast<float*>(c.a_scale);
+  a.C = (char*)c.C; a.M = (int)c.M; a.N = (int)c.N; a.K = (int)c.K; a.out = c.out; a.early = early ? 1 : 0;
+  if (c.M <= 1) return launch_dot<1>(a, stream);
+  if (c.M <= 2) return launch_dot<2>(a, stream);
+  if (c.M <= 4) return launch_dot<4>(a, stream);
+  return launch_dot<8>(a, stream);
+}
+
+// MT rows of the next power of two must fit.
+static bool takes_dot(const I8Call& c) {
+  const int64_t mt = c.M <= 1 ? 1 : c.M <= 2 ? 2 : c.M <= 4 ? 4 : 8;
+  return c.few && c.M <= kDotTokens && mt * c.K <= kDotBytes;
+}
+
 template <int NT>
 static int launch_few(const I8Call& c, const CUtensorMap& tmW, FewArgs args, cudaStream_t stream) {
   using C = FewCfg<NT>;
@@ -518,6 +793,7 @@ static int launch_tiles(const I8Call& c, const ProdArgs& pa, const typename EpiI
 }
 
 static int run_i8(const I8Call& c, bool early, cudaStream_t stream) {
+  if (takes_dot(c)) return run_dot(c, nullptr, 0, 0, early, stream);
   LibraryState st;
   int rc = library_state(c.few ? nullptr : &c.sched, c.host_perm, stream, &st);
   if (rc != SP_OK) return rc;
@@ -596,6 +872,7 @@ int sp_linear_i8(const void* x, int32_t x_dtype, int8_t* q, float* q_scale, cons
   rc = current_device(&dev);
   if (rc != SP_OK) return rc;
   std::lock_guard<std::mutex> lock(g_i8_mu);
+  if (takes_dot(call) && M * call.K <= kDotQuantize) return run_dot(call, x, x_dtype, K, false, (cudaStream_t)stream);
   rc = quantize(x, x_dtype, M, K, q, q_scale, (cudaStream_t)stream);
   if (rc != SP_OK) return rc;
   return run_i8(call, true, (cudaStream_t)stream);

@@ -114,6 +114,7 @@ struct EpiTile {
 struct EpiStage {
   uint32_t base;
   int chunk;
+  __device__ __forceinline__ uint32_t last() const { return base + (uint32_t)((chunk - 2) & 1) * 4096u; }   // the slice before the one handed out
   __device__ __forceinline__ uint32_t next(int lane) {   // whole warp
     if (chunk >= 2) {
       if (lane == 0) bulk_wait_read_1();
@@ -137,22 +138,59 @@ __device__ __forceinline__ uint32_t ld_shared_32(uint32_t addr) {
   return v;
 }
 
-// A staged slice to a matrix whose rows a bulk store cannot take (row pitch or address not a multiple of 16 bytes, but whole elements):
-// row by row, each store instruction of the warp on consecutive addresses.
+// A staged slice to a matrix whose rows a bulk store cannot take (row pitch or address not a multiple of 16 bytes, but whole elements).
+// The slices of a tile come from left to right.  Each row is cut where its own addresses are multiples of 16: a window takes its first
+// bytes from the slice before (still staged) and the rest from this one, so that all but a tile's two edges is written 16 bytes
+// at a time, four rows per instruction.  (One element per lane, a row per instruction: 2001 x 4999 fp32 results of a
+// 2048-long product 50 us, this way FILLPLAIN.)  `len`: bytes of this slice inside the matrix.
 template <int ELT>
-__device__ __forceinline__ void store_slice_plain(uint32_t slice, int lane, char* out, int64_t ld_bytes, int row0, int col, int M, int N) {
+__device__ __forceinline__ void store_slice_plain(uint32_t before, uint32_t slice, int lane, char* out, int64_t ld_bytes, int row0, int col, int M, int len,
+                                                  bool first, bool last) {
   __syncwarp();
-  const int rows = min(32, M - row0);
-  for (int r = 0; r < rows; ++r) {
-    const uint32_t w = ld_shared_32(slice + (uint32_t)r * 128u + (((((uint32_t)lane >> 2) ^ ((uint32_t)r & 7u)) << 4) | (((uint32_t)lane & 3u) << 2)));
-    char* p = out + (int64_t)(row0 + r) * ld_bytes;
-    if constexpr (ELT == 4) {
-      if (col + lane < N) *reinterpret_cast<uint32_t*>(p + (int64_t)(col + lane) * 4) = w;
-    } else {
-      const int c = col + 2 * lane;
-      if (c < N) *reinterpret_cast<uint16_t*>(p + (int64_t)c * 2) = (uint16_t)(w & 0xffffu);
-      if (c + 1 < N) *reinterpret_cast<uint16_t*>(p + (int64_t)(c + 1) * 2) = (uint16_t)(w >> 16);
+  auto scalar = [&](int row, int w) {      // a window that is not whole: element by element
+    char* a = out + (int64_t)(row0 + row) * ld_bytes + (int64_t)col * ELT;
+    const int p = 16 * w - (int)((uintptr_t)a & 15u), lo = first && p < 0 ? 0 : p, hi = min(p + 16, len);
+#pragma unroll 1
+    for (int q = lo; q < hi; q += ELT) {
+      const uint32_t b = (uint32_t)q & 127u, addr = (q < 0 ? before : slice) + (uint32_t)row * 128u + ((((b >> 4) ^ ((uint32_t)row & 7u)) << 4) | (b & 12u));
+      const uint32_t v = ld_shared_32(addr);
+      if constexpr (ELT == 4) *reinterpret_cast<uint32_t*>(a + q) = v;
+      else *reinterpret_cast<uint16_t*>(a + q) = (uint16_t)(b & 2u ? v >> 16 : v);
     }
+  };
+  // Lane 8 i + w has window w of rows i, i + 4, ...: bytes 16 w - m on, m the row's address modulo 16, are the tail of unit w - 1 and the head of
+  // unit w, put together by a shift of m bytes.  One warp runs per scheduler here, so the count of instructions is what costs.
+  const int w = lane & 7, i0 = lane >> 3;
+  char* a = out + (int64_t)(row0 + i0) * ld_bytes + (int64_t)col * ELT;
+  const uint32_t left = w ? slice : before, wl = (uint32_t)(w - 1) & 7u;
+  const uint32_t ua = (uint32_t)i0 * 128u + (((uint32_t)w ^ (uint32_t)i0) << 4), ub = (uint32_t)i0 * 128u + ((wl ^ (uint32_t)i0) << 4);
+  // straight-line code: the eight rounds' reads are in flight together
+#pragma unroll
+  for (int r = 0; r < 32; r += 4, a += 4 * ld_bytes) {
+    const uint32_t m = (uint32_t)(uintptr_t)a & 15u;
+    const int p = 16 * w - (int)m;
+    uint32_t x[4], y[4], t[5], o[5];
+    const uint32_t flip = r & 4 ? 64u : 0u;      // bit 2 of the row turns the unit by 4
+    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(x[0]), "=r"(x[1]), "=r"(x[2]), "=r"(x[3]) : "r"(left + (uint32_t)r * 128u + (ub ^ flip)));
+    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(y[0]), "=r"(y[1]), "=r"(y[2]), "=r"(y[3]) : "r"(slice + (uint32_t)r * 128u + (ua ^ flip)));
+    const bool m8 = m & 8u, m4 = m & 4u;      // x, y shifted by two words, by one word, by half a word
+    t[0] = m8 ? x[1] : x[3]; t[1] = m8 ? x[2] : y[0]; t[2] = m8 ? x[3] : y[1]; t[3] = m8 ? y[0] : y[2]; t[4] = m8 ? y[1] : y[3];
+    o[0] = m4 ? (m8 ? x[0] : x[2]) : t[0];
+#pragma unroll
+    for (int i = 1; i < 5; ++i) o[i] = m4 ? t[i - 1] : t[i];
+    if constexpr (ELT == 2) {
+      const uint32_t sel = m & 2u ? 0x5432u : 0x7654u;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) o[i] = __byte_perm(o[i], o[i + 1], sel);
+#pragma unroll
+      for (int i = 4; i > 0; --i) o[i] = o[i - 1];
+    }
+    if (row0 + r + i0 < M && p + 16 <= len && !(first && p < 0)) *reinterpret_cast<uint4*>(a + p) = make_uint4(o[1], o[2], o[3], o[4]);
+  }
+  if ((first || last) && row0 + lane < M) {      // a row's two edges in this tile
+    const int m = (int)((uintptr_t)(out + (int64_t)(row0 + lane) * ld_bytes + (int64_t)col * ELT) & 15u), end = (len + m) >> 4;
+    if (first && m) scalar(lane, 0);
+    if (last && ((len + m) & 15) && !(first && m && end == 0)) scalar(lane, end);
   }
   __syncwarp();
 }
