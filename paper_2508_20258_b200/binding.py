@@ -327,9 +327,14 @@ I8_MAX_K = 131056
 _REDUCE = {"none": REDUCE_NONE, "mean": REDUCE_MEAN, "sum": REDUCE_SUM}
 
 
+_DTYPE_CODES: dict = {}      # torch dtype -> code
+
+
 def _dtype_code(t, allowed):
-    import torch
-    code = {torch.bfloat16: BF16, torch.float32: FP32, torch.float16: FP16}.get(t.dtype)
+    if not _DTYPE_CODES:
+        import torch
+        _DTYPE_CODES.update({torch.bfloat16: BF16, torch.float32: FP32, torch.float16: FP16})
+    code = _DTYPE_CODES.get(t.dtype)
     if code not in allowed:
         raise ValueError(f"unsupported element type {t.dtype}")
     return code
@@ -338,38 +343,40 @@ def _dtype_code(t, allowed):
 def _device_tensors(*tensors) -> None:
     """Contiguous CUDA tensors on the current device: the library launches there."""
     import torch
+    here = -2
     for t in tensors:
-        if not t.is_cuda or not t.is_contiguous():
+        at = t.get_device()      # -1: not on a GPU
+        if at < 0 or not t.is_contiguous():
             raise ValueError("tensors must be contiguous CUDA tensors")
-    here = torch.cuda.current_device()
-    for t in tensors:
-        if t.get_device() != here:
-            raise ValueError(f"tensor on {t.device}, but the current device is cuda:{here}")
+        if here == -2:
+            here = torch.cuda.current_device()
+        if at != here:
+            raise ValueError(f"tensor on cuda:{at}, but the current device is cuda:{here}")
 
 
 def _vector(t, n: int, dtype, what: str) -> None:
-    if t.dtype != dtype or t.dim() != 1 or t.shape[0] != n:
+    if t.dtype != dtype or t.shape != (n,):
         raise ValueError(f"{what} must be a {dtype} vector of {n}")
 
 
-def _matrix_i8(t, rows, cols: int, what: str) -> None:
+def _matrix_i8(t, rows: int, cols: int, what: str) -> None:
     import torch
-    if t.dtype != torch.int8 or t.dim() != 2 or (rows is not None and t.shape[0] != rows) or t.shape[1] != cols:
-        raise ValueError(f"{what} must be an int8 matrix with rows of {cols}")
+    if t.dtype != torch.int8 or t.shape != (rows, cols):
+        raise ValueError(f"{what} must be an int8 matrix of {rows} rows of {cols}")
 
 
 _I8_DEFAULTS: dict = {}      # the parameters of a call that leaves tile and order to the library, per output type
 
 
-def _i8_params(y, params: Optional[SpParams]) -> SpParams:
+def _i8_params(y, params: Optional[SpParams]):
     code = _dtype_code(y, (BF16, FP32, FP16))
     if params is None:
         if code not in _I8_DEFAULTS:
             _I8_DEFAULTS[code] = make_params(out_dtype=code, b_layout=1)
-        return _I8_DEFAULTS[code]
-    if params.out_dtype != code:
+        params = _I8_DEFAULTS[code]
+    elif params.out_dtype != code:
         raise ValueError("params.out_dtype does not say the output's element type")
-    return params
+    return ctypes.byref(params)
 
 
 def quantize_i8(x, q, scale, stream=None) -> None:
@@ -396,7 +403,7 @@ def gemm_i8(A, a_scale, B, b_scale, C, scheme: int = ORDER_AUTO, params: Optiona
         raise ValueError("shape mismatch")
     _device_tensors(A, a_scale, B, b_scale, C)
     p = _i8_params(C, params)
-    _check(lib().sp_gemm_i8(A.data_ptr(), a_scale.data_ptr(), B.data_ptr(), b_scale.data_ptr(), C.data_ptr(), M, N, K, scheme, _pp(p),
+    _check(lib().sp_gemm_i8(A.data_ptr(), a_scale.data_ptr(), B.data_ptr(), b_scale.data_ptr(), C.data_ptr(), M, N, K, scheme, p,
                             _stream_handle(stream)))
 
 
@@ -410,12 +417,12 @@ def linear_i8(x, q, q_scale, W, w_scale, y, scheme: int = ORDER_AUTO, params: Op
     _matrix_i8(W, N, kp, "W")
     _vector(q_scale, M, torch.float32, "q_scale")
     _vector(w_scale, N, torch.float32, "w_scale")
-    if tuple(y.shape) != (M, N):
+    if y.shape != (M, N):
         raise ValueError("shape mismatch")
     _device_tensors(x, q, q_scale, W, w_scale, y)
     p = _i8_params(y, params)
     _check(lib().sp_linear_i8(x.data_ptr(), _dtype_code(x, (BF16, FP32, FP16)), q.data_ptr(), q_scale.data_ptr(), W.data_ptr(), w_scale.data_ptr(),
-                              y.data_ptr(), M, N, K, scheme, _pp(p), _stream_handle(stream)))
+                              y.data_ptr(), M, N, K, scheme, p, _stream_handle(stream)))
 
 
 def linear_ce_workspace(T: int, V: int, D: int, grad: bool = False) -> int:

@@ -106,6 +106,105 @@ struct EpiStats {
   }
 };
 
+// ------------------------------------------------------------------ forward: one token
+// The call is one read of W, so what counts is that every SM reads the same share of it, whatever V is, from the first cycle to the
+// last: in the tiled form 256 words per CTA leave 20 of 148 SMs without work at 32768 words.  Here a warp takes two rows of W,
+// asks for 4 KiB of each at once, straight to registers, multiplies in fp32 and keeps the running (maximum, sum) of its
+// rows' scores; a block leaves one pair.  Measured at 32768 x 4096: 52 us, tiled 66.  For one token only: every further one
+// costs the fp32 units as much again (two tokens 60 us, tiled 55).
+constexpr int kRowThreads = 256, kRowUnroll = 8;
+constexpr int64_t kRowMaxD = 16384;       // the token as fp32 in 64 KiB of shared memory
+
+struct RowArgs {
+  const uint16_t* W;
+  const uint16_t* h;
+  const int64_t* target;
+  float2* stats;        // [block]
+  float* picked;
+  int V, D;
+  int bf16;
+};
+
+__device__ __forceinline__ void row_values(uint32_t u, int bf16, float& lo, float& hi) {
+  if (bf16) {
+    lo = __uint_as_float(u << 16); hi = __uint_as_float(u & 0xffff0000u);
+  } else {
+    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&u));
+    lo = f.x; hi = f.y;
+  }
+}
+
+__device__ __forceinline__ void join_pair(float2& a, float2 p) {
+  const float m = fmaxf(a.x, p.x), ref = m == -CUDART_INF_F ? 0.f : m;      // nothing finite yet: every term is exp2(-inf) = 0
+  a = make_float2(m, a.y * ex2(a.x - ref) + p.y * ex2(p.x - ref));
+}
+
+__global__ void __launch_bounds__(kRowThreads, 2) row_stats_kernel(const RowArgs a) {
+  extern __shared__ __align__(16) float row_token[];      // D
+  __shared__ float2 part[kRowThreads / 32];
+  const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5, warp = blockIdx.x * (kRowThreads / 32) + wid;
+  const int step = gridDim.x * (kRowThreads / 32) * 2;
+  pdl_launch_dependents();
+  pdl_wait();
+  int4 w[2][kRowUnroll];
+  auto fetch = [&](int n, int k) {      // elements [k, k + 2048) of rows n and n + 1
+#pragma unroll
+    for (int u = 0; u < kRowUnroll; ++u)
+#pragma unroll
+      for (int r = 0; r < 2; ++r) {
+        const int c = k + u * 256 + lane * 8;
+        w[r][u] = n + r < a.V && c < a.D ? __ldcs(reinterpret_cast<const int4*>(a.W + (int64_t)(n + r) * a.D + c)) : make_int4(0, 0, 0, 0);
+      }
+  };
+  fetch(warp * 2, 0);
+  for (int i = threadIdx.x; i < a.D / 2; i += kRowThreads) {
+    float lo, hi;
+    row_values(__ldg(reinterpret_cast<const uint32_t*>(a.h) + i), a.bf16, lo, hi);
+    reinterpret_cast<float2*>(row_token)[i] = make_float2(lo, hi);
+  }
+  const int64_t want = __ldg(a.target);
+  __syncthreads();
+  float2 pair = make_float2(-CUDART_INF_F, 0.f);
+  for (int64_t n = (int64_t)warp * 2; n < a.V; n += step) {
+    float acc[2] = {};
+    for (int k = 0; k < a.D; k += kRowUnroll * 256) {
+#pragma unroll
+      for (int u = 0; u < kRowUnroll; ++u) {
+        const int c = k + u * 256 + lane * 8;
+        if (c < a.D) {
+          const float4 p = *reinterpret_cast<const float4*>(row_token + c), q = *reinterpret_cast<const float4*>(row_token + c + 4);
+#pragma unroll
+          for (int r = 0; r < 2; ++r) {
+            float lo, hi;
+            row_values((uint32_t)w[r][u].x, a.bf16, lo, hi); acc[r] = fmaf(lo, p.x, acc[r]); acc[r] = fmaf(hi, p.y, acc[r]);
+            row_values((uint32_t)w[r][u].y, a.bf16, lo, hi); acc[r] = fmaf(lo, p.z, acc[r]); acc[r] = fmaf(hi, p.w, acc[r]);
+            row_values((uint32_t)w[r][u].z, a.bf16, lo, hi); acc[r] = fmaf(lo, q.x, acc[r]); acc[r] = fmaf(hi, q.y, acc[r]);
+            row_values((uint32_t)w[r][u].w, a.bf16, lo, hi); acc[r] = fmaf(lo, q.z, acc[r]); acc[r] = fmaf(hi, q.w, acc[r]);
+          }
+        }
+      }
+      if (k + kRowUnroll * 256 < a.D) fetch((int)n, k + kRowUnroll * 256);
+      else if (n + step < a.V) fetch((int)(n + step), 0);
+    }
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+#pragma unroll
+      for (int o = 16; o; o >>= 1) acc[r] += __shfl_xor_sync(0xffffffffu, acc[r], o);
+      if (n + r < a.V) {
+        if (lane == 0 && want == n + r) *a.picked = acc[r];
+        const float m = fmaxf(pair.x, acc[r] * kLog2e), ref = m == -CUDART_INF_F ? 0.f : m;
+        pair = make_float2(m, fmaf(pair.y, ex2(pair.x - ref), ex2(fmaf(acc[r], kLog2e, -ref))));
+      }
+    }
+  }
+  if (lane == 0) part[wid] = pair;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    for (int i = 1; i < kRowThreads / 32; ++i) join_pair(pair, part[i]);
+    a.stats[blockIdx.x] = pair;
+  }
+}
+
 struct CeJoin {
   const float2* stats;
   const float* picked;
@@ -146,21 +245,16 @@ __global__ void __launch_bounds__(256) ce_join_kernel(const CeJoin a) {
   pdl_wait();
   __shared__ float2 part[8][33];
   const int r = threadIdx.x & 31, g = threadIdx.x >> 5, row = blockIdx.x * 32 + r;
-  float m = -CUDART_INF_F, s = 0.f;
-  auto join = [&](float2 p) {
-    const float mn = fmaxf(m, p.x), ref = mn == -CUDART_INF_F ? 0.f : mn;
-    s = s * ex2(m - ref) + p.y * ex2(p.x - ref);
-    m = mn;
-  };
+  float2 pair = make_float2(-CUDART_INF_F, 0.f);
   if (row < a.T) {
 #pragma unroll 4
-    for (int i = g; i < a.tiles; i += 8) join(__ldg(a.stats + (int64_t)i * a.T + row));
+    for (int i = g; i < a.tiles; i += 8) join_pair(pair, __ldg(a.stats + (int64_t)i * a.T + row));
   }
-  part[g][r] = make_float2(m, s);
+  part[g][r] = pair;
   __syncthreads();
   if (g == 0 && row < a.T) {
-    for (int i = 1; i < 8; ++i) join(part[i][r]);
-    const float lse = (m + log2f(s)) * kLn2;
+    for (int i = 1; i < 8; ++i) join_pair(pair, part[i][r]);
+    const float lse = (pair.x + log2f(pair.y)) * kLn2;
     const int64_t t = a.target[row];
     a.lse[row] = lse;
     a.each[row] = t == a.ignore ? 0.f : t >= 0 && t < a.V ? lse - a.picked[row] : CUDART_NAN_F;
@@ -409,7 +503,8 @@ static int64_t div_up(int64_t a, int64_t b) { return (a + b - 1) / b; }
 struct CePlan {
   int64_t T, V, D;
   int tile_m;                 // rows of a token tile: a CTA pair's 256, or 128 where no more tokens are there
-  int64_t tiles;              // vocabulary tiles of the forward product
+  bool row;                   // forward: the form for one token
+  int64_t tiles;              // pairs per token that the forward product leaves: one per vocabulary tile, or per block
   int64_t piece, ld_g;        // gradient: vocabulary rows of a piece, row pitch of g
   int pieces, slices;         // slices of the vocabulary in the product for dh
   int64_t off_picked, off_each, forward_bytes;
@@ -420,7 +515,9 @@ static CePlan ce_plan(int64_t T, int64_t V, int64_t D) {
   CePlan p = {};
   p.T = T; p.V = V; p.D = D;
   p.tile_m = T <= 128 ? 128 : 256;
+  p.row = T == 1 && D <= kRowMaxD;
   p.tiles = div_up(V, kCeTile);
+  if (p.row) p.tiles = div_up(V, 2 * kRowThreads / 32) < 2 * 148 ? div_up(V, 2 * kRowThreads / 32) : 2 * 148;   // blocks: two per SM
   p.off_picked = up256(p.tiles * T * 8);
   p.off_each = p.off_picked + up256(T * 4);
   p.forward_bytes = p.off_each + up256(T * 4);
@@ -494,9 +591,19 @@ static int ce_scores(const char* what, const CePlan& p, const void* h, const voi
   if (rc == SP_OK) rc = make_map_any(&tmA, h, 2, p.T, p.D, p.D, 128, 64);
   if (rc == SP_OK) rc = make_map_any(&tmB, W, 2, cols, p.D, p.D, p.tile_m == 256 ? 128 : 256, 64);
   if (rc != SP_OK) return rc;
-  const ProdArgs a = ce_args(sched, status, p.T, cols, p.D, 1);
+  ProdArgs a = ce_args(sched, status, p.T, cols, p.D, 1);
+  a.turn = sched.Tm == 1;
   if (p.tile_m == 256) return launch_product<2, 256, kElem16, false, false, Epi>(what, tmA, tmB, tmC ? *tmC : tmA, a, bf16, ea, stream);
   return launch_product<1, 256, kElem16, false, false, Epi>(what, tmA, tmB, tmC ? *tmC : tmA, a, bf16, ea, stream);
+}
+
+static int launch_row(const RowArgs& a, int blocks, cudaStream_t stream) {
+  static uint64_t configured = 0;
+  if (first_use_on_this_device(configured)) {
+    const cudaError_t e = cudaFuncSetAttribute(row_stats_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(kRowMaxD * 4));
+    if (e != cudaSuccess) { configured = 0; set_error("cudaFuncSetAttribute failed: %s", cudaGetErrorString(e)); return SP_ERR_CUDA; }
+  }
+  return launch_pdl("row products", row_stats_kernel, dim3((unsigned)blocks), kRowThreads, (size_t)a.D * 4, 1, stream, a);
 }
 
 }  // namespace sp
@@ -528,7 +635,12 @@ int sp_linear_ce(const void* h, const void* W, const int64_t* target, float* lse
   if (rc != SP_OK) return rc;
   char* ws = (char*)workspace;
   const EpiStats::Args ea = {(float2*)ws, (float*)(ws + p.off_picked), target};
-  rc = ce_scores<EpiStats>("vocabulary product", p, h, W, V, st.status, dtype == SP_BF16, nullptr, ea, (cudaStream_t)stream);
+  if (p.row) {
+    const RowArgs ra = {(const uint16_t*)W, (const uint16_t*)h, target, ea.stats, ea.picked, (int)V, (int)D, dtype == SP_BF16};
+    rc = launch_row(ra, (int)p.tiles, (cudaStream_t)stream);
+  } else {
+    rc = ce_scores<EpiStats>("vocabulary product", p, h, W, V, st.status, dtype == SP_BF16, nullptr, ea, (cudaStream_t)stream);
+  }
   if (rc != SP_OK) return rc;
   CeJoin j = {};
   j.stats = ea.stats; j.picked = ea.picked; j.target = target; j.lse = lse;

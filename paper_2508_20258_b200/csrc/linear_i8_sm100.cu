@@ -498,18 +498,22 @@ few_tokens_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant
   if (warp == 0) {
     bool ok = true;
     auto stage_addr = [&](int i) { return smem_base + (uint32_t)(i % S) * C::kStageBytes; };
+    // Blocks start their walk along k at different places: they all read the same few lines of the tokens, and in step would queue for
+    // them in one L2 slice.
+    const int n_k = k1 - k0, turn = (int)(blockIdx.x / nranks) * 5 % n_k;
+    auto k_at = [&](int i) { return (k0 + (i + turn < n_k ? i + turn : i + turn - n_k)) * 128; };
     const int ahead = min(S, k1 - k0);
     if (!args.early) pdl_wait();
     if (elect_one()) {
       for (int i = 0; i < ahead; ++i) {
         mbar_arrive_expect_tx(bar_full + 8 * i, C::kStageBytes);
-        tma_load_2d<1>(stage_addr(i), &tmW, (k0 + i) * 128, n0, bar_full + 8 * i);
+        tma_load_2d<1>(stage_addr(i), &tmW, k_at(i), n0, bar_full + 8 * i);
       }
     }
     __syncwarp();
     if (args.early) pdl_wait();
     if (elect_one()) {
-      for (int i = 0; i < ahead; ++i) tma_load_2d<1>(stage_addr(i) + C::kWBytes, &tmQ, (k0 + i) * 128, 0, bar_full + 8 * i);
+      for (int i = 0; i < ahead; ++i) tma_load_2d<1>(stage_addr(i) + C::kWBytes, &tmQ, k_at(i), 0, bar_full + 8 * i);
     }
     __syncwarp();
     for (int i = S; i < k1 - k0; ++i) {
@@ -519,8 +523,8 @@ few_tokens_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant
       if (!ok) break;
       if (elect_one()) {
         mbar_arrive_expect_tx(bar_full + 8 * st, C::kStageBytes);
-        tma_load_2d<1>(stage_addr(i), &tmW, (k0 + i) * 128, n0, bar_full + 8 * st);
-        tma_load_2d<1>(stage_addr(i) + C::kWBytes, &tmQ, (k0 + i) * 128, 0, bar_full + 8 * st);
+        tma_load_2d<1>(stage_addr(i), &tmW, k_at(i), n0, bar_full + 8 * st);
+        tma_load_2d<1>(stage_addr(i) + C::kWBytes, &tmQ, k_at(i), 0, bar_full + 8 * st);
       }
       __syncwarp();
     }

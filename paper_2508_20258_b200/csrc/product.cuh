@@ -49,7 +49,8 @@ struct ProdArgs {
   int M, N;              // rows of A, rows of B
   int kblocks;           // stages that cover k
   int splits, kb_split;  // slices of k, stages per slice (slice z: [z * kb_split, min(kblocks, (z + 1) * kb_split)))
-  int k_last_first;      // 1: slices are walked from the last to the first (see launch_product's callers)
+  int turn;              // 1: units start their walk along k at different places (one tile row: all read the same few lines of A, and
+                         //    in step they would queue for them in one L2 slice: one token, 32768 x 4096 words, FILLTURN)
   int units;             // CTAs or CTA pairs launched
   uint32_t idesc;        // instruction descriptor
   Sched sched;
@@ -237,7 +238,6 @@ product_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
     const int o = s - z * T;
     const int t = args.sched.use_table ? __ldg(args.perm + o) : slot_to_tile(args.sched, o);
     tm = t / Tn; tn = t - tm * Tn;
-    if (args.k_last_first) z = args.splits - 1 - z;
   };
   auto k_range = [&](int z, int& k0, int& k1) {
     k0 = z * args.kb_split;
@@ -254,6 +254,7 @@ product_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
       tile_at(s, tm, tn, z);
       k_range(z, k0, k1);
       const int row0 = tm * 128 * CG + (int)rank * 128, col0 = tn * BN + (int)rank * C::kBCols;
+      int at = args.turn ? k0 + (unit * 5) % (k1 - k0) : k0;      // the k-block to load
       for (int kb = k0; kb < k1; ++kb) {
         ok = mbar_wait(bar_empty + 8 * stage, phase ^ 1u, args.status, (kProdProducer << 8) | 1);
         ok = __all_sync(0xffffffffu, ok);
@@ -261,7 +262,8 @@ product_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
         const uint32_t full_local = bar_full + 8 * stage;
         const uint32_t full_leader = CG == 1 ? full_local : mapa(full_local, 0);
         const uint32_t sa = smem_base + stage * C::kStageBytes, sb = sa + C::kABytes;
-        const int k = kb * C::kBK;
+        const int k = at * C::kBK;
+        if (++at == k1) at = k0;
         if (elect_one()) {
           if (rank == 0) mbar_arrive_expect_tx(full_local, CG * C::kStageBytes);
           if constexpr (A_MN) {
