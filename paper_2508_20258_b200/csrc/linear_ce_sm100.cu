@@ -3,8 +3,8 @@
 //   z = h . W^T  (T x V),   lse_t = log sum_v exp z_tv,   loss_t = lse_t - z_t,target(t)
 //   g_tv = c_t (exp(z_tv - lse_t) - [v = target(t)]),     dh = g . W,   dW = g^T . h
 //
-// Forward: the product runs tile by tile on the tensor cores; the epilogue reduces each tile's 256 columns of a row to a
-// (maximum, sum of exponentials) pair, so T x V scores become T x V / 256 pairs, which a second kernel joins.
+// Forward: the product runs tile by tile on the tensor cores; the epilogue reduces 128 columns of a row to a
+// (maximum, sum of exponentials) pair, so T x V scores become T x V / 128 pairs, which a second kernel joins.
 // Gradient: the vocabulary is walked in pieces.  A piece's scores are made again, turned into g in the epilogue and written as 16 bits;
 // two more products read them: dh += g . W_piece (k = the vocabulary) and dW_piece = g^T . h (k = the tokens).
 #include <math_constants.h>
@@ -20,6 +20,7 @@ namespace sp {
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr int kCeTile = 256;     // vocabulary columns of one tile
+constexpr int kCePart = 128;     // and of one epilogue warp
 constexpr int kMaxSplits = 64;   // slices of the vocabulary in the product for dh
 
 __device__ __forceinline__ float ex2(float x) {
@@ -38,69 +39,65 @@ __device__ __forceinline__ void tma_add_3d(const CUtensorMap* map, uint32_t src,
 }
 
 // ------------------------------------------------------------------ forward: statistics of a tile's rows
-// Per row the running maximum m (in powers of two: m = max z * log2 e, rounded once) and s = sum 2^(z log2 e - m).  Any m serves as
-// long as the joined result uses the same one, so its rounding costs nothing.  64 columns at a time: one rescaling of
-// s per 64 exponentials.
+// Per row and 128 columns the maximum m (in powers of two: m = max z * log2 e, rounded once) and s = sum 2^(z log2 e - m).  Any m serves
+// as long as the joined result uses the same one, so its rounding costs nothing.
+//
+// The tensor cores cut what they add off behind the accumulator's last bit, 16 products at a time, always towards zero: over D = 4096 the scores
+// came out 3e-6 too small.  So an accumulator takes 512 products only and the epilogue adds such sums, rounded to nearest.
+// What bounds it: 128 x 256 exponentials per CTA and tile at 16 a clock, 2048 cycles beside 512 for every 64 of D.
+constexpr int kCeSum = 8;      // stages of 64 products per accumulator
 struct EpiStats {
   static constexpr uint32_t kBytes = 0;
+  static constexpr bool kSums = true;
   struct Args {
-    float2* stats;            // [tile column][row]
+    float2* stats;            // [column / 128][row]
     float* picked;            // score of the row's target
     const int64_t* target;
   };
   const Args& a;
   int lane;
-  int rel;                    // the row's target, as a column of this tile; -1: not here
+  int rel;                    // the row's target, as a column of this part; -1: not here
   __device__ EpiStats(const Args& args, const CUtensorMap*, uint32_t, int, int l) : a(args), lane(l) {}
   __device__ __forceinline__ void before(const EpiTile& e, int M, int N) {
     const int row = e.row0 + lane;
     const int64_t t = row < M ? __ldg(a.target + row) : -1;
-    rel = t >= e.col0 && t < N && t < (int64_t)e.col0 + kCeTile ? (int)(t - e.col0) : -1;
+    rel = t >= e.col0 && t < N && t < (int64_t)e.col0 + kCePart ? (int)(t - e.col0) : -1;
   }
-  template <int BN>
-  __device__ __forceinline__ void tile(const EpiTile& e, int M, int N) {
-    static_assert(BN == kCeTile, "");
-    float m = -CUDART_INF_F, s = 0.f, hit = 0.f;
-#pragma unroll 1
-    for (int q = 0; q < BN / 64; ++q) {
-      uint32_t v[32], w[32];
-      tmem_ld_32x32b_x32(e.taddr + (uint32_t)(q * 64), v);
-      tmem_ld_32x32b_x32(e.taddr + (uint32_t)(q * 64 + 32), w);
-      tmem_ld_wait();
-      const int col = e.col0 + q * 64;
-      if (col + 64 > N) {     // columns beyond the vocabulary
+  template <int COLS>
+  __device__ __forceinline__ void finish(uint32_t (&v)[COLS], const EpiTile& e, int M, int N) {
+    static_assert(COLS == kCePart, "");
+    if (e.col0 >= N) return;
+    if (e.col0 + COLS > N) {     // columns beyond the vocabulary
 #pragma unroll
-        for (int j = 0; j < 32; ++j) {
-          if (col + j >= N) v[j] = 0xff800000u;
-          if (col + 32 + j >= N) w[j] = 0xff800000u;
-        }
-      }
-      if (rel >= q * 64 && rel < q * 64 + 64) {
-#pragma unroll
-        for (int j = 0; j < 32; ++j) {
-          if (rel == q * 64 + j) hit = __uint_as_float(v[j]);
-          if (rel == q * 64 + 32 + j) hit = __uint_as_float(w[j]);
-        }
-      }
-      float top = __uint_as_float(v[0]);
-#pragma unroll
-      for (int j = 0; j < 32; ++j) top = fmaxf(fmaxf(top, __uint_as_float(v[j])), __uint_as_float(w[j]));
-      const float mn = fmaxf(m, top * kLog2e);
-      const float ref = mn == -CUDART_INF_F ? 0.f : mn;    // nothing finite yet: every term is exp2(-inf) = 0
-      float s0 = 0.f, s1 = 0.f, s2 = 0.f, s3 = 0.f;
-#pragma unroll
-      for (int j = 0; j < 32; j += 2) {
-        s0 += ex2(fmaf(__uint_as_float(v[j]), kLog2e, -ref));
-        s1 += ex2(fmaf(__uint_as_float(w[j]), kLog2e, -ref));
-        s2 += ex2(fmaf(__uint_as_float(v[j + 1]), kLog2e, -ref));
-        s3 += ex2(fmaf(__uint_as_float(w[j + 1]), kLog2e, -ref));
-      }
-      s = fmaf(s, ex2(m - ref), (s0 + s1) + (s2 + s3));
-      m = mn;
+      for (int j = 0; j < COLS; ++j)
+        if (e.col0 + j >= N) v[j] = 0xff800000u;
     }
+    float hit = 0.f;
+    if (__any_sync(0xffffffffu, rel >= 0)) {
+#pragma unroll
+      for (int j = 0; j < COLS; ++j)
+        if (rel == j) hit = __uint_as_float(v[j]);
+    }
+    float t[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) t[i] = __uint_as_float(v[i]);
+#pragma unroll
+    for (int j = 8; j < COLS; j += 16) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) t[i] = j + 8 + i < COLS ? fmaxf(fmaxf(t[i], __uint_as_float(v[j + i])), __uint_as_float(v[j + 8 + i])) : fmaxf(t[i], __uint_as_float(v[j + i]));
+    }
+    const float m = fmaxf(fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3])), fmaxf(fmaxf(t[4], t[5]), fmaxf(t[6], t[7]))) * kLog2e;
+    const float ref = m == -CUDART_INF_F ? 0.f : m;    // nothing finite here: every term is exp2(-inf) = 0
+    float s[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) s[i] = 0.f;
+#pragma unroll
+    for (int j = 0; j < COLS; j += 8)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) s[i] += ex2(fmaf(__uint_as_float(v[j + i]), kLog2e, -ref));
     const int row = e.row0 + lane;
     if (row < M) {
-      a.stats[(int64_t)e.tn * M + row] = make_float2(m, s);
+      a.stats[(int64_t)(e.col0 / kCePart) * M + row] = make_float2(m, ((s[0] + s[1]) + (s[2] + s[3])) + ((s[4] + s[5]) + (s[6] + s[7])));
       if (rel >= 0) a.picked[row] = hit;
     }
   }
@@ -335,10 +332,23 @@ __global__ void __launch_bounds__(1024) ce_coef_kernel(const CeCoef a) {
   if (threadIdx.x == 0) *a.factor = factor * exp2f((float)-up);
 }
 
+// One staged slice of 64 16-bit columns to a matrix.
+__device__ __forceinline__ void store_part(const EpiStage& stage, const CUtensorMap* map, int lane, const uint32_t (&p)[32], bool inside, int col, int row) {
+  const uint32_t slice = stage.free();
+  stage_row(slice, lane, p);
+  fence_async_smem();
+  __syncwarp();
+  if (lane == 0 && inside) {
+    tma_store_2d(map, slice, col, row);
+    bulk_commit();
+  }
+}
+
 // g of a tile, to 16 bits: its rounding (half a step, 2^-9 of bf16 or 2^-12 of fp16 relative) is independent from entry to entry and
 // enters sums over the vocabulary or the tokens, so it moves a gradient by less than the gradient's own rounding to the same type.
 struct EpiG {
-  static constexpr uint32_t kBytes = 4 * 2 * 4096;
+  static constexpr uint32_t kBytes = 8 * 4096;
+  static constexpr bool kSums = false;
   struct Args {
     const float* lse;
     const float* coef;
@@ -351,54 +361,33 @@ struct EpiG {
   EpiStage stage;
   int lane, rel;
   float lse2, c;
-  __device__ EpiG(const Args& args, const CUtensorMap* m, uint32_t base, int w, int l)
-      : a(args), map(m), stage{base + (uint32_t)w * 8192u, 0}, lane(l) {}
+  __device__ EpiG(const Args& args, const CUtensorMap* m, uint32_t base, int w, int l) : a(args), map(m), stage{base + (uint32_t)w * 4096u, l}, lane(l) {}
   __device__ __forceinline__ void before(const EpiTile& e, int M, int) {
     const int row = e.row0 + lane;
     const bool in = row < M;
     c = in ? __ldg(a.coef + row) : 0.f;
     lse2 = in ? __ldg(a.lse + row) * kLog2e : 0.f;
     const int64_t t = in ? __ldg(a.target + row) - a.v0 - e.col0 : -1;
-    rel = t >= 0 && t < kCeTile ? (int)t : -1;
+    rel = t >= 0 && t < kCePart ? (int)t : -1;
   }
-  template <int BN>
-  __device__ __forceinline__ void tile(const EpiTile& e, int M, int N) {
-#pragma unroll 1
-    for (int q = 0; q < BN / 64; ++q) {
-      uint32_t v[32], w[32], p[32];
-      tmem_ld_32x32b_x32(e.taddr + (uint32_t)(q * 64), v);
-      tmem_ld_32x32b_x32(e.taddr + (uint32_t)(q * 64 + 32), w);
-      tmem_ld_wait();
+  template <int COLS>
+  __device__ __forceinline__ void finish(uint32_t (&v)[COLS], const EpiTile& e, int M, int N) {
+#pragma unroll
+    for (int j = 0; j < COLS; ++j) v[j] = __float_as_uint(ex2(fmaf(__uint_as_float(v[j]), kLog2e, -lse2)));
+    if (__any_sync(0xffffffffu, rel >= 0)) {
+#pragma unroll
+      for (int j = 0; j < COLS; ++j)
+        if (rel == j) v[j] = __float_as_uint(__uint_as_float(v[j]) - 1.f);
+    }
+#pragma unroll
+    for (int q = 0; q < COLS / 64; ++q) {
+      uint32_t p[32];
 #pragma unroll
       for (int j = 0; j < 32; ++j) {
-        v[j] = __float_as_uint(ex2(fmaf(__uint_as_float(v[j]), kLog2e, -lse2)));
-        w[j] = __float_as_uint(ex2(fmaf(__uint_as_float(w[j]), kLog2e, -lse2)));
+        p[j] = pack_16(__uint_as_float(v[q * 64 + 2 * j]) * c, __uint_as_float(v[q * 64 + 2 * j + 1]) * c, a.bf16);
+        if (c == 0.f) p[j] = 0;     // a token that does not count: exactly nothing, whatever its scores are
       }
-      if (rel >= q * 64 && rel < q * 64 + 64) {
-#pragma unroll
-        for (int j = 0; j < 32; ++j) {
-          if (rel == q * 64 + j) v[j] = __float_as_uint(__uint_as_float(v[j]) - 1.f);
-          if (rel == q * 64 + 32 + j) w[j] = __float_as_uint(__uint_as_float(w[j]) - 1.f);
-        }
-      }
-#pragma unroll
-      for (int j = 0; j < 16; ++j) {
-        p[j] = pack_16(__uint_as_float(v[2 * j]) * c, __uint_as_float(v[2 * j + 1]) * c, a.bf16);
-        p[16 + j] = pack_16(__uint_as_float(w[2 * j]) * c, __uint_as_float(w[2 * j + 1]) * c, a.bf16);
-      }
-      if (c == 0.f) {          // a token that does not count: exactly nothing, whatever its scores are
-#pragma unroll
-        for (int j = 0; j < 32; ++j) p[j] = 0;
-      }
-      const uint32_t slice = stage.next(lane);
-      stage_row(slice, lane, p);
-      fence_async_smem();
-      __syncwarp();
-      if (lane == 0) {
-        const int col = e.col0 + q * 64;
-        if (e.row0 < M && col < N) tma_store_2d(map, slice, col, e.row0);
-        bulk_commit();
-      }
+      store_part(stage, map, lane, p, e.row0 < M && e.col0 + q * 64 < N, e.col0 + q * 64, e.row0);
     }
   }
 };
@@ -406,32 +395,27 @@ struct EpiG {
 // fp32 sums of a slice of the vocabulary: stored by the first piece, added to by the later ones (each element once per piece,
 // in stream order: the same bits every time).
 struct EpiSum {
-  static constexpr uint32_t kBytes = 4 * 2 * 4096;
+  static constexpr uint32_t kBytes = 8 * 4096;
+  static constexpr bool kSums = false;
   struct Args { int add; };
   const Args& a;
   const CUtensorMap* map;
   EpiStage stage;
   int lane;
-  __device__ EpiSum(const Args& args, const CUtensorMap* m, uint32_t base, int w, int l)
-      : a(args), map(m), stage{base + (uint32_t)w * 8192u, 0}, lane(l) {}
+  __device__ EpiSum(const Args& args, const CUtensorMap* m, uint32_t base, int w, int l) : a(args), map(m), stage{base + (uint32_t)w * 4096u, l}, lane(l) {}
   __device__ __forceinline__ void before(const EpiTile&, int, int) {}
-  template <int BN>
-  __device__ __forceinline__ void tile(const EpiTile& e, int M, int N) {
-#pragma unroll 1
-    for (int q = 0; q < BN / 32; ++q) {
-      uint32_t v[32];
-      tmem_ld_32x32b_x32(e.taddr + (uint32_t)(q * 32), v);
-      tmem_ld_wait();
-      const uint32_t slice = stage.next(lane);
-      stage_row(slice, lane, v);
+  template <int COLS>
+  __device__ __forceinline__ void finish(uint32_t (&v)[COLS], const EpiTile& e, int M, int N) {
+#pragma unroll
+    for (int q = 0; q < COLS / 32; ++q) {
+      const uint32_t slice = stage.free();
+      stage_row(slice, lane, *reinterpret_cast<uint32_t(*)[32]>(v + q * 32));
       fence_async_smem();
       __syncwarp();
-      if (lane == 0) {
-        const int col = e.col0 + q * 32;
-        if (e.row0 < M && col < N) {
-          if (a.add) tma_add_3d(map, slice, col, e.row0, e.z);
-          else tma_store_3d(map, slice, col, e.row0, e.z);
-        }
+      const int col = e.col0 + q * 32;
+      if (lane == 0 && e.row0 < M && col < N) {
+        if (a.add) tma_add_3d(map, slice, col, e.row0, e.z);
+        else tma_store_3d(map, slice, col, e.row0, e.z);
         bulk_commit();
       }
     }
@@ -440,7 +424,8 @@ struct EpiSum {
 
 // A finished gradient, to its 16-bit type.
 struct EpiOut16 {
-  static constexpr uint32_t kBytes = 4 * 2 * 4096;
+  static constexpr uint32_t kBytes = 8 * 4096;
+  static constexpr bool kSums = false;
   struct Args {
     const float* factor;
     int bf16;
@@ -451,29 +436,16 @@ struct EpiOut16 {
   int lane;
   float factor;
   __device__ EpiOut16(const Args& args, const CUtensorMap* m, uint32_t base, int w, int l)
-      : a(args), map(m), stage{base + (uint32_t)w * 8192u, 0}, lane(l), factor(__ldg(args.factor)) {}
+      : a(args), map(m), stage{base + (uint32_t)w * 4096u, l}, lane(l), factor(__ldg(args.factor)) {}
   __device__ __forceinline__ void before(const EpiTile&, int, int) {}
-  template <int BN>
-  __device__ __forceinline__ void tile(const EpiTile& e, int M, int N) {
-#pragma unroll 1
-    for (int q = 0; q < BN / 64; ++q) {
-      uint32_t v[32], w[32];
-      tmem_ld_32x32b_x32(e.taddr + (uint32_t)(q * 64), v);
-      tmem_ld_32x32b_x32(e.taddr + (uint32_t)(q * 64 + 32), w);
-      tmem_ld_wait();
+  template <int COLS>
+  __device__ __forceinline__ void finish(uint32_t (&v)[COLS], const EpiTile& e, int M, int N) {
 #pragma unroll
-      for (int j = 0; j < 16; ++j) v[j] = pack_16(__uint_as_float(v[2 * j]) * factor, __uint_as_float(v[2 * j + 1]) * factor, a.bf16);
+    for (int q = 0; q < COLS / 64; ++q) {
+      uint32_t p[32];
 #pragma unroll
-      for (int j = 0; j < 16; ++j) v[16 + j] = pack_16(__uint_as_float(w[2 * j]) * factor, __uint_as_float(w[2 * j + 1]) * factor, a.bf16);
-      const uint32_t slice = stage.next(lane);
-      stage_row(slice, lane, v);
-      fence_async_smem();
-      __syncwarp();
-      if (lane == 0) {
-        const int col = e.col0 + q * 64;
-        if (e.row0 < M && col < N) tma_store_2d(map, slice, col, e.row0);
-        bulk_commit();
-      }
+      for (int j = 0; j < 32; ++j) p[j] = pack_16(__uint_as_float(v[q * 64 + 2 * j]) * factor, __uint_as_float(v[q * 64 + 2 * j + 1]) * factor, a.bf16);
+      store_part(stage, map, lane, p, e.row0 < M && e.col0 + q * 64 < N, e.col0 + q * 64, e.row0);
     }
   }
 };
@@ -504,7 +476,7 @@ struct CePlan {
   int64_t T, V, D;
   int tile_m;                 // rows of a token tile: a CTA pair's 256, or 128 where no more tokens are there
   bool row;                   // forward: the form for one token
-  int64_t tiles;              // pairs per token that the forward product leaves: one per vocabulary tile, or per block
+  int64_t tiles;              // pairs per token that the forward product leaves: one per 128 words, or per block
   int64_t piece, ld_g;        // gradient: vocabulary rows of a piece, row pitch of g
   int pieces, slices;         // slices of the vocabulary in the product for dh
   int64_t off_picked, off_each, forward_bytes;
@@ -516,7 +488,7 @@ static CePlan ce_plan(int64_t T, int64_t V, int64_t D) {
   p.T = T; p.V = V; p.D = D;
   p.tile_m = T <= 128 ? 128 : 256;
   p.row = T == 1 && D <= kRowMaxD;
-  p.tiles = div_up(V, kCeTile);
+  p.tiles = div_up(V, kCePart);
   if (p.row) p.tiles = div_up(V, 2 * kRowThreads / 32) < 2 * 148 ? div_up(V, 2 * kRowThreads / 32) : 2 * 148;   // blocks: two per SM
   p.off_picked = up256(p.tiles * T * 8);
   p.off_each = p.off_picked + up256(T * 4);
@@ -577,6 +549,7 @@ static ProdArgs ce_args(const Sched& sched, int32_t* status, int64_t M, int64_t 
   a.kblocks = (int)div_up(K, 64);
   a.kb_split = (int)div_up(a.kblocks, slices);
   a.splits = (int)div_up(a.kblocks, a.kb_split);
+  a.kb_sum = kCeSum;
   a.sched = sched;
   return a;
 }

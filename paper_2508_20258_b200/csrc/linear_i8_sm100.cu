@@ -195,84 +195,74 @@ __global__ void __launch_bounds__(kQuantThreads, sizeof(T) == 2 ? 5 : 4) quantiz
 }
 
 // ------------------------------------------------------------------ epilogue of the tiled product
+// PLAIN: rows of C that a bulk store cannot take.
 // c = (float(acc) * a_scale[row]) * b_scale[col]: the integer rounds once to fp32, then one rounding per factor (the two
 // scales are not multiplied first: their product can leave fp32's range where the result does not).
-template <bool OUT_F32>
+template <bool OUT_F32, bool PLAIN>
 struct EpiI8 {
-  static constexpr uint32_t kBytes = 4 * 2 * 4096 + 4 * 256;   // staging, then 64 column scales per warp
+  static constexpr uint32_t kBytes = 8 * 4096 + (PLAIN ? 8 * 512 : 0);   // staging, then what rows without bulk stores carry from slice to slice
+  static constexpr bool kSums = false;
   struct Args {
     const float* a_scale;
     const float* b_scale;
     char* C;
     int64_t ld_bytes;
     int bf16;     // 16-bit output: bf16, else fp16
-    int plain;    // rows of C that a bulk store cannot take
   };
   const Args& a;
   const CUtensorMap* map;
   EpiStage stage;
-  uint32_t scales;
+  uint32_t carry;
   int lane;
   float rs;
-  float b0, b1;      // column scales of the chunk to come, a column (two for 16-bit results) per lane
+  float bs[4];      // column scales: column 32 i + lane
   __device__ EpiI8(const Args& args, const CUtensorMap* m, uint32_t base, int w, int l)
-      : a(args), map(m), stage{base + (uint32_t)w * 8192u, 0}, scales(base + 32768u + (uint32_t)w * 256u), lane(l) {}
-  __device__ __forceinline__ void fetch(int col, int N) {
-    b0 = col + lane < N ? __ldg(a.b_scale + col + lane) : 0.f;
-    if constexpr (!OUT_F32) b1 = col + 32 + lane < N ? __ldg(a.b_scale + col + 32 + lane) : 0.f;
-  }
+      : a(args), map(m), stage{base + (uint32_t)w * 4096u, l}, carry(base + 32768u + (uint32_t)w * 512u), lane(l) {}
   __device__ __forceinline__ void before(const EpiTile& e, int M, int N) {
     rs = e.row0 + lane < M ? __ldg(a.a_scale + e.row0 + lane) : 0.f;
-    fetch(e.col0, N);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) bs[i] = e.col0 + 32 * i + lane < N ? __ldg(a.b_scale + e.col0 + 32 * i + lane) : 0.f;
   }
-  template <int BN>
-  __device__ __forceinline__ void tile(const EpiTile& e, int M, int N) {
+  template <int COLS>
+  __device__ __forceinline__ void finish(uint32_t (&v)[COLS], const EpiTile& e, int M, int N) {
+    // the column scales pass through the (free) slice: every lane needs all of them
+    const uint32_t slice = stage.free();
+#pragma unroll
+    for (int i = 0; i < COLS / 32; ++i) asm volatile("st.shared.f32 [%0], %1;" ::"r"(slice + i * 128 + lane * 4), "f"(bs[i]) : "memory");
+    __syncwarp();
+#pragma unroll
+    for (int j = 0; j < COLS / 4; ++j) {
+      float4 f;
+      asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(f.x), "=f"(f.y), "=f"(f.z), "=f"(f.w) : "r"(slice + j * 16));
+      v[4 * j] = __float_as_uint((float)(int)v[4 * j] * rs * f.x);
+      v[4 * j + 1] = __float_as_uint((float)(int)v[4 * j + 1] * rs * f.y);
+      v[4 * j + 2] = __float_as_uint((float)(int)v[4 * j + 2] * rs * f.z);
+      v[4 * j + 3] = __float_as_uint((float)(int)v[4 * j + 3] * rs * f.w);
+    }
+    __syncwarp();
     constexpr int kCols = OUT_F32 ? 32 : 64;
-    // a loop, not unrolled: both ways of storing make it long, and four warps with one instruction stream each live on the instruction cache
-#pragma unroll 1
-    for (int q = 0; q < BN / kCols; ++q) {
-      uint32_t v[32], w[32];
-      tmem_ld_32x32b_x32(e.taddr + (uint32_t)(q * kCols), v);
-      if constexpr (!OUT_F32) tmem_ld_32x32b_x32(e.taddr + (uint32_t)(q * kCols + 32), w);
-      asm volatile("st.shared.f32 [%0], %1;" ::"r"(scales + lane * 4), "f"(b0) : "memory");
-      if constexpr (!OUT_F32) asm volatile("st.shared.f32 [%0], %1;" ::"r"(scales + 128 + lane * 4), "f"(b1) : "memory");
-      if (q + 1 < BN / kCols) fetch(e.col0 + (q + 1) * kCols, N);
-      __syncwarp();
-      tmem_ld_wait();
-      auto scaled = [&](uint32_t (&r)[32], uint32_t at) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          float4 f;
-          asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(f.x), "=f"(f.y), "=f"(f.z), "=f"(f.w) : "r"(at + j * 16) : "memory");
-          r[4 * j] = __float_as_uint((float)(int)r[4 * j] * rs * f.x);
-          r[4 * j + 1] = __float_as_uint((float)(int)r[4 * j + 1] * rs * f.y);
-          r[4 * j + 2] = __float_as_uint((float)(int)r[4 * j + 2] * rs * f.z);
-          r[4 * j + 3] = __float_as_uint((float)(int)r[4 * j + 3] * rs * f.w);
-        }
-      };
-      scaled(v, scales);
-      if constexpr (!OUT_F32) {
-        scaled(w, scales + 128);
+    for (int q = 0; q < COLS / kCols; ++q) {
+      uint32_t p[32];
 #pragma unroll
-        for (int j = 0; j < 16; ++j) v[j] = pack_16(__uint_as_float(v[2 * j]), __uint_as_float(v[2 * j + 1]), a.bf16);
-#pragma unroll
-        for (int j = 0; j < 16; ++j) v[16 + j] = pack_16(__uint_as_float(w[2 * j]), __uint_as_float(w[2 * j + 1]), a.bf16);
+      for (int j = 0; j < 32; ++j) {
+        if constexpr (OUT_F32) p[j] = v[q * 32 + j];
+        else p[j] = pack_16(__uint_as_float(v[q * 64 + 2 * j]), __uint_as_float(v[q * 64 + 2 * j + 1]), a.bf16);
       }
-      const uint32_t slice = stage.next(lane);
-      stage_row(slice, lane, v);
+      if (q) stage.free();
+      stage_row(slice, lane, p);
       const int col = e.col0 + q * kCols;
       const bool inside = e.row0 < M && col < N;
-      if (a.plain) {
+      if constexpr (PLAIN) {
         constexpr int kElt = OUT_F32 ? 4 : 2;
-        if (inside) store_slice_plain<kElt>(stage.last(), slice, lane, a.C, a.ld_bytes, e.row0, col, M, min(128, (N - col) * kElt), q == 0,
-                                            q == BN / kCols - 1 || col + kCols >= N);
-        else __syncwarp();
+        if (inside) store_slice_plain<kElt>(carry, slice, lane, a.C, a.ld_bytes, e.row0, col, M, min(128, (N - col) * kElt), q == 0,
+                                            q == COLS / kCols - 1 || col + kCols >= N);
       } else {
         fence_async_smem();
         __syncwarp();
-        if (lane == 0) {
-          if (inside) tma_store_2d(map, slice, col, e.row0);
-          bulk_commit();   // also when nothing was stored: keeps the group count in step
+        if (lane == 0 && inside) {
+          tma_store_2d(map, slice, col, e.row0);
+          bulk_commit();
         }
       }
     }
@@ -697,8 +687,8 @@ static int check_i8(const void* A, const void* a_scale, const void* B, const voi
   }
   int tile_m = params ? params->tile_m : 0, tile_n = params ? params->tile_n : 0;
   const bool pick = tile_m == 0 && tile_n == 0;
-  if (!pick && !((tile_m == 256 && tile_n == 256) || (tile_m == 128 && (tile_n == 256 || tile_n == 128)))) {
-    set_error("unsupported tile %dx%d (supported: 128x128, 128x256, 256x256)", tile_m, tile_n);
+  if (!pick && !((tile_m == 256 && tile_n == 256) || (tile_m == 128 && tile_n == 128))) {
+    set_error("unsupported tile %dx%d (supported: 128x128, 256x256)", tile_m, tile_n);
     return SP_ERR_UNSUPPORTED;
   }
   call->A = A; call->B = B; call->a_scale = (const float*)a_scale; call->b_scale = (const float*)b_scale; call->C = const_cast<void*>(C);
@@ -707,7 +697,7 @@ static int check_i8(const void* A, const void* a_scale, const void* B, const voi
   if (call->few) return SP_OK;
   if (pick) {
     // the tile with the least waves x area / (CTAs per tile x relative rate of its shape); rates measured at 4096^3 and 8192^3
-    static const struct { int tm, tn; double eff; } kTiles[] = {{256, 256, 1.00}, {128, 256, 0.92}, {128, 128, 0.70}};
+    static const struct { int tm, tn; double eff; } kTiles[] = {{256, 256, 1.00}, {128, 128, 0.70}};
     double best = 0;
     for (const auto& t : kTiles) {
       const int64_t T = ((M + t.tm - 1) / t.tm) * ((N + t.tn - 1) / t.tn);
@@ -788,12 +778,12 @@ static int launch_few(const I8Call& c, const CUtensorMap& tmW, FewArgs args, cud
   return launch_pdl("few-token product", kern, dim3((unsigned)(blocks * split)), 192, C::kSmemBytes, split, stream, tmW, tmQ, args);
 }
 
-template <bool OUT_F32>
-static int launch_tiles(const I8Call& c, const ProdArgs& pa, const typename EpiI8<OUT_F32>::Args& ea, const CUtensorMap& tmA, const CUtensorMap& tmB,
-                        const CUtensorMap& tmC, cudaStream_t stream) {
-  if (c.tile_m == 256) return launch_product<2, 256, kElemI8, false, false, EpiI8<OUT_F32>>("8-bit product", tmA, tmB, tmC, pa, false, ea, stream);
-  if (c.tile_n == 256) return launch_product<1, 256, kElemI8, false, false, EpiI8<OUT_F32>>("8-bit product", tmA, tmB, tmC, pa, false, ea, stream);
-  return launch_product<1, 128, kElemI8, false, false, EpiI8<OUT_F32>>("8-bit product", tmA, tmB, tmC, pa, false, ea, stream);
+template <bool OUT_F32, bool PLAIN>
+static int launch_tiles(const I8Call& c, const ProdArgs& pa, const CUtensorMap& tmA, const CUtensorMap& tmB, const CUtensorMap& tmC, cudaStream_t stream) {
+  using Epi = EpiI8<OUT_F32, PLAIN>;
+  const typename Epi::Args ea = {c.a_scale, c.b_scale, (char*)c.C, c.N * (OUT_F32 ? 4 : 2), c.out == SP_BF16};
+  if (c.tile_m == 256) return launch_product<2, 256, kElemI8, false, false, Epi>("8-bit product", tmA, tmB, tmC, pa, false, ea, stream);
+  return launch_product<1, 128, kElemI8, false, false, Epi>("8-bit product", tmA, tmB, tmC, pa, false, ea, stream);
 }
 
 static int run_i8(const I8Call& c, bool early, cudaStream_t stream) {
@@ -827,12 +817,8 @@ static int run_i8(const I8Call& c, bool early, cudaStream_t stream) {
   if (plain) tmC = tmB;    // not used
   else rc = make_map_any(&tmC, c.C, elt, c.M, c.N, c.N, 32, 128 / elt);
   if (rc != SP_OK) return rc;
-  if (c.out == SP_FP32) {
-    EpiI8<true>::Args ea = {c.a_scale, c.b_scale, (char*)c.C, ld, 0, plain};
-    return launch_tiles<true>(c, pa, ea, tmA, tmB, tmC, stream);
-  }
-  EpiI8<false>::Args ea = {c.a_scale, c.b_scale, (char*)c.C, ld, c.out == SP_BF16, plain};
-  return launch_tiles<false>(c, pa, ea, tmA, tmB, tmC, stream);
+  if (c.out == SP_FP32) return plain ? launch_tiles<true, true>(c, pa, tmA, tmB, tmC, stream) : launch_tiles<true, false>(c, pa, tmA, tmB, tmC, stream);
+  return plain ? launch_tiles<false, true>(c, pa, tmA, tmB, tmC, stream) : launch_tiles<false, false>(c, pa, tmA, tmB, tmC, stream);
 }
 
 }  // namespace sp

@@ -1,10 +1,12 @@
 // The persistent tcgen05 pipeline of the linear-layer operators: D = A . B^T on tiles of 128*CG x BN, an epilogue of the
 // operator's own on the accumulator while the next tile's products run.
 //
-// Same machine as the bf16 GEMM (TMA producer warp, MMA issuer warp, four epilogue warps, two accumulator buffers in
+// Same machine as the bf16 GEMM (TMA producer warp, MMA issuer warp, epilogue warps, two accumulator buffers in
 // TMEM, mbarriers only, every wait bounded), cut down to what these operators need: a fixed stride through the slots
-// of a tile order, optionally repeated for `splits` slices of the k axis, and an `Epi` type that is handed 32 rows of
-// the accumulator at a time.  Operands are 8-bit integers (kind::i8, exact 32-bit integer sums) or 16-bit floats
+// of a tile order, optionally repeated for `splits` slices of the k axis, and an `Epi` type that is handed the accumulator.
+// Eight epilogue warps, two on each quarter of the TMEM lanes: a warp moves its 32 rows x half of the columns to registers, hands
+// the buffer back at once and only then computes (with four warps that worked on the buffer piece by piece the
+// epilogue of the cross entropy took 11.5 thousand cycles a tile and bounded every D up to 1024).  Operands are 8-bit integers (kind::i8, exact 32-bit integer sums) or 16-bit floats
 // (kind::f16, fp32 sums); either may be stored with k or with its other axis contiguous (16-bit types only).
 //
 // One stage holds 128 bytes of k per row (one swizzle row): 128 int8 or 64 16-bit elements.  CTA pairs (CG = 2) compute
@@ -40,7 +42,11 @@ struct ProdCfg {
   static constexpr int kStages = kFit > 8 ? 8 : kFit;
   static constexpr uint32_t kSmemBytes = kStages * kStageBytes + EPI_BYTES + kProdBarrierBytes + 1024;  // + alignment slack
   static constexpr int kTmemCols = 2 * BN;                      // two accumulator buffers (a power of two)
-  static constexpr int kThreads = 192;
+  // Warps: producer, MMA issuer, two that idle, eight of the epilogue.  The register file is re-divided between groups of four
+  // warps: 128 threads x 72 + 256 x 216 = 64512, what 384 threads x 168 were launched with.
+  static constexpr int kEpiWarps = 8, kEpi0 = 4;
+  static constexpr int kThreads = 32 * (kEpi0 + kEpiWarps);
+  static constexpr int kRegsIssue = 72, kRegsEpilogue = 216;
 };
 
 struct ProdArgs {
@@ -49,6 +55,7 @@ struct ProdArgs {
   int M, N;              // rows of A, rows of B
   int kblocks;           // stages that cover k
   int splits, kb_split;  // slices of k, stages per slice (slice z: [z * kb_split, min(kblocks, (z + 1) * kb_split)))
+  int kb_sum;            // stages whose products one accumulator takes before the epilogue adds it to its own sum (Epi::kSums; else a slice)
   int turn;              // 1: units start their walk along k at different places (one tile row: all read the same few lines of A, and
                          //    in step they would queue for them in one L2 slice: one token, 32768 x 4096 words, FILLTURN)
   int units;             // CTAs or CTA pairs launched
@@ -102,26 +109,20 @@ __device__ __forceinline__ uint32_t pack_16(float lo, float hi, bool bf16) {
   return *reinterpret_cast<const uint32_t*>(&v);
 }
 
-// What an epilogue is given: 32 rows of one tile's accumulator.
+// What an epilogue is given with the values of its part of a tile's accumulator (one row per lane).
 struct EpiTile {
-  uint32_t taddr;    // TMEM address of (first of the 32 lanes, first column of the tile)
-  int row0, col0;    // row of lane 0, first column of the tile
-  int tn;            // tile column
+  int row0, col0;    // row of lane 0, first column of the part
   int z;             // slice of k
 };
 
-// Staging of one epilogue warp: two slices of 32 rows x 128 bytes, used in turn; a slice may be overwritten once the
-// bulk store before last has read it.
+// Staging of one epilogue warp: 32 rows x 128 bytes on their way to a bulk store.
 struct EpiStage {
-  uint32_t base;
-  int chunk;
-  __device__ __forceinline__ uint32_t last() const { return base + (uint32_t)((chunk - 2) & 1) * 4096u; }   // the slice before the one handed out
-  __device__ __forceinline__ uint32_t next(int lane) {   // whole warp
-    if (chunk >= 2) {
-      if (lane == 0) bulk_wait_read_1();
-      __syncwarp();
-    }
-    return base + (uint32_t)(chunk++ & 1) * 4096u;
+  uint32_t slice;
+  int lane;
+  __device__ __forceinline__ uint32_t free() const {   // whole warp: the last store has read the slice
+    if (lane == 0) bulk_wait_read_0();
+    __syncwarp();
+    return slice;
   }
 };
 
@@ -140,12 +141,12 @@ __device__ __forceinline__ uint32_t ld_shared_32(uint32_t addr) {
 }
 
 // A staged slice to a matrix whose rows a bulk store cannot take (row pitch or address not a multiple of 16 bytes, but whole elements).
-// The slices of a tile come from left to right.  Each row is cut where its own addresses are multiples of 16: a window takes its first
-// bytes from the slice before (still staged) and the rest from this one, so that all but a tile's two edges is written 16 bytes
-// at a time, four rows per instruction.  (One element per lane, a row per instruction: 2001 x 4999 fp32 results of a
+// The slices of a part come from left to right.  Each row is cut where its own addresses are multiples of 16: a window takes its first
+// bytes from the slice before (its last 16 bytes are carried over) and the rest from this one, so that all but a part's two edges is
+// written 16 bytes at a time, four rows per instruction.  (One element per lane, a row per instruction: 2001 x 4999 fp32 results of a
 // 2048-long product 50 us, this way FILLPLAIN.)  `len`: bytes of this slice inside the matrix.
 template <int ELT>
-__device__ __forceinline__ void store_slice_plain(uint32_t before, uint32_t slice, int lane, char* out, int64_t ld_bytes, int row0, int col, int M, int len,
+__device__ __forceinline__ void store_slice_plain(uint32_t carry, uint32_t slice, int lane, char* out, int64_t ld_bytes, int row0, int col, int M, int len,
                                                   bool first, bool last) {
   __syncwarp();
   auto scalar = [&](int row, int w) {      // a window that is not whole: element by element
@@ -153,7 +154,8 @@ __device__ __forceinline__ void store_slice_plain(uint32_t before, uint32_t slic
     const int p = 16 * w - (int)((uintptr_t)a & 15u), lo = first && p < 0 ? 0 : p, hi = min(p + 16, len);
 #pragma unroll 1
     for (int q = lo; q < hi; q += ELT) {
-      const uint32_t b = (uint32_t)q & 127u, addr = (q < 0 ? before : slice) + (uint32_t)row * 128u + ((((b >> 4) ^ ((uint32_t)row & 7u)) << 4) | (b & 12u));
+      const uint32_t b = (uint32_t)q & 127u, addr = q < 0 ? carry + (uint32_t)row * 16u + (b & 12u)
+                                                            : slice + (uint32_t)row * 128u + ((((b >> 4) ^ ((uint32_t)row & 7u)) << 4) | (b & 12u));
       const uint32_t v = ld_shared_32(addr);
       if constexpr (ELT == 4) *reinterpret_cast<uint32_t*>(a + q) = v;
       else *reinterpret_cast<uint16_t*>(a + q) = (uint16_t)(b & 2u ? v >> 16 : v);
@@ -163,8 +165,7 @@ __device__ __forceinline__ void store_slice_plain(uint32_t before, uint32_t slic
   // unit w, put together by a shift of m bytes.  One warp runs per scheduler here, so the count of instructions is what costs.
   const int w = lane & 7, i0 = lane >> 3;
   char* a = out + (int64_t)(row0 + i0) * ld_bytes + (int64_t)col * ELT;
-  const uint32_t left = w ? slice : before, wl = (uint32_t)(w - 1) & 7u;
-  const uint32_t ua = (uint32_t)i0 * 128u + (((uint32_t)w ^ (uint32_t)i0) << 4), ub = (uint32_t)i0 * 128u + ((wl ^ (uint32_t)i0) << 4);
+    const uint32_t ua = (uint32_t)i0 * 128u + (((uint32_t)w ^ (uint32_t)i0) << 4), ub = (uint32_t)i0 * 128u + (((uint32_t)(w - 1) ^ (uint32_t)i0) << 4);
   // straight-line code: the eight rounds' reads are in flight together
 #pragma unroll
   for (int r = 0; r < 32; r += 4, a += 4 * ld_bytes) {
@@ -172,7 +173,7 @@ __device__ __forceinline__ void store_slice_plain(uint32_t before, uint32_t slic
     const int p = 16 * w - (int)m;
     uint32_t x[4], y[4], t[5], o[5];
     const uint32_t flip = r & 4 ? 64u : 0u;      // bit 2 of the row turns the unit by 4
-    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(x[0]), "=r"(x[1]), "=r"(x[2]), "=r"(x[3]) : "r"(left + (uint32_t)r * 128u + (ub ^ flip)));
+    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(x[0]), "=r"(x[1]), "=r"(x[2]), "=r"(x[3]) : "r"(w ? slice + (uint32_t)r * 128u + (ub ^ flip) : carry + (uint32_t)(r + i0) * 16u));
     asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(y[0]), "=r"(y[1]), "=r"(y[2]), "=r"(y[3]) : "r"(slice + (uint32_t)r * 128u + (ua ^ flip)));
     const bool m8 = m & 8u, m4 = m & 4u;      // x, y shifted by two words, by one word, by half a word
     t[0] = m8 ? x[1] : x[3]; t[1] = m8 ? x[2] : y[0]; t[2] = m8 ? x[3] : y[1]; t[3] = m8 ? y[0] : y[2]; t[4] = m8 ? y[1] : y[3];
@@ -194,10 +195,17 @@ __device__ __forceinline__ void store_slice_plain(uint32_t before, uint32_t slic
     if (last && ((len + m) & 15) && !(first && m && end == 0)) scalar(lane, end);
   }
   __syncwarp();
+  if (!last) {      // unit 7 of each row goes on to the next slice
+    uint32_t x[4];
+    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(x[0]), "=r"(x[1]), "=r"(x[2]), "=r"(x[3])
+                 : "r"(slice + (uint32_t)lane * 128u + ((7u ^ ((uint32_t)lane & 7u)) << 4)));
+    st_shared_16(carry + (uint32_t)lane * 16u, x[0], x[1], x[2], x[3]);
+    __syncwarp();
+  }
 }
 
 template <int CG, int BN, int ELEM, bool A_MN, bool B_MN, class Epi>
-__global__ void __launch_bounds__(192, 1)
+__global__ void __launch_bounds__(384, 1)
 product_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const __grid_constant__ CUtensorMap tmC,
                const ProdArgs args, const typename Epi::Args eargs) {
   using C = ProdCfg<CG, BN, ELEM, A_MN, B_MN, Epi::kBytes>;
@@ -220,7 +228,7 @@ product_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
   if (threadIdx.x == 32) { prefetch_tensormap(&tmA); prefetch_tensormap(&tmB); }
   if (threadIdx.x == 0) {
     for (int i = 0; i < S; ++i) { mbar_init(bar_full + 8 * i, 1); mbar_init(bar_empty + 8 * i, 1); }
-    for (int i = 0; i < 2; ++i) { mbar_init(bar_tfull + 8 * i, 1); mbar_init(bar_tempty + 8 * i, 4 * CG); }
+    for (int i = 0; i < 2; ++i) { mbar_init(bar_tfull + 8 * i, 1); mbar_init(bar_tempty + 8 * i, C::kEpiWarps * CG); }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == 1) {
@@ -244,6 +252,8 @@ product_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
     k1 = min(args.kblocks, k0 + args.kb_split);
   };
 
+  if (warp < C::kEpi0) {
+  asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(C::kRegsIssue));
   if (warp == 0) {
     // ---------------------------------------------------------------- TMA producer
     int stage = 0;
@@ -308,60 +318,87 @@ product_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
       uint32_t phase = 0;
       int it = 0;
       bool ok = true;
-      for (int s = unit; s < total && ok; s += args.units, ++it) {
+      for (int s = unit; s < total && ok; s += args.units) {
         int tm, tn, z, k0, k1;
         tile_at(s, tm, tn, z);
         k_range(z, k0, k1);
-        const int buf = it & 1;
-        const uint32_t use = (uint32_t)(it >> 1) & 1u;
-        ok = mbar_wait(bar_tempty + 8 * buf, use ^ 1u, args.status, (kProdMma << 8) | 1);
-        ok = __all_sync(0xffffffffu, ok);
-        if (!ok) break;
-        tcgen05_fence_after();
-        const uint32_t d = tmem_base + (uint32_t)(buf * BN);
-        for (int kb = k0; kb < k1; ++kb) {
-          ok = mbar_wait(bar_full + 8 * stage, phase, args.status, (kProdMma << 8) | 2);
+        for (int ks = k0; ks < k1 && ok; ks += args.kb_sum, ++it) {
+          const int ke = min(k1, ks + args.kb_sum), buf = it & 1;
+          ok = mbar_wait(bar_tempty + 8 * buf, ((uint32_t)(it >> 1) & 1u) ^ 1u, args.status, (kProdMma << 8) | 1);
           ok = __all_sync(0xffffffffu, ok);
           if (!ok) break;
           tcgen05_fence_after();
-          if (elect_one()) {
-            const uint32_t sa = smem_base + stage * C::kStageBytes, sb = sa + C::kABytes;
+          const uint32_t d = tmem_base + (uint32_t)(buf * BN);
+          for (int kb = ks; kb < ke; ++kb) {
+            ok = mbar_wait(bar_full + 8 * stage, phase, args.status, (kProdMma << 8) | 2);
+            ok = __all_sync(0xffffffffu, ok);
+            if (!ok) break;
+            tcgen05_fence_after();
+            if (elect_one()) {
+              const uint32_t sa = smem_base + stage * C::kStageBytes, sb = sa + C::kABytes;
 #pragma unroll
-            for (int k = 0; k < 4; ++k)
-              prod_mma<CG, ELEM>(d, prod_desc_at(da0, sa + k * ka), prod_desc_at(db0, sb + k * kb_), args.idesc, (uint32_t)(kb > k0 || k != 0));
-            umma_commit<CG>(bar_empty + 8 * stage);
-            if (kb == k1 - 1) umma_commit<CG>(bar_tfull + 8 * buf);
+              for (int k = 0; k < 4; ++k)
+                prod_mma<CG, ELEM>(d, prod_desc_at(da0, sa + k * ka), prod_desc_at(db0, sb + k * kb_), args.idesc, (uint32_t)(kb > ks || k != 0));
+              umma_commit<CG>(bar_empty + 8 * stage);
+              if (kb == ke - 1) umma_commit<CG>(bar_tfull + 8 * buf);
+            }
+            __syncwarp();
+            if (++stage == S) { stage = 0; phase ^= 1u; }
           }
-          __syncwarp();
-          if (++stage == S) { stage = 0; phase ^= 1u; }
         }
       }
     }
     __syncwarp();
+  }
   } else {
     // ---------------------------------------------------------------- epilogue
-    const int quarter = warp & 3;   // TMEM lanes [32 * quarter, 32 * quarter + 32)
-    Epi epi(eargs, &tmC, epi_base, warp - 2, lane);
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(C::kRegsEpilogue));
+    constexpr int kCols = BN / 2;   // columns of one warp
+    const int quarter = warp & 3, half = (warp - C::kEpi0) >> 2;   // TMEM lanes [32 * quarter, 32 * quarter + 32)
+    const uint32_t taddr = tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(half * kCols);
+    Epi epi(eargs, &tmC, epi_base, warp - C::kEpi0, lane);
     int it = 0;
     bool ok = true;
-    for (int s = unit; s < total && ok; s += args.units, ++it) {
+    for (int s = unit; s < total && ok; s += args.units) {
       EpiTile e;
-      int tm;
-      tile_at(s, tm, e.tn, e.z);
-      const int buf = it & 1;
-      const uint32_t use = (uint32_t)(it >> 1) & 1u;
+      int tm, tn, k0, k1;
+      tile_at(s, tm, tn, e.z);
+      k_range(e.z, k0, k1);
       e.row0 = tm * 128 * CG + (int)rank * 128 + quarter * 32;
-      e.col0 = e.tn * BN;
-      e.taddr = tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(buf * BN);
+      e.col0 = tn * BN + half * kCols;
       epi.before(e, args.M, args.N);
-      ok = mbar_wait(bar_tfull + 8 * buf, use, args.status, (kProdEpilogue << 8) | 1);
-      ok = __all_sync(0xffffffffu, ok);
+      uint32_t v[kCols];
+      for (int ks = k0; ks < k1; ks += args.kb_sum, ++it) {
+        const int buf = it & 1;
+        ok = mbar_wait(bar_tfull + 8 * buf, (uint32_t)(it >> 1) & 1u, args.status, (kProdEpilogue << 8) | 1);
+        ok = __all_sync(0xffffffffu, ok);
+        if (!ok) break;
+        tcgen05_fence_after();
+        if (!Epi::kSums || ks == k0) {
+#pragma unroll
+          for (int q = 0; q < kCols / 32; ++q) tmem_ld_32x32b_x32(taddr + (uint32_t)(buf * BN + q * 32), *reinterpret_cast<uint32_t(*)[32]>(v + q * 32));
+          tmem_ld_wait();
+        } else {
+#pragma unroll
+          for (int q = 0; q < kCols / 32; ++q) {
+            uint32_t w[32];
+            tmem_ld_32x32b_x32(taddr + (uint32_t)(buf * BN + q * 32), w);
+            tmem_ld_wait();
+#pragma unroll
+            for (int j = 0; j < 32; ++j) v[q * 32 + j] = __float_as_uint(__uint_as_float(v[q * 32 + j]) + __uint_as_float(w[j]));
+          }
+        }
+        tcgen05_fence_before();
+        __syncwarp();
+        // Relaxed: the values are in registers, nothing was written that the issuer reads.  With release the arrival would wait for the
+        // stores of the tile before to reach memory.
+        if (lane == 0) {
+          if constexpr (CG == 1) mbar_arrive_relaxed(bar_tempty + 8 * buf);
+          else mbar_arrive_relaxed_cluster(mapa(bar_tempty + 8 * buf, 0));
+        }
+      }
       if (!ok) break;
-      tcgen05_fence_after();
-      epi.template tile<BN>(e, args.M, args.N);
-      tcgen05_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive_cluster(CG == 1 ? bar_tempty + 8 * buf : mapa(bar_tempty + 8 * buf, 0));
+      epi.template finish<kCols>(v, e, args.M, args.N);
     }
     if (lane == 0) bulk_wait_all();   // every store of this warp has reached global memory
     __syncwarp();
@@ -407,6 +444,7 @@ int launch_product(const char* what, const CUtensorMap& tmA, const CUtensorMap& 
   if (work > 0x3fffffff) { set_error("%s: too many tiles", what); return SP_ERR_UNSUPPORTED; }
   args.units = gemm_units(128 * CG, BN, work);   // one CTA per SM, or as many CTA pairs as fit: same as sp_gemm's tiles of this shape
   if (args.units <= 0) { set_error("could not size the grid"); return SP_ERR_CUDA; }
+  if (!Epi::kSums) args.kb_sum = args.kblocks;
   args.idesc = ELEM == kElemI8 ? idesc_i8(128 * CG, BN) : idesc_16(128 * CG, BN, bf16, A_MN, B_MN);
   return launch_pdl(what, kern, dim3((unsigned)(args.units * CG)), C::kThreads, C::kSmemBytes, CG, stream, tmA, tmB, tmC, args, eargs);
 }

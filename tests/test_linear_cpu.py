@@ -84,7 +84,7 @@ def test_gemm_i8_refusals():
     assert _gemm(M=1 << 31) == sp.ERR_UNSUPPORTED
     assert _gemm(b_layout=0) == sp.ERR_UNSUPPORTED
     assert _gemm(out_dtype=3) == sp.ERR_INVALID_ARG
-    assert _gemm(tile_m=256, tile_n=512) == sp.ERR_UNSUPPORTED
+    assert _gemm(tile_m=256, tile_n=512) == sp.ERR_UNSUPPORTED and _gemm(tile_m=128, tile_n=256) == sp.ERR_UNSUPPORTED
     assert _gemm(tile_m=256, tile_n=0) == sp.ERR_UNSUPPORTED
     assert _gemm(flags=sp.FLAG_STREAM_K) == sp.ERR_INVALID_ARG
     assert _gemm(scheme=-2) == sp.ERR_INVALID_ARG and _gemm(scheme=sp.GROUP_M, group=0) == sp.ERR_INVALID_ARG
@@ -140,7 +140,7 @@ def test_linear_ce_refusals_of_one_call():
 def test_workspace_is_in_pieces_and_never_holds_the_scores():
     for T, V, D in [(1, 2, 8), (16, 65536, 4096), (8192, 131072, 4096), (65536, 262144, 1024), (1 << 20, 1000, 64), (100, 1 << 24, 8)]:
         fwd, grad = sp.linear_ce_workspace(T, V, D), sp.linear_ce_workspace(T, V, D, True)
-        assert 0 < fwd <= T * ((V + 255) // 256 * 8 + 8) + 4096                # a pair per 256 scores
+        assert 0 < fwd <= T * ((V + 127) // 128 * 8 + 8) + 4096                # a pair per 128 scores
         sums = 64 * T * D * 4                                                   # at most 64 slices of dh
         assert 0 < grad <= max(256 << 20, T * 1024 * 2) + T * 20 + sums + 4096
     L = sp.lib()

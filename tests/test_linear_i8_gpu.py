@@ -126,7 +126,7 @@ def test_few_tokens(M, N, K, out):
 # ragged both ways; rows of C that no bulk store can take (odd N); K of less than a stage; more tiles than units
 @pytest.mark.parametrize("M,N,K", [(129, 128, 128), (130, 1, 16), (256, 256, 272), (300, 301, 1040), (1000, 504, 96), (513, 2050, 400), (2600, 3001, 128)])
 @pytest.mark.parametrize("out", ["bf16", "fp16", "fp32"])
-@pytest.mark.parametrize("tile", [(0, 0), (128, 128), (128, 256), (256, 256)])
+@pytest.mark.parametrize("tile", [(0, 0), (128, 128), (256, 256)])
 def test_tiles(M, N, K, out, tile):
     q, s, w, ws, dev = operands(M, N, K, M + N + K)
     code = {"bf16": sp.BF16, "fp16": sp.FP16, "fp32": sp.FP32}[out]
