@@ -409,7 +409,7 @@ int sp_linear_ce(const void* h, const void* W, const int64_t* target, float* lse
  *   grad_loss : DEVICE, fp32, T values or one; NULL: 1.
  *   dh, dW    : DEVICE, T x D and V x D, same type as h and W, fully overwritten, or NULL: not wanted (at most one of them).
  *   workspace : DEVICE, sp_linear_ce_workspace(T, V, D, 1) bytes, as above.
- * A token that is ignored adds exactly nothing, and its row of dh is zero; its row of h must still be finite where dW is wanted.  A target
+ * A token that is ignored adds exactly nothing, whatever its row of h holds, and its row of dh is zero.  A target
  * outside the vocabulary makes the gradients NaN.  Errors as sp_linear_ce. */
 int sp_linear_ce_grad(const void* h, const void* W, const int64_t* target, const float* lse, const float* grad_loss, void* dh, void* dW, int64_t T,
                       int64_t V, int64_t D, int32_t dtype, int64_t ignore_index, int32_t reduction, void* workspace, int64_t workspace_bytes,

@@ -42,8 +42,9 @@ __device__ __forceinline__ void tma_add_3d(const CUtensorMap* map, uint32_t src,
 // Per row and 128 columns the maximum m (in powers of two: m = max z * log2 e, rounded once) and s = sum 2^(z log2 e - m).  Any m serves
 // as long as the joined result uses the same one, so its rounding costs nothing.
 //
-// The tensor cores cut what they add off behind the accumulator's last bit, 16 products at a time, always towards zero: over D = 4096 the scores
-// came out 3e-6 too small.  So an accumulator takes 512 products only and the epilogue adds such sums, rounded to nearest.
+// The tensor cores cut what they add off behind the accumulator's last bit, 16 products at a time, always towards zero: over D = 4096 lse
+// came out 1.8e-6 too small, over 8192 4e-6.  So an accumulator takes 512 products only and the epilogue adds such sums, rounded to
+// nearest: 2e-7, in the same time (256 products: 1e-7, and 11 % more time at D = 1024).
 // What bounds it: 128 x 256 exponentials per CTA and tile at 16 a clock, 2048 cycles beside 512 for every 64 of D.
 constexpr int kCeSum = 8;      // stages of 64 products per accumulator
 struct EpiStats {
@@ -144,13 +145,13 @@ __global__ void __launch_bounds__(kRowThreads, 2) row_stats_kernel(const RowArgs
   pdl_launch_dependents();
   pdl_wait();
   int4 w[2][kRowUnroll];
-  auto fetch = [&](int n, int k) {      // elements [k, k + 2048) of rows n and n + 1
+  auto fetch = [&](int64_t n, int k) {      // elements [k, k + 2048) of rows n and n + 1
 #pragma unroll
     for (int u = 0; u < kRowUnroll; ++u)
 #pragma unroll
       for (int r = 0; r < 2; ++r) {
         const int c = k + u * 256 + lane * 8;
-        w[r][u] = n + r < a.V && c < a.D ? __ldcs(reinterpret_cast<const int4*>(a.W + (int64_t)(n + r) * a.D + c)) : make_int4(0, 0, 0, 0);
+        w[r][u] = n + r < a.V && c < a.D ? __ldcs(reinterpret_cast<const int4*>(a.W + (n + r) * a.D + c)) : make_int4(0, 0, 0, 0);
       }
   };
   fetch(warp * 2, 0);
@@ -180,8 +181,8 @@ __global__ void __launch_bounds__(kRowThreads, 2) row_stats_kernel(const RowArgs
           }
         }
       }
-      if (k + kRowUnroll * 256 < a.D) fetch((int)n, k + kRowUnroll * 256);
-      else if (n + step < a.V) fetch((int)(n + step), 0);
+      if (k + kRowUnroll * 256 < a.D) fetch(n, k + kRowUnroll * 256);
+      else if (n + step < a.V) fetch(n + step, 0);
     }
 #pragma unroll
     for (int r = 0; r < 2; ++r) {
@@ -220,7 +221,7 @@ __device__ void reduce_losses(const CeJoin& a) {
   __shared__ int part_n[32];
   double s = 0;
   int n = 0;
-  for (int t = threadIdx.x; t < a.T; t += blockDim.x) {
+  for (int64_t t = threadIdx.x; t < a.T; t += blockDim.x) {
     s += a.each[t];
     n += a.target[t] != a.ignore;
   }
@@ -269,15 +270,38 @@ __global__ void __launch_bounds__(1024) ce_reduce_kernel(const CeJoin a) {
 }
 
 // ------------------------------------------------------------------ gradient
-struct CeCoef {
+struct CePrep {
   const int64_t* target;
   const float* grad;     // per token (none) or one number; nullptr: 1
   float* coef;           // per token
   float* factor;         // one number
-  int T, V;
+  const uint4* h;        // rows of `vecs` vectors of 8 elements ...
+  uint4* rows;           // ... copied to rows of `ld` vectors
+  int64_t T;
+  int vecs, ld;
+  int V;
   int64_t ignore;
   int reduction, fp16;
+  int masked;            // 1: rows of ignored tokens become zeros
 };
+
+// The tokens' rows once more, each on a cache line of its own (a row of a tile's 128 bytes then takes one line of L2, not two: 1001 x 50001 x
+// 1032 forward 124 us without, FILLROWS with) and, for the gradient, zeros where a token does not count: dW adds 0 x h for those, and what an
+// ignored row holds need not be finite.
+__device__ __forceinline__ void ce_copy_rows(const CePrep& a, int block, int blocks) {
+  const int64_t n = a.T * a.vecs;
+  for (int64_t i = (int64_t)block * blockDim.x + threadIdx.x; i < n; i += (int64_t)blocks * blockDim.x) {
+    const int64_t t = i / a.vecs;
+    const uint4 v = __ldg(a.h + i);
+    a.rows[t * a.ld + (i - t * a.vecs)] = a.masked && __ldg(a.target + t) == a.ignore ? make_uint4(0u, 0u, 0u, 0u) : v;
+  }
+}
+
+__global__ void __launch_bounds__(1024) ce_rows_kernel(const CePrep a) {
+  pdl_launch_dependents();
+  pdl_wait();
+  ce_copy_rows(a, blockIdx.x, gridDim.x);
+}
 
 // What the loss's gradient puts on each token, c_t = factor * coef_t: g is made with coef_t and rounded to 16 bits, the two products
 // multiply by `factor` in fp32.
@@ -285,15 +309,19 @@ struct CeCoef {
 //   largest entry, p - 1 ~ -1, which 16 bits hold well.
 //   A weight per token (none): coef_t.
 // fp16 reaches down to 2^-24 only, and p ranges down to 1 / V and below: there coef is scaled by a power of two that brings
-// its largest value to [2^14, 2^15] (|g| <= coef stays below 65504), and `factor` by the inverse.  One block.
-__global__ void __launch_bounds__(1024) ce_coef_kernel(const CeCoef a) {
+// its largest value to [2^14, 2^15] (|g| <= coef stays below 65504), and `factor` by the inverse.  Block 0; the others copy rows.
+__global__ void __launch_bounds__(1024) ce_prep_kernel(const CePrep a) {
   pdl_launch_dependents();
   pdl_wait();
+  if (blockIdx.x > 0) {
+    ce_copy_rows(a, blockIdx.x - 1, gridDim.x - 1);
+    return;
+  }
   __shared__ int part_n[32];
   __shared__ float part_m[32];
   int n = 0;
   float top = 0.f;
-  for (int t = threadIdx.x; t < a.T; t += 1024) {
+  for (int64_t t = threadIdx.x; t < a.T; t += 1024) {
     const bool kept = a.target[t] != a.ignore;
     n += kept;
     if (kept && a.reduction == SP_REDUCE_NONE && a.grad) top = fmaxf(top, fabsf(a.grad[t]));
@@ -323,7 +351,7 @@ __global__ void __launch_bounds__(1024) ce_coef_kernel(const CeCoef a) {
     up = max(-100, min(100, each ? 15 - e : 15));
   }
   const float scale = exp2f((float)up);
-  for (int t = threadIdx.x; t < a.T; t += 1024) {
+  for (int64_t t = threadIdx.x; t < a.T; t += 1024) {
     const int64_t y = a.target[t];
     float c = 0.f;
     if (y != a.ignore) c = y < 0 || y >= a.V ? CUDART_NAN_F : (each ? a.grad[t] : wild) * scale;
@@ -474,25 +502,35 @@ static int64_t div_up(int64_t a, int64_t b) { return (a + b - 1) / b; }
 // Everything that follows from the sizes alone.
 struct CePlan {
   int64_t T, V, D;
-  int tile_m;                 // rows of a token tile: a CTA pair's 256, or 128 where no more tokens are there
   bool row;                   // forward: the form for one token
   int64_t tiles;              // pairs per token that the forward product leaves: one per 128 words, or per block
   int64_t piece, ld_g;        // gradient: vocabulary rows of a piece, row pitch of g
-  int pieces, slices;         // slices of the vocabulary in the product for dh
-  int64_t off_picked, off_each, forward_bytes;
-  int64_t off_factor, off_g, off_acc, grad_bytes;
+  int pieces;
+  int slices;                 // of the vocabulary in the product for dh
+  bool copy;                  // forward: the tokens' rows are copied to cache lines of their own
+  int64_t ld_h;               // row pitch of such copies
+  int64_t off_picked, off_each, off_rows, forward_bytes;
+  int64_t off_factor, off_grad_rows, off_g, off_acc, grad_bytes;
 };
+
+// Rows of a token tile: a CTA pair's 256, or one CTA's 128 where no more tokens are there.  (Also for token counts that fill their last tile
+// badly the smaller one does not pay: it moves half as much again through L2 per product.  777 x 20011 x 1032: forward 54 us on
+// 4 x 256 rows, 58 on 7 x 128; dh 51 and 55.)
+static int ce_rows(int64_t T) { return T <= 128 ? 128 : 256; }
 
 static CePlan ce_plan(int64_t T, int64_t V, int64_t D) {
   CePlan p = {};
   p.T = T; p.V = V; p.D = D;
-  p.tile_m = T <= 128 ? 128 : 256;
   p.row = T == 1 && D <= kRowMaxD;
   p.tiles = div_up(V, kCePart);
   if (p.row) p.tiles = div_up(V, 2 * kRowThreads / 32) < 2 * 148 ? div_up(V, 2 * kRowThreads / 32) : 2 * 148;   // blocks: two per SM
   p.off_picked = up256(p.tiles * T * 8);
   p.off_each = p.off_picked + up256(T * 4);
-  p.forward_bytes = p.off_each + up256(T * 4);
+  p.ld_h = (D + 63) / 64 * 64;
+  // a launch of its own pays from about 50 us of products on
+  p.copy = D % 64 != 0 && T > 128 && (double)T * (double)V * (double)D > 2.5e10;
+  p.off_rows = p.off_each + up256(T * 4);
+  p.forward_bytes = p.off_rows + (p.copy ? up256(T * p.ld_h * 2) : 0);
   // g of one piece takes at most 256 MiB: 27 waves of tiles on the whole device, whatever T is
   constexpr int64_t kEntries = 128ll << 20;
   p.piece = V;
@@ -502,16 +540,17 @@ static CePlan ce_plan(int64_t T, int64_t V, int64_t D) {
     if (p.piece > V) p.piece = V;
   }
   p.pieces = (int)div_up(V, p.piece);
-  p.ld_g = (p.piece + 7) / 8 * 8;
-  // Few tiles of dh and a long k axis: the vocabulary is cut into slices until every SM has one, each at least 16 stages long.
-  const int64_t out_tiles = div_up(T, p.tile_m) * div_up(D, 256), units = p.tile_m == 256 ? 74 : 148, kb = div_up(p.piece, 64);
+  p.ld_g = (p.piece + 63) / 64 * 64;      // rows of g start on cache lines
+  // Few tiles of dh and a long k axis: the vocabulary is cut into slices of at least four stages until every SM has one.
+  const int64_t out_tiles = div_up(T, ce_rows(T)) * div_up(D, 256), units = ce_rows(T) == 256 ? 74 : 148, kb = div_up(p.piece, 64);
   int64_t s = out_tiles < units ? units / out_tiles : 1;
-  if (s > kb / 16) s = kb / 16;
+  if (s > kb / 4) s = kb / 4;
   if (s > kMaxSplits) s = kMaxSplits;
   if (s < 1) s = 1;
   p.slices = (int)div_up(kb, div_up(kb, s));
   p.off_factor = up256(T * 4);
-  p.off_g = p.off_factor + 256;
+  p.off_grad_rows = p.off_factor + 256;
+  p.off_g = p.off_grad_rows + up256(T * p.ld_h * 2);
   p.off_acc = p.off_g + up256(T * p.ld_g * 2);
   p.grad_bytes = p.off_acc + ((p.pieces > 1 || p.slices > 1) ? up256(p.slices * T * D * 4) : 0);
   return p;
@@ -556,18 +595,31 @@ static ProdArgs ce_args(const Sched& sched, int32_t* status, int64_t M, int64_t 
 
 // h . W_piece^T with an epilogue of scores.
 template <class Epi>
-static int ce_scores(const char* what, const CePlan& p, const void* h, const void* W, int64_t cols, int32_t* status, bool bf16, const CUtensorMap* tmC,
+static int ce_scores(const char* what, const CePlan& p, const void* h, int64_t ld_h, const void* W, int64_t cols, int32_t* status, bool bf16, const CUtensorMap* tmC,
                      const typename Epi::Args& ea, cudaStream_t stream) {
   CUtensorMap tmA, tmB;
   Sched sched;
-  int rc = ce_sched(p.T, cols, p.tile_m, &sched);
-  if (rc == SP_OK) rc = make_map_any(&tmA, h, 2, p.T, p.D, p.D, 128, 64);
-  if (rc == SP_OK) rc = make_map_any(&tmB, W, 2, cols, p.D, p.D, p.tile_m == 256 ? 128 : 256, 64);
+  const int rows = ce_rows(p.T);
+  int rc = ce_sched(p.T, cols, rows, &sched);
+  if (rc == SP_OK) rc = make_map_any(&tmA, h, 2, p.T, p.D, ld_h, 128, 64);
+  if (rc == SP_OK) rc = make_map_any(&tmB, W, 2, cols, p.D, p.D, rows == 256 ? 128 : 256, 64);
   if (rc != SP_OK) return rc;
   ProdArgs a = ce_args(sched, status, p.T, cols, p.D, 1);
   a.turn = sched.Tm == 1;
-  if (p.tile_m == 256) return launch_product<2, 256, kElem16, false, false, Epi>(what, tmA, tmB, tmC ? *tmC : tmA, a, bf16, ea, stream);
+  if (rows == 256) return launch_product<2, 256, kElem16, false, false, Epi>(what, tmA, tmB, tmC ? *tmC : tmA, a, bf16, ea, stream);
   return launch_product<1, 256, kElem16, false, false, Epi>(what, tmA, tmB, tmC ? *tmC : tmA, a, bf16, ea, stream);
+}
+
+static CePrep ce_rows_args(const CePlan& p, const void* h, void* rows, const int64_t* target, int64_t ignore, bool masked) {
+  CePrep a = {};
+  a.target = target; a.h = (const uint4*)h; a.rows = (uint4*)rows; a.T = p.T; a.vecs = (int)(p.D / 8); a.ld = (int)(p.ld_h / 8);
+  a.ignore = ignore; a.masked = masked;
+  return a;
+}
+
+static unsigned ce_copy_blocks(const CePlan& p) {      // four vectors per thread, at most two blocks per SM
+  const int64_t b = div_up(p.T * (p.D / 8), 4096);
+  return (unsigned)(b < 296 ? b : 296);
 }
 
 static int launch_row(const RowArgs& a, int blocks, cudaStream_t stream) {
@@ -612,7 +664,12 @@ int sp_linear_ce(const void* h, const void* W, const int64_t* target, float* lse
     const RowArgs ra = {(const uint16_t*)W, (const uint16_t*)h, target, ea.stats, ea.picked, (int)V, (int)D, dtype == SP_BF16};
     rc = launch_row(ra, (int)p.tiles, (cudaStream_t)stream);
   } else {
-    rc = ce_scores<EpiStats>("vocabulary product", p, h, W, V, st.status, dtype == SP_BF16, nullptr, ea, (cudaStream_t)stream);
+    if (p.copy) {
+      CePrep prep = ce_rows_args(p, h, ws + p.off_rows, target, ignore_index, false);
+      rc = launch_pdl("copy of the tokens", ce_rows_kernel, dim3(ce_copy_blocks(p)), 1024, 0, 1, (cudaStream_t)stream, prep);
+      if (rc != SP_OK) return rc;
+    }
+    rc = ce_scores<EpiStats>("vocabulary product", p, p.copy ? ws + p.off_rows : h, p.copy ? p.ld_h : D, W, V, st.status, dtype == SP_BF16, nullptr, ea, (cudaStream_t)stream);
   }
   if (rc != SP_OK) return rc;
   CeJoin j = {};
@@ -650,8 +707,10 @@ int sp_linear_ce_grad(const void* h, const void* W, const int64_t* target, const
   char* ws = (char*)workspace;
   float *coef = (float*)ws, *factor = (float*)(ws + p.off_factor), *acc = (float*)(ws + p.off_acc);
   char* g = ws + p.off_g;
-  const CeCoef cc = {target, grad_loss, coef, factor, (int)T, (int)V, ignore_index, reduction, !bf16};
-  rc = launch_pdl("token coefficients", ce_coef_kernel, dim3(1), 1024, 0, 1, stream, cc);
+  char* rows = ws + p.off_grad_rows;
+  CePrep prep = ce_rows_args(p, h, rows, target, ignore_index, true);
+  prep.grad = grad_loss; prep.coef = coef; prep.factor = factor; prep.V = (int)V; prep.reduction = reduction; prep.fp16 = !bf16;
+  rc = launch_pdl("coefficients and rows of the tokens", ce_prep_kernel, dim3(1 + ce_copy_blocks(p)), 1024, 0, 1, stream, prep);
   if (rc != SP_OK) return rc;
   const bool summed = p.pieces > 1 || p.slices > 1;     // dh passes through fp32 sums
   for (int i = 0; i < p.pieces; ++i) {
@@ -661,11 +720,11 @@ int sp_linear_ce_grad(const void* h, const void* W, const int64_t* target, const
     rc = make_map_any(&tmG, g, 2, T, cols, p.ld_g, 32, 64);
     if (rc != SP_OK) return rc;
     const EpiG::Args ea = {lse, coef, target, v0, bf16};
-    rc = ce_scores<EpiG>("gradient of the scores", p, h, Wp, cols, st.status, bf16, &tmG, ea, stream);
+    rc = ce_scores<EpiG>("gradient of the scores", p, rows, p.ld_h, Wp, cols, st.status, bf16, &tmG, ea, stream);
     if (rc != SP_OK) return rc;
     if (dh) {
       Sched sched;
-      rc = ce_sched(T, D, p.tile_m, &sched);
+      rc = ce_sched(T, D, ce_rows(T), &sched);
       if (rc == SP_OK) rc = make_map_any(&tmA, g, 2, T, cols, p.ld_g, 128, 64);
       if (rc == SP_OK) rc = make_map_any(&tmB, Wp, 2, cols, D, D, 64, 64);
       if (rc != SP_OK) return rc;
@@ -674,13 +733,13 @@ int sp_linear_ce_grad(const void* h, const void* W, const int64_t* target, const
         rc = make_map_3d_f32(&tmC, acc, p.slices, T, D, 32, 32);
         if (rc != SP_OK) return rc;
         const EpiSum::Args es = {i > 0};
-        rc = p.tile_m == 256 ? launch_product<2, 256, kElem16, false, true, EpiSum>("gradient of h", tmA, tmB, tmC, a, bf16, es, stream)
+        rc = ce_rows(T) == 256 ? launch_product<2, 256, kElem16, false, true, EpiSum>("gradient of h", tmA, tmB, tmC, a, bf16, es, stream)
                              : launch_product<1, 256, kElem16, false, true, EpiSum>("gradient of h", tmA, tmB, tmC, a, bf16, es, stream);
       } else {
         rc = make_map_any(&tmC, dh, 2, T, D, D, 32, 64);
         if (rc != SP_OK) return rc;
         const EpiOut16::Args eo = {factor, bf16};
-        rc = p.tile_m == 256 ? launch_product<2, 256, kElem16, false, true, EpiOut16>("gradient of h", tmA, tmB, tmC, a, bf16, eo, stream)
+        rc = ce_rows(T) == 256 ? launch_product<2, 256, kElem16, false, true, EpiOut16>("gradient of h", tmA, tmB, tmC, a, bf16, eo, stream)
                              : launch_product<1, 256, kElem16, false, true, EpiOut16>("gradient of h", tmA, tmB, tmC, a, bf16, eo, stream);
       }
       if (rc != SP_OK) return rc;
@@ -689,7 +748,7 @@ int sp_linear_ce_grad(const void* h, const void* W, const int64_t* target, const
       Sched sched;
       rc = ce_sched(cols, D, 256, &sched);
       if (rc == SP_OK) rc = make_map_any(&tmA, g, 2, T, cols, p.ld_g, 64, 64);
-      if (rc == SP_OK) rc = make_map_any(&tmB, h, 2, T, D, D, 64, 64);
+      if (rc == SP_OK) rc = make_map_any(&tmB, rows, 2, T, D, p.ld_h, 64, 64);
       if (rc == SP_OK) rc = make_map_any(&tmC, (char*)dW + v0 * D * 2, 2, cols, D, D, 32, 64);
       if (rc != SP_OK) return rc;
       const ProdArgs a = ce_args(sched, st.status, cols, D, T, 1);

@@ -374,13 +374,13 @@ __global__ void __launch_bounds__(kDotThreads, 2) dot_tokens_kernel(const DotArg
   const int step = gridDim.x * (kDotThreads / 32) * 2;
   pdl_launch_dependents();
   int4 w[2][kDotUnroll];
-  auto fetch = [&](int n, int k) {     // bytes [k, k + 4096) of rows n and n + 1
+  auto fetch = [&](int64_t n, int k) {     // bytes [k, k + 4096) of rows n and n + 1
 #pragma unroll
     for (int u = 0; u < kDotUnroll; ++u)
 #pragma unroll
       for (int r = 0; r < 2; ++r) {
         const int c = k + u * 512 + lane * 16;
-        w[r][u] = n + r < a.N && c < a.K ? __ldcs(reinterpret_cast<const int4*>(a.W + (int64_t)(n + r) * a.K + c)) : make_int4(0, 0, 0, 0);
+        w[r][u] = n + r < a.N && c < a.K ? __ldcs(reinterpret_cast<const int4*>(a.W + (n + r) * a.K + c)) : make_int4(0, 0, 0, 0);
       }
   };
   if (!a.early) pdl_wait();
@@ -396,7 +396,7 @@ __global__ void __launch_bounds__(kDotThreads, 2) dot_tokens_kernel(const DotArg
     if (threadIdx.x < a.M) scales[threadIdx.x] = __ldg(a.q_scale + threadIdx.x);
   }
   __syncthreads();
-  for (int n = warp * 2; n < a.N; n += step) {
+  for (int64_t n = (int64_t)warp * 2; n < a.N; n += step) {
     int acc[2][MT] = {};
     for (int k = 0; k < a.K; k += kDotUnroll * 512) {
 #pragma unroll
@@ -423,7 +423,8 @@ __global__ void __launch_bounds__(kDotThreads, 2) dot_tokens_kernel(const DotArg
         const int sum = __reduce_add_sync(0xffffffffu, acc[r][m]);
         if (lane == 2 * m + r) mine = sum;
       }
-    const int m = lane >> 1, col = n + (lane & 1);
+    const int m = lane >> 1;
+    const int64_t col = n + (lane & 1);
     if (m < a.M && col < a.N) store_y(a.C, a.out, (int64_t)m * a.N + col, (float)mine * scales[m] * __ldg(a.w_scale + col));
   }
 }

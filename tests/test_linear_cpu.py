@@ -140,9 +140,10 @@ def test_linear_ce_refusals_of_one_call():
 def test_workspace_is_in_pieces_and_never_holds_the_scores():
     for T, V, D in [(1, 2, 8), (16, 65536, 4096), (8192, 131072, 4096), (65536, 262144, 1024), (1 << 20, 1000, 64), (100, 1 << 24, 8)]:
         fwd, grad = sp.linear_ce_workspace(T, V, D), sp.linear_ce_workspace(T, V, D, True)
-        assert 0 < fwd <= T * ((V + 127) // 128 * 8 + 8) + 4096                # a pair per 128 scores
+        rows = T * (D + 64) * 2                                                 # the tokens once more
+        assert 0 < fwd <= T * ((V + 127) // 128 * 8 + 8) + rows + 4096         # a pair per 128 scores
         sums = 64 * T * D * 4                                                   # at most 64 slices of dh
-        assert 0 < grad <= max(256 << 20, T * 1024 * 2) + T * 20 + sums + 4096
+        assert 0 < grad <= max(256 << 20, T * 1024 * 2) + T * 20 + T * 128 + sums + rows + 4096
     L = sp.lib()
     for bad in [(0, 8, 8), (8, -1, 8), (8, 8, 0), (1 << 31, 8, 8)]:
         assert L.sp_linear_ce_workspace(*bad, 0) == -1
