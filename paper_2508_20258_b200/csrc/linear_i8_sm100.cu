@@ -806,7 +806,7 @@ static int run_i8(const I8Call& c, bool early, cudaStream_t stream) {
   }
   ProdArgs pa = {};
   pa.perm = st.perm; pa.status = st.status; pa.M = (int)c.M; pa.N = (int)c.N;
-  pa.kblocks = (int)((c.K + 127) / 128); pa.splits = 1; pa.kb_split = pa.kblocks;
+  pa.kblocks = (int)((c.K + 127) / 128); pa.splits = 1;
   pa.sched = c.sched;
   const int cg = c.tile_m / 128;
   rc = make_map_any(&tmA, c.A, 1, c.M, c.K, c.K, 128, 128);

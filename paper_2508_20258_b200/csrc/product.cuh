@@ -54,7 +54,7 @@ struct ProdArgs {
   int32_t* status;
   int M, N;              // rows of A, rows of B
   int kblocks;           // stages that cover k
-  int splits, kb_split;  // slices of k, stages per slice (slice z: [z * kb_split, min(kblocks, (z + 1) * kb_split)))
+  int splits;            // slices of k: slice z takes stages z, z + splits, z + 2 splits, ...: units that run together read k in step
   int kb_sum;            // stages whose products one accumulator takes before the epilogue adds it to its own sum (Epi::kSums; else a slice)
   int turn;              // 1: units start their walk along k at different places (one tile row: all read the same few lines of A, and
                          //    in step they would queue for them in one L2 slice: one token, 32768 x 4096 words, FILLTURN)
@@ -247,10 +247,7 @@ product_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
     const int t = args.sched.use_table ? __ldg(args.perm + o) : slot_to_tile(args.sched, o);
     tm = t / Tn; tn = t - tm * Tn;
   };
-  auto k_range = [&](int z, int& k0, int& k1) {
-    k0 = z * args.kb_split;
-    k1 = min(args.kblocks, k0 + args.kb_split);
-  };
+  auto stages_of = [&](int z) { return (args.kblocks - z + args.splits - 1) / args.splits; };
 
   if (warp < C::kEpi0) {
   asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(C::kRegsIssue));
@@ -260,20 +257,20 @@ product_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
     uint32_t phase = 0;
     bool ok = true;
     for (int s = unit; s < total && ok; s += args.units) {
-      int tm, tn, z, k0, k1;
+      int tm, tn, z;
       tile_at(s, tm, tn, z);
-      k_range(z, k0, k1);
+      const int n = stages_of(z);
       const int row0 = tm * 128 * CG + (int)rank * 128, col0 = tn * BN + (int)rank * C::kBCols;
-      int at = args.turn ? k0 + (unit * 5) % (k1 - k0) : k0;      // the k-block to load
-      for (int kb = k0; kb < k1; ++kb) {
+      int at = args.turn ? (unit * 5) % n : 0;      // the stage to load, of this slice's
+      for (int kb = 0; kb < n; ++kb) {
         ok = mbar_wait(bar_empty + 8 * stage, phase ^ 1u, args.status, (kProdProducer << 8) | 1);
         ok = __all_sync(0xffffffffu, ok);
         if (!ok) break;
         const uint32_t full_local = bar_full + 8 * stage;
         const uint32_t full_leader = CG == 1 ? full_local : mapa(full_local, 0);
         const uint32_t sa = smem_base + stage * C::kStageBytes, sb = sa + C::kABytes;
-        const int k = at * C::kBK;
-        if (++at == k1) at = k0;
+        const int k = (z + at * args.splits) * C::kBK;
+        if (++at == n) at = 0;
         if (elect_one()) {
           if (rank == 0) mbar_arrive_expect_tx(full_local, CG * C::kStageBytes);
           if constexpr (A_MN) {
@@ -319,11 +316,11 @@ product_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
       int it = 0;
       bool ok = true;
       for (int s = unit; s < total && ok; s += args.units) {
-        int tm, tn, z, k0, k1;
+        int tm, tn, z;
         tile_at(s, tm, tn, z);
-        k_range(z, k0, k1);
-        for (int ks = k0; ks < k1 && ok; ks += args.kb_sum, ++it) {
-          const int ke = min(k1, ks + args.kb_sum), buf = it & 1;
+        const int n = stages_of(z);
+        for (int ks = 0; ks < n && ok; ks += args.kb_sum, ++it) {
+          const int ke = min(n, ks + args.kb_sum), buf = it & 1;
           ok = mbar_wait(bar_tempty + 8 * buf, ((uint32_t)(it >> 1) & 1u) ^ 1u, args.status, (kProdMma << 8) | 1);
           ok = __all_sync(0xffffffffu, ok);
           if (!ok) break;
@@ -361,20 +358,20 @@ product_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
     bool ok = true;
     for (int s = unit; s < total && ok; s += args.units) {
       EpiTile e;
-      int tm, tn, k0, k1;
+      int tm, tn;
       tile_at(s, tm, tn, e.z);
-      k_range(e.z, k0, k1);
+      const int n = stages_of(e.z);
       e.row0 = tm * 128 * CG + (int)rank * 128 + quarter * 32;
       e.col0 = tn * BN + half * kCols;
       epi.before(e, args.M, args.N);
       uint32_t v[kCols];
-      for (int ks = k0; ks < k1; ks += args.kb_sum, ++it) {
+      for (int ks = 0; ks < n; ks += args.kb_sum, ++it) {
         const int buf = it & 1;
         ok = mbar_wait(bar_tfull + 8 * buf, (uint32_t)(it >> 1) & 1u, args.status, (kProdEpilogue << 8) | 1);
         ok = __all_sync(0xffffffffu, ok);
         if (!ok) break;
         tcgen05_fence_after();
-        if (!Epi::kSums || ks == k0) {
+        if (!Epi::kSums || ks == 0) {
 #pragma unroll
           for (int q = 0; q < kCols / 32; ++q) tmem_ld_32x32b_x32(taddr + (uint32_t)(buf * BN + q * 32), *reinterpret_cast<uint32_t(*)[32]>(v + q * 32));
           tmem_ld_wait();
@@ -429,7 +426,7 @@ inline int launch_pdl(const char* what, void (*kern)(KArgs...), dim3 grid, int t
   return SP_OK;
 }
 
-// Fills args.idesc, args.units and launches one product.  The caller has set M, N, kblocks, splits, kb_split, sched, perm, status.
+// Fills args.idesc, args.units and launches one product.  The caller has set M, N, kblocks, splits (at most kblocks), sched, perm, status.
 template <int CG, int BN, int ELEM, bool A_MN, bool B_MN, class Epi>
 int launch_product(const char* what, const CUtensorMap& tmA, const CUtensorMap& tmB, const CUtensorMap& tmC, ProdArgs args, bool bf16,
                    const typename Epi::Args& eargs, cudaStream_t stream) {
