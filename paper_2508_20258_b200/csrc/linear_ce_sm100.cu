@@ -729,7 +729,8 @@ int sp_linear_ce_grad(const void* h, const void* W, const int64_t* target, const
       if (rc == SP_OK) rc = make_map_any(&tmA, g, 2, T, cols, p.ld_g, 128, 64);
       if (rc == SP_OK) rc = make_map_any(&tmB, Wp, 2, cols, D, D, 64, 64);
       if (rc != SP_OK) return rc;
-      const ProdArgs a = ce_args(sched, st.status, T, D, cols, p.slices);
+      ProdArgs a = ce_args(sched, st.status, T, D, cols, p.slices);
+      a.trigger_late = 1;     // dW below reads g and h only: its CTAs take the SMs that this product leaves free
       if (summed) {
         rc = make_map_3d_f32(&tmC, acc, p.slices, T, D, 32, 32);
         if (rc != SP_OK) return rc;
@@ -752,7 +753,8 @@ int sp_linear_ce_grad(const void* h, const void* W, const int64_t* target, const
       if (rc == SP_OK) rc = make_map_any(&tmB, rows, 2, T, D, p.ld_h, 64, 64);
       if (rc == SP_OK) rc = make_map_any(&tmC, (char*)dW + v0 * D * 2, 2, cols, D, D, 32, 64);
       if (rc != SP_OK) return rc;
-      const ProdArgs a = ce_args(sched, st.status, cols, D, T, 1);
+      ProdArgs a = ce_args(sched, st.status, cols, D, T, 1);
+      a.overlap = dh != nullptr;
       const EpiOut16::Args eo = {factor, bf16};
       rc = launch_product<2, 256, kElem16, true, true, EpiOut16>("gradient of W", tmA, tmB, tmC, a, bf16, eo, stream);
       if (rc != SP_OK) return rc;

@@ -58,6 +58,10 @@ struct ProdArgs {
   int kb_sum;            // stages whose products one accumulator takes before the epilogue adds it to its own sum (Epi::kSums; else a slice)
   int turn;              // 1: units start their walk along k at different places (one tile row: all read the same few lines of A, and
                          //    in step they would queue for them in one L2 slice: one token, 32768 x 4096 words, FILLTURN)
+  // A product and the next one on the stream that reads nothing of it may run side by side: the first lets its successor start only once
+  // everything before itself is complete (`trigger_late`), the second goes straight to work and waits before it ends instead
+  // (`overlap`), so that whatever follows it follows both.
+  int trigger_late, overlap;
   int units;             // CTAs or CTA pairs launched
   uint32_t idesc;        // instruction descriptor
   Sched sched;
@@ -224,7 +228,7 @@ product_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
   const int unit = blockIdx.x / CG;
   const int T = args.sched.T, Tn = args.sched.Tn, total = T * args.splits;
 
-  pdl_launch_dependents();
+  if (!args.trigger_late) pdl_launch_dependents();
   if (threadIdx.x == 32) { prefetch_tensormap(&tmA); prefetch_tensormap(&tmB); }
   if (threadIdx.x == 0) {
     for (int i = 0; i < S; ++i) { mbar_init(bar_full + 8 * i, 1); mbar_init(bar_empty + 8 * i, 1); }
@@ -239,7 +243,8 @@ product_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
   unit_sync<CG>();
   tcgen05_fence_after();
   const uint32_t tmem_base = ld_shared_32(tmem_slot);
-  pdl_wait();   // set-up may overlap the kernel before this one; global memory is touched only from here on
+  if (!args.overlap) pdl_wait();   // set-up may overlap the kernel before this one; global memory is touched only from here on
+  if (args.trigger_late) pdl_launch_dependents();
 
   auto tile_at = [&](int s, int& tm, int& tn, int& z) {
     z = s / T;
@@ -404,6 +409,7 @@ product_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
   tcgen05_fence_before();
   unit_sync<CG>();
   if (warp == 1) tmem_dealloc<CG>(tmem_base, C::kTmemCols);
+  if (args.overlap && threadIdx.x == 0) pdl_wait();
 }
 
 // Launch with programmatic stream serialisation: the next kernel's set-up overlaps this one's tail.
