@@ -365,9 +365,9 @@ int sp_quantize_i8(const void* x, int32_t x_dtype, int64_t M, int64_t K, int8_t*
  *   C : DEVICE, M x N row-major, params->out_dtype SP_BF16, SP_FP32 or SP_FP16 (params NULL: SP_BF16); must not overlap an input.
  *   scheme, params : the order of the tile grid, exactly as for sp_tile_map(M, N, tile_m, tile_n, ...), or SP_ORDER_AUTO.  Tiles
  *       128x128, 256x256, or 0,0: the one with the least estimated time.  Of the flags only SP_FLAG_SERPENTINE applies;
- *       b_layout must be 1.  With SP_ORDER_AUTO, tile 0,0 and at most 128 tokens the call is bound by reading B and takes
- *       another form: 128 rows of B per block, the k axis split over a cluster of blocks, partial sums joined through distributed
- *       shared memory.  Every order and form gives the same bits.
+ *       b_layout must be 1.  With SP_ORDER_AUTO, tile 0,0 and at most 64 tokens the call is bound by reading B and takes
+ *       other forms: 128 rows of B per block, the k axis split over a cluster of blocks, partial sums joined through distributed
+ *       shared memory; or, for one to four tokens, dot products of whole rows.  Every order and form gives the same bits.
  * K must be a multiple of 16 (pad rows with zeros, as sp_quantize_i8 does) and at most SP_I8_MAX_K; M and N are free (rows of C that do not
  * start on 16-byte boundaries are written with plain stores).
  * Caching, first call, stream capture and the status word: as sp_gemm.  Errors: as sp_gemm; SP_ERR_UNSUPPORTED also for

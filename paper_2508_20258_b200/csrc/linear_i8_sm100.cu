@@ -50,15 +50,17 @@ struct Vec8 {
     }
     return top;
   }
-  __device__ __forceinline__ void values(float (&v)[8]) const {
+  __device__ __forceinline__ void values(float (&v)[8]) const { values_as<T>(v); }
+  template <class U>
+  __device__ __forceinline__ void values_as(float (&v)[8]) const {
     const uint32_t* u = reinterpret_cast<const uint32_t*>(w);
-    if constexpr (sizeof(T) == 4) {
+    if constexpr (sizeof(U) == 4) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(u[i]);
     } else {
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        if constexpr (std::is_same<T, __half>::value) {
+        if constexpr (std::is_same<U, __half>::value) {
           const float2 f = __half22float2(*reinterpret_cast<const __half2*>(u + i));
           v[2 * i] = f.x; v[2 * i + 1] = f.y;
         } else {
@@ -81,6 +83,7 @@ __device__ __forceinline__ float quant_top(uint32_t bits) {
 struct QuantScale {
   float s, inv;
   bool zero;      // all q are zero: a row of zeros, or one that is not finite
+  __device__ __forceinline__ QuantScale(float scale, float inverse) : s(scale), inv(inverse), zero(inverse < 0.f) {}   // made before; inverse -1: zero
   __device__ __forceinline__ explicit QuantScale(float top) {
     const bool bad = !(top <= 3.402823466e38f);
     s = bad ? __uint_as_float(0x7fffffffu) : __fdiv_rn(top, 127.f);
@@ -277,23 +280,28 @@ __device__ __forceinline__ void store_y(char* C, int out, int64_t at, float y) {
 }
 
 // ------------------------------------------------------------------ a handful of tokens
-// Up to 8 tokens whose 8-bit rows fit 64 KiB of shared memory: what counts is the time from launch to the first weight and from the last
+// One or two tokens, or up to four under a small matrix: what counts is the time from launch to the first weight and from the last
 // weight to the result.  So no tensor memory, barriers or clusters: a warp takes two weight rows, asks for 4 KiB of each at
 // once (16 bytes per lane and load, straight to registers), multiplies them with the tokens in shared memory four bytes at a
-// time, and sums over the warp.  The weights are asked for before the tokens are read, and, where the tokens are small, each
-// block quantises them itself while the weights are on their way (a launch less).
-// Two blocks per SM walk the rows with a fixed stride.  FILLDOT
-constexpr int kDotThreads = 256, kDotUnroll = 8, kDotTokens = 8;
+// time, and sums over the warp.  Two blocks per SM walk the rows with a fixed stride.  Where the tokens are short and 16-bit,
+// each block quantises them itself while its first weights are on their way: a launch less.
+// Measured (us; weights from HBM; the few-token form below in brackets): 1 x 1024 x 1024 2.6 (4.1), 1 x 4096 x 4096 4.6 (6.8), 4 x 4096 x 4096
+// 5.7 (6.8), 1 x 8192 x 8192 13.7 (14.7), 4 x 16384 x 8192 27.4 (25.2), 8 x 8192 x 8192 21.5 (15.0): every token costs the
+// integer units as much again.
+constexpr int kDotThreads = 256, kDotUnroll = 8, kDotTokens = 4;
+constexpr int64_t kDotAlways = 2;           // tokens up to which this form is taken whatever the matrix ...
+constexpr int64_t kDotWeights = 1 << 25;    // ... and bytes of weights up to which it is for kDotTokens
 constexpr int64_t kDotBytes = 65536;        // tokens x K that a block holds
-constexpr int64_t kDotQuantize = 8192;      // tokens x K up to which a block quantises for itself: at most 4 vectors per thread
+constexpr int64_t kDotQuantize = 4096;      // tokens x K up to which a block quantises for itself
+constexpr int kDotVecs = (int)(kDotQuantize / 8 / kDotThreads);
 
 struct DotArgs {
   const int8_t* W;
   const float* w_scale;
   const int8_t* q;        // tokens, already 8 bits ...
   const float* q_scale;
-  const void* x;          // ... or not (nullptr: they are): quantised here, into q_out and scale_out as well
-  int x_dtype;
+  const uint16_t* x;      // ... or not (QUANT): quantised here, into q_out and scale_out as well
+  int x_bf16;             // bf16, else fp16
   int64_t cols;           // of x
   int8_t* q_out;
   float* scale_out;
@@ -303,72 +311,80 @@ struct DotArgs {
   int early;              // as FewArgs
 };
 
-// Eight elements of x as floats; elements from n on are zero.
-__device__ __forceinline__ void dot_load(const void* x, int dtype, int64_t at, int n, bool aligned, float (&f)[8]) {
-  auto as = [&](auto v, auto* p) {
-    if (n == 8 && aligned) v.load(p + at);
-    else v.load_some(p + at, n);
-    v.values(f);
-  };
-  if (dtype == SP_BF16) as(Vec8<__nv_bfloat16>(), static_cast<const __nv_bfloat16*>(x));
-  else if (dtype == SP_FP16) as(Vec8<__half>(), static_cast<const __half*>(x));
-  else as(Vec8<float>(), static_cast<const float*>(x));
+// The tokens to 8 bits, by the whole block.  Their vectors were asked for before the first weights: behind those they would arrive last.
+__device__ __forceinline__ void dot_fetch_tokens(const DotArgs& a, Vec8<uint16_t> (&v)[kDotVecs]) {
+  const int nvec = a.K / 8, total = a.M * nvec;
+  const bool aligned = (((uintptr_t)a.x | (uintptr_t)(a.cols * 2)) & 15u) == 0;
+#pragma unroll
+  for (int i = 0; i < kDotVecs; ++i) {
+    const int at = (int)threadIdx.x + i * kDotThreads;
+    if (at < total) {
+      const int m = at / nvec, j = at - m * nvec;
+      const uint16_t* p = a.x + (int64_t)m * a.cols + (int64_t)j * 8;
+      const int n = (int)min((int64_t)8, max((int64_t)0, a.cols - (int64_t)j * 8));
+      if (n == 8 && aligned) v[i].load(p);
+      else v[i].load_some(p, n);
+    }
+  }
 }
 
-// The tokens to 8 bits, by the whole block.  x is read twice, the second time from the nearest cache: held in registers between the
-// passes it would push out the weights that are on their way, and the block would wait for those first.
-__device__ __forceinline__ void dot_quantize(const DotArgs& a, int8_t* tokens, float* scales, uint32_t* tops) {
+__device__ __forceinline__ float dot_top(uint32_t bits, int bf16) { return bf16 ? quant_top<__nv_bfloat16>(bits) : quant_top<__half>(bits); }
+
+__device__ __forceinline__ void dot_quantize(const DotArgs& a, const Vec8<uint16_t> (&v)[kDotVecs], int8_t* tokens, float* scales, float* inverses, uint32_t* tops) {
   const int nvec = a.K / 8, total = a.M * nvec, lane = threadIdx.x & 31;
-  const bool aligned = (((uintptr_t)a.x | (uintptr_t)(a.cols * (a.x_dtype == SP_FP32 ? 4 : 2))) & 15u) == 0;
-  auto load = [&](int at, int& m, int& j, float (&f)[8]) {
-    m = at / nvec; j = at - m * nvec;
-    dot_load(a.x, a.x_dtype, (int64_t)m * a.cols + (int64_t)j * 8, (int)min((int64_t)8, max((int64_t)0, a.cols - (int64_t)j * 8)), aligned, f);
-  };
-#pragma unroll 2
-  for (int first = (int)threadIdx.x - lane; first < total; first += kDotThreads) {      // of this warp
-    float f[8];
-    int m = 0, j;
-    uint32_t top = 0;
-    if (first + lane < total) {
-      load(first + lane, m, j, f);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(f[e]) & 0x7fffffffu);
-    }
-    if (first / nvec == (first + 31) / nvec) {       // the warp is inside one row
-      top = __reduce_max_sync(0xffffffffu, top);
-      if (lane == 0) atomicMax(tops + m, top);
-    } else if (first + lane < total) {
-      atomicMax(tops + m, top);
+  for (int i = 0; i < kDotVecs; ++i) {
+    const int first = (int)threadIdx.x - lane + i * kDotThreads;      // of this warp
+    if (first < total) {
+      const int at = first + lane, m = at / nvec;
+      const uint32_t top = at < total ? __float_as_uint(dot_top(v[i].larger(0u), a.x_bf16)) : 0u;
+      if (first / nvec == (first + 31) / nvec) {       // the warp is inside one row
+        const uint32_t all = __reduce_max_sync(0xffffffffu, top);
+        if (lane == 0) atomicMax(tops + m, all);
+      } else if (at < total) {
+        atomicMax(tops + m, top);
+      }
     }
   }
   __syncthreads();
-#pragma unroll 2
-  for (int at = threadIdx.x; at < total; at += kDotThreads) {
-    float f[8];
-    int m, j;
-    load(at, m, j, f);
-    const QuantScale k(__uint_as_float(tops[m]));
-    uint2 b = make_uint2(0u, 0u);
-    if (!k.zero && k.inv != 0.f) b = quant_pack(f, k);
-    if (!k.zero && k.inv == 0.f) {
-      uint64_t bytes = 0;
+  if (threadIdx.x < (unsigned)a.M) {
+    const QuantScale k(__uint_as_float(tops[threadIdx.x]));
+    scales[threadIdx.x] = k.s;
+    inverses[threadIdx.x] = k.zero ? -1.f : k.inv;
+    if (blockIdx.x == 0) a.scale_out[threadIdx.x] = k.s;
+  }
+  __syncthreads();
 #pragma unroll
-      for (int e = 0; e < 8; ++e) bytes |= (uint64_t)(uint8_t)quant_by_remainder(f[e], k.s) << (8 * e);
-      b = make_uint2((uint32_t)bytes, (uint32_t)(bytes >> 32));
-    }
-    *reinterpret_cast<uint2*>(tokens + (int64_t)m * a.K + (int64_t)j * 8) = b;
-    if (j == 0) scales[m] = k.s;
-    if (blockIdx.x == 0) {
-      *reinterpret_cast<uint2*>(a.q_out + (int64_t)m * a.K + (int64_t)j * 8) = b;
-      if (j == 0) a.scale_out[m] = k.s;
+  for (int i = 0; i < kDotVecs; ++i) {
+    const int at = (int)threadIdx.x + i * kDotThreads;
+    if (at < total) {
+      const int m = at / nvec, j = at - m * nvec;
+      const QuantScale k(scales[m], inverses[m]);
+      uint2 b = make_uint2(0u, 0u);
+      if (!k.zero) {
+        float f[8];
+        if (a.x_bf16) v[i].template values_as<__nv_bfloat16>(f);
+        else v[i].template values_as<__half>(f);
+        if (k.inv != 0.f) {
+          b = quant_pack(f, k);
+        } else {
+          uint64_t bytes = 0;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) bytes |= (uint64_t)(uint8_t)quant_by_remainder(f[e], k.s) << (8 * e);
+          b = make_uint2((uint32_t)bytes, (uint32_t)(bytes >> 32));
+        }
+      }
+      *reinterpret_cast<uint2*>(tokens + (int64_t)m * a.K + (int64_t)j * 8) = b;
+      if (blockIdx.x == 0) *reinterpret_cast<uint2*>(a.q_out + (int64_t)m * a.K + (int64_t)j * 8) = b;
     }
   }
 }
 
-template <int MT>
+// QUANT: the tokens are quantised here (its registers would cost the other form half a microsecond).
+template <int MT, bool QUANT>
 __global__ void __launch_bounds__(kDotThreads, 2) dot_tokens_kernel(const DotArgs a) {
   extern __shared__ __align__(16) int8_t dot_tokens[];     // MT rows of K bytes; rows beyond M are read and not used
-  __shared__ float scales[kDotTokens];
+  __shared__ float scales[kDotTokens], inverses[kDotTokens];
   __shared__ uint32_t tops[kDotTokens];
   const int lane = threadIdx.x & 31, warp = blockIdx.x * (kDotThreads / 32) + (threadIdx.x >> 5);
   const int step = gridDim.x * (kDotThreads / 32) * 2;
@@ -383,13 +399,15 @@ __global__ void __launch_bounds__(kDotThreads, 2) dot_tokens_kernel(const DotArg
         w[r][u] = n + r < a.N && c < a.K ? __ldcs(reinterpret_cast<const int4*>(a.W + (n + r) * a.K + c)) : make_int4(0, 0, 0, 0);
       }
   };
+  Vec8<uint16_t> own[QUANT ? kDotVecs : 1];
   if (!a.early) pdl_wait();
+  if constexpr (QUANT) dot_fetch_tokens(a, own);
   fetch(warp * 2, 0);
   if (a.early) pdl_wait();
-  if (a.x != nullptr) {
+  if constexpr (QUANT) {
     if (threadIdx.x < kDotTokens) tops[threadIdx.x] = 0;
     __syncthreads();
-    dot_quantize(a, dot_tokens, scales, tops);
+    dot_quantize(a, own, dot_tokens, scales, inverses, tops);
   } else {
     for (int i = threadIdx.x; i < a.M * (a.K / 16); i += kDotThreads)
       reinterpret_cast<int4*>(dot_tokens)[i] = __ldg(reinterpret_cast<const int4*>(a.q) + i);
@@ -433,6 +451,8 @@ __global__ void __launch_bounds__(kDotThreads, 2) dot_tokens_kernel(const DotArg
 // At most NT rows of A: the call is bound by reading the weights once, so the weights take the 128-row side of the MMA and the
 // tokens its N side, and the k axis of each 128-row block is split over the S CTAs of a cluster to occupy every SM.  The
 // partial sums are integers: they meet through distributed shared memory, in any order with one result.
+// For up to 64 tokens.  Measured (us; as 128 x 128 tiles in brackets): 16 x 4096 x 4096 7.7 (12.3), 64 x 4096 x 4096 12.3 (12.8), 24 x 16384 x 8192
+// 26.5 (36), 128 x 4096 x 4096 19.1 (12.9).
 template <int NT>
 struct FewCfg {
   static constexpr uint32_t kWBytes = 128 * 128, kQBytes = NT * 128, kStageBytes = kWBytes + kQBytes;
@@ -664,7 +684,7 @@ struct I8Call {
   std::vector<int32_t> host_perm;
 };
 
-constexpr int64_t kFewTokens = 128;
+constexpr int64_t kFewTokens = 64;
 
 // Checks everything the host can check; chooses tile and order where they are left to the library.
 static int check_i8(const void* A, const void* a_scale, const void* B, const void* b_scale, const void* C, int64_t M, int64_t N, int64_t K,
@@ -727,9 +747,9 @@ static int check_i8(const void* A, const void* a_scale, const void* B, const voi
   return SP_OK;
 }
 
-template <int MT>
+template <int MT, bool QUANT>
 static int launch_dot(const DotArgs& a, cudaStream_t stream) {
-  auto kern = dot_tokens_kernel<MT>;
+  auto kern = dot_tokens_kernel<MT, QUANT>;
   static uint64_t configured = 0;
   if (first_use_on_this_device(configured)) {
     const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kDotBytes);
@@ -740,21 +760,19 @@ static int launch_dot(const DotArgs& a, cudaStream_t stream) {
 }
 
 // The tokens come quantised (x == nullptr) or are quantised by every block.
-static int run_dot(const I8Call& c, const void* x, int x_dtype, int64_t cols, bool early, cudaStream_t stream) {
+static int run_dot(const I8Call& c, const void* x, int x_dtype, int64_t cols, bool early, cudaStream_t stream) {   // x: bf16 or fp16
   DotArgs a = {};
   a.W = (const int8_t*)c.B; a.w_scale = c.b_scale; a.q = (const int8_t*)c.A; a.q_scale = c.a_scale;
-  a.x = x; a.x_dtype = x_dtype; a.cols = cols; a.q_out = (int8_t*)const_cast<void*>(c.A); a.scale_out = const_cast<float*>(c.a_scale);
+  a.x = (const uint16_t*)x; a.x_bf16 = x_dtype == SP_BF16; a.cols = cols; a.q_out = (int8_t*)const_cast<void*>(c.A); a.scale_out = const_cast<float*>(c.a_scale);
   a.C = (char*)c.C; a.M = (int)c.M; a.N = (int)c.N; a.K = (int)c.K; a.out = c.out; a.early = early ? 1 : 0;
-  if (c.M <= 1) return launch_dot<1>(a, stream);
-  if (c.M <= 2) return launch_dot<2>(a, stream);
-  if (c.M <= 4) return launch_dot<4>(a, stream);
-  return launch_dot<8>(a, stream);
+  if (c.M <= 1) return x ? launch_dot<1, true>(a, stream) : launch_dot<1, false>(a, stream);
+  if (c.M <= 2) return x ? launch_dot<2, true>(a, stream) : launch_dot<2, false>(a, stream);
+  return x ? launch_dot<4, true>(a, stream) : launch_dot<4, false>(a, stream);
 }
 
-// MT rows of the next power of two must fit.
 static bool takes_dot(const I8Call& c) {
-  const int64_t mt = c.M <= 1 ? 1 : c.M <= 2 ? 2 : c.M <= 4 ? 4 : 8;
-  return c.few && c.M <= kDotTokens && mt * c.K <= kDotBytes;
+  const int64_t mt = c.M <= 2 ? c.M : 4;      // rows of shared memory
+  return c.few && (c.M <= kDotAlways || (c.M <= kDotTokens && c.N * c.K <= kDotWeights)) && mt * c.K <= kDotBytes;
 }
 
 template <int NT>
@@ -801,8 +819,7 @@ static int run_i8(const I8Call& c, bool early, cudaStream_t stream) {
     a.M = (int)c.M; a.N = (int)c.N; a.kblocks = (int)((c.K + 127) / 128); a.out = c.out; a.early = early ? 1 : 0;
     if (c.M <= 16) return launch_few<16>(c, tmB, a, stream);
     if (c.M <= 32) return launch_few<32>(c, tmB, a, stream);
-    if (c.M <= 64) return launch_few<64>(c, tmB, a, stream);
-    return launch_few<128>(c, tmB, a, stream);
+    return launch_few<64>(c, tmB, a, stream);
   }
   ProdArgs pa = {};
   pa.perm = st.perm; pa.status = st.status; pa.M = (int)c.M; pa.N = (int)c.N;
@@ -863,7 +880,7 @@ int sp_linear_i8(const void* x, int32_t x_dtype, int8_t* q, float* q_scale, cons
   rc = current_device(&dev);
   if (rc != SP_OK) return rc;
   std::lock_guard<std::mutex> lock(g_i8_mu);
-  if (takes_dot(call) && M * call.K <= kDotQuantize) return run_dot(call, x, x_dtype, K, false, (cudaStream_t)stream);
+  if (takes_dot(call) && M * call.K <= kDotQuantize && x_dtype != SP_FP32) return run_dot(call, x, x_dtype, K, false, (cudaStream_t)stream);
   rc = quantize(x, x_dtype, M, K, q, q_scale, (cudaStream_t)stream);
   if (rc != SP_OK) return rc;
   return run_i8(call, true, (cudaStream_t)stream);
