@@ -114,9 +114,11 @@ def test_quantizer_reads_rows_at_any_address():
         assert same(s, rs) and same(q, rq)
 
 
-# tokens: both sides of each few-token width; N: one channel, edges of 128-row blocks, odd; K: one stage, edges, several slices
+# tokens: both sides of each few-token width and of the dot products' limits (tokens, weights, bytes of tokens); N: one channel, edges of
+# 128-row blocks, odd; K: one stage, edges, several slices
 @pytest.mark.parametrize("M,N,K", [(1, 1, 16), (1, 128, 128), (1, 129, 2048), (2, 4096, 4096), (16, 200, 1040), (17, 1000, 528), (33, 77, 4096), (64, 640, 4112),
-                                   (65, 300, 1024), (128, 257, 8192), (128, 20000, 256)])
+                                   (65, 300, 1024), (128, 257, 8192), (128, 20000, 256),
+                                   (2, 17, 16), (3, 1000, 4112), (4, 130, 16384), (3, 8300, 4112), (2, 100, 32784), (4, 33, 16400), (5, 1000, 512)])
 @pytest.mark.parametrize("out", ["bf16", "fp16", "fp32"])
 def test_few_tokens(M, N, K, out):
     q, s, w, ws, dev = operands(M, N, K, M + N + K)
@@ -170,7 +172,7 @@ def test_scales_that_would_leave_the_range_together():
     assert same(product(dev[0][:9].contiguous(), dev[1][:9].contiguous(), dev[2], dev[3], "fp32").cpu().numpy(), ref[:9])
 
 
-@pytest.mark.parametrize("M", [1, 40, 200])
+@pytest.mark.parametrize("M", [1, 3, 4, 5, 40, 200])
 @pytest.mark.parametrize("dtype,out", [("bf16", "bf16"), ("fp16", "fp32"), ("fp32", "fp16")])
 def test_linear_is_its_two_calls(M, dtype, out):
     N, K = 333, 1003
@@ -191,9 +193,29 @@ def test_linear_is_its_two_calls(M, dtype, out):
     assert np.isnan(ref[M // 2]).all() == (M > 1) and np.isfinite(np.delete(ref, M // 2, 0)).all()
 
 
-def test_weights_written_just_before_the_call_are_the_ones_used():
+@pytest.mark.parametrize("M", [2, 70])
+def test_linear_on_rows_of_zeros_and_denormal_numbers(M):
+    N, K = 40, 72
+    x = torch.randn(M, K, generator=torch.Generator().manual_seed(M)).float()
+    x[0] *= 1e-39
+    x[1] = 0
+    x = x.bfloat16()
+    w = torch.randint(-127, 128, (N, 80), generator=torch.Generator().manual_seed(1), dtype=torch.int32).to(torch.int8)
+    w[:, K:] = 0
+    ws = torch.full((N,), 3e38)
+    q, s, y = torch.empty(M, 80, dtype=torch.int8, device="cuda"), torch.empty(M, device="cuda"), torch.empty(M, N, device="cuda")
+    sp.linear_i8(x.cuda(), q, s, w.cuda(), ws.cuda(), y)
+    rq, rs = LN.quantize_i8(x.double().numpy())
+    assert same(q.cpu().numpy(), rq) and same(s.cpu().numpy(), rs) and 0 < rs[0] < 1.2e-38
+    with np.errstate(over="ignore"):
+        assert same(y.cpu().numpy(), LN.gemm_i8(rq, rs, w.numpy(), ws.numpy()))
+    assert (y[1] == 0).all()
+
+
+@pytest.mark.parametrize("tokens", [1, 2, 24])
+def test_weights_written_just_before_the_call_are_the_ones_used(tokens):
     # the few-token form fetches weights while x is being quantised: they may still have been written by the kernel before the call
-    M, N, K = 4, 8192, 4096
+    M, N, K = tokens, 8192, 4096
     g = torch.Generator(device="cuda").manual_seed(0)
     x = torch.randn(M, K, device="cuda", generator=g).bfloat16()
     ws = torch.ones(N, device="cuda")
@@ -245,6 +267,30 @@ def test_calls_on_two_streams_at_once():
         assert sp.get_status(st) == 0
     for (q, s, w, ws, _), y in zip((a, b), ys):
         assert same(y.cpu().numpy(), LN.gemm_i8(q, s, w, ws))
+
+
+def test_calls_from_two_host_threads():
+    import threading
+    cases = [operands(2, 500, 512, 1), operands(30, 900, 1024, 2), operands(300, 301, 272, 3)]
+    wrong = []
+
+    def work(k):
+        try:
+            st = torch.cuda.Stream()
+            for i in range(15):
+                q, s, w, ws, dev = cases[(i + k) % 3]
+                y = torch.empty(q.shape[0], w.shape[0], device="cuda")
+                torch.cuda.synchronize()
+                sp.gemm_i8(*dev, y, stream=st)
+                assert sp.get_status(st) == 0
+                assert same(y.cpu().numpy(), LN.gemm_i8(q, s, w, ws))
+        except BaseException as e:      # noqa: BLE001 - reported by the main thread
+            wrong.append(repr(e))
+
+    threads = [threading.Thread(target=work, args=(k,)) for k in range(2)]
+    [t.start() for t in threads]
+    [t.join() for t in threads]
+    assert not wrong, wrong
 
 
 def test_offsets_beyond_32_bits():
