@@ -4,7 +4,7 @@
 //   g_tv = c_t (exp(z_tv - lse_t) - [v = target(t)]),     dh = g . W,   dW = g^T . h
 //
 // Forward: the product runs tile by tile on the tensor cores; the epilogue reduces 128 columns of a row to a
-// (maximum, sum of exponentials) pair, so T x V scores become T x V / 128 pairs, which a second kernel joins.
+// (maximum, sum of exponentials) pair, so T x V scores become about T x V / 128 pairs, which a second kernel joins.
 // Gradient: the vocabulary is walked in pieces.  A piece's scores are made again, turned into g in the epilogue and written as 16 bits;
 // two more products read them: dh += g . W_piece (k = the vocabulary) and dW_piece = g^T . h (k = the tokens).
 #include <math_constants.h>
@@ -19,8 +19,8 @@ namespace sp {
 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
-constexpr int kCeTile = 256;     // vocabulary columns of one tile
-constexpr int kCePart = 128;     // and of one epilogue warp
+constexpr int kCeTile = 256;     // vocabulary columns of one tile, at most
+constexpr int kCePart = 128;     // and of one epilogue warp, at most
 constexpr int kMaxSplits = 64;   // slices of the vocabulary in the product for dh
 
 __device__ __forceinline__ float ex2(float x) {
@@ -51,7 +51,7 @@ struct EpiStats {
   static constexpr uint32_t kBytes = 0;
   static constexpr bool kSums = true;
   struct Args {
-    float2* stats;            // [column / 128][row]
+    float2* stats;            // [part of the columns][row]
     float* picked;            // score of the row's target
     const int64_t* target;
   };
@@ -62,13 +62,12 @@ struct EpiStats {
   __device__ __forceinline__ void before(const EpiTile& e, int M, int N) {
     const int row = e.row0 + lane;
     const int64_t t = row < M ? __ldg(a.target + row) : -1;
-    rel = t >= e.col0 && t < N && t < (int64_t)e.col0 + kCePart ? (int)(t - e.col0) : -1;
+    rel = t >= e.col0 && t < N && t < (int64_t)e.col0 + kCePart ? (int)(t - e.col0) : -1;      // N: the tile's edge
   }
   template <int COLS>
   __device__ __forceinline__ void finish(uint32_t (&v)[COLS], const EpiTile& e, int M, int N) {
     static_assert(COLS == kCePart, "");
-    if (e.col0 >= N) return;
-    if (e.col0 + COLS > N) {     // columns beyond the vocabulary
+    if (e.col0 + COLS > N) {     // columns beyond the tile or the vocabulary
 #pragma unroll
       for (int j = 0; j < COLS; ++j)
         if (e.col0 + j >= N) v[j] = 0xff800000u;
@@ -98,7 +97,7 @@ struct EpiStats {
       for (int i = 0; i < 8; ++i) s[i] += ex2(fmaf(__uint_as_float(v[j + i]), kLog2e, -ref));
     const int row = e.row0 + lane;
     if (row < M) {
-      a.stats[(int64_t)(e.col0 / kCePart) * M + row] = make_float2(m, ((s[0] + s[1]) + (s[2] + s[3])) + ((s[4] + s[5]) + (s[6] + s[7])));
+      a.stats[(int64_t)e.part * M + row] = make_float2(m, ((s[0] + s[1]) + (s[2] + s[3])) + ((s[4] + s[5]) + (s[6] + s[7])));
       if (rel >= 0) a.picked[row] = hit;
     }
   }
@@ -531,7 +530,7 @@ static int64_t div_up(int64_t a, int64_t b) { return (a + b - 1) / b; }
 struct CePlan {
   int64_t T, V, D;
   bool row;                   // forward: the form for one token
-  int64_t tiles;              // pairs per token that the forward product leaves: one per 128 words, or per block
+  int64_t tiles;              // pairs per token that the forward product leaves: two per vocabulary tile, or one per block
   int64_t piece, ld_g;        // gradient: vocabulary rows of a piece, row pitch of g
   int pieces;
   int slices;                 // of the vocabulary in the product for dh
@@ -550,7 +549,7 @@ static CePlan ce_plan(int64_t T, int64_t V, int64_t D) {
   CePlan p = {};
   p.T = T; p.V = V; p.D = D;
   p.row = T == 1 && D <= kRowMaxD;
-  p.tiles = div_up(V, kCePart);
+  p.tiles = 2 * div_up(V, tile_width(T, V, ce_rows(T) / 128, 32));
   if (p.row) p.tiles = div_up(V, 2 * kRowThreads / 32) < 2 * 148 ? div_up(V, 2 * kRowThreads / 32) : 2 * 148;   // blocks: two per SM
   p.off_picked = up256(p.tiles * T * 8);
   p.off_each = p.off_picked + up256(T * 4);
@@ -602,19 +601,19 @@ static int check_ce(const void* h, const void* W, const void* target, const void
 // The tile grid of one product in bands of eight tile rows, walked serpentine-wise: a wave of tiles is then about as
 // tall as it is wide, so it needs few operand panels, and a band starts on the panels the last one used last.  `rows`: row-major, for an
 // output whose writing is what bounds the product: a wave then writes whole rows (dW of 16 tokens, 65536 x 4096: 106 us, in bands 114).
-static int ce_sched(int64_t M, int64_t N, int tile_m, Sched* out, bool rows = false) {
-  if (rows) return resolve_sched(M, N, tile_m, 256, SP_ROW_MAJOR, nullptr, out);
+static int ce_sched(int64_t M, int64_t N, int tile_m, int tile_n, Sched* out, bool rows = false) {
+  if (rows) return resolve_sched(M, N, tile_m, tile_n, SP_ROW_MAJOR, nullptr, out);
   sp_params p = {};
   p.struct_size = sizeof p;
   p.group = 8;
   p.flags = SP_FLAG_SERPENTINE;
-  return resolve_sched(M, N, tile_m, 256, SP_GROUP_M, &p, out);
+  return resolve_sched(M, N, tile_m, tile_n, SP_GROUP_M, &p, out);
 }
 
 static ProdArgs ce_args(const Sched& sched, int32_t* status, int64_t M, int64_t N, int64_t K, int slices) {
   ProdArgs a = {};
   a.status = status;
-  a.M = (int)M; a.N = (int)N;
+  a.M = (int)M; a.N = (int)N; a.bn = 256;
   a.kblocks = (int)div_up(K, 64);
   a.splits = a.kblocks < slices ? a.kblocks : slices;
   a.kb_sum = kCeSum;
@@ -628,13 +627,14 @@ static int ce_scores(const char* what, const CePlan& p, const void* h, int64_t l
                      const typename Epi::Args& ea, cudaStream_t stream) {
   CUtensorMap tmA, tmB;
   Sched sched;
-  const int rows = ce_rows(p.T);
-  int rc = ce_sched(p.T, cols, rows, &sched);
+  const int rows = ce_rows(p.T), width = tile_width(p.T, cols, rows / 128, tmC ? 64 : 32);      // g is stored 64 columns at a time
+  int rc = ce_sched(p.T, cols, rows, width, &sched);
   if (rc == SP_OK) rc = make_map_any(&tmA, h, 2, p.T, p.D, ld_h, 128, 64);
-  if (rc == SP_OK) rc = make_map_any(&tmB, W, 2, cols, p.D, p.D, rows == 256 ? 128 : 256, 64);
+  if (rc == SP_OK) rc = make_map_any(&tmB, W, 2, cols, p.D, p.D, width / (rows / 128), 64);
   if (rc != SP_OK) return rc;
   ProdArgs a = ce_args(sched, status, p.T, cols, p.D, 1);
   a.turn = sched.Tm == 1;
+  a.bn = width;
   if (rows == 256) return launch_product<2, 256, kElem16, false, false, Epi>(what, tmA, tmB, tmC ? *tmC : tmA, a, bf16, ea, stream);
   return launch_product<1, 256, kElem16, false, false, Epi>(what, tmA, tmB, tmC ? *tmC : tmA, a, bf16, ea, stream);
 }
@@ -755,7 +755,7 @@ int sp_linear_ce_grad(const void* h, const void* W, const int64_t* target, const
     if (rc != SP_OK) return rc;
     if (dh) {
       Sched sched;
-      rc = ce_sched(T, D, ce_rows(T), &sched);
+      rc = ce_sched(T, D, ce_rows(T), 256, &sched);
       if (rc == SP_OK) rc = make_map_any(&tmA, g, 2, T, cols, p.ld_g, 128, 64);
       if (rc == SP_OK) rc = make_map_any(&tmB, Wp, 2, cols, D, D, 64, 64);
       if (rc != SP_OK) return rc;
@@ -778,7 +778,7 @@ int sp_linear_ce_grad(const void* h, const void* W, const int64_t* target, const
     }
     if (dW) {
       Sched sched;
-      rc = ce_sched(cols, D, 256, &sched, T * D <= (8ll << 20));
+      rc = ce_sched(cols, D, 256, 256, &sched, T * D <= (8ll << 20));
       if (rc == SP_OK) rc = make_map_any(&tmA, g, 2, T, cols, p.ld_g, 64, 64);
       if (rc == SP_OK) rc = make_map_any(&tmB, rows, 2, T, D, p.ld_h, 64, 64);
       if (rc == SP_OK) rc = make_map_any(&tmC, (char*)dW + v0 * D * 2, 2, cols, D, D, 32, 64);

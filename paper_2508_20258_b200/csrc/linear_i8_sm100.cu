@@ -680,6 +680,7 @@ struct I8Call {
   int out;
   int few;              // few-token form (library's choice of tile and order, M <= kFewTokens)
   int tile_m, tile_n;
+  bool plain;           // rows of C that a bulk store cannot take
   Sched sched;
   std::vector<int32_t> host_perm;
 };
@@ -716,16 +717,15 @@ static int check_i8(const void* A, const void* a_scale, const void* B, const voi
   call->M = M; call->N = N; call->K = K; call->out = out;
   call->few = scheme == SP_ORDER_AUTO && pick && M <= kFewTokens;
   if (call->few) return SP_OK;
+  const int64_t ld = N * (int64_t)elt_bytes(out);
+  call->plain = ((uintptr_t)C & 15u) || (ld & 15);
   if (pick) {
-    // the tile with the least waves x area / (CTAs per tile x relative rate of its shape); rates measured at 4096^3 and 8192^3
-    static const struct { int tm, tn; double eff; } kTiles[] = {{256, 256, 1.00}, {128, 128, 0.70}};
-    double best = 0;
-    for (const auto& t : kTiles) {
-      const int64_t T = ((M + t.tm - 1) / t.tm) * ((N + t.tn - 1) / t.tn);
-      const int cg = t.tm / 128, units = 148 / cg;
-      const double cost = (double)((T + units - 1) / units) * t.tm * t.tn / (cg * t.eff);
-      if (tile_m == 0 || cost < best) { tile_m = t.tm; tile_n = t.tn; best = cost; }
-    }
+    // 256 rows by the width that fills the waves best (bulk stores of 16-bit results come in 64 columns), or 128 x 128 where that is less: a tile of
+    // 128 x 128 runs at 0.70 of the rate of 256 x 256 (4096^3 and 8192^3)
+    tile_m = 256;
+    tile_n = tile_width(M, N, 2, out == SP_FP32 || call->plain ? 32 : 64);
+    const auto waves = [&](int tm, int tn, int units) { return (double)((((M + tm - 1) / tm) * ((N + tn - 1) / tn) + units - 1) / units); };
+    if (waves(128, 128, 148) * 128 * 128 * (304.0 / 256) / 0.70 < waves(256, tile_n, 74) * 128 * (tile_n + 48)) tile_m = tile_n = 128;
   }
   sp_params own = {};
   own.struct_size = sizeof own;
@@ -822,7 +822,7 @@ static int run_i8(const I8Call& c, bool early, cudaStream_t stream) {
     return launch_few<64>(c, tmB, a, stream);
   }
   ProdArgs pa = {};
-  pa.perm = st.perm; pa.status = st.status; pa.M = (int)c.M; pa.N = (int)c.N;
+  pa.perm = st.perm; pa.status = st.status; pa.M = (int)c.M; pa.N = (int)c.N; pa.bn = c.tile_n;
   pa.kblocks = (int)((c.K + 127) / 128); pa.splits = 1;
   pa.sched = c.sched;
   const int cg = c.tile_m / 128;
@@ -830,13 +830,11 @@ static int run_i8(const I8Call& c, bool early, cudaStream_t stream) {
   if (rc == SP_OK) rc = make_map_any(&tmB, c.B, 1, c.N, c.K, c.K, c.tile_n / cg, 128);
   if (rc != SP_OK) return rc;
   const int elt = (int)elt_bytes(c.out);
-  const int64_t ld = c.N * elt;
-  const bool plain = ((uintptr_t)c.C & 15u) || (ld & 15);
-  if (plain) tmC = tmB;    // not used
+  if (c.plain) tmC = tmB;    // not used
   else rc = make_map_any(&tmC, c.C, elt, c.M, c.N, c.N, 32, 128 / elt);
   if (rc != SP_OK) return rc;
-  if (c.out == SP_FP32) return plain ? launch_tiles<true, true>(c, pa, tmA, tmB, tmC, stream) : launch_tiles<true, false>(c, pa, tmA, tmB, tmC, stream);
-  return plain ? launch_tiles<false, true>(c, pa, tmA, tmB, tmC, stream) : launch_tiles<false, false>(c, pa, tmA, tmB, tmC, stream);
+  if (c.out == SP_FP32) return c.plain ? launch_tiles<true, true>(c, pa, tmA, tmB, tmC, stream) : launch_tiles<true, false>(c, pa, tmA, tmB, tmC, stream);
+  return c.plain ? launch_tiles<false, true>(c, pa, tmA, tmB, tmC, stream) : launch_tiles<false, false>(c, pa, tmA, tmB, tmC, stream);
 }
 
 }  // namespace sp

@@ -53,6 +53,7 @@ struct ProdArgs {
   const int32_t* perm;   // tile table (orders that are not arithmetic), else nullptr
   int32_t* status;
   int M, N;              // rows of A, rows of B
+  int bn;                // columns of a tile: BN, or less where that fills the last wave better (a multiple of 32; B k-major)
   int kblocks;           // stages that cover k
   int splits;            // slices of k: slice z takes stages z, z + splits, z + 2 splits, ...: units that run together read k in step
   int kb_sum;            // stages whose products one accumulator takes before the epilogue adds it to its own sum (Epi::kSums; else a slice)
@@ -116,6 +117,7 @@ __device__ __forceinline__ uint32_t pack_16(float lo, float hi, bool bf16) {
 // What an epilogue is given with the values of its part of a tile's accumulator (one row per lane).
 struct EpiTile {
   int row0, col0;    // row of lane 0, first column of the part
+  int part;          // number of the part among all columns: 2 x tile column + half
   int z;             // slice of k
 };
 
@@ -265,7 +267,7 @@ product_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
       int tm, tn, z;
       tile_at(s, tm, tn, z);
       const int n = stages_of(z);
-      const int row0 = tm * 128 * CG + (int)rank * 128, col0 = tn * BN + (int)rank * C::kBCols;
+      const int row0 = tm * 128 * CG + (int)rank * 128, col0 = tn * args.bn + (int)rank * (args.bn / CG);
       int at = args.turn ? (unit * 5) % n : 0;      // the stage to load, of this slice's
       for (int kb = 0; kb < n; ++kb) {
         ok = mbar_wait(bar_empty + 8 * stage, phase ^ 1u, args.status, (kProdProducer << 8) | 1);
@@ -277,7 +279,7 @@ product_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
         const int k = (z + at * args.splits) * C::kBK;
         if (++at == n) at = 0;
         if (elect_one()) {
-          if (rank == 0) mbar_arrive_expect_tx(full_local, CG * C::kStageBytes);
+          if (rank == 0) mbar_arrive_expect_tx(full_local, CG * C::kABytes + (uint32_t)args.bn * 128u);
           if constexpr (A_MN) {
 #pragma unroll
             for (int j = 0; j < 2; ++j) tma_load_2d<CG>(sa + j * 8192, &tmA, row0 + j * 64, k, full_leader);   // boxes of 64 k x 64 rows
@@ -367,8 +369,10 @@ product_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
       tile_at(s, tm, tn, e.z);
       const int n = stages_of(e.z);
       e.row0 = tm * 128 * CG + (int)rank * 128 + quarter * 32;
-      e.col0 = tn * BN + half * kCols;
-      epi.before(e, args.M, args.N);
+      e.col0 = tn * args.bn + half * kCols;
+      e.part = 2 * tn + half;
+      const int edge = min(args.N, (tn + 1) * args.bn);   // what the accumulator holds beyond the tile's own columns is not used
+      epi.before(e, args.M, edge);
       uint32_t v[kCols];
       for (int ks = 0; ks < n; ks += args.kb_sum, ++it) {
         const int buf = it & 1;
@@ -400,7 +404,7 @@ product_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
         }
       }
       if (!ok) break;
-      epi.template finish<kCols>(v, e, args.M, args.N);
+      epi.template finish<kCols>(v, e, args.M, edge);
     }
     if (lane == 0) bulk_wait_all();   // every store of this warp has reached global memory
     __syncwarp();
@@ -410,6 +414,22 @@ product_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
   unit_sync<CG>();
   if (warp == 1) tmem_dealloc<CG>(tmem_base, C::kTmemCols);
   if (args.overlap && threadIdx.x == 0) pdl_wait();
+}
+
+// Columns of a tile of 128 * CG rows for M x N results: the width, from 256 down in steps of `step`, with the least waves x (width + 48) (the
+// tensor cores' time goes with the width, the operands' way through L2 with 256 + width), while 256 would make up to three waves.  8-bit
+// 1000 x 3000 x 4000: 13.3 us at 192 columns, 15.4 at 256; 2001 x 4999 x 2048: 28.8 and 30.9.  Beyond three waves the power limit decides, not
+// the last wave (4096^3: 54.7 and 52.6), and with one tile row the reading of B does (16 tokens x 65536 x 4096: 101 and 97).
+inline int tile_width(int64_t M, int64_t N, int cg, int step) {
+  const int64_t units = 148 / cg, rows = (M + 128 * cg - 1) / (128 * cg);
+  int best = 256;
+  int64_t least = 0;
+  if (rows == 1 || rows * ((N + 255) / 256) > 3 * units) return best;
+  for (int w = 256; w >= 160; w -= step) {
+    const int64_t cost = (rows * ((N + w - 1) / w) + units - 1) / units * (w + 48);
+    if (least == 0 || cost < least) { least = cost; best = w; }
+  }
+  return best;
 }
 
 // Launch with programmatic stream serialisation: the next kernel's set-up overlaps this one's tail.
@@ -432,7 +452,7 @@ inline int launch_pdl(const char* what, void (*kern)(KArgs...), dim3 grid, int t
   return SP_OK;
 }
 
-// Fills args.idesc, args.units and launches one product.  The caller has set M, N, kblocks, splits (at most kblocks), sched, perm, status.
+// Fills args.idesc, args.units and launches one product.  The caller has set M, N, bn, kblocks, splits (at most kblocks), sched, perm, status.
 template <int CG, int BN, int ELEM, bool A_MN, bool B_MN, class Epi>
 int launch_product(const char* what, const CUtensorMap& tmA, const CUtensorMap& tmB, const CUtensorMap& tmC, ProdArgs args, bool bf16,
                    const typename Epi::Args& eargs, cudaStream_t stream) {
@@ -448,7 +468,7 @@ int launch_product(const char* what, const CUtensorMap& tmA, const CUtensorMap& 
   args.units = gemm_units(128 * CG, BN, work);   // one CTA per SM, or as many CTA pairs as fit: same as sp_gemm's tiles of this shape
   if (args.units <= 0) { set_error("could not size the grid"); return SP_ERR_CUDA; }
   if (!Epi::kSums) args.kb_sum = args.kblocks;
-  args.idesc = ELEM == kElemI8 ? idesc_i8(128 * CG, BN) : idesc_16(128 * CG, BN, bf16, A_MN, B_MN);
+  args.idesc = ELEM == kElemI8 ? idesc_i8(128 * CG, args.bn) : idesc_16(128 * CG, args.bn, bf16, A_MN, B_MN);
   return launch_pdl(what, kern, dim3((unsigned)(args.units * CG)), C::kThreads, C::kSmemBytes, CG, stream, tmA, tmB, tmC, args, eargs);
 }
 
