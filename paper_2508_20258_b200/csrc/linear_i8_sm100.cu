@@ -451,12 +451,13 @@ __global__ void __launch_bounds__(kDotThreads, 2) dot_tokens_kernel(const DotArg
 // At most NT rows of A: the call is bound by reading the weights once, so the weights take the 128-row side of the MMA and the
 // tokens its N side, and the k axis of each 128-row block is split over the S CTAs of a cluster to occupy every SM.  The
 // partial sums are integers: they meet through distributed shared memory, in any order with one result.
-// For up to 64 tokens.  Measured (us; as 128 x 128 tiles in brackets): 16 x 4096 x 4096 7.7 (12.3), 64 x 4096 x 4096 12.3 (12.8), 24 x 16384 x 8192
-// 26.5 (36), 128 x 4096 x 4096 19.1 (12.9).
+// Measured (us; as tiles in brackets): 16 x 4096 x 4096 6.6 (12.3), 24 x 16384 x 8192 26.0 (28.6), 64 x 1024 x 1024 5.1 (6.1), 128 x 4096 x 4096 10.9
+// (12.9), 256 x 4096 x 11008 20.0 (28.9); on the other side of the rule 128 x 1024 x 1024 6.7 (6.1), 128 x 11008 x 4096 17.7 (14.4).
 template <int NT>
 struct FewCfg {
   static constexpr uint32_t kWBytes = 128 * 128, kQBytes = NT * 128, kStageBytes = kWBytes + kQBytes;
-  static constexpr int kFit = (114688 - 1024 - 512) / kStageBytes;    // two CTAs per SM
+  static constexpr int kPerSm = NT > 128 ? 1 : 2;                     // CTAs per SM
+  static constexpr int kFit = (229376 / kPerSm - 1024 - 512) / kStageBytes;
   static constexpr int kStages = kFit > 6 ? 6 : kFit;
   static constexpr uint32_t kSmemBytes = kStages * kStageBytes + 512 + 1024;
   static constexpr int kTmemCols = NT < 32 ? 32 : NT;
@@ -477,7 +478,7 @@ struct FewArgs {
 
 
 template <int NT>
-__global__ void __launch_bounds__(192, 2)
+__global__ void __launch_bounds__(192, FewCfg<NT>::kPerSm)
 few_tokens_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmQ, const FewArgs args) {
   using C = FewCfg<NT>;
   constexpr int S = C::kStages;
@@ -571,68 +572,74 @@ few_tokens_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant
     }
   } else {
     pdl_wait();
-    const int quarter = warp & 3, row = quarter * 32 + lane, n = n0 + row;
-    const float bs = nranks == 1 && n < args.N ? __ldg(args.b_scale + n) : 0.f;
+    const int quarter = warp & 3;
     bool ok = mbar_wait(bar_done, 0, args.status, (kProdEpilogue << 8) | 3);
     ok = __all_sync(0xffffffffu, ok);
     tcgen05_fence_after();
     if (ok) {
-#pragma unroll
-      for (int q = 0; q < (NT + 31) / 32; ++q) {
+      // [token][row of W] in shared memory, over the stages; a short loop: code that runs once costs its own loading (unrolled over the tokens:
+      // 125 cycles per token, 128 x 4096 x 4096 17.4 us)
+#pragma unroll 1
+      for (int q = 0; q < (args.M + 31) / 32; ++q) {
         uint32_t v[32];
         tmem_ld_32x32b_x32(tmem + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(q * 32), v);
         tmem_ld_wait();
+        const uint32_t at = smem_base + (uint32_t)(q * 32 * 128 + quarter * 32 + lane) * 4u;
 #pragma unroll
-        for (int j = 0; j < (NT < 32 ? NT : 32); ++j) {
-          const int tok = q * 32 + j;
-          if (tok >= args.M) break;
-          if (nranks == 1) {
-            if (n < args.N) store_y(args.C, args.out, (int64_t)tok * args.N + n, (float)(int)v[j] * __ldg(args.a_scale + tok) * bs);
-          } else {
-            asm volatile("st.shared.b32 [%0], %1;" ::"r"(smem_base + (uint32_t)(tok * 128 + row) * 4u), "r"(v[j]) : "memory");
-          }
-        }
+        for (int j = 0; j < (NT < 32 ? NT : 32); ++j) asm volatile("st.shared.b32 [%0], %1;" ::"r"(at + j * 512u), "r"(v[j]) : "memory");
       }
     }
   }
   tcgen05_fence_before();
+  __syncwarp();
   if (nranks > 1) {
-    __syncwarp();
     asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
-    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
-    if (warp >= 2) {
-      // Each CTA of the cluster finishes every S-th token.  Four tokens at a time, their remote reads in flight together: one after
-      // the other they cost a trip between SMs each (24 tokens, 16384 x 8192: 36 us that way).
-      const int quarter = warp & 3, row = quarter * 32 + lane, n = n0 + row;
-      const float bs = n < args.N ? __ldg(args.b_scale + n) : 0.f;
-      for (int tok = (int)rank; tok < args.M; tok += 4 * (int)nranks) {
-        int acc[4] = {0, 0, 0, 0};
-        float as[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) as[i] = tok + i * (int)nranks < args.M ? __ldg(args.a_scale + tok + i * (int)nranks) : 0.f;
-#pragma unroll
-        for (uint32_t r = 0; r < 8; ++r) {
-          if (r < nranks) {
-            const uint32_t peer = mapa(smem_base, r) + (uint32_t)row * 4u;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              int p = 0;
-              if (tok + i * (int)nranks < args.M)
-                asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(p) : "r"(peer + (uint32_t)(tok + i * (int)nranks) * 512u));
-              acc[i] += p;
-            }
-          }
-        }
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          if (tok + i * (int)nranks < args.M && n < args.N) store_y(args.C, args.out, (int64_t)(tok + i * (int)nranks) * args.N + n, (float)acc[i] * as[i] * bs);
-      }
-    }
-    __syncwarp();
-    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");   // nobody leaves while a peer may read its partial sums
     asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
   } else {
     __syncthreads();
+  }
+  if (warp >= 2) {
+    // Each CTA of the cluster finishes every S-th token: a warp per token, four rows per lane, the reads of all partial sums in flight
+    // together (one element at a time, trip after trip between SMs, 24 tokens x 16384 x 8192 took 36 us).
+    const int row = lane * 4, n = n0 + row;
+    float bs[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) bs[i] = n + i < args.N ? __ldg(args.b_scale + n + i) : 0.f;
+    const bool whole = n + 3 < args.N && (args.N & 3) == 0 && ((uintptr_t)args.C & 15u) == 0;
+#pragma unroll 2
+    for (int tok = (int)rank + (warp - 2) * (int)nranks; tok < args.M; tok += 4 * (int)nranks) {
+      const float as = __ldg(args.a_scale + tok);
+      int p[8][4];
+#pragma unroll
+      for (uint32_t r = 0; r < 8; ++r) {
+        p[r][0] = p[r][1] = p[r][2] = p[r][3] = 0;
+        if (r < nranks)
+          asm volatile("ld.shared::cluster.v4.s32 {%0, %1, %2, %3}, [%4];" : "=r"(p[r][0]), "=r"(p[r][1]), "=r"(p[r][2]), "=r"(p[r][3])
+                       : "r"(mapa(smem_base, r) + (uint32_t)(tok * 128 + row) * 4u));
+      }
+      float y[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        int acc = 0;
+#pragma unroll
+        for (int r = 0; r < 8; ++r) acc += p[r][i];
+        y[i] = (float)acc * as * bs[i];
+      }
+      const int64_t at = (int64_t)tok * args.N + n;
+      if (whole) {
+        if (args.out == SP_FP32) *reinterpret_cast<float4*>(args.C + at * 4) = make_float4(y[0], y[1], y[2], y[3]);
+        else *reinterpret_cast<uint2*>(args.C + at * 2) = make_uint2(pack_16(y[0], y[1], args.out == SP_BF16), pack_16(y[2], y[3], args.out == SP_BF16));
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (n + i < args.N) store_y(args.C, args.out, at + i, y[i]);
+      }
+    }
+  }
+  __syncwarp();
+  if (nranks > 1) {      // nobody leaves while a peer may read its partial sums
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
   }
   if (warp == 1) {
     tcgen05_fence_after();
@@ -685,7 +692,8 @@ struct I8Call {
   std::vector<int32_t> host_perm;
 };
 
-constexpr int64_t kFewTokens = 64;
+// The few-token form: always up to 64 tokens; up to 256 where 128 x 128 tiles would occupy less than half of the SMs and k is long enough to split.
+constexpr int64_t kFewAlways = 64, kFewTokens = 256;
 
 // Checks everything the host can check; chooses tile and order where they are left to the library.
 static int check_i8(const void* A, const void* a_scale, const void* B, const void* b_scale, const void* C, int64_t M, int64_t N, int64_t K,
@@ -715,7 +723,7 @@ static int check_i8(const void* A, const void* a_scale, const void* B, const voi
   }
   call->A = A; call->B = B; call->a_scale = (const float*)a_scale; call->b_scale = (const float*)b_scale; call->C = const_cast<void*>(C);
   call->M = M; call->N = N; call->K = K; call->out = out;
-  call->few = scheme == SP_ORDER_AUTO && pick && M <= kFewTokens;
+  call->few = scheme == SP_ORDER_AUTO && pick && (M <= kFewAlways || (M <= kFewTokens && K >= 2048 && (M + 127) / 128 * ((N + 127) / 128) <= 64));
   if (call->few) return SP_OK;
   const int64_t ld = N * (int64_t)elt_bytes(out);
   call->plain = ((uintptr_t)C & 15u) || (ld & 15);
@@ -788,9 +796,9 @@ static int launch_few(const I8Call& c, const CUtensorMap& tmW, FewArgs args, cud
     if (e != cudaSuccess) { configured = 0; set_error("cudaFuncSetAttribute(smem=%u) failed: %s", C::kSmemBytes, cudaGetErrorString(e)); return SP_ERR_CUDA; }
   }
   const int64_t blocks = (c.N + 127) / 128;
-  // as many slices of k as two CTAs per SM allow, each with at least two stages of work
+  // as many slices of k as the CTAs that run at once allow, each with at least two stages of work
   int split = 1;
-  while (split < 8 && blocks * split * 2 <= 2 * 148 && args.kblocks >= split * 2 * 2) split *= 2;
+  while (split < 8 && blocks * split * 2 <= C::kPerSm * 148 && args.kblocks >= split * 2 * 2) split *= 2;
   args.kb_split = (args.kblocks + split - 1) / split;
   while (split > 1 && (split - 1) * args.kb_split >= args.kblocks) { split /= 2; args.kb_split = (args.kblocks + split - 1) / split; }   // every slice has work
   args.idesc = idesc_i8(128, NT);
@@ -819,7 +827,9 @@ static int run_i8(const I8Call& c, bool early, cudaStream_t stream) {
     a.M = (int)c.M; a.N = (int)c.N; a.kblocks = (int)((c.K + 127) / 128); a.out = c.out; a.early = early ? 1 : 0;
     if (c.M <= 16) return launch_few<16>(c, tmB, a, stream);
     if (c.M <= 32) return launch_few<32>(c, tmB, a, stream);
-    return launch_few<64>(c, tmB, a, stream);
+    if (c.M <= 64) return launch_few<64>(c, tmB, a, stream);
+    if (c.M <= 128) return launch_few<128>(c, tmB, a, stream);
+    return launch_few<256>(c, tmB, a, stream);
   }
   ProdArgs pa = {};
   pa.perm = st.perm; pa.status = st.status; pa.M = (int)c.M; pa.N = (int)c.N; pa.bn = c.tile_n;

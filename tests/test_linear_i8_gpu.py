@@ -117,7 +117,7 @@ def test_quantizer_reads_rows_at_any_address():
 # tokens: both sides of each few-token width and of the dot products' limits (tokens, weights, bytes of tokens); N: one channel, edges of
 # 128-row blocks, odd; K: one stage, edges, several slices
 @pytest.mark.parametrize("M,N,K", [(1, 1, 16), (1, 128, 128), (1, 129, 2048), (2, 4096, 4096), (16, 200, 1040), (17, 1000, 528), (33, 77, 4096), (64, 640, 4112),
-                                   (65, 300, 1024), (128, 257, 8192), (128, 20000, 256),
+                                   (65, 300, 1024), (128, 257, 8192), (128, 20000, 256), (129, 300, 2048), (256, 4096, 2064), (255, 1001, 4096),
                                    (2, 17, 16), (3, 1000, 4112), (4, 130, 16384), (3, 8300, 4112), (2, 100, 32784), (4, 33, 16400), (5, 1000, 512)])
 @pytest.mark.parametrize("out", ["bf16", "fp16", "fp32"])
 def test_few_tokens(M, N, K, out):
