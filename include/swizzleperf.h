@@ -364,7 +364,8 @@ int sp_quantize_i8(const void* x, int32_t x_dtype, int64_t M, int64_t K, int8_t*
  *   B : DEVICE, N x K int8 row-major (weights, one row per output channel).   b_scale : DEVICE, N fp32.
  *   C : DEVICE, M x N row-major, params->out_dtype SP_BF16, SP_FP32 or SP_FP16 (params NULL: SP_BF16); must not overlap an input.
  *   scheme, params : the order of the tile grid, exactly as for sp_tile_map(M, N, tile_m, tile_n, ...), or SP_ORDER_AUTO.  Tiles
- *       128x128, 256x256, or 0,0: the library's choice, which may also be 256 rows by 160 to 224 columns.  Of the flags only SP_FLAG_SERPENTINE applies;
+ *       128x128, 256x256, or 0,0: the library's choice, which may also be 256 rows by 160 to 224 columns
+ *       (not with SP_CUSTOM, whose table is that of one grid).  Of the flags only SP_FLAG_SERPENTINE applies;
  *       b_layout must be 1.  With SP_ORDER_AUTO, tile 0,0 and few tokens (at most 64, or 256 under a B of few rows) the call is bound by reading B and takes
  *       other forms: 128 rows of B per block, the k axis split over a cluster of blocks, partial sums joined through distributed
  *       shared memory; or, for one to four tokens, dot products of whole rows.  Every order and form gives the same bits.

@@ -340,8 +340,8 @@ def _dtype_code(t, allowed):
     return code
 
 
-def _device_tensors(*tensors) -> None:
-    """Contiguous CUDA tensors on the current device: the library launches there."""
+def _device_tensors(*tensors) -> int:
+    """Contiguous CUDA tensors on the current device (returned): the library launches there."""
     import torch
     here = -2
     for t in tensors:
@@ -352,6 +352,15 @@ def _device_tensors(*tensors) -> None:
             here = torch.cuda.current_device()
         if at != here:
             raise ValueError(f"tensor on cuda:{at}, but the current device is cuda:{here}")
+    return here
+
+
+def _stream_on(here: int, stream) -> int:
+    """_stream_handle for a caller that knows the current device."""
+    if stream is None:
+        import torch
+        return torch._C._cuda_getCurrentRawStream(here)
+    return _stream_handle(stream)
 
 
 def _vector(t, n: int, dtype, what: str) -> None:
@@ -385,8 +394,8 @@ def quantize_i8(x, q, scale, stream=None) -> None:
     M, K = x.shape
     _matrix_i8(q, M, (K + 15) // 16 * 16, "q")
     _vector(scale, M, torch.float32, "scale")
-    _device_tensors(x, q, scale)
-    _check(lib().sp_quantize_i8(x.data_ptr(), _dtype_code(x, (BF16, FP32, FP16)), M, K, q.data_ptr(), scale.data_ptr(), _stream_handle(stream)))
+    here = _device_tensors(x, q, scale)
+    _check(lib().sp_quantize_i8(x.data_ptr(), _dtype_code(x, (BF16, FP32, FP16)), M, K, q.data_ptr(), scale.data_ptr(), _stream_on(here, stream)))
 
 
 def gemm_i8(A, a_scale, B, b_scale, C, scheme: int = ORDER_AUTO, params: Optional[SpParams] = None, stream=None) -> None:
@@ -401,10 +410,10 @@ def gemm_i8(A, a_scale, B, b_scale, C, scheme: int = ORDER_AUTO, params: Optiona
     _vector(b_scale, N, torch.float32, "b_scale")
     if tuple(C.shape) != (M, N):
         raise ValueError("shape mismatch")
-    _device_tensors(A, a_scale, B, b_scale, C)
+    here = _device_tensors(A, a_scale, B, b_scale, C)
     p = _i8_params(C, params)
     _check(lib().sp_gemm_i8(A.data_ptr(), a_scale.data_ptr(), B.data_ptr(), b_scale.data_ptr(), C.data_ptr(), M, N, K, scheme, p,
-                            _stream_handle(stream)))
+                            _stream_on(here, stream)))
 
 
 def linear_i8(x, q, q_scale, W, w_scale, y, scheme: int = ORDER_AUTO, params: Optional[SpParams] = None, stream=None) -> None:
@@ -419,10 +428,10 @@ def linear_i8(x, q, q_scale, W, w_scale, y, scheme: int = ORDER_AUTO, params: Op
     _vector(w_scale, N, torch.float32, "w_scale")
     if y.shape != (M, N):
         raise ValueError("shape mismatch")
-    _device_tensors(x, q, q_scale, W, w_scale, y)
+    here = _device_tensors(x, q, q_scale, W, w_scale, y)
     p = _i8_params(y, params)
     _check(lib().sp_linear_i8(x.data_ptr(), _dtype_code(x, (BF16, FP32, FP16)), q.data_ptr(), q_scale.data_ptr(), W.data_ptr(), w_scale.data_ptr(),
-                              y.data_ptr(), M, N, K, scheme, p, _stream_handle(stream)))
+                              y.data_ptr(), M, N, K, scheme, p, _stream_on(here, stream)))
 
 
 def linear_ce_workspace(T: int, V: int, D: int, grad: bool = False) -> int:

@@ -699,6 +699,7 @@ constexpr int64_t kFewAlways = 64, kFewTokens = 256;
 static int check_i8(const void* A, const void* a_scale, const void* B, const void* b_scale, const void* C, int64_t M, int64_t N, int64_t K,
                     int scheme, const sp_params* params, I8Call* call) {
   if (!A || !a_scale || !B || !b_scale || !C) { set_error("A, B, C and the scales must not be NULL"); return SP_ERR_INVALID_ARG; }
+  if (C == A || C == B) { set_error("C must not overlap an input"); return SP_ERR_INVALID_ARG; }
   if (M <= 0 || N <= 0 || K <= 0) { set_error("M, N, K must be positive"); return SP_ERR_INVALID_ARG; }
   if (M >= (1ll << 31) - 512 || N >= (1ll << 31) - 512) { set_error("dimension too large"); return SP_ERR_UNSUPPORTED; }
   if (K > SP_I8_MAX_K) { set_error("K must be at most %d: a longer sum can leave 32 bits", SP_I8_MAX_K); return SP_ERR_UNSUPPORTED; }
@@ -721,6 +722,7 @@ static int check_i8(const void* A, const void* a_scale, const void* B, const voi
     set_error("unsupported tile %dx%d (supported: 128x128, 256x256)", tile_m, tile_n);
     return SP_ERR_UNSUPPORTED;
   }
+  if (pick && scheme == kCustom) { set_error("SP_CUSTOM needs tile_m and tile_n: its table is that grid's"); return SP_ERR_INVALID_ARG; }
   call->A = A; call->B = B; call->a_scale = (const float*)a_scale; call->b_scale = (const float*)b_scale; call->C = const_cast<void*>(C);
   call->M = M; call->N = N; call->K = K; call->out = out;
   call->few = scheme == SP_ORDER_AUTO && pick && (M <= kFewAlways || (M <= kFewTokens && K >= 2048 && (M + 127) / 128 * ((N + 127) / 128) <= 64));
@@ -881,6 +883,7 @@ int sp_linear_i8(const void* x, int32_t x_dtype, int8_t* q, float* q_scale, cons
                  int64_t K, int scheme, const sp_params* params, void* stream) try {
   int rc = check_quantize(x, x_dtype, M, K, q, q_scale);
   if (rc != SP_OK) return rc;
+  if (y == x) { set_error("y must not overlap an input"); return SP_ERR_INVALID_ARG; }
   I8Call call;
   rc = check_i8(q, q_scale, W, w_scale, y, M, N, (K + 15) / 16 * 16, scheme, params, &call);
   if (rc != SP_OK) return rc;

@@ -6,8 +6,9 @@
 // of a tile order, optionally repeated for `splits` slices of the k axis, and an `Epi` type that is handed the accumulator.
 // Eight epilogue warps, two on each quarter of the TMEM lanes: a warp moves its 32 rows x half of the columns to registers, hands
 // the buffer back at once and only then computes (with four warps that worked on the buffer piece by piece the
-// epilogue of the cross entropy took 11.5 thousand cycles a tile and bounded every D up to 1024).  Operands are 8-bit integers (kind::i8, exact 32-bit integer sums) or 16-bit floats
-// (kind::f16, fp32 sums); either may be stored with k or with its other axis contiguous (16-bit types only).
+// epilogue of the cross entropy took 11.5 thousand cycles a tile and bounded every D up to 1024).
+// Operands are 8-bit integers (kind::i8, exact 32-bit integer sums) or 16-bit floats (kind::f16, fp32 sums); 16-bit operands may
+// be stored with k or with their other axis contiguous.
 //
 // One stage holds 128 bytes of k per row (one swizzle row): 128 int8 or 64 16-bit elements.  CTA pairs (CG = 2) compute
 // 256 rows per tile; each CTA supplies half of the B columns.
@@ -30,10 +31,9 @@ enum : int { kProdProducer = 0x11, kProdMma = 0x12, kProdEpilogue = 0x13 };
 
 enum : int { kElemI8 = 0, kElem16 = 1 };
 
-template <int CG, int BN, int ELEM, bool A_MN, bool B_MN, uint32_t EPI_BYTES>
+template <int CG, int BN, int ELEM, uint32_t EPI_BYTES>
 struct ProdCfg {
   static constexpr int kBK = ELEM == kElemI8 ? 128 : 64;        // elements of k per stage
-  static constexpr int kUmmaK = ELEM == kElemI8 ? 32 : 16;      // elements of k per MMA: 32 bytes
   static constexpr int kBCols = BN / CG;                        // columns of B one CTA supplies
   static constexpr uint32_t kABytes = 128 * 128;
   static constexpr uint32_t kBBytes = kBCols * 128;
@@ -161,17 +161,17 @@ __device__ __forceinline__ void store_slice_plain(uint32_t carry, uint32_t slice
 #pragma unroll 1
     for (int q = lo; q < hi; q += ELT) {
       const uint32_t b = (uint32_t)q & 127u, addr = q < 0 ? carry + (uint32_t)row * 16u + (b & 12u)
-                                                            : slice + (uint32_t)row * 128u + ((((b >> 4) ^ ((uint32_t)row & 7u)) << 4) | (b & 12u));
+                                                          : slice + (uint32_t)row * 128u + ((((b >> 4) ^ ((uint32_t)row & 7u)) << 4) | (b & 12u));
       const uint32_t v = ld_shared_32(addr);
       if constexpr (ELT == 4) *reinterpret_cast<uint32_t*>(a + q) = v;
       else *reinterpret_cast<uint16_t*>(a + q) = (uint16_t)(b & 2u ? v >> 16 : v);
     }
   };
   // Lane 8 i + w has window w of rows i, i + 4, ...: bytes 16 w - m on, m the row's address modulo 16, are the tail of unit w - 1 and the head of
-  // unit w, put together by a shift of m bytes.  One warp runs per scheduler here, so the count of instructions is what costs.
+  // unit w, put together by a shift of m bytes.  Two warps run per scheduler here, so the count of instructions is what costs.
   const int w = lane & 7, i0 = lane >> 3;
   char* a = out + (int64_t)(row0 + i0) * ld_bytes + (int64_t)col * ELT;
-    const uint32_t ua = (uint32_t)i0 * 128u + (((uint32_t)w ^ (uint32_t)i0) << 4), ub = (uint32_t)i0 * 128u + (((uint32_t)(w - 1) ^ (uint32_t)i0) << 4);
+  const uint32_t ua = (uint32_t)i0 * 128u + (((uint32_t)w ^ (uint32_t)i0) << 4), ub = (uint32_t)i0 * 128u + (((uint32_t)(w - 1) ^ (uint32_t)i0) << 4);
   // straight-line code: the eight rounds' reads are in flight together
 #pragma unroll
   for (int r = 0; r < 32; r += 4, a += 4 * ld_bytes) {
@@ -214,7 +214,7 @@ template <int CG, int BN, int ELEM, bool A_MN, bool B_MN, class Epi>
 __global__ void __launch_bounds__(384, 1)
 product_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const __grid_constant__ CUtensorMap tmC,
                const ProdArgs args, const typename Epi::Args eargs) {
-  using C = ProdCfg<CG, BN, ELEM, A_MN, B_MN, Epi::kBytes>;
+  using C = ProdCfg<CG, BN, ELEM, Epi::kBytes>;
   constexpr int S = C::kStages;
   static_assert(ELEM == kElem16 || (!A_MN && !B_MN), "8-bit operands are k-major");
 
@@ -456,7 +456,7 @@ inline int launch_pdl(const char* what, void (*kern)(KArgs...), dim3 grid, int t
 template <int CG, int BN, int ELEM, bool A_MN, bool B_MN, class Epi>
 int launch_product(const char* what, const CUtensorMap& tmA, const CUtensorMap& tmB, const CUtensorMap& tmC, ProdArgs args, bool bf16,
                    const typename Epi::Args& eargs, cudaStream_t stream) {
-  using C = ProdCfg<CG, BN, ELEM, A_MN, B_MN, Epi::kBytes>;
+  using C = ProdCfg<CG, BN, ELEM, Epi::kBytes>;
   auto kern = product_kernel<CG, BN, ELEM, A_MN, B_MN, Epi>;
   static uint64_t configured = 0;   // per instantiation, one bit per device
   if (first_use_on_this_device(configured)) {

@@ -89,6 +89,8 @@ def test_gemm_i8_refusals():
     assert _gemm(flags=sp.FLAG_STREAM_K) == sp.ERR_INVALID_ARG
     assert _gemm(scheme=-2) == sp.ERR_INVALID_ARG and _gemm(scheme=sp.GROUP_M, group=0) == sp.ERR_INVALID_ARG
     assert _gemm(M=256, N=512, scheme=sp.CUSTOM, tile_m=256, tile_n=256, custom_perm=[1, 1]) == sp.ERR_NOT_BIJECTIVE
+    assert _gemm(M=256, N=512, scheme=sp.CUSTOM, custom_perm=[0, 1]) == sp.ERR_INVALID_ARG          # whose grid?
+    assert _gemm(c=A) == sp.ERR_INVALID_ARG
     assert _gemm(M=1280, N=512, scheme=sp.XCD, tile_m=256, tile_n=256, num_xcds=4) == sp.ERR_NOT_BIJECTIVE
     p = sp.make_params(b_layout=1)
     p.struct_size = 4
@@ -104,6 +106,8 @@ def test_linear_i8_refuses_what_its_two_calls_refuse():
     assert f(A, sp.BF16, A, A, A, A, B, 4, 0, 4, -1, ctypes.byref(p), None) == sp.ERR_INVALID_ARG
     assert f(A, sp.BF16, A, A, A, A, B, 4, 4, sp.I8_MAX_K + 1, -1, ctypes.byref(p), None) == sp.ERR_UNSUPPORTED
     assert f(A, sp.BF16, A + 4, A, A, A, B, 4, 4, 4, -1, ctypes.byref(p), None) == sp.ERR_ALIGNMENT
+    assert f(A, sp.BF16, 2 * A, A, A, A, A, 4, 4, 4, -1, ctypes.byref(p), None) == sp.ERR_INVALID_ARG      # y = x
+    assert f(A, sp.BF16, B, A, A, A, B, 4, 4, 4, -1, ctypes.byref(p), None) == sp.ERR_INVALID_ARG          # y = q
 
 
 def _ce(h=A, W=A, t=A, lse=A, loss=B, T=8, V=100, D=64, dtype=sp.BF16, red=1, ws=B, n=1 << 40):
