@@ -343,16 +343,17 @@ def _dtype_code(t, allowed):
 def _device_tensors(*tensors) -> int:
     """Contiguous CUDA tensors on the current device (returned): the library launches there."""
     import torch
-    here = -2
+    at = tensors[0].get_device()      # -1: not on a GPU
+    if at < 0:
+        raise ValueError("tensors must be contiguous CUDA tensors")
     for t in tensors:
-        at = t.get_device()      # -1: not on a GPU
-        if at < 0 or not t.is_contiguous():
+        if not t.is_contiguous():
             raise ValueError("tensors must be contiguous CUDA tensors")
-        if here == -2:
-            here = torch.cuda.current_device()
-        if at != here:
-            raise ValueError(f"tensor on cuda:{at}, but the current device is cuda:{here}")
-    return here
+        if t.get_device() != at:
+            raise ValueError("tensors must all be on one CUDA device")
+    if at != torch.cuda.current_device():
+        raise ValueError(f"tensors on cuda:{at}, but the current device is cuda:{torch.cuda.current_device()}")
+    return at
 
 
 def _stream_on(here: int, stream) -> int:
@@ -363,15 +364,10 @@ def _stream_on(here: int, stream) -> int:
     return _stream_handle(stream)
 
 
-def _vector(t, n: int, dtype, what: str) -> None:
-    if t.dtype != dtype or t.shape != (n,):
-        raise ValueError(f"{what} must be a {dtype} vector of {n}")
-
-
-def _matrix_i8(t, rows: int, cols: int, what: str) -> None:
-    import torch
-    if t.dtype != torch.int8 or t.shape != (rows, cols):
-        raise ValueError(f"{what} must be an int8 matrix of {rows} rows of {cols}")
+def _expect(what: str, got, want) -> None:
+    """One comparison for a call's shapes (or types): a call of a few microseconds has no time for one by one."""
+    if got != want:
+        raise ValueError(f"{what}: got {[tuple(g) if isinstance(g, tuple) else g for g in got]}, expected {list(want)}")
 
 
 _I8_DEFAULTS: dict = {}      # the parameters of a call that leaves tile and order to the library, per output type
@@ -392,8 +388,8 @@ def quantize_i8(x, q, scale, stream=None) -> None:
     """q [M, ceil(K / 16) * 16] int8 and scale [M] fp32 such that x [M, K] ~ scale * q, row by row (asynchronous)."""
     import torch
     M, K = x.shape
-    _matrix_i8(q, M, (K + 15) // 16 * 16, "q")
-    _vector(scale, M, torch.float32, "scale")
+    _expect("shapes of q, scale", (q.shape, scale.shape), ((M, (K + 15) // 16 * 16), (M,)))
+    _expect("types of q, scale", (q.dtype, scale.dtype), (torch.int8, torch.float32))
     here = _device_tensors(x, q, scale)
     _check(lib().sp_quantize_i8(x.data_ptr(), _dtype_code(x, (BF16, FP32, FP16)), M, K, q.data_ptr(), scale.data_ptr(), _stream_on(here, stream)))
 
@@ -404,15 +400,10 @@ def gemm_i8(A, a_scale, B, b_scale, C, scheme: int = ORDER_AUTO, params: Optiona
     import torch
     M, K = A.shape
     N = B.shape[0]
-    _matrix_i8(A, M, K, "A")
-    _matrix_i8(B, N, K, "B")
-    _vector(a_scale, M, torch.float32, "a_scale")
-    _vector(b_scale, N, torch.float32, "b_scale")
-    if tuple(C.shape) != (M, N):
-        raise ValueError("shape mismatch")
+    _expect("shapes of B, a_scale, b_scale, C", (B.shape, a_scale.shape, b_scale.shape, C.shape), ((N, K), (M,), (N,), (M, N)))
+    _expect("types of A, B, a_scale, b_scale", (A.dtype, B.dtype, a_scale.dtype, b_scale.dtype), (torch.int8, torch.int8, torch.float32, torch.float32))
     here = _device_tensors(A, a_scale, B, b_scale, C)
-    p = _i8_params(C, params)
-    _check(lib().sp_gemm_i8(A.data_ptr(), a_scale.data_ptr(), B.data_ptr(), b_scale.data_ptr(), C.data_ptr(), M, N, K, scheme, p,
+    _check(lib().sp_gemm_i8(A.data_ptr(), a_scale.data_ptr(), B.data_ptr(), b_scale.data_ptr(), C.data_ptr(), M, N, K, scheme, _i8_params(C, params),
                             _stream_on(here, stream)))
 
 
@@ -422,16 +413,11 @@ def linear_i8(x, q, q_scale, W, w_scale, y, scheme: int = ORDER_AUTO, params: Op
     import torch
     M, K = x.shape
     N, kp = W.shape[0], (K + 15) // 16 * 16
-    _matrix_i8(q, M, kp, "q")
-    _matrix_i8(W, N, kp, "W")
-    _vector(q_scale, M, torch.float32, "q_scale")
-    _vector(w_scale, N, torch.float32, "w_scale")
-    if y.shape != (M, N):
-        raise ValueError("shape mismatch")
+    _expect("shapes of q, q_scale, W, w_scale, y", (q.shape, q_scale.shape, W.shape, w_scale.shape, y.shape), ((M, kp), (M,), (N, kp), (N,), (M, N)))
+    _expect("types of q, q_scale, W, w_scale", (q.dtype, q_scale.dtype, W.dtype, w_scale.dtype), (torch.int8, torch.float32, torch.int8, torch.float32))
     here = _device_tensors(x, q, q_scale, W, w_scale, y)
-    p = _i8_params(y, params)
     _check(lib().sp_linear_i8(x.data_ptr(), _dtype_code(x, (BF16, FP32, FP16)), q.data_ptr(), q_scale.data_ptr(), W.data_ptr(), w_scale.data_ptr(),
-                              y.data_ptr(), M, N, K, scheme, p, _stream_on(here, stream)))
+                              y.data_ptr(), M, N, K, scheme, _i8_params(y, params), _stream_on(here, stream)))
 
 
 def linear_ce_workspace(T: int, V: int, D: int, grad: bool = False) -> int:
@@ -442,13 +428,16 @@ def linear_ce_workspace(T: int, V: int, D: int, grad: bool = False) -> int:
     return n
 
 
-def _ce_workspace(workspace, need: int, device, stream):
+def _ce_workspace(workspace, like, sizes, grad: int, stream):
     """The caller's workspace, or one of torch's allocator's that outlives the work on the stream it is used on."""
     import torch
     if workspace is not None:
         _device_tensors(workspace)
         return workspace, workspace.numel() * workspace.element_size()
-    buf = torch.empty(need, dtype=torch.uint8, device=device)
+    need = lib().sp_linear_ce_workspace(*sizes, grad)
+    if need < 0:
+        raise SpError(ERR_INVALID_ARG, "sizes must be positive and below 2^31")
+    buf = like.new_empty(need, dtype=torch.uint8)
     if stream is not None:
         handle = _stream_handle(stream)
         if handle != _stream_handle(None):
@@ -456,52 +445,48 @@ def _ce_workspace(workspace, need: int, device, stream):
     return buf, need
 
 
-def _ce_shapes(h, W, target, lse, reduction: str):
-    import torch
-    if h.dim() != 2 or W.dim() != 2 or h.shape[1] != W.shape[1]:
-        raise ValueError("h must be [T, D] and W [V, D]")
-    if h.dtype != W.dtype:
-        raise ValueError("h and W must have the same element type")
-    if reduction not in _REDUCE:
-        raise ValueError(f"unknown reduction {reduction!r}")
-    T, D = h.shape
-    _vector(target, T, torch.int64, "target")
-    _vector(lse, T, torch.float32, "lse")
-    return T, W.shape[0], D, _dtype_code(h, (BF16, FP16))
-
-
 def linear_ce(h, W, target, lse, loss, reduction: str = "mean", ignore_index: int = -100, workspace=None, stream=None) -> None:
     """Softmax cross entropy of the scores h [T, D] . W [V, D]^T against target [T] (int64), without storing the scores (asynchronous).
     Fills lse [T] (kept for linear_ce_grad) and loss: [T] for reduction "none", [1] for "mean" (over the tokens that are not
     ignored) and "sum".  ``workspace``: a CUDA tensor of linear_ce_workspace(T, V, D) bytes, allocated here when not given."""
     import torch
-    T, V, D, code = _ce_shapes(h, W, target, lse, reduction)
-    _vector(loss, T if reduction == "none" else 1, torch.float32, "loss")
-    _device_tensors(h, W, target, lse, loss)
-    ws, n = _ce_workspace(workspace, linear_ce_workspace(T, V, D), h.device, stream)
+    if reduction not in _REDUCE:
+        raise ValueError(f"unknown reduction {reduction!r}")
+    T, D = h.shape
+    V = W.shape[0]
+    _expect("shapes of W, target, lse, loss", (W.shape, target.shape, lse.shape, loss.shape), ((V, D), (T,), (T,), (T if reduction == "none" else 1,)))
+    _expect("types of W, target, lse, loss", (W.dtype, target.dtype, lse.dtype, loss.dtype), (h.dtype, torch.int64, torch.float32, torch.float32))
+    code = _dtype_code(h, (BF16, FP16))
+    here = _device_tensors(h, W, target, lse, loss)
+    ws, n = _ce_workspace(workspace, h, (T, V, D), 0, stream)
     _check(lib().sp_linear_ce(h.data_ptr(), W.data_ptr(), target.data_ptr(), lse.data_ptr(), loss.data_ptr(), T, V, D, code, ignore_index,
-                              _REDUCE[reduction], ws.data_ptr(), n, _stream_handle(stream)))
+                              _REDUCE[reduction], ws.data_ptr(), n, _stream_on(here, stream)))
 
 
 def linear_ce_grad(h, W, target, lse, grad_loss, dh, dW, reduction: str = "mean", ignore_index: int = -100, workspace=None, stream=None) -> None:
     """Gradients of linear_ce: dh [T, D] and dW [V, D] (either may be None) for the gradient ``grad_loss`` of the loss ([T] or [1]
     fp32; None: ones).  ``lse`` as linear_ce left it; ``workspace``: linear_ce_workspace(T, V, D, grad=True) bytes (asynchronous)."""
     import torch
-    T, V, D, code = _ce_shapes(h, W, target, lse, reduction)
+    if reduction not in _REDUCE:
+        raise ValueError(f"unknown reduction {reduction!r}")
+    T, D = h.shape
+    V = W.shape[0]
+    _expect("shapes of W, target, lse", (W.shape, target.shape, lse.shape), ((V, D), (T,), (T,)))
+    _expect("types of W, target, lse", (W.dtype, target.dtype, lse.dtype), (h.dtype, torch.int64, torch.float32))
     tensors = [h, W, target, lse]
     if grad_loss is not None:
-        _vector(grad_loss, T if reduction == "none" else 1, torch.float32, "grad_loss")
+        _expect("shape and type of grad_loss", (grad_loss.shape, grad_loss.dtype), ((T if reduction == "none" else 1,), torch.float32))
         tensors.append(grad_loss)
     for g, like in ((dh, h), (dW, W)):
         if g is not None:
-            if g.shape != like.shape or g.dtype != like.dtype:
-                raise ValueError("a gradient must have its input's shape and element type")
+            _expect("shape and type of a gradient", (g.shape, g.dtype), (like.shape, like.dtype))
             tensors.append(g)
-    _device_tensors(*tensors)
-    ws, n = _ce_workspace(workspace, linear_ce_workspace(T, V, D, True), h.device, stream)
-    ptr = lambda t: None if t is None else t.data_ptr()  # noqa: E731
-    _check(lib().sp_linear_ce_grad(h.data_ptr(), W.data_ptr(), target.data_ptr(), lse.data_ptr(), ptr(grad_loss), ptr(dh), ptr(dW), T, V, D, code,
-                                   ignore_index, _REDUCE[reduction], ws.data_ptr(), n, _stream_handle(stream)))
+    code = _dtype_code(h, (BF16, FP16))
+    here = _device_tensors(*tensors)
+    ws, n = _ce_workspace(workspace, h, (T, V, D), 1, stream)
+    _check(lib().sp_linear_ce_grad(h.data_ptr(), W.data_ptr(), target.data_ptr(), lse.data_ptr(), None if grad_loss is None else grad_loss.data_ptr(),
+                                   None if dh is None else dh.data_ptr(), None if dW is None else dW.data_ptr(), T, V, D, code, ignore_index,
+                                   _REDUCE[reduction], ws.data_ptr(), n, _stream_on(here, stream)))
 
 
 def gemm_units(tile_m: int, tile_n: int, T: int) -> int:

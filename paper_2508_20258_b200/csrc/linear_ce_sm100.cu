@@ -244,45 +244,47 @@ __global__ void __launch_bounds__(1024) ce_join_kernel(const CeJoin a, int shift
   __shared__ float2 part[1024];
   const int rows = 1 << shift, groups = (int)blockDim.x >> shift;
   const int r = threadIdx.x & (rows - 1), g = threadIdx.x >> shift, lane = threadIdx.x & 31;
-  const int64_t first = (int64_t)blockIdx.x << shift;
-  const bool ends = (int)threadIdx.x < rows && first + r < a.T;      // this thread finishes a row
-  const int64_t y = ends ? __ldg(a.target + first + r) : -1;
-  const float picked = ends && y >= 0 && y < a.V ? a.picked[first + r] : CUDART_NAN_F;
-  float2 pair = make_float2(-CUDART_INF_F, 0.f);
-  if (first + r < a.T) {
-    const float2* at = a.stats + first + r;
-    for (int i = g; i < a.tiles; i += 8 * groups) {
-      float2 p[8];
+  for (int64_t first = (int64_t)blockIdx.x << shift; first < a.T; first += (int64_t)gridDim.x << shift) {
+    const bool ends = (int)threadIdx.x < rows && first + r < a.T;      // this thread finishes a row
+    const int64_t y = ends ? __ldg(a.target + first + r) : -1;
+    const float picked = ends && y >= 0 && y < a.V ? a.picked[first + r] : CUDART_NAN_F;
+    float2 pair = make_float2(-CUDART_INF_F, 0.f);
+    if (first + r < a.T) {
+      const float2* at = a.stats + first + r;
+      for (int i = g; i < a.tiles; i += 8 * groups) {
+        float2 p[8];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) p[j] = i + j * groups < a.tiles ? __ldg(at + (int64_t)(i + j * groups) * a.T) : make_float2(-CUDART_INF_F, 0.f);
-      float m = pair.x;
+        for (int j = 0; j < 8; ++j) p[j] = i + j * groups < a.tiles ? __ldg(at + (int64_t)(i + j * groups) * a.T) : make_float2(-CUDART_INF_F, 0.f);
+        float m = pair.x;
 #pragma unroll
-      for (int j = 0; j < 8; ++j) m = fmaxf(m, p[j].x);
-      const float ref = m == -CUDART_INF_F ? 0.f : m;
-      float s = pair.y * ex2(pair.x - ref);
+        for (int j = 0; j < 8; ++j) m = fmaxf(m, p[j].x);
+        const float ref = m == -CUDART_INF_F ? 0.f : m;
+        float s = pair.y * ex2(pair.x - ref);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) s = fmaf(p[j].y, ex2(p[j].x - ref), s);
-      pair = make_float2(m, s);
+        for (int j = 0; j < 8; ++j) s = fmaf(p[j].y, ex2(p[j].x - ref), s);
+        pair = make_float2(m, s);
+      }
     }
-  }
-  part[threadIdx.x] = pair;
-  __syncthreads();
-  if (groups > 8) {      // a warp per row first
-    for (int row = threadIdx.x >> 5; row < rows; row += blockDim.x >> 5) {
-      pair = make_float2(-CUDART_INF_F, 0.f);
-      for (int i = lane; i < groups; i += 32) join_pair(pair, part[i * rows + row]);
-#pragma unroll
-      for (int o = 16; o; o >>= 1) join_pair(pair, make_float2(__shfl_xor_sync(0xffffffffu, pair.x, o), __shfl_xor_sync(0xffffffffu, pair.y, o)));
-      if (lane == 0) part[row] = pair;      // slot `row` is group 0's of this row: read above by this warp only
-    }
+    part[threadIdx.x] = pair;
     __syncthreads();
-  }
-  if (ends) {
-    pair = part[r];
-    for (int i = 1; i < groups && groups <= 8; ++i) join_pair(pair, part[i * rows + r]);
-    const float lse = (pair.x + log2f(pair.y)) * kLn2;
-    a.lse[first + r] = lse;
-    a.each[first + r] = y == a.ignore ? 0.f : lse - picked;
+    if (groups > 8) {      // a warp per row first
+      for (int row = threadIdx.x >> 5; row < rows; row += blockDim.x >> 5) {
+        pair = make_float2(-CUDART_INF_F, 0.f);
+        for (int i = lane; i < groups; i += 32) join_pair(pair, part[i * rows + row]);
+#pragma unroll
+        for (int o = 16; o; o >>= 1) join_pair(pair, make_float2(__shfl_xor_sync(0xffffffffu, pair.x, o), __shfl_xor_sync(0xffffffffu, pair.y, o)));
+        if (lane == 0) part[row] = pair;      // slot `row` is group 0's of this row: read above by this warp only
+      }
+      __syncthreads();
+    }
+    if (ends) {
+      pair = part[r];
+      for (int i = 1; i < groups && groups <= 8; ++i) join_pair(pair, part[i * rows + r]);
+      const float lse = (pair.x + log2f(pair.y)) * kLn2;
+      a.lse[first + r] = lse;
+      a.each[first + r] = y == a.ignore ? 0.f : lse - picked;
+    }
+    __syncthreads();      // before the next rows' pairs
   }
   if (a.loss != nullptr && gridDim.x == 1) {
     __syncthreads();
@@ -707,9 +709,11 @@ int sp_linear_ce(const void* h, const void* W, const int64_t* target, float* lse
   j.loss = reduction == SP_REDUCE_NONE ? nullptr : loss;
   j.T = (int)T; j.V = (int)V; j.tiles = (int)p.tiles; j.ignore = ignore_index; j.mean = reduction == SP_REDUCE_MEAN;
   // 256 threads while a row's pairs are one batch of reads, else 1024
+  // One block does up to 64 tokens of few pairs, and the sum of their losses with them: a launch less.
   const int shift = T <= 4 ? 2 : 5, threads = p.tiles <= 8 * (256 >> shift) ? 256 : 1024;
-  rc = launch_pdl("join of the row statistics", ce_join_kernel, dim3((unsigned)div_up(T, 1 << shift)), threads, 0, 1, (cudaStream_t)stream, j, shift);
-  if (rc == SP_OK && j.loss && T > 32) rc = launch_pdl("sum of the losses", ce_reduce_kernel, dim3(1), 1024, 0, 1, (cudaStream_t)stream, j);
+  const unsigned blocks = j.loss && T <= 64 && p.tiles <= 256 ? 1u : (unsigned)div_up(T, 1 << shift);
+  rc = launch_pdl("join of the row statistics", ce_join_kernel, dim3(blocks), threads, 0, 1, (cudaStream_t)stream, j, shift);
+  if (rc == SP_OK && j.loss && blocks > 1) rc = launch_pdl("sum of the losses", ce_reduce_kernel, dim3(1), 1024, 0, 1, (cudaStream_t)stream, j);
   return rc;
 } catch (const std::exception& e) {
   set_error("sp_linear_ce: %s", e.what());

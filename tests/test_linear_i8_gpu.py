@@ -52,8 +52,8 @@ def rounded(y32, out):
     return torch.from_numpy(np.ascontiguousarray(y32)).to(BITS[out]).float().numpy()
 
 
-# one element, one vector, rows of one warp and of one block, both re-reading limits and just beyond, odd row pitches
-@pytest.mark.parametrize("M,K", [(1, 1), (1, 8), (3, 15), (9, 17), (5, 1000), (8, 1024), (7, 1025), (3, 2035), (2, 8192), (2, 8193), (1, 20011), (70, 64), (1, 40000)])
+# one element, one vector, rows of one, two, four and eight warps with blocks partly empty, the re-reading limit and beyond, odd row pitches
+@pytest.mark.parametrize("M,K", [(1, 1), (1, 8), (3, 15), (9, 17), (5, 1000), (8, 1024), (7, 1025), (3, 2035), (5, 2048), (5, 2049), (3, 4096), (3, 4097), (2, 8192), (2, 8193), (1, 20011), (70, 64), (1, 40000)])
 @pytest.mark.parametrize("dtype", ["bf16", "fp16", "fp32"])
 def test_quantizer(M, K, dtype):
     rng = np.random.default_rng(M * 31 + K)
