@@ -983,7 +983,7 @@ static int cached_map(CUtensorMap* out, const void* base, int64_t rows, int64_t 
   return SP_OK;
 }
 
-static bool log_enabled() {
+bool log_enabled() {
   static const bool on = getenv("SP_LOG") != nullptr;   // read once per process
   return on;
 }

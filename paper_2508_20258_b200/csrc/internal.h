@@ -21,6 +21,7 @@ constexpr size_t kSkFlagBytes = 4096;
 constexpr size_t kSkWorkspaceBytes = (size_t)148 * 128 * 256 * 4;
 
 void set_error(const char* fmt, ...);
+bool log_enabled();      // SP_LOG was set when the library was first used
 
 // Per-function set-up that CUDA keeps per device (cudaFuncSetAttribute): true the first time it is asked for the
 // current device with this mask.  A lost race only repeats a harmless call.

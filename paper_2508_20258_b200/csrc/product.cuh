@@ -17,6 +17,7 @@
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
+#include <stdio.h>
 
 #include "internal.h"
 #include "ptx.cuh"
@@ -447,6 +448,7 @@ inline int launch_pdl(const char* what, void (*kern)(KArgs...), dim3 grid, int t
   attr[1].val.clusterDim.x = (unsigned)cluster; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = cluster > 1 ? 2 : 1;
+  if (log_enabled()) fprintf(stderr, "[swizzleperf] %s: grid=%u threads=%d cluster=%d smem=%zu\n", what, grid.x, threads, cluster, smem);
   const cudaError_t e = cudaLaunchKernelEx(&cfg, kern, static_cast<KArgs>(args)...);
   if (e != cudaSuccess) { set_error("launching %s failed: %s", what, cudaGetErrorString(e)); return SP_ERR_CUDA; }
   return SP_OK;

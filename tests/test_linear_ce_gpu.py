@@ -93,7 +93,7 @@ def inside(got, ref, tol):
 
 # one token (by rows, in one and several reads of a row, and too long for it); a vocabulary of two, of a tile and one more, odd; one stage of D, one
 # sum of 512 and several, ragged ones; both tile heights and their edges
-SHAPES = [(1, 2, 8), (1, 256, 64), (1, 999, 2056), (1, 300, 16384), (1, 257, 16392), (130, 300, 1544), (2, 257, 72), (5, 1000, 136), (31, 513, 1032), (33, 511, 64), (128, 300, 64), (129, 4097, 128), (256, 256, 64), (300, 2049, 520)]
+SHAPES = [(1, 2, 8), (3, 1, 8), (1, 256, 64), (1, 999, 2056), (1, 300, 16384), (1, 257, 16392), (130, 300, 1544), (2, 257, 72), (5, 1000, 136), (31, 513, 1032), (33, 511, 64), (128, 300, 64), (129, 4097, 128), (256, 256, 64), (300, 2049, 520)]
 
 
 @pytest.mark.parametrize("T,V,D", SHAPES)
@@ -359,6 +359,19 @@ def test_a_stream_that_is_not_the_current_one():
             assert sp.get_status(stream) == 0
             assert torch.equal(lse, want[0]) and torch.equal(loss, want[1])
             del junk
+
+
+def test_the_default_stream_by_its_handle_beside_another_current_one():
+    h, W, t = [v.cuda() for v in inputs(100, 900, 64, "bf16")]
+    want = forward(h, W, t, "sum")
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        lse, loss = torch.empty(100, device="cuda"), torch.empty(1, device="cuda")
+        torch.cuda.synchronize()
+        sp.linear_ce(h, W, t, lse, loss, reduction="sum", stream=0)
+        assert sp.get_status(0) == 0
+    assert torch.equal(lse, want[0]) and torch.equal(loss, want[1])
 
 
 def test_a_head_trained_on_an_8_bit_trunk():
