@@ -40,7 +40,8 @@ __device__ __forceinline__ void tma_add_3d(const CUtensorMap* map, uint32_t src,
 
 // ------------------------------------------------------------------ forward: statistics of a tile's rows
 // Per row and 128 columns the maximum m (in powers of two: m = max z * log2 e, rounded once) and s = sum 2^(z log2 e - m).  Any m serves
-// as long as the joined result uses the same one, so its rounding costs nothing.
+// as long as the joined result uses the same one, so its rounding costs nothing.  The row's target is left out of both: its score
+// goes to `picked`, and the join adds its term, so that a loss of 1e-6 is a sum of the others' terms and not a difference of 32-bit numbers.
 //
 // The tensor cores cut what they add off behind the accumulator's last bit, 16 products at a time, always towards zero: over D = 4096 lse
 // came out 1.8e-6 too small, over 8192 4e-6.  So an accumulator takes 512 products only and the epilogue adds such sums, rounded to
@@ -76,7 +77,7 @@ struct EpiStats {
     if (__any_sync(0xffffffffu, rel >= 0)) {
 #pragma unroll
       for (int j = 0; j < COLS; ++j)
-        if (rel == j) hit = __uint_as_float(v[j]);
+        if (rel == j) { hit = __uint_as_float(v[j]); v[j] = 0xff800000u; }
     }
     float t[8];
 #pragma unroll
@@ -187,8 +188,9 @@ __global__ void __launch_bounds__(kRowThreads, 2) row_stats_kernel(const RowArgs
     for (int r = 0; r < 2; ++r) {
 #pragma unroll
       for (int o = 16; o; o >>= 1) acc[r] += __shfl_xor_sync(0xffffffffu, acc[r], o);
-      if (n + r < a.V) {
-        if (lane == 0 && want == n + r) *a.picked = acc[r];
+      if (want == n + r) {      // the target's term is the join's
+        if (lane == 0 && n + r < a.V) *a.picked = acc[r];
+      } else if (n + r < a.V) {
         const float m = fmaxf(pair.x, acc[r] * kLog2e), ref = m == -CUDART_INF_F ? 0.f : m;
         pair = make_float2(m, fmaf(pair.y, ex2(pair.x - ref), ex2(fmaf(acc[r], kLog2e, -ref))));
       }
@@ -203,8 +205,8 @@ __global__ void __launch_bounds__(kRowThreads, 2) row_stats_kernel(const RowArgs
 }
 
 struct CeJoin {
-  const float2* stats;
-  const float* picked;
+  const float2* stats;  // without the target
+  const float* picked;  // the target's score
   const int64_t* target;
   float* lse;
   float* each;        // loss per token
@@ -247,7 +249,8 @@ __global__ void __launch_bounds__(1024) ce_join_kernel(const CeJoin a, int shift
   for (int64_t first = (int64_t)blockIdx.x << shift; first < a.T; first += (int64_t)gridDim.x << shift) {
     const bool ends = (int)threadIdx.x < rows && first + r < a.T;      // this thread finishes a row
     const int64_t y = ends ? __ldg(a.target + first + r) : -1;
-    const float picked = ends && y >= 0 && y < a.V ? a.picked[first + r] : CUDART_NAN_F;
+    const bool hit = ends && y >= 0 && y < a.V;
+    const float picked = hit ? a.picked[first + r] : -CUDART_INF_F;      // no word of the vocabulary: no term of its own
     float2 pair = make_float2(-CUDART_INF_F, 0.f);
     if (first + r < a.T) {
       const float2* at = a.stats + first + r;
@@ -280,9 +283,14 @@ __global__ void __launch_bounds__(1024) ce_join_kernel(const CeJoin a, int shift
     if (ends) {
       pair = part[r];
       for (int i = 1; i < groups && groups <= 8; ++i) join_pair(pair, part[i * rows + r]);
-      const float lse = (pair.x + log2f(pair.y)) * kLn2;
-      a.lse[first + r] = lse;
-      a.each[first + r] = y == a.ignore ? 0.f : lse - picked;
+      // With `own` the target's exponent against the larger maximum, its product not rounded, and `rest` the sum of the others: lse = ref + log2(rest +
+      // 2^own), and the loss is log(1 + rest / 2^own), whose digits do not depend on the size of the scores.  (lse - picked, in scores of 30:
+      // losses below 1e-5 were noise of +-4e-6.)
+      const float top = fmaxf(pair.x, picked * kLog2e), ref = top == -CUDART_INF_F ? 0.f : top;
+      const float own = fmaf(picked, kLog2e, -ref), mine = ex2(own), rest = pair.y * ex2(pair.x - ref);
+      const float bits = log2f(rest + mine);
+      a.lse[first + r] = (ref + bits) * kLn2;
+      a.each[first + r] = y == a.ignore ? 0.f : !hit ? CUDART_NAN_F : rest < mine ? log1pf(rest / mine) : (bits - own) * kLn2;
     }
     __syncthreads();      // before the next rows' pairs
   }

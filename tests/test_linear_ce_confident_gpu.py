@@ -1,0 +1,84 @@
+"""The vocabulary cross entropy where a token is nearly certain of its word: 1 - p from 1e-1 down to 1e-7.  The loss is then about
+1 - p and the gradient at the token's own word is p - 1, so both are held to errors relative to themselves, not to the scores.
+
+Tolerances, from the arithmetic (u = 2^-23; e = eps / 2 of the 16-bit type).
+  score     16 products at a time are added to an accumulator that may cut instead of rounding, 512 products at a time in fp32:
+            dz = (D / 16 + D / 512 + 2) u sum_d |h_d W_vd|, the largest over v.
+  2^x       of z log2 e - m: the argument is rounded up to three times on its way (product, part to row, row to lse), |argument| <=
+            2 log2(e) max|z|, and the hardware's 2^x is good to 2^-22:  r = (6 log2(e) max|z| + 4) u, relative.
+  loss      log(1 + sum_{v != y} e^(z_v - z_y)): relative error at most that of the sum, 2 dz + 2 r, and 2^-17 for the additions (as in
+            test_linear_ce_gpu) and the logarithm.
+  g         every p is off by q = 2 dz + 2 r + 2^-17 relative; lse is a 32-bit number, off by |lse| u / 2, which r covers.  A token's own
+            entry is minus the sum of the others' p (relative q), or p - 1 where 1 - p is at least |lse| 2^-9, in which case it
+            is off by |lse| u / (1 - p) <= 2^-13 relative.  Then half a step of the 16-bit type: e |g|.
+  dh, dW    those errors summed, (V + 2) u and (T + 2) u of the absolute sums for the additions, and the result's own rounding."""
+
+import numpy as np
+import pytest
+
+import paper_2508_20258_b200 as sp
+
+pytestmark = pytest.mark.gpu
+torch = pytest.importorskip("torch")
+
+BITS = {"bf16": torch.bfloat16, "fp16": torch.float16}
+U = 2.0 ** -23
+LOG2E = 1.4426950408889634
+
+
+def confident(T, V, D, dtype, seed=0, shift=24.0, sure=1.0):
+    """Hidden states along their target's row of W, so long that 1 - p runs from 1e-1 to 1e-7 (the first ``sure`` of the tokens; the
+    others are random), and `shift` added to every score."""
+    g = torch.Generator(device="cuda").manual_seed(seed * 1000 + T + V + D)
+    W = torch.randn(V, D, device="cuda", generator=g) / D ** 0.5
+    W[:, 0] = 1.0
+    W = W.to(BITS[dtype])
+    t = torch.randint(0, V, (T,), device="cuda", generator=g)
+    far = torch.linspace(0.5, 17.0, T, device="cuda")[torch.randperm(T, device="cuda", generator=g)] if T > 1 else torch.full((1,), 9.0, device="cuda")
+    goal = np.log(V) + far
+    a = D - (D * D - 2 * D * goal).clamp_min(0).sqrt()       # a - a^2 / (2 D) = log V + far: the others' scores have deviation a / sqrt D
+    h = a[:, None] * W[t].float()
+    n = int(round(T * sure))
+    if n < T:
+        h[n:] = torch.randn(T - n, D, device="cuda", generator=g) * 2
+    h[:, 0] = shift
+    h = h.to(BITS[dtype])
+    if T > 3:
+        t[3::7] = -100
+    return h, W, t
+
+
+def reference(h, W, t, c):
+    """Loss, lse, 1 - p, p, g and gradients in float64, the sum of the others taken as such."""
+    hd, Wd = h.double(), W.double()
+    z = hd @ Wd.t()
+    kept = t != -100
+    at = torch.where(kept, t, 0)[:, None]
+    zy = z.gather(1, at)
+    others = (z - zy).exp().scatter(1, at, 0.0).sum(1)       # over p of the target
+    loss = torch.where(kept, torch.log1p(others), 0.0)
+    lse = torch.logsumexp(z, 1)
+    rest = others / (1 + others)
+    g = (z - lse[:, None]).exp().scatter(1, at, 0.0)
+    g = g.scatter(1, at, -rest[:, None]) * torch.where(kept, c, 0.0)[:, None]
+    size = (hd.abs() @ Wd.abs().t()).amax(1)
+    zmax = z.abs().amax(1)
+    return loss, lse, rest, g, size, zmax, kept
+
+
+def slack(size, zmax, D):
+    return 2 * (D / 16 + D / 512 + 2) * U * size + 2 * (6 * LOG2E * zmax + 4) * U + 2.0 ** -17
+
+
+@pytest.mark.parametrize("T,V,D", [(1, 1001, 256), (1, 999, 16392), (4, 3001, 256), (60, 1001, 512), (128, 40001, 256), (300, 1001, 256), (700, 9001, 1032)])
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+def test_small_losses_keep_their_digits(T, V, D, dtype):
+    h, W, t = confident(T, V, D, dtype)
+    lse, loss = torch.empty(T, device="cuda"), torch.empty(T, device="cuda")
+    sp.linear_ce(h, W, t, lse, loss, reduction="none")
+    want, want_lse, rest, _, size, zmax, kept = reference(h, W, t, torch.ones(T, device="cuda"))
+    if T > 50:
+        assert float(rest[kept].min()) < 1e-6 and float(rest[kept].max()) > 1e-2
+    assert (loss >= 0).all()
+    assert ((loss.double() - want).abs() <= slack(size, zmax, D) * want).all()
+    assert ((lse.double() - want_lse).abs() <= slack(size, zmax, D) + want_lse.abs() * U).all()
