@@ -409,11 +409,11 @@ __device__ __forceinline__ void store_part(const EpiStage& stage, const CUtensor
   }
 }
 
-// g of a tile, to 16 bits: its rounding (half a step, 2^-9 of bf16 or 2^-12 of fp16 relative) is independent from entry to entry and
+// g of a tile, to 16 bits: its rounding (at most half a step, 2^-8 of bf16 or 2^-11 of fp16 relative) is independent from entry to entry and
 // enters sums over the vocabulary or the tokens, so it moves a gradient by less than the gradient's own rounding to the same type.
 struct EpiG {
   static constexpr uint32_t kBytes = 8 * 4096;
-  static constexpr bool kSums = false;
+  static constexpr bool kSums = true;       // the scores as the forward product made them: a sum that is cut off all along D is too small, and with it every p
   struct Args {
     const float* lse;
     const float* coef;

@@ -82,3 +82,19 @@ def test_small_losses_keep_their_digits(T, V, D, dtype):
     assert (loss >= 0).all()
     assert ((loss.double() - want).abs() <= slack(size, zmax, D) * want).all()
     assert ((lse.double() - want_lse).abs() <= slack(size, zmax, D) + want_lse.abs() * U).all()
+
+
+@pytest.mark.parametrize("T", [2, 300])
+def test_scores_made_again_are_those_of_the_forward(T):
+    # All scores are one large sum of equal products, so all p are 1 / V.  An accumulator that cuts off every addition of such a sum (2048 of them) leaves
+    # the score 0.03 too small, and every p with it.  Sums of 512 lose at most 32 x 2^-23 x 247 in their own additions and 64 x 2^-24 x 247 in
+    # those of the sums: 1.9e-3.
+    V, D = 64, 32768
+    # 11-bit factors: products of 22 bits, whose sums need rounding from the first hundred on
+    h, W = torch.full((T, D), 4 / 3, dtype=torch.float16, device="cuda"), torch.full((V, D), 150 / D * 1.2346, dtype=torch.float16, device="cuda")
+    t = torch.zeros(T, dtype=torch.int64, device="cuda")
+    lse, loss, dh, dW = torch.empty(T, device="cuda"), torch.empty(T, device="cuda"), torch.empty_like(h), torch.empty_like(W)
+    sp.linear_ce(h, W, t, lse, loss, reduction="none")
+    sp.linear_ce_grad(h, W, t, lse, None, dh, dW, reduction="none")
+    # p: 3.8e-3 (scores made twice), g's rounding and the result's: 2^-11 each
+    assert ((dW[1:].double() * V / T / h[0].double() - 1).abs() <= 3.8e-3 + 2 * 2.0 ** -11 + 2.0 ** -16).all()
