@@ -375,33 +375,41 @@ product_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
       const int edge = min(args.N, (tn + 1) * args.bn);   // what the accumulator holds beyond the tile's own columns is not used
       epi.before(e, args.M, edge);
       uint32_t v[kCols];
-      for (int ks = 0; ks < n; ks += args.kb_sum, ++it) {
-        const int buf = it & 1;
-        ok = mbar_wait(bar_tfull + 8 * buf, (uint32_t)(it >> 1) & 1u, args.status, (kProdEpilogue << 8) | 1);
+      const auto full = [&]() {      // the next accumulator is complete
+        ok = mbar_wait(bar_tfull + 8 * (it & 1), (uint32_t)(it >> 1) & 1u, args.status, (kProdEpilogue << 8) | 1);
         ok = __all_sync(0xffffffffu, ok);
-        if (!ok) break;
         tcgen05_fence_after();
-        if (!Epi::kSums || ks == 0) {
-#pragma unroll
-          for (int q = 0; q < kCols / 32; ++q) tmem_ld_32x32b_x32(taddr + (uint32_t)(buf * BN + q * 32), *reinterpret_cast<uint32_t(*)[32]>(v + q * 32));
-          tmem_ld_wait();
-        } else {
-#pragma unroll
-          for (int q = 0; q < kCols / 32; ++q) {
-            uint32_t w[32];
-            tmem_ld_32x32b_x32(taddr + (uint32_t)(buf * BN + q * 32), w);
-            tmem_ld_wait();
-#pragma unroll
-            for (int j = 0; j < 32; ++j) v[q * 32 + j] = __float_as_uint(__uint_as_float(v[q * 32 + j]) + __uint_as_float(w[j]));
-          }
-        }
+      };
+      const auto hand_back = [&]() {
         tcgen05_fence_before();
         __syncwarp();
         // Relaxed: the values are in registers, nothing was written that the issuer reads.  With release the arrival would wait for the
         // stores of the tile before to reach memory.
         if (lane == 0) {
-          if constexpr (CG == 1) mbar_arrive_relaxed(bar_tempty + 8 * buf);
-          else mbar_arrive_relaxed_cluster(mapa(bar_tempty + 8 * buf, 0));
+          if constexpr (CG == 1) mbar_arrive_relaxed(bar_tempty + 8 * (it & 1));
+          else mbar_arrive_relaxed_cluster(mapa(bar_tempty + 8 * (it & 1), 0));
+        }
+        ++it;
+      };
+      full();
+      if (!ok) break;
+#pragma unroll
+      for (int q = 0; q < kCols / 32; ++q) tmem_ld_32x32b_x32(taddr + (uint32_t)((it & 1) * BN + q * 32), *reinterpret_cast<uint32_t(*)[32]>(v + q * 32));
+      tmem_ld_wait();
+      hand_back();
+      if constexpr (Epi::kSums) {
+        for (int ks = args.kb_sum; ks < n; ks += args.kb_sum) {
+          full();
+          if (!ok) break;
+#pragma unroll
+          for (int q = 0; q < kCols / 16; ++q) {      // 16 columns at a time: v and 32 more do not fit the registers
+            uint32_t w[16];
+            tmem_ld_32x32b_x16(taddr + (uint32_t)((it & 1) * BN + q * 16), w);
+            tmem_ld_wait();
+#pragma unroll
+            for (int j = 0; j < 16; ++j) v[q * 16 + j] = __float_as_uint(__uint_as_float(v[q * 16 + j]) + __uint_as_float(w[j]));
+          }
+          hand_back();
         }
       }
       if (!ok) break;

@@ -98,3 +98,34 @@ def test_scores_made_again_are_those_of_the_forward(T):
     sp.linear_ce_grad(h, W, t, lse, None, dh, dW, reduction="none")
     # p: 3.8e-3 (scores made twice), g's rounding and the result's: 2^-11 each
     assert ((dW[1:].double() * V / T / h[0].double() - 1).abs() <= 3.8e-3 + 2 * 2.0 ** -11 + 2.0 ** -16).all()
+
+
+def test_sums_over_many_tokens_and_many_words_are_not_cut_off():
+    # Sums of 65536 positive terms.  What is common to all entries is what the additions cut off: 32 x 2^-23 in a sum of 512, against 4e-4 if
+    # one accumulator took them all; g is off by lse's 32 bits (|lse| <= 12: 12 x 2^-24 and as much again on its way) and 2^x (2^-22).  The roundings to 16 bits
+    # are the results' own: `off` compares with the rounded reference, mean with mean.  An entry next to a border then
+    # moves by a whole step, but as many as the common error would move on average, so twice that error bounds the mean; the chance part
+    # (g's own roundings, 2^-11 / sqrt(3 x 65536) per entry) moves n entries' mean by at most 5 times that / sqrt n.
+    g = torch.Generator(device="cuda").manual_seed(0)
+    T, V, D = 65536, 64, 64
+    h, W = (torch.rand(T, D, device="cuda", generator=g) + 0.5).half(), (torch.randn(V, D, device="cuda", generator=g) * 0.01).half()
+    t = torch.randint(0, 8, (T,), device="cuda", generator=g)
+    lse, loss, up = torch.empty(T, device="cuda"), torch.empty(1, device="cuda"), torch.full((1,), 1024.0, device="cuda")
+    dh, dW = torch.empty_like(h), torch.empty_like(W)
+    sp.linear_ce(h, W, t, lse, loss)
+    sp.linear_ce_grad(h, W, t, lse, up, dh, dW)
+    p = (h.double() @ W.double().t()).softmax(1)[:, 8:]                 # words that are nobody's target
+    want = p.t() @ h.double() * 1024 / T
+    off, common = (dW[8:].double() - want.half().double()) / want, 32 * U + 12 * U + 2 * U
+    assert abs(float(off.mean())) <= 2 * common + 5 * 2.0 ** -11 / (3 * T * off.numel()) ** 0.5 * 2
+    T, V, D = 2048, 65536, 2560                                         # tiles of dh for every SM: no slices of the vocabulary
+    h, W = (torch.randn(T, D, device="cuda", generator=g) * 0.1).half(), (torch.rand(V, D, device="cuda", generator=g) * 0.01 + 0.005).half()
+    W[:8] = 0
+    t = torch.randint(0, 8, (T,), device="cuda", generator=g)
+    lse, dh = torch.empty(T, device="cuda"), torch.empty_like(h)
+    sp.linear_ce(h, W, t, lse, loss, reduction="sum")
+    sp.linear_ce_grad(h, W, t, lse, up, dh, None, reduction="sum")
+    z = h.double() @ W.double().t()
+    want = z.softmax(1) @ W.double() * 1024
+    off = (dh.double() - want.half().double()) / want
+    assert abs(float(off.mean())) <= 2 * common + 5 * 2.0 ** -11 / (3 * V * off.numel()) ** 0.5 * 2
