@@ -406,6 +406,8 @@ int sp_linear_ce(const void* h, const void* W, const int64_t* target, float* lse
 /* Its gradients:  g[t][v] = c[t] * (exp(z[t][v] - lse[t]) - [v = target[t]]),  dh = g . W,  dW = g^T . h,  with c[t] = 0 where ignored, else
  * grad_loss[t] (SP_REDUCE_NONE), grad_loss[0] (SP_REDUCE_SUM) or grad_loss[0] / number of tokens not ignored (SP_REDUCE_MEAN).
  * The scores are made again, the vocabulary in pieces; g is held in h's type (fp16: scaled by a power of two in between), sums in fp32.
+ * The entry of a token's own word, p - 1, is relatively as exact as the others however small 1 - p is: where it would cancel it is made as minus
+ * the sum of the others.  When T * V is above 2^27 that takes one more product for the share of tokens with p near 1.
  *   lse       : DEVICE, T fp32, as sp_linear_ce left it.
  *   grad_loss : DEVICE, fp32, T values or one; NULL: 1.
  *   dh, dW    : DEVICE, T x D and V x D, same type as h and W, fully overwritten, or NULL: not wanted (at most one of them).

@@ -29,6 +29,24 @@ __device__ __forceinline__ float ex2(float x) {
   return y;
 }
 
+// Two fp32 numbers in one register pair, an instruction for both.
+__device__ __forceinline__ uint64_t pair_of(float lo, float hi) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+  return r;
+}
+__device__ __forceinline__ void halves_of(uint64_t r, float& lo, float& hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(r)); }
+__device__ __forceinline__ uint64_t fma_pair(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ uint64_t add_pair(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+
 __device__ __forceinline__ void tma_store_3d(const CUtensorMap* map, uint32_t src, int x, int y, int z) {
   asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.tile.bulk_group [%0, {%1, %2, %3}], [%4];"
                ::"l"(map), "r"(x), "r"(y), "r"(z), "r"(src) : "memory");
@@ -320,6 +338,8 @@ struct CePrep {
   int64_t ignore;
   int reduction, fp16;
   int masked;            // 1: rows of ignored tokens become zeros
+  unsigned long long* rest;   // per token: set to 0 ...
+  int32_t* count;             // ... and this one number too
 };
 
 // The tokens' rows once more, each on a cache line of its own (a row of a tile's 128 bytes then takes one line of L2, not two: 1001 x 50001 x
@@ -393,9 +413,163 @@ __global__ void __launch_bounds__(1024) ce_prep_kernel(const CePrep a) {
     float c = 0.f;
     if (y != a.ignore) c = y < 0 || y >= a.V ? CUDART_NAN_F : (each ? a.grad[t] : wild) * scale;
     a.coef[t] = c;
+    a.rest[t] = 0;
   }
-  if (threadIdx.x == 0) *a.factor = factor * exp2f((float)-up);
+  if (threadIdx.x == 0) { *a.factor = factor * exp2f((float)-up); *a.count = 0; }
 }
+
+// The entry of a token's own word, p - 1, is the one that cancels: lse is a 32-bit number of the size of the scores, so p is off by |lse| 2^-23 or so,
+// and of a token that is sure of its word (1 - p = 1e-5, scores of 30) nothing would be left.  But 1 - p is also the sum of the
+// others' p, each good to a few 2^-23 of itself.  So that sum is what such tokens get.
+//
+// It is added up by all tiles of a row in any order, in whole steps of 2^-62: 62 bits and two to spare, the same result whatever the order.
+constexpr float kRestStep = 0x1p-62f;
+constexpr unsigned long long kRestNone = ~0ull;
+
+// Scores of a part's columns to p, in place, and the sum of them.  The row's own word (`rel`, -1: not here) and what lies beyond the vocabulary or the
+// tile count nothing and become 0; `hit`: the own word's score.  (Taken out before the exponentials, so that these and the additions run together.)
+template <int COLS>
+__device__ __forceinline__ float ce_probabilities(uint32_t (&v)[COLS], float lse2, int rel, int cols, float& hit) {
+  hit = 0.f;
+  if (__any_sync(0xffffffffu, rel >= 0)) {
+#pragma unroll
+    for (int j = 0; j < COLS; ++j)
+      if (rel == j) { hit = __uint_as_float(v[j]); v[j] = 0xff800000u; }
+  }
+  if (cols < COLS) {
+#pragma unroll
+    for (int j = 0; j < COLS; ++j)
+      if (j >= cols) v[j] = 0xff800000u;
+  }
+  const uint64_t scale = pair_of(kLog2e, kLog2e), off = pair_of(-lse2, -lse2);
+  uint64_t s[4] = {0, 0, 0, 0};
+#pragma unroll
+  for (int j = 0; j < COLS; j += 8)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int k = j + 2 * i;
+      float lo, hi;
+      halves_of(fma_pair(pair_of(__uint_as_float(v[k]), __uint_as_float(v[k + 1])), scale, off), lo, hi);
+      lo = ex2(lo); hi = ex2(hi);
+      s[i] = add_pair(s[i], pair_of(lo, hi));
+      v[k] = __float_as_uint(lo); v[k + 1] = __float_as_uint(hi);
+    }
+  float lo, hi;
+  halves_of(add_pair(add_pair(s[0], s[1]), add_pair(s[2], s[3])), lo, hi);
+  return lo + hi;
+}
+
+// While the vocabulary is one piece, the gradient's own tiles add the sums up and this kernel puts them into g, before anything reads g.  (Tokens whose
+// p is at most 1/2 keep p - 1, which does not cancel there.)  Sums and launch cost 2 to 3 us in a short step (60 x 5000 x 304: 39 to 40), 3 % at 777 x 20011 x 1032.
+struct CeOwn {
+  const int64_t* target;
+  const float* lse;
+  const float* coef;
+  const unsigned long long* rest;
+  uint16_t* g;
+  int64_t ld;
+  int T, V, bf16;
+};
+
+__global__ void __launch_bounds__(256) ce_own_kernel(const CeOwn a) {
+  pdl_launch_dependents();
+  pdl_wait();
+  const int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (t >= a.T) return;
+  const int64_t y = __ldg(a.target + t);
+  const float c = __ldg(a.coef + t), rest = __ull2float_rn(a.rest[t]) * kRestStep;
+  const bool finite = fabsf(__ldg(a.lse + t)) < CUDART_INF_F && fabsf(c) < CUDART_INF_F;      // else the row is NaN as it stands
+  if (finite && c != 0.f && y >= 0 && y < a.V && rest < 0.5f) a.g[t * a.ld + y] = (uint16_t)pack_16(-rest * c, 0.f, a.bf16);
+}
+
+// With the vocabulary in pieces the sum has to be there before the first piece is used.  So the tokens that are sure of their word (and only
+// they) are put together in rows of their own, and one more product over the whole vocabulary makes their sums.  A warp per token:
+// its own score, and with it 1 - p, well enough to tell.  Tokens with 1 - p of 1/16 + |lse| 2^-9 and more keep p - 1: it is off by
+// |lse| 2^-23 / (1 - p) < 2^-13 relative there, less than 16 bits keep.
+// The price is a fourth product for the share of tokens that are sure.  Gradient of 8192 x 131072 x 4096: 20.5 ms where none is, 22.7 where 30 % are, 27.5
+// where all are.
+struct CeSure {
+  const int64_t* target;
+  const float* lse;
+  const float* coef;
+  unsigned long long* rest;    // kRestNone for the tokens that are not sure
+  const uint4* rows;           // the tokens, and the same pitch for
+  uint4* sure;                 // those that are sure
+  int32_t* list;               // whose these are
+  int32_t* count;
+  const uint4* W;
+  int vecs, ld;
+  int T, V, bf16;
+};
+
+__global__ void __launch_bounds__(256) ce_sure_kernel(const CeSure a) {
+  pdl_launch_dependents();
+  pdl_wait();
+  const int lane = threadIdx.x & 31;
+  for (int64_t t = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); t < a.T; t += (int64_t)gridDim.x * 8) {
+    const int64_t y = __ldg(a.target + t);
+    const float lse = __ldg(a.lse + t), c = a.coef[t];
+    bool sure = fabsf(lse) < CUDART_INF_F && fabsf(c) < CUDART_INF_F && c != 0.f && y >= 0 && y < a.V;
+    const uint4* row = a.rows + t * a.ld;
+    if (sure) {
+      float z = 0.f;
+      for (int i = lane; i < a.vecs; i += 32) {
+        const uint4 p = row[i], q = __ldg(a.W + y * a.vecs + i);
+        const uint32_t u[4] = {p.x, p.y, p.z, p.w}, w[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          float ul, uh, wl, wh;
+          row_values(u[k], a.bf16, ul, uh);
+          row_values(w[k], a.bf16, wl, wh);
+          z = fmaf(ul, wl, z);
+          z = fmaf(uh, wh, z);
+        }
+      }
+      for (int o = 16; o; o >>= 1) z += __shfl_xor_sync(0xffffffffu, z, o);
+      sure = -expm1f(z - lse) < fminf(0.5f, 0.0625f + fabsf(lse) * 0x1p-9f);
+    }
+    if (!sure) {
+      if (lane == 0) a.rest[t] = kRestNone;
+      continue;
+    }
+    int at = 0;
+    if (lane == 0) {
+      at = atomicAdd(a.count, 1);      // any order: a token's sum does not depend on its place
+      a.list[at] = (int)t;
+    }
+    at = __shfl_sync(0xffffffffu, at, 0);
+    for (int i = lane; i < a.vecs; i += 32) a.sure[(int64_t)at * a.ld + i] = row[i];
+  }
+}
+
+// The sums of the tokens that are sure.
+struct EpiRest {
+  static constexpr uint32_t kBytes = 0;
+  static constexpr bool kSums = true;
+  struct Args {
+    const float* lse;
+    const int64_t* target;
+    const int32_t* list;
+    const int32_t* count;
+    unsigned long long* rest;
+  };
+  const Args& a;
+  int lane, token, rel;
+  float lse2;
+  __device__ EpiRest(const Args& args, const CUtensorMap*, uint32_t, int, int l) : a(args), lane(l) {}
+  __device__ __forceinline__ void before(const EpiTile& e, int, int) {
+    token = e.row0 + lane < *a.count ? a.list[e.row0 + lane] : -1;
+    lse2 = token >= 0 ? __ldg(a.lse + token) * kLog2e : 0.f;
+    const int64_t t = token >= 0 ? __ldg(a.target + token) - e.col0 : -1;
+    rel = t >= 0 && t < kCePart ? (int)t : -1;
+  }
+  template <int COLS>
+  __device__ __forceinline__ void finish(uint32_t (&v)[COLS], const EpiTile& e, int, int N) {
+    float hit;
+    const float s = ce_probabilities<COLS>(v, lse2, rel, N - e.col0, hit);
+    if (token >= 0) atomicAdd(a.rest + token, __float2ull_rn(s / kRestStep));
+  }
+};
 
 // One staged slice of 64 16-bit columns to a matrix.
 __device__ __forceinline__ void store_part(const EpiStage& stage, const CUtensorMap* map, int lane, const uint32_t (&p)[32], bool inside, int col, int row) {
@@ -419,13 +593,15 @@ struct EpiG {
     const float* coef;
     const int64_t* target;
     int64_t v0;              // first column of the piece
+    unsigned long long* rest;
+    int given;               // 1: sums of the others' p are in `rest` (or kRestNone), 0: they are added up there
     int bf16;
   };
   const Args& a;
   const CUtensorMap* map;
   EpiStage stage;
   int lane, rel;
-  float lse2, c;
+  float lse2, c, minus;      // minus: 1 - p of the own word, where it is given
   __device__ EpiG(const Args& args, const CUtensorMap* m, uint32_t base, int w, int l) : a(args), map(m), stage{base + (uint32_t)w * 4096u, l}, lane(l) {}
   __device__ __forceinline__ void before(const EpiTile& e, int M, int) {
     const int row = e.row0 + lane;
@@ -434,16 +610,18 @@ struct EpiG {
     lse2 = in ? __ldg(a.lse + row) * kLog2e : 0.f;
     const int64_t t = in ? __ldg(a.target + row) - a.v0 - e.col0 : -1;
     rel = t >= 0 && t < kCePart ? (int)t : -1;
+    minus = -1.f;
+    if (a.given && rel >= 0) {
+      const unsigned long long r = a.rest[row];
+      if (r != kRestNone) minus = __ull2float_rn(r) * kRestStep;
+    }
   }
   template <int COLS>
   __device__ __forceinline__ void finish(uint32_t (&v)[COLS], const EpiTile& e, int M, int N) {
-#pragma unroll
-    for (int j = 0; j < COLS; ++j) v[j] = __float_as_uint(ex2(fmaf(__uint_as_float(v[j]), kLog2e, -lse2)));
-    if (__any_sync(0xffffffffu, rel >= 0)) {
-#pragma unroll
-      for (int j = 0; j < COLS; ++j)
-        if (rel == j) v[j] = __float_as_uint(__uint_as_float(v[j]) - 1.f);
-    }
+    float hit;
+    const float s = ce_probabilities<COLS>(v, lse2, rel, N - e.col0, hit);
+    if (!a.given && e.row0 + lane < M && c != 0.f) atomicAdd(a.rest + e.row0 + lane, __float2ull_rn(s / kRestStep));
+    const float own = minus >= 0.f ? -minus : ex2(fmaf(hit, kLog2e, -lse2)) - 1.f;
 #pragma unroll
     for (int q = 0; q < COLS / 64; ++q) {
       uint32_t p[32];
@@ -452,7 +630,19 @@ struct EpiG {
         p[j] = pack_16(__uint_as_float(v[q * 64 + 2 * j]) * c, __uint_as_float(v[q * 64 + 2 * j + 1]) * c, a.bf16);
         if (c == 0.f) p[j] = 0;     // a token that does not count: exactly nothing, whatever its scores are
       }
-      store_part(stage, map, lane, p, e.row0 < M && e.col0 + q * 64 < N, e.col0 + q * 64, e.row0);
+      const uint32_t slice = stage.free();
+      stage_row(slice, lane, p);
+      const uint32_t at = (uint32_t)(rel - q * 64);
+      if (at < 64u && c != 0.f)      // the own word's entry, over the zero
+        asm volatile("st.shared.b16 [%0], %1;" ::"r"(slice + (uint32_t)lane * 128u + (((at >> 3) ^ ((uint32_t)lane & 7u)) << 4) + (at & 7u) * 2u),
+                     "h"((uint16_t)pack_16(own * c, 0.f, a.bf16)) : "memory");
+      fence_async_smem();
+      __syncwarp();
+      const int col = e.col0 + q * 64;
+      if (lane == 0 && e.row0 < M && col < N) {
+        tma_store_2d(map, slice, col, e.row0);
+        bulk_commit();
+      }
     }
   }
 };
@@ -550,7 +740,7 @@ struct CePlan {
   bool copy;                  // forward: the tokens' rows are copied to cache lines of their own
   int64_t ld_h;               // row pitch of such copies
   int64_t off_picked, off_each, off_rows, forward_bytes;
-  int64_t off_factor, off_grad_rows, off_g, off_acc, grad_bytes;
+  int64_t off_factor, off_rest, off_list, off_grad_rows, off_g, off_acc, off_sure, grad_bytes;
 };
 
 // Rows of a token tile: a CTA pair's 256, or one CTA's 128 where no more tokens are there.  (Also for token counts that fill their last tile
@@ -589,10 +779,14 @@ static CePlan ce_plan(int64_t T, int64_t V, int64_t D) {
   if (s < 1) s = 1;
   p.slices = (int)s;
   p.off_factor = up256(T * 4);
-  p.off_grad_rows = p.off_factor + 256;
+  p.off_rest = p.off_factor + 256;
+  p.off_list = p.off_rest + up256(T * 8);
+  p.off_grad_rows = p.off_list + (p.pieces > 1 ? up256(T * 4) : 0);
   p.off_g = p.off_grad_rows + up256(T * p.ld_h * 2);
   p.off_acc = p.off_g + up256(T * p.ld_g * 2);
   p.grad_bytes = p.off_acc + ((p.pieces > 1 || p.slices > 1) ? up256(p.slices * T * D * 4) : 0);
+  // With pieces, rows of the tokens that are sure lie where g or the sums of dh come later: a row of g has at least 1024 entries of 2 bytes, one of dh's sums D of 4.
+  p.off_sure = p.ld_h <= p.ld_g ? p.off_g : p.off_acc;
   return p;
 }
 
@@ -637,7 +831,7 @@ static ProdArgs ce_args(const Sched& sched, int32_t* status, int64_t M, int64_t 
 // h . W_piece^T with an epilogue of scores.
 template <class Epi>
 static int ce_scores(const char* what, const CePlan& p, const void* h, int64_t ld_h, const void* W, int64_t cols, int32_t* status, bool bf16, const CUtensorMap* tmC,
-                     const typename Epi::Args& ea, cudaStream_t stream) {
+                     const typename Epi::Args& ea, cudaStream_t stream, const int32_t* live = nullptr) {
   CUtensorMap tmA, tmB;
   Sched sched;
   const int rows = ce_rows(p.T), width = tile_width(p.T, cols, rows / 128, tmC ? 64 : 32);      // g is stored 64 columns at a time
@@ -647,6 +841,7 @@ static int ce_scores(const char* what, const CePlan& p, const void* h, int64_t l
   if (rc != SP_OK) return rc;
   ProdArgs a = ce_args(sched, status, p.T, cols, p.D, 1);
   a.turn = sched.Tm == 1;
+  a.live = live;
   a.bn = width;
   if (rows == 256) return launch_product<2, 256, kElem16, false, false, Epi>(what, tmA, tmB, tmC ? *tmC : tmA, a, bf16, ea, stream);
   return launch_product<1, 256, kElem16, false, false, Epi>(what, tmA, tmB, tmC ? *tmC : tmA, a, bf16, ea, stream);
@@ -754,10 +949,23 @@ int sp_linear_ce_grad(const void* h, const void* W, const int64_t* target, const
   float *coef = (float*)ws, *factor = (float*)(ws + p.off_factor), *acc = (float*)(ws + p.off_acc);
   char* g = ws + p.off_g;
   char* rows = ws + p.off_grad_rows;
+  auto* rest = (unsigned long long*)(ws + p.off_rest);
+  int32_t *count = (int32_t*)(ws + p.off_factor + 4), *list = (int32_t*)(ws + p.off_list);
   CePrep prep = ce_rows_args(p, h, rows, target, ignore_index, true);
+  prep.rest = rest; prep.count = count;
   prep.grad = grad_loss; prep.coef = coef; prep.factor = factor; prep.V = (int)V; prep.reduction = reduction; prep.fp16 = !bf16;
   rc = launch_pdl("coefficients and rows of the tokens", ce_prep_kernel, dim3(1 + ce_copy_blocks(p)), 1024, 0, 1, stream, prep);
   if (rc != SP_OK) return rc;
+  if (p.pieces > 1) {
+    uint4* sure = (uint4*)(ws + p.off_sure);
+    const CeSure cs = {target, lse, coef, rest, (const uint4*)rows, sure, list, count, (const uint4*)W, (int)(D / 8), (int)(p.ld_h / 8), (int)T, (int)V, bf16};
+    const int64_t blocks = div_up(T, 8);
+    rc = launch_pdl("tokens that are sure", ce_sure_kernel, dim3((unsigned)(blocks < 8 * 148 ? blocks : 8 * 148)), 256, 0, 1, stream, cs);
+    if (rc != SP_OK) return rc;
+    const EpiRest::Args er = {lse, target, list, count, rest};
+    rc = ce_scores<EpiRest>("sums of the others", p, sure, p.ld_h, W, V, st.status, bf16, nullptr, er, stream, count);
+    if (rc != SP_OK) return rc;
+  }
   const bool summed = p.pieces > 1 || p.slices > 1;     // dh passes through fp32 sums
   for (int i = 0; i < p.pieces; ++i) {
     const int64_t v0 = i * p.piece, cols = V - v0 < p.piece ? V - v0 : p.piece;
@@ -765,9 +973,14 @@ int sp_linear_ce_grad(const void* h, const void* W, const int64_t* target, const
     CUtensorMap tmG, tmA, tmB, tmC;
     rc = make_map_any(&tmG, g, 2, T, cols, p.ld_g, 32, 64);
     if (rc != SP_OK) return rc;
-    const EpiG::Args ea = {lse, coef, target, v0, bf16};
+    const EpiG::Args ea = {lse, coef, target, v0, rest, p.pieces > 1, bf16};
     rc = ce_scores<EpiG>("gradient of the scores", p, rows, p.ld_h, Wp, cols, st.status, bf16, &tmG, ea, stream);
     if (rc != SP_OK) return rc;
+    if (p.pieces == 1) {
+      const CeOwn co = {target, lse, coef, rest, (uint16_t*)g, p.ld_g, (int)T, (int)V, bf16};
+      rc = launch_pdl("own words", ce_own_kernel, dim3((unsigned)div_up(T, 256)), 256, 0, 1, stream, co);
+      if (rc != SP_OK) return rc;
+    }
     if (dh) {
       Sched sched;
       rc = ce_sched(T, D, ce_rows(T), 256, &sched);

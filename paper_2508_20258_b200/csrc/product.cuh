@@ -52,6 +52,7 @@ struct ProdCfg {
 
 struct ProdArgs {
   const int32_t* perm;   // tile table (orders that are not arithmetic), else nullptr
+  const int32_t* live;   // on the device: rows of A that are there, if that is known there only (tiles beyond them are passed over), else nullptr
   int32_t* status;
   int M, N;              // rows of A, rows of B
   int bn;                // columns of a tile: BN, or less where that fills the last wave better (a multiple of 32; B k-major)
@@ -255,6 +256,8 @@ product_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
     const int t = args.sched.use_table ? __ldg(args.perm + o) : slot_to_tile(args.sched, o);
     tm = t / Tn; tn = t - tm * Tn;
   };
+  const int live = args.live ? *args.live : args.M;
+  auto passed_over = [&](int tm) { return tm * 128 * CG >= live; };
   auto stages_of = [&](int z) { return (args.kblocks - z + args.splits - 1) / args.splits; };
 
   if (warp < C::kEpi0) {
@@ -267,6 +270,7 @@ product_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
     for (int s = unit; s < total && ok; s += args.units) {
       int tm, tn, z;
       tile_at(s, tm, tn, z);
+      if (passed_over(tm)) continue;
       const int n = stages_of(z);
       const int row0 = tm * 128 * CG + (int)rank * 128, col0 = tn * args.bn + (int)rank * (args.bn / CG);
       int at = args.turn ? (unit * 5) % n : 0;      // the stage to load, of this slice's
@@ -326,6 +330,7 @@ product_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
       for (int s = unit; s < total && ok; s += args.units) {
         int tm, tn, z;
         tile_at(s, tm, tn, z);
+        if (passed_over(tm)) continue;
         const int n = stages_of(z);
         for (int ks = 0; ks < n && ok; ks += args.kb_sum, ++it) {
           const int ke = min(n, ks + args.kb_sum), buf = it & 1;
@@ -368,6 +373,7 @@ product_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
       EpiTile e;
       int tm, tn;
       tile_at(s, tm, tn, e.z);
+      if (passed_over(tm)) continue;
       const int n = stages_of(e.z);
       e.row0 = tm * 128 * CG + (int)rank * 128 + quarter * 32;
       e.col0 = tn * args.bn + half * kCols;

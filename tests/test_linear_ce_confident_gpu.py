@@ -84,6 +84,56 @@ def test_small_losses_keep_their_digits(T, V, D, dtype):
     assert ((lse.double() - want_lse).abs() <= slack(size, zmax, D) + want_lse.abs() * U).all()
 
 
+def near(got, want, tol):
+    """Within the tolerance, or infinite where the type ends within it (a scaled-up gradient may leave fp16's range)."""
+    over = (want.abs() + tol > torch.finfo(got.dtype).max) & torch.isinf(got) & (got.sign() == want.sign())
+    return bool((((got.double() - want).abs() <= tol) | over).all())
+
+
+def check_gradients(h, W, t, reduction, dtype, up):
+    T, D = h.shape
+    V = W.shape[0]
+    e = float(torch.finfo(BITS[dtype]).eps) / 2
+    tiny = 2.0 ** -25 if dtype == "fp16" else 0.0
+    lse, loss = torch.empty(T, device="cuda"), torch.empty(T if reduction == "none" else 1, device="cuda")
+    sp.linear_ce(h, W, t, lse, loss, reduction=reduction)
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    grad = (torch.rand(T if reduction == "none" else 1, device="cuda", generator=gen) + 0.5) * up
+    dh, dW = torch.full_like(h, float("nan")), torch.full_like(W, float("nan"))
+    sp.linear_ce_grad(h, W, t, lse, grad, dh, dW, reduction=reduction)
+    assert sp.get_status() == 0
+    kept = t != -100
+    c = grad.double().expand(T) / (kept.sum() if reduction == "mean" else 1)
+    hd, Wd = h.double(), W.double()
+    rW, sW = torch.zeros(V, D, dtype=torch.float64, device="cuda"), torch.zeros(V, D, dtype=torch.float64, device="cuda")
+    for i in range(0, T, 512):
+        part = slice(i, i + 512)
+        _, _, rest, g, size, zmax, _ = reference(h[part], W, t[part], c[part])
+        dg = (e + slack(size, zmax, D) + 2.0 ** -13)[:, None] * g.abs() + torch.where(kept[part], c.max() * tiny / 2.0 ** 14, 0.0)[:, None]
+        rh, sh = g @ Wd, dg @ Wd.abs() + (V + 2) * U * (g.abs() @ Wd.abs())
+        assert near(dh[part], rh, sh + (e + 2 * U) * rh.abs() + tiny)
+        rW += g.t() @ hd[part]
+        sW += dg.t() @ hd[part].abs() + (T + 2) * U * (g.abs().t() @ hd[part].abs())
+        assert (dh[part][~kept[part]] == 0).all()
+    assert near(dW, rW, sW + (e + 2 * U) * rW.abs() + tiny)
+
+
+@pytest.mark.parametrize("T,V,D", [(1, 1001, 256), (2, 2, 64), (4, 3001, 256), (60, 1001, 512), (128, 40001, 256), (300, 1001, 256), (700, 9001, 1032)])
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("reduction", ["none", "mean", "sum"])
+def test_gradients_of_confident_tokens(T, V, D, dtype, reduction):
+    h, W, t = confident(T, V, D, dtype)
+    check_gradients(h, W, t, reduction, dtype, (4096.0 if dtype == "fp16" else 1.0) * (T if reduction == "mean" else 1))
+
+
+# the vocabulary in pieces (more than 128 Mi entries of g): all tokens sure, some, one, none
+@pytest.mark.parametrize("T,V,D,dtype,sure", [(2048, 70001, 256, "bf16", 1.0), (2048, 70001, 256, "fp16", 0.3), (3000, 50000, 264, "bf16", 1 / 3000), (3000, 50000, 264, "fp16", 0.0),
+                                              (130, 1100000, 256, "bf16", 0.5), (100, 1400001, 256, "fp16", 0.5)])
+def test_gradients_of_confident_tokens_in_pieces(T, V, D, dtype, sure):
+    h, W, t = confident(T, V, D, dtype, sure=sure)
+    check_gradients(h, W, t, "none", dtype, 4096.0 if dtype == "fp16" else 1.0)
+
+
 @pytest.mark.parametrize("T", [2, 300])
 def test_scores_made_again_are_those_of_the_forward(T):
     # All scores are one large sum of equal products, so all p are 1 / V.  An accumulator that cuts off every addition of such a sum (2048 of them) leaves
