@@ -680,12 +680,16 @@ struct EpiSum {
   }
 };
 
-// A finished gradient, to its 16-bit type.
+// A finished gradient, to its 16-bit type.  Rows of dh of tokens that do not count are zero also where W is not finite (0 x infinity).
+// TOKENS: rows are tokens (dh); else words (dW, whose writing bounds it for few tokens: 16 x 65536 x 4096 takes 484 us a step with the test of a row, 399
+// without).
+template <bool TOKENS>
 struct EpiOut16 {
   static constexpr uint32_t kBytes = 8 * 4096;
   static constexpr bool kSums = true;
   struct Args {
     const float* factor;
+    const float* coef;       // of the tokens
     int bf16;
   };
   const Args& a;
@@ -693,23 +697,29 @@ struct EpiOut16 {
   EpiStage stage;
   int lane;
   float factor;
+  bool none;
   __device__ EpiOut16(const Args& args, const CUtensorMap* m, uint32_t base, int w, int l)
       : a(args), map(m), stage{base + (uint32_t)w * 4096u, l}, lane(l), factor(__ldg(args.factor)) {}
-  __device__ __forceinline__ void before(const EpiTile&, int, int) {}
+  __device__ __forceinline__ void before(const EpiTile& e, int M, int) {
+    if constexpr (TOKENS) none = e.row0 + lane < M && __ldg(a.coef + e.row0 + lane) == 0.f;
+  }
   template <int COLS>
   __device__ __forceinline__ void finish(uint32_t (&v)[COLS], const EpiTile& e, int M, int N) {
 #pragma unroll
     for (int q = 0; q < COLS / 64; ++q) {
       uint32_t p[32];
 #pragma unroll
-      for (int j = 0; j < 32; ++j) p[j] = pack_16(__uint_as_float(v[q * 64 + 2 * j]) * factor, __uint_as_float(v[q * 64 + 2 * j + 1]) * factor, a.bf16);
+      for (int j = 0; j < 32; ++j) {
+        p[j] = pack_16(__uint_as_float(v[q * 64 + 2 * j]) * factor, __uint_as_float(v[q * 64 + 2 * j + 1]) * factor, a.bf16);
+        if (TOKENS && none) p[j] = 0;
+      }
       store_part(stage, map, lane, p, e.row0 < M && e.col0 + q * 64 < N, e.col0 + q * 64, e.row0);
     }
   }
 };
 
-// dh from the fp32 sums of its slices, added in slice order.  Four elements per thread (T x D is a multiple of 8).
-__global__ void __launch_bounds__(256) ce_finish_kernel(const float4* acc, int64_t n4, int slices, const float* factor, int bf16, uint2* out) {
+// dh from the fp32 sums of its slices, added in slice order.  Four elements per thread (D is a multiple of 8); zeros as above.
+__global__ void __launch_bounds__(256) ce_finish_kernel(const float4* acc, int64_t n4, int d4, int slices, const float* factor, const float* coef, int bf16, uint2* out) {
   pdl_launch_dependents();
   pdl_wait();
   const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
@@ -720,7 +730,7 @@ __global__ void __launch_bounds__(256) ce_finish_kernel(const float4* acc, int64
     s.x += p.x; s.y += p.y; s.z += p.z; s.w += p.w;
   }
   const float f = __ldg(factor);
-  out[i] = make_uint2(pack_16(s.x * f, s.y * f, bf16), pack_16(s.z * f, s.w * f, bf16));
+  out[i] = __ldg(coef + i / d4) == 0.f ? make_uint2(0u, 0u) : make_uint2(pack_16(s.x * f, s.y * f, bf16), pack_16(s.z * f, s.w * f, bf16));
 }
 
 // ------------------------------------------------------------------ host side
@@ -998,9 +1008,9 @@ int sp_linear_ce_grad(const void* h, const void* W, const int64_t* target, const
       } else {
         rc = make_map_any(&tmC, dh, 2, T, D, D, 32, 64);
         if (rc != SP_OK) return rc;
-        const EpiOut16::Args eo = {factor, bf16};
-        rc = ce_rows(T) == 256 ? launch_product<2, 256, kElem16, false, true, EpiOut16>("gradient of h", tmA, tmB, tmC, a, bf16, eo, stream)
-                             : launch_product<1, 256, kElem16, false, true, EpiOut16>("gradient of h", tmA, tmB, tmC, a, bf16, eo, stream);
+        const EpiOut16<true>::Args eo = {factor, coef, bf16};
+        rc = ce_rows(T) == 256 ? launch_product<2, 256, kElem16, false, true, EpiOut16<true>>("gradient of h", tmA, tmB, tmC, a, bf16, eo, stream)
+                             : launch_product<1, 256, kElem16, false, true, EpiOut16<true>>("gradient of h", tmA, tmB, tmC, a, bf16, eo, stream);
       }
       if (rc != SP_OK) return rc;
     }
@@ -1013,15 +1023,15 @@ int sp_linear_ce_grad(const void* h, const void* W, const int64_t* target, const
       if (rc != SP_OK) return rc;
       ProdArgs a = ce_args(sched, st.status, cols, D, T, 1);
       a.overlap = dh != nullptr;
-      const EpiOut16::Args eo = {factor, bf16};
-      rc = launch_product<2, 256, kElem16, true, true, EpiOut16>("gradient of W", tmA, tmB, tmC, a, bf16, eo, stream);
+      const EpiOut16<false>::Args eo = {factor, nullptr, bf16};
+      rc = launch_product<2, 256, kElem16, true, true, EpiOut16<false>>("gradient of W", tmA, tmB, tmC, a, bf16, eo, stream);
       if (rc != SP_OK) return rc;
     }
   }
   if (dh && summed) {
     const int64_t n4 = T * D / 4;
-    rc = launch_pdl("sum of the slices", ce_finish_kernel, dim3((unsigned)div_up(n4, 256)), 256, 0, 1, stream, (const float4*)acc, n4, p.slices,
-                    (const float*)factor, (int)bf16, (uint2*)dh);
+    rc = launch_pdl("sum of the slices", ce_finish_kernel, dim3((unsigned)div_up(n4, 256)), 256, 0, 1, stream, (const float4*)acc, n4, (int)(D / 4), p.slices,
+                    (const float*)factor, (const float*)coef, (int)bf16, (uint2*)dh);
   }
   return rc;
 } catch (const std::exception& e) {

@@ -179,3 +179,20 @@ def test_sums_over_many_tokens_and_many_words_are_not_cut_off():
     want = z.softmax(1) @ W.double() * 1024
     off = (dh.double() - want.half().double()) / want
     assert abs(float(off.mean())) <= 2 * common + 5 * 2.0 ** -11 / (3 * V * off.numel()) ** 0.5 * 2
+
+
+# dh in slices of the vocabulary, in whole tiles, in pieces
+@pytest.mark.parametrize("T,V,D", [(4, 700, 64), (300, 700, 72), (2560, 600, 2048), (2048, 70001, 64)])
+@pytest.mark.parametrize("value", [float("inf"), -float("inf"), float("nan")])
+def test_rows_of_dh_of_ignored_tokens_are_zero_whatever_w_holds(T, V, D, value):
+    g = torch.Generator(device="cuda").manual_seed(T)
+    h, W = torch.randn(T, D, device="cuda", generator=g).bfloat16(), torch.randn(V, D, device="cuda", generator=g).bfloat16()
+    t = torch.randint(0, V, (T,), device="cuda", generator=g)
+    t[1::3] = -100
+    W[5, 1] = value
+    lse, loss = torch.empty(T, device="cuda"), torch.empty(T, device="cuda")
+    dh, dW = torch.full_like(h, 7.0), torch.empty_like(W)
+    sp.linear_ce(h, W, t, lse, loss, reduction="none")
+    sp.linear_ce_grad(h, W, t, lse, None, dh, dW, reduction="none")
+    assert sp.get_status() == 0
+    assert (dh[t == -100] == 0).all() and torch.isnan(dh[t != -100]).any()
