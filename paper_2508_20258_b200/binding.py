@@ -429,7 +429,8 @@ def linear_ce_workspace(T: int, V: int, D: int, grad: bool = False) -> int:
 
 
 def _ce_workspace(workspace, like, sizes, grad: int, stream):
-    """The caller's workspace, or one of torch's allocator's that outlives the work on the stream it is used on."""
+    """The caller's workspace, or one of torch's allocator's, taken for the stream it is used on: memory of another stream's may still be at
+    work in that stream's kernels, which the call would not wait for."""
     import torch
     if workspace is not None:
         _device_tensors(workspace)
@@ -437,12 +438,12 @@ def _ce_workspace(workspace, like, sizes, grad: int, stream):
     need = lib().sp_linear_ce_workspace(*sizes, grad)
     if need < 0:
         raise SpError(ERR_INVALID_ARG, "sizes must be positive and below 2^31")
-    buf = like.new_empty(need, dtype=torch.uint8)
     if stream is not None:
         handle = _stream_handle(stream)
         if handle != _stream_handle(None):
-            buf.record_stream(torch.cuda.ExternalStream(handle) if isinstance(stream, int) else stream)
-    return buf, need
+            with torch.cuda.stream(stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(handle)):
+                return like.new_empty(need, dtype=torch.uint8), need
+    return like.new_empty(need, dtype=torch.uint8), need
 
 
 def linear_ce(h, W, target, lse, loss, reduction: str = "mean", ignore_index: int = -100, workspace=None, stream=None) -> None:

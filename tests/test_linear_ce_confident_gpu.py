@@ -196,3 +196,31 @@ def test_rows_of_dh_of_ignored_tokens_are_zero_whatever_w_holds(T, V, D, value):
     sp.linear_ce_grad(h, W, t, lse, None, dh, dW, reduction="none")
     assert sp.get_status() == 0
     assert (dh[t == -100] == 0).all() and torch.isnan(dh[t != -100]).any()
+
+
+def test_a_workspace_on_another_stream_is_not_memory_still_in_use():
+    # what the current stream has given back but is still writing must not become the workspace of a call on another stream
+    T, V, D = 700, 9000, 64
+    g = torch.Generator(device="cuda").manual_seed(2)
+    h, W = torch.randn(T, D, device="cuda", generator=g).bfloat16(), torch.randn(V, D, device="cuda", generator=g).bfloat16()
+    t = torch.randint(0, V, (T,), device="cuda", generator=g)
+    want = [torch.empty(T, device="cuda"), torch.empty(1, device="cuda"), torch.empty_like(h), torch.empty_like(W)]
+    sp.linear_ce(h, W, t, want[0], want[1])
+    sp.linear_ce_grad(h, W, t, want[0], None, want[2], want[3])
+    big = torch.randn(8192, 8192, device="cuda").bfloat16()
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for stream in (side, int(side.cuda_stream)):
+        got = [torch.full_like(v, 3.0) for v in want]
+        torch.cuda.synchronize()
+        used = [torch.empty(sp.linear_ce_workspace(T, V, D, grad), dtype=torch.uint8, device="cuda") for grad in (False, True)]
+        for _ in range(10):
+            big @ big                                           # some milliseconds
+        for u in used:
+            u.fill_(255)
+        del used, u
+        sp.linear_ce(h, W, t, got[0], got[1], stream=stream)
+        sp.linear_ce_grad(h, W, t, got[0], None, got[2], got[3], stream=stream)
+        torch.cuda.synchronize()
+        assert sp.get_status() == 0
+        assert all(torch.equal(a, b) for a, b in zip(want, got))

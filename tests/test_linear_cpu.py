@@ -182,3 +182,35 @@ def test_constants_match_the_header():
     defs = {m.group(1): int(m.group(2)) for m in re.finditer(r"#define\s+SP_([A-Z_0-9]+)\s+\(?(-?\d+)\)?", text)}
     for name in ("BF16", "FP32", "FP16", "ORDER_AUTO", "I8_MAX_K", "REDUCE_NONE", "REDUCE_MEAN", "REDUCE_SUM"):
         assert defs[name] == getattr(binding, name), name
+
+
+def test_a_workspace_is_taken_for_the_stream_it_is_used_on(monkeypatch):
+    torch = pytest.importorskip("torch")
+    import contextlib
+    active, taken = ["current"], []
+
+    class Stream:
+        def __init__(self, handle):
+            self.cuda_stream = handle
+
+    @contextlib.contextmanager
+    def use(stream):
+        active.append(stream.cuda_stream)
+        yield
+        active.pop()
+
+    class Like:
+        def new_empty(self, n, dtype):
+            taken.append(active[-1])
+            return torch.empty(n, dtype=dtype)
+
+    monkeypatch.setattr(torch.cuda, "Stream", Stream)
+    monkeypatch.setattr(torch.cuda, "ExternalStream", Stream)
+    monkeypatch.setattr(torch.cuda, "stream", use)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda *a: Stream(11))
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda d: 11, raising=False)
+    for stream, want in ((None, "current"), (Stream(11), "current"), (11, "current"), (Stream(77), 77), (77, 77), (0, 0)):
+        for grad in (0, 1):
+            buf, n = binding._ce_workspace(None, Like(), (8, 100, 64), grad, stream)
+            assert buf.numel() == n == sp.linear_ce_workspace(8, 100, 64, bool(grad)) and taken.pop() == want
