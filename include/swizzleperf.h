@@ -109,7 +109,9 @@ typedef enum {
                                  before it has completed and its writes are visible (so only launch latency and set-up
                                  overlap, and the stream order is the usual one); a launch with this flag does not wait.  CTAs of the next GEMM then take over SMs as the CTAs of the
                                  previous one finish, which fills the partly empty last wave of back-to-back independent
-                                 GEMMs.  The paper has no counterpart.  Not with SP_FLAG_DIE_PINNED,
+                                 GEMMs.  Behind a call of several kernels (sp_linear_i8, sp_linear_ce, sp_linear_ce_grad) the
+                                 statement is about the whole call; what came before that call is complete when this launch
+                                 starts.  The paper has no counterpart.  Not with SP_FLAG_DIE_PINNED,
                                  SP_FLAG_STREAM_K or tracing (SP_ERR_INVALID_ARG).  It still completes after its predecessor, so the
                                  stream order seen by everything else (copies, events, other kernels) is unchanged. */
 

@@ -160,8 +160,7 @@ __global__ void __launch_bounds__(kRowThreads, 2) row_stats_kernel(const RowArgs
   __shared__ float2 part[kRowThreads / 32];
   const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5, warp = blockIdx.x * (kRowThreads / 32) + wid;
   const int step = gridDim.x * (kRowThreads / 32) * 2;
-  pdl_launch_dependents();
-  pdl_wait();
+  pdl_begin();
   int4 w[2][kRowUnroll];
   auto fetch = [&](int64_t n, int k) {      // elements [k, k + 2048) of rows n and n + 1
 #pragma unroll
@@ -259,8 +258,7 @@ __device__ void reduce_losses(const CeJoin& a) {
 // 2^shift rows per block (32, or 4 when no more tokens are there); blockDim >> shift threads share a row's pairs, whose reads do not wait
 // for one another.  (Eight threads per row, joining pair after pair, took 6 us for one token's 296 pairs: a chain of trips to L2.)
 __global__ void __launch_bounds__(1024) ce_join_kernel(const CeJoin a, int shift) {
-  pdl_launch_dependents();
-  pdl_wait();
+  pdl_begin();
   __shared__ float2 part[1024];
   const int rows = 1 << shift, groups = (int)blockDim.x >> shift;
   const int r = threadIdx.x & (rows - 1), g = threadIdx.x >> shift, lane = threadIdx.x & 31;
@@ -319,8 +317,7 @@ __global__ void __launch_bounds__(1024) ce_join_kernel(const CeJoin a, int shift
 }
 
 __global__ void __launch_bounds__(1024) ce_reduce_kernel(const CeJoin a) {
-  pdl_launch_dependents();
-  pdl_wait();
+  pdl_begin();
   reduce_losses(a);
 }
 
@@ -355,8 +352,7 @@ __device__ __forceinline__ void ce_copy_rows(const CePrep& a, int block, int blo
 }
 
 __global__ void __launch_bounds__(1024) ce_rows_kernel(const CePrep a) {
-  pdl_launch_dependents();
-  pdl_wait();
+  pdl_begin();
   ce_copy_rows(a, blockIdx.x, gridDim.x);
 }
 
@@ -368,8 +364,7 @@ __global__ void __launch_bounds__(1024) ce_rows_kernel(const CePrep a) {
 // fp16 reaches down to 2^-24 only, and p ranges down to 1 / V and below: there coef is scaled by a power of two that brings
 // its largest value to [2^14, 2^15] (|g| <= coef stays below 65504), and `factor` by the inverse.  Block 0; the others copy rows.
 __global__ void __launch_bounds__(1024) ce_prep_kernel(const CePrep a) {
-  pdl_launch_dependents();
-  pdl_wait();
+  pdl_begin();
   if (blockIdx.x > 0) {
     ce_copy_rows(a, blockIdx.x - 1, gridDim.x - 1);
     return;
@@ -472,8 +467,7 @@ struct CeOwn {
 };
 
 __global__ void __launch_bounds__(256) ce_own_kernel(const CeOwn a) {
-  pdl_launch_dependents();
-  pdl_wait();
+  pdl_begin();
   const int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x;
   if (t >= a.T) return;
   const int64_t y = __ldg(a.target + t);
@@ -503,8 +497,7 @@ struct CeSure {
 };
 
 __global__ void __launch_bounds__(256) ce_sure_kernel(const CeSure a) {
-  pdl_launch_dependents();
-  pdl_wait();
+  pdl_begin();
   const int lane = threadIdx.x & 31;
   for (int64_t t = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); t < a.T; t += (int64_t)gridDim.x * 8) {
     const int64_t y = __ldg(a.target + t);
@@ -720,8 +713,7 @@ struct EpiOut16 {
 
 // dh from the fp32 sums of its slices, added in slice order.  Four elements per thread (D is a multiple of 8); zeros as above.
 __global__ void __launch_bounds__(256) ce_finish_kernel(const float4* acc, int64_t n4, int d4, int slices, const float* factor, const float* coef, int bf16, uint2* out) {
-  pdl_launch_dependents();
-  pdl_wait();
+  pdl_begin();
   const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
   if (i >= n4) return;
   float4 s = __ldcs(acc + i);
@@ -998,7 +990,6 @@ int sp_linear_ce_grad(const void* h, const void* W, const int64_t* target, const
       if (rc == SP_OK) rc = make_map_any(&tmB, Wp, 2, cols, D, D, 64, 64);
       if (rc != SP_OK) return rc;
       ProdArgs a = ce_args(sched, st.status, T, D, cols, p.slices);
-      a.trigger_late = 1;     // dW below reads g and h only: its CTAs take the SMs that this product leaves free
       if (summed) {
         rc = make_map_3d_f32(&tmC, acc, p.slices, T, D, 32, 32);
         if (rc != SP_OK) return rc;
@@ -1022,7 +1013,7 @@ int sp_linear_ce_grad(const void* h, const void* W, const int64_t* target, const
       if (rc == SP_OK) rc = make_map_any(&tmC, (char*)dW + v0 * D * 2, 2, cols, D, D, 32, 64);
       if (rc != SP_OK) return rc;
       ProdArgs a = ce_args(sched, st.status, cols, D, T, 1);
-      a.overlap = dh != nullptr;
+      a.overlap = dh != nullptr;      // it reads g and h only: its CTAs take the SMs that dh leaves free
       const EpiOut16<false>::Args eo = {factor, nullptr, bf16};
       rc = launch_product<2, 256, kElem16, true, true, EpiOut16<false>>("gradient of W", tmA, tmB, tmC, a, bf16, eo, stream);
       if (rc != SP_OK) return rc;

@@ -149,10 +149,7 @@ __device__ __forceinline__ void quant_extreme(const T* row, int64_t c, int64_t c
 // TPR threads share a row: as few as hold it in registers (8192 x 4096 bf16: 128 threads 22.5 us, 256 27.6).
 template <class T, int TPR>
 __global__ void __launch_bounds__(kQuantThreads, sizeof(T) == 2 ? 5 : 4) quantize_kernel(const T* x, int rows, int64_t cols, int64_t kp, int8_t* q, float* scale) {
-  pdl_wait();
-  // Only now may the next kernel start: one that reads nothing of this kernel before its own wait then finds everything
-  // before this kernel complete (the few-token product fetches weights that early).
-  pdl_launch_dependents();
+  pdl_begin();      // the few-token products fetch weights while this kernel runs: everything before it is complete
   constexpr int kRows = kQuantThreads / TPR;
   const int t = threadIdx.x % TPR;
   const int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / TPR;
@@ -415,7 +412,6 @@ __global__ void __launch_bounds__(kDotThreads, 2) dot_tokens_kernel(const DotArg
   __shared__ uint32_t tops[kDotTokens];
   const int lane = threadIdx.x & 31, warp = blockIdx.x * (kDotThreads / 32) + (threadIdx.x >> 5);
   const int step = gridDim.x * (kDotThreads / 32) * 2;
-  pdl_launch_dependents();
   int4 w[2][kDotUnroll];
   auto fetch = [&](int64_t n, int k) {     // bytes [k, k + 4096) of rows n and n + 1
 #pragma unroll
@@ -427,10 +423,10 @@ __global__ void __launch_bounds__(kDotThreads, 2) dot_tokens_kernel(const DotArg
       }
   };
   Vec8<uint16_t> own[QUANT ? kDotVecs : 1];
-  if (!a.early) pdl_wait();
+  if (!a.early) pdl_begin();
   if constexpr (QUANT) dot_fetch_tokens(a, own);
   fetch(warp * 2, 0);
-  if (a.early) pdl_wait();
+  if (a.early) pdl_begin();
   if constexpr (QUANT) {
     if (threadIdx.x < kDotTokens) tops[threadIdx.x] = 0;
     __syncthreads();
@@ -518,7 +514,6 @@ few_tokens_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant
   const int n0 = (int)(blockIdx.x / nranks) * 128;
   const int k0 = (int)rank * args.kb_split, k1 = min(args.kblocks, k0 + args.kb_split);
 
-  pdl_launch_dependents();
   if (threadIdx.x == 32) { prefetch_tensormap(&tmW); prefetch_tensormap(&tmQ); }
   if (threadIdx.x == 0) {
     for (int i = 0; i < S; ++i) { mbar_init(bar_full + 8 * i, 1); mbar_init(bar_empty + 8 * i, 1); }
@@ -542,7 +537,7 @@ few_tokens_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant
     const int n_k = k1 - k0, turn = (int)(blockIdx.x / nranks) * 5 % n_k;
     auto k_at = [&](int i) { return (k0 + (i + turn < n_k ? i + turn : i + turn - n_k)) * 128; };
     const int ahead = min(S, k1 - k0);
-    if (!args.early) pdl_wait();
+    if (!args.early) pdl_begin();
     if (elect_one()) {
       for (int i = 0; i < ahead; ++i) {
         mbar_arrive_expect_tx(bar_full + 8 * i, C::kStageBytes);
@@ -550,7 +545,7 @@ few_tokens_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant
       }
     }
     __syncwarp();
-    if (args.early) pdl_wait();
+    if (args.early) pdl_begin();
     if (elect_one()) {
       for (int i = 0; i < ahead; ++i) tma_load_2d<1>(stage_addr(i) + C::kWBytes, &tmQ, k_at(i), 0, bar_full + 8 * i);
     }
@@ -578,7 +573,7 @@ few_tokens_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant
     }
     __syncwarp();
   } else if (warp == 1) {
-    pdl_wait();
+    pdl_begin();
     bool ok = true;
     for (int i = 0; i < k1 - k0; ++i) {
       const int st = i % S;
@@ -598,7 +593,7 @@ few_tokens_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant
       __syncwarp();
     }
   } else {
-    pdl_wait();
+    pdl_begin();
     const int quarter = warp & 3;
     bool ok = mbar_wait(bar_done, 0, args.status, (kProdEpilogue << 8) | 3);
     ok = __all_sync(0xffffffffu, ok);

@@ -61,10 +61,9 @@ struct ProdArgs {
   int kb_sum;            // stages whose products one accumulator takes before the epilogue adds it to its own sum (Epi::kSums; else a slice)
   int turn;              // 1: units start their walk along k at different places (one tile row: all read the same few lines of A, and
                          //    in step they would queue for them in one L2 slice: one token's scores, 131072 x 4096, 219 us in step, 191 so)
-  // A product and the next one on the stream that reads nothing of it may run side by side: the first lets its successor start only once
-  // everything before itself is complete (`trigger_late`), the second goes straight to work and waits before it ends instead
-  // (`overlap`), so that whatever follows it follows both.
-  int trigger_late, overlap;
+  // A product that reads nothing of the kernel before it may run beside it: it goes straight to work (everything before that kernel is
+  // complete, see pdl_begin) and waits before it ends instead, so that whatever follows it follows both.
+  int overlap;
   int units;             // CTAs or CTA pairs launched
   uint32_t idesc;        // instruction descriptor
   Sched sched;
@@ -106,6 +105,12 @@ __device__ __forceinline__ void prod_mma(uint32_t d, uint64_t a, uint64_t b, uin
 
 __device__ __forceinline__ void pdl_launch_dependents() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 __device__ __forceinline__ void pdl_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+// Waits for the kernel before this one, and only then lets the one behind it start.  So whatever starts early, a product with `overlap` or an sp_gemm with
+// SP_FLAG_OVERLAP, runs beside one kernel only, the one before it: everything before that is complete.
+__device__ __forceinline__ void pdl_begin() {
+  pdl_wait();
+  pdl_launch_dependents();
+}
 
 __device__ __forceinline__ uint32_t pack_16(float lo, float hi, bool bf16) {
   if (bf16) {
@@ -232,7 +237,6 @@ product_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
   const int unit = blockIdx.x / CG;
   const int T = args.sched.T, Tn = args.sched.Tn, total = T * args.splits;
 
-  if (!args.trigger_late) pdl_launch_dependents();
   if (threadIdx.x == 32) { prefetch_tensormap(&tmA); prefetch_tensormap(&tmB); }
   if (threadIdx.x == 0) {
     for (int i = 0; i < S; ++i) { mbar_init(bar_full + 8 * i, 1); mbar_init(bar_empty + 8 * i, 1); }
@@ -247,8 +251,7 @@ product_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
   unit_sync<CG>();
   tcgen05_fence_after();
   const uint32_t tmem_base = ld_shared_32(tmem_slot);
-  if (!args.overlap) pdl_wait();   // set-up may overlap the kernel before this one; global memory is touched only from here on
-  if (args.trigger_late) pdl_launch_dependents();
+  if (!args.overlap) pdl_begin();   // set-up may overlap the kernel before this one; global memory is touched only from here on
 
   auto tile_at = [&](int s, int& tm, int& tn, int& z) {
     z = s / T;
@@ -428,7 +431,7 @@ product_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
   tcgen05_fence_before();
   unit_sync<CG>();
   if (warp == 1) tmem_dealloc<CG>(tmem_base, C::kTmemCols);
-  if (args.overlap && threadIdx.x == 0) pdl_wait();
+  if (args.overlap && threadIdx.x == 0) pdl_begin();
 }
 
 // Columns of a tile of 128 * CG rows for M x N results: the width, from 256 down in steps of `step`, with the least waves x (width + 48) (the
