@@ -104,10 +104,12 @@ typedef enum {
 #define SP_FLAG_OVERLAP 16u   /* sp_gemm only.  The caller states that this launch is independent of the kernel before it on the
                                  stream: it reads nothing that kernel writes, and it may start writing C while that kernel is
                                  still running.  Every GEMM launch of this library is made with programmatic stream
-                                 serialisation and signals at its start that its successor may be scheduled; an ordinary
-                                 launch then waits, after its set-up and before it touches global memory, until the kernel
-                                 before it has completed and its writes are visible (so only launch latency and set-up
-                                 overlap, and the stream order is the usual one); a launch with this flag does not wait.  CTAs of the next GEMM then take over SMs as the CTAs of the
+                                 serialisation; an ordinary launch waits, after its set-up and before it touches global memory,
+                                 until the kernel before it has completed and its writes are visible, and signals then that its
+                                 successor may be scheduled (so only launch latency and set-up overlap, and the stream order is
+                                 the usual one); a launch with this flag does not wait and signals at its start.  In a chain of
+                                 launches with this flag each may run beside all of them and beside the ordinary launch in
+                                 front, so the statement is about all of these.  CTAs of the next GEMM then take over SMs as the CTAs of the
                                  previous one finish, which fills the partly empty last wave of back-to-back independent
                                  GEMMs.  Behind a call of several kernels (sp_linear_i8, sp_linear_ce, sp_linear_ce_grad) the
                                  statement is about the whole call; what came before that call is complete when this launch

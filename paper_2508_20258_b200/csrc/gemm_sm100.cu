@@ -161,9 +161,9 @@ gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUt
   const int T = args.sched.T, Tn = args.sched.Tn;
   const int KB = args.kblocks;
 
-  // A GEMM launched behind this one with SP_FLAG_OVERLAP may be scheduled from now on: its CTAs become resident as
-  // ours exit (shared memory admits one CTA per SM).  Without such a successor this is a no-op.
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  // A launch that does not wait for its predecessor lets its own successor do the same from the start: the CTAs of a chain of such launches become
+  // resident as the ones before exit (shared memory admits one CTA per SM).
+  if (args.overlap) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   if (threadIdx.x == 32) { prefetch_tensormap(&tmA); prefetch_tensormap(&tmB); prefetch_tensormap(&tmC); }
   if (threadIdx.x == 0) {
     for (int i = 0; i < S; ++i) { mbar_init(bar_full + 8 * i, 1); mbar_init(bar_empty + 8 * i, 1); }
@@ -216,7 +216,11 @@ gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUt
   // this one on the stream is still finishing (its CTAs leaving free the SMs ours start on).  From here on global
   // memory is touched, so an ordinary launch now waits until that kernel has completed and its writes are visible;
   // a launch declared independent of it (SP_FLAG_OVERLAP) goes straight on and waits only before it exits.
-  if (!args.overlap) asm volatile("griddepcontrol.wait;" ::: "memory");
+  // Only then does an ordinary launch let its successor start: a flagged one behind it runs beside this kernel, not beside those before it.
+  if (!args.overlap) {
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  }
 
   const int n_items = n_whole + sk_segments(args.sk, unit, KB);
   // The i-th piece of work of this unit; slot < 0 when there is none.  Called by whole warps, every role with its own

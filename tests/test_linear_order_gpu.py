@@ -50,7 +50,12 @@ def gradient(T, V=700, D=64, dh=True, dW=True):
     return lambda: sp.linear_ce_grad(h, W, t, lse, None, dh, dW, workspace=ws), [v for v in (dh, dW) if v is not None]
 
 
-CALLS = {"quantiser": quantiser, "linear 1": lambda: linear(1), "linear 1 long": lambda: linear(1, 16384), "linear 1 fp32": lambda: linear(1, dtype=torch.float32),
+def gemm():
+    a, b, y = randn(256, 64, seed=13), randn(64, 256, seed=14), torch.empty(256, 256, dtype=torch.bfloat16, device="cuda")
+    return lambda: sp.gemm(a, b, y, sp.ROW_MAJOR, sp.make_params(tile_m=128, tile_n=128)), [y]
+
+
+CALLS = {"bf16 product": gemm, "quantiser": quantiser, "linear 1": lambda: linear(1), "linear 1 long": lambda: linear(1, 16384), "linear 1 fp32": lambda: linear(1, dtype=torch.float32),
          "linear 24": lambda: linear(24), "linear 300": lambda: linear(300), "product 2": lambda: product(2), "product 20": lambda: product(20), "product 300": lambda: product(300),
          "loss 1": lambda: loss(1), "loss 20": lambda: loss(20), "loss 200": lambda: loss(200, reduction="sum"), "loss copied": lambda: loss(400, 900000, 72),
          "gradient 1": lambda: gradient(1), "gradient 20": lambda: gradient(20), "gradient dh": lambda: gradient(20, dW=False), "gradient dW": lambda: gradient(20, dh=False),
