@@ -358,7 +358,7 @@ int sp_softmax(const void* in, void* out, int64_t M, int64_t N, int32_t mode, in
  *   x     : DEVICE, M x K row-major, x_dtype SP_BF16, SP_FP32 or SP_FP16, read-only.  Any K.
  *   q     : DEVICE, M x ceil(K / 16) * 16 int8 row-major; the columns beyond K are written as zeros (they add nothing to a product).
  *   scale : DEVICE, M fp32.
- * Asynchronous on `stream`; allocates nothing.  Errors: SP_ERR_INVALID_ARG, SP_ERR_UNSUPPORTED (sizes of 2^31 and beyond),
+ * q, scale and x must not overlap (here and below that is SP_ERR_INVALID_ARG).  Asynchronous on `stream`; allocates nothing.  Errors: SP_ERR_INVALID_ARG, SP_ERR_UNSUPPORTED (sizes of 2^31 and beyond),
  * SP_ERR_ALIGNMENT (q not 16-byte aligned, x or scale not aligned to their elements), SP_ERR_DEVICE, SP_ERR_CUDA. */
 int sp_quantize_i8(const void* x, int32_t x_dtype, int64_t M, int64_t K, int8_t* q, float* scale, void* stream);
 
@@ -381,7 +381,7 @@ int sp_gemm_i8(const int8_t* A, const float* a_scale, const int8_t* B, const flo
                int scheme, const sp_params* params, void* stream);
 
 /* A linear layer on 8-bit weights in one call: x is quantised (sp_quantize_i8) into q and q_scale, which stay with the caller, and
- * y = sp_gemm_i8(q, q_scale, W, w_scale).  Same results as the two calls; with few tokens the weights are fetched while x is
+ * y = sp_gemm_i8(q, q_scale, W, w_scale).  q, q_scale and y must not overlap each other or an input.  Same results as the two calls; with few tokens the weights are fetched while x is
  * being quantised.  K is x's own number of columns; q and W have rows of ceil(K / 16) * 16.  Errors: those of the two calls. */
 int sp_linear_i8(const void* x, int32_t x_dtype, int8_t* q, float* q_scale, const int8_t* W, const float* w_scale, void* y, int64_t M, int64_t N,
                  int64_t K, int scheme, const sp_params* params, void* stream);
@@ -397,7 +397,7 @@ int sp_linear_i8(const void* x, int32_t x_dtype, int8_t* q, float* q_scale, cons
  *            not ignored (SP_REDUCE_MEAN; 0 / 0 = NaN when every token is).
  *   workspace : DEVICE, 16-byte aligned, sp_linear_ce_workspace(T, V, D, 0) bytes, the caller's, free again when the
  *            call's work on `stream` is done; calls that may overlap need one each.
- * Scores that are not finite give NaN (minus infinity: probability 0).  D must be a multiple of 8; T and V are free.  Sums are
+ * What is written (lse, loss, workspace) must not overlap anything else of the call.  Scores that are not finite give NaN (minus infinity: probability 0).  D must be a multiple of 8; T and V are free.  Sums are
  * taken in a fixed order: the same bits every time.  Asynchronous on `stream`; apart from the library's first call on a device it allocates and synchronises
  * nothing and can be captured.  Errors: SP_ERR_INVALID_ARG (NULL, sizes, reduction, workspace too small),
  * SP_ERR_UNSUPPORTED (dtype, sizes), SP_ERR_ALIGNMENT, SP_ERR_DEVICE, SP_ERR_CUDA. */
@@ -416,6 +416,7 @@ int sp_linear_ce(const void* h, const void* W, const int64_t* target, float* lse
  *   grad_loss : DEVICE, fp32, T values or one; NULL: 1.
  *   dh, dW    : DEVICE, T x D and V x D, same type as h and W, fully overwritten, or NULL: not wanted (at most one of them).
  *   workspace : DEVICE, sp_linear_ce_workspace(T, V, D, 1) bytes, as above.
+ * dh, dW and workspace must not overlap anything else of the call.
  * A token that is ignored adds exactly nothing, whatever its row of h holds, and its row of dh is zero.  A target
  * outside the vocabulary makes the gradients NaN.  Errors as sp_linear_ce. */
 int sp_linear_ce_grad(const void* h, const void* W, const int64_t* target, const float* lse, const float* grad_loss, void* dh, void* dW, int64_t T,

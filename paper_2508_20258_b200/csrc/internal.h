@@ -34,6 +34,24 @@ inline bool first_use_on_this_device(uint64_t& done_mask) {
   return true;
 }
 
+// A call's matrices and vectors in memory, for the check that nothing it writes lies in anything else of the call.
+struct Span {
+  const char* name;
+  const void* at;              // NULL: not given
+  unsigned __int128 bytes;     // sizes of 2^31 on both sides and more
+};
+// SP_ERR_INVALID_ARG if one of the first `outs` spans shares memory with any other.
+inline int refuse_overlaps(const Span* spans, int outs, int all) {
+  for (int i = 0; i < outs; ++i)
+    for (int j = i + 1; j < all; ++j) {
+      const Span &a = spans[i], &b = spans[j];
+      if (!a.at || !b.at) continue;
+      const uintptr_t pa = (uintptr_t)a.at, pb = (uintptr_t)b.at;
+      if (pa < pb ? pb - pa < a.bytes : pa - pb < b.bytes) { set_error("%s must not overlap %s", a.name, b.name); return SP_ERR_INVALID_ARG; }
+    }
+  return SP_OK;
+}
+
 // The current device, after checking (once per host thread and device) that it exists, is sm_100 and has its primary
 // context bound to this thread.  Returns an sp_status.  Allocates nothing.
 int current_device(int* dev);

@@ -874,6 +874,8 @@ static int launch_row(const RowArgs& a, int blocks, cudaStream_t stream) {
 
 using namespace sp;
 
+using Bytes = unsigned __int128;
+
 extern "C" {
 
 int64_t sp_linear_ce_workspace(int64_t T, int64_t V, int64_t D, int32_t grad) {
@@ -890,6 +892,10 @@ int sp_linear_ce(const void* h, const void* W, const int64_t* target, float* lse
   if ((uintptr_t)loss & 3u) { set_error("loss must be aligned to its elements"); return SP_ERR_ALIGNMENT; }
   const CePlan p = ce_plan(T, V, D);
   if (workspace_bytes < p.forward_bytes) { set_error("workspace of %lld bytes, %lld needed", (long long)workspace_bytes, (long long)p.forward_bytes); return SP_ERR_INVALID_ARG; }
+  const Span spans[] = {{"lse", lse, (Bytes)T * 4}, {"loss", loss, reduction == SP_REDUCE_NONE ? (Bytes)T * 4 : 4}, {"workspace", workspace, (Bytes)p.forward_bytes},
+                        {"h", h, (Bytes)T * (Bytes)D * 2}, {"W", W, (Bytes)V * (Bytes)D * 2}, {"target", target, (Bytes)T * 8}};
+  rc = refuse_overlaps(spans, 3, 6);
+  if (rc != SP_OK) return rc;
   int dev = 0;
   rc = current_device(&dev);
   if (rc != SP_OK) return rc;
@@ -934,10 +940,14 @@ int sp_linear_ce_grad(const void* h, const void* W, const int64_t* target, const
   int rc = check_ce(h, W, target, lse, T, V, D, dtype, reduction, workspace);
   if (rc != SP_OK) return rc;
   if (!dh && !dW) { set_error("dh and dW must not both be NULL"); return SP_ERR_INVALID_ARG; }
-  if (dh == h || dW == W) { set_error("a gradient must not overlap an input"); return SP_ERR_INVALID_ARG; }
   if ((((uintptr_t)dh | (uintptr_t)dW) & 15u) || ((uintptr_t)grad_loss & 3u)) { set_error("dh and dW must be 16-byte aligned, grad_loss aligned to its elements"); return SP_ERR_ALIGNMENT; }
   const CePlan p = ce_plan(T, V, D);
   if (workspace_bytes < p.grad_bytes) { set_error("workspace of %lld bytes, %lld needed", (long long)workspace_bytes, (long long)p.grad_bytes); return SP_ERR_INVALID_ARG; }
+  const Span spans[] = {{"dh", dh, (Bytes)T * (Bytes)D * 2}, {"dW", dW, (Bytes)V * (Bytes)D * 2}, {"workspace", workspace, (Bytes)p.grad_bytes},
+                        {"h", h, (Bytes)T * (Bytes)D * 2}, {"W", W, (Bytes)V * (Bytes)D * 2}, {"target", target, (Bytes)T * 8}, {"lse", lse, (Bytes)T * 4},
+                        {"grad_loss", grad_loss, reduction == SP_REDUCE_NONE ? (Bytes)T * 4 : 4}};
+  rc = refuse_overlaps(spans, 3, 8);
+  if (rc != SP_OK) return rc;
   int dev = 0;
   rc = current_device(&dev);
   if (rc != SP_OK) return rc;

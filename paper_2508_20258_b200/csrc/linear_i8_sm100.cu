@@ -727,7 +727,6 @@ constexpr int64_t kFewAlways = 64, kFewTokens = 256;
 static int check_i8(const void* A, const void* a_scale, const void* B, const void* b_scale, const void* C, int64_t M, int64_t N, int64_t K,
                     int scheme, const sp_params* params, I8Call* call) {
   if (!A || !a_scale || !B || !b_scale || !C) { set_error("A, B, C and the scales must not be NULL"); return SP_ERR_INVALID_ARG; }
-  if (C == A || C == B) { set_error("C must not overlap an input"); return SP_ERR_INVALID_ARG; }
   if (M <= 0 || N <= 0 || K <= 0) { set_error("M, N, K must be positive"); return SP_ERR_INVALID_ARG; }
   if (M >= (1ll << 31) - 512 || N >= (1ll << 31) - 512) { set_error("dimension too large"); return SP_ERR_UNSUPPORTED; }
   if (K > SP_I8_MAX_K) { set_error("K must be at most %d: a longer sum can leave 32 bits", SP_I8_MAX_K); return SP_ERR_UNSUPPORTED; }
@@ -881,10 +880,15 @@ static int run_i8(const I8Call& c, bool early, cudaStream_t stream) {
 
 using namespace sp;
 
+using Bytes = unsigned __int128;
+
 extern "C" {
 
 int sp_quantize_i8(const void* x, int32_t x_dtype, int64_t M, int64_t K, int8_t* q, float* scale, void* stream) {
   int rc = check_quantize(x, x_dtype, M, K, q, scale);
+  if (rc != SP_OK) return rc;
+  const Span spans[] = {{"q", q, (Bytes)M * (Bytes)((K + 15) / 16 * 16)}, {"scale", scale, (Bytes)M * 4}, {"x", x, (Bytes)M * (Bytes)K * elt_bytes(x_dtype)}};
+  rc = refuse_overlaps(spans, 2, 3);
   if (rc != SP_OK) return rc;
   int dev = 0;
   rc = current_device(&dev);
@@ -896,6 +900,10 @@ int sp_gemm_i8(const int8_t* A, const float* a_scale, const int8_t* B, const flo
                int scheme, const sp_params* params, void* stream) try {
   I8Call call;
   int rc = check_i8(A, a_scale, B, b_scale, C, M, N, K, scheme, params, &call);
+  if (rc != SP_OK) return rc;
+  const Span spans[] = {{"C", C, (Bytes)M * (Bytes)N * elt_bytes(call.out)}, {"A", A, (Bytes)M * (Bytes)K}, {"a_scale", a_scale, (Bytes)M * 4},
+                        {"B", B, (Bytes)N * (Bytes)K}, {"b_scale", b_scale, (Bytes)N * 4}};
+  rc = refuse_overlaps(spans, 1, 5);
   if (rc != SP_OK) return rc;
   int dev = 0;
   rc = current_device(&dev);
@@ -911,9 +919,13 @@ int sp_linear_i8(const void* x, int32_t x_dtype, int8_t* q, float* q_scale, cons
                  int64_t K, int scheme, const sp_params* params, void* stream) try {
   int rc = check_quantize(x, x_dtype, M, K, q, q_scale);
   if (rc != SP_OK) return rc;
-  if (y == x) { set_error("y must not overlap an input"); return SP_ERR_INVALID_ARG; }
   I8Call call;
-  rc = check_i8(q, q_scale, W, w_scale, y, M, N, (K + 15) / 16 * 16, scheme, params, &call);
+  const int64_t kp = (K + 15) / 16 * 16;
+  rc = check_i8(q, q_scale, W, w_scale, y, M, N, kp, scheme, params, &call);
+  if (rc != SP_OK) return rc;
+  const Span spans[] = {{"y", y, (Bytes)M * (Bytes)N * elt_bytes(call.out)}, {"q", q, (Bytes)M * (Bytes)kp}, {"q_scale", q_scale, (Bytes)M * 4},
+                        {"x", x, (Bytes)M * (Bytes)K * elt_bytes(x_dtype)}, {"W", W, (Bytes)N * (Bytes)kp}, {"w_scale", w_scale, (Bytes)N * 4}};
+  rc = refuse_overlaps(spans, 3, 6);
   if (rc != SP_OK) return rc;
   int dev = 0;
   rc = current_device(&dev);

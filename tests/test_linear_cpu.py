@@ -214,3 +214,52 @@ def test_a_workspace_is_taken_for_the_stream_it_is_used_on(monkeypatch):
         for grad in (0, 1):
             buf, n = binding._ce_workspace(None, Like(), (8, 100, 64), grad, stream)
             assert buf.numel() == n == sp.linear_ce_workspace(8, 100, 64, bool(grad)) and taken.pop() == want
+
+
+# Addresses far apart, one for each argument, and then one output moved into another argument: to its start, its last element, or so that it ends in it.
+FAR = {name: (i + 1) << 24 for i, name in enumerate("abcdefghij")}
+
+
+def _moved(call, sizes, outs):
+    """``call`` with every output moved into every other argument; ``sizes``: bytes of each argument."""
+    at = {name: FAR["abcdefghij"[i]] for i, name in enumerate(sizes)}
+    for out in outs:
+        for other in sizes:
+            if other != out:
+                first = at[other]
+                for where in (first, first + (sizes[other] - 1) // 16 * 16, first - (sizes[out] - 1) // 16 * 16):
+                    assert call(**{**at, out: where}) == sp.ERR_INVALID_ARG, (out, other, where - first)
+                    assert "overlap" in sp.last_error()
+
+
+def test_what_is_written_must_not_lie_in_anything_else_of_the_call():
+    L = sp.lib()
+    p = sp.make_params(b_layout=1)
+    M, N, K, kp = 70, 130, 300, 304
+    _moved(lambda x, q, s: L.sp_quantize_i8(x, sp.BF16, M, K, q, s, None), dict(x=M * K * 2, q=M * kp, s=M * 4), ["q", "s"])
+    _moved(lambda a, sa, b, sb, c: L.sp_gemm_i8(a, sa, b, sb, c, M, N, kp, -1, ctypes.byref(p), None), dict(a=M * kp, sa=M * 4, b=N * kp, sb=N * 4, c=M * N * 2), ["c"])
+    _moved(lambda x, q, s, w, ws, y: L.sp_linear_i8(x, sp.FP32, q, s, w, ws, y, M, N, K, -1, ctypes.byref(p), None),
+           dict(x=M * K * 4, q=M * kp, s=M * 4, w=N * kp, ws=N * 4, y=M * N * 2), ["q", "s", "y"])
+    T, V, D = 40, 500, 64
+    for red, n in ((sp.REDUCE_NONE, T), (sp.REDUCE_SUM, 1)):
+        f, g = sp.linear_ce_workspace(T, V, D), sp.linear_ce_workspace(T, V, D, True)
+        _moved(lambda h, W, t, lse, loss, ws: L.sp_linear_ce(h, W, t, lse, loss, T, V, D, sp.BF16, -100, red, ws, f, None),
+               dict(h=T * D * 2, W=V * D * 2, t=T * 8, lse=T * 4, loss=n * 4, ws=f), ["lse", "loss", "ws"])
+        _moved(lambda h, W, t, lse, grad, dh, dW, ws: L.sp_linear_ce_grad(h, W, t, lse, grad, dh, dW, T, V, D, sp.BF16, -100, red, ws, g, None),
+               dict(h=T * D * 2, W=V * D * 2, t=T * 8, lse=T * 4, grad=n * 4, dh=T * D * 2, dW=V * D * 2, ws=g), ["dh", "dW", "ws"])
+
+
+def test_arguments_side_by_side_are_accepted():
+    # one byte behind the other: the checks pass, and the call ends where it asks for a device (or runs, on a GPU: not here)
+    torch = pytest.importorskip("torch")
+    if torch.cuda.is_available():
+        pytest.skip("made-up addresses")
+    L = sp.lib()
+    M, K = 32, 64
+    assert L.sp_quantize_i8(FAR["a"], sp.BF16, M, K, FAR["a"] + M * K * 2, FAR["a"] + M * K * 3, None) not in (sp.OK, sp.ERR_INVALID_ARG)
+    T, V, D = 32, 64, 64
+    n = sp.linear_ce_workspace(T, V, D)
+    at = [FAR["a"]]
+    for size in (T * D * 2, V * D * 2, T * 8, T * 4, T * 4):
+        at.append(at[-1] + size)
+    assert L.sp_linear_ce(at[0], at[1], at[2], at[3], at[4], T, V, D, sp.BF16, -100, sp.REDUCE_NONE, at[5], n, None) not in (sp.OK, sp.ERR_INVALID_ARG)
