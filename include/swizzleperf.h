@@ -397,7 +397,8 @@ int sp_linear_i8(const void* x, int32_t x_dtype, int8_t* q, float* q_scale, cons
  *            not ignored (SP_REDUCE_MEAN; 0 / 0 = NaN when every token is).
  *   workspace : DEVICE, 16-byte aligned, sp_linear_ce_workspace(T, V, D, 0) bytes, the caller's, free again when the
  *            call's work on `stream` is done; calls that may overlap need one each.
- * What is written (lse, loss, workspace) must not overlap anything else of the call.  Scores that are not finite give NaN (minus infinity: probability 0).  D must be a multiple of 8; T and V are free.  Sums are
+ * What is written (lse, loss, workspace) must not overlap anything else of the call.  Scores that are not finite give NaN (minus infinity: probability 0).  D must be a multiple of 8; T and V are free (T * V, T * D and V * D
+ * up to about 2^39: 2^24 tiles).  Sums are
  * taken in a fixed order: the same bits every time.  Asynchronous on `stream`; apart from the library's first call on a device it allocates and synchronises
  * nothing and can be captured.  Errors: SP_ERR_INVALID_ARG (NULL, sizes, reduction, workspace too small),
  * SP_ERR_UNSUPPORTED (dtype, sizes), SP_ERR_ALIGNMENT, SP_ERR_DEVICE, SP_ERR_CUDA. */
@@ -423,7 +424,9 @@ int sp_linear_ce_grad(const void* h, const void* W, const int64_t* target, const
                       int64_t V, int64_t D, int32_t dtype, int64_t ignore_index, int32_t reduction, void* workspace, int64_t workspace_bytes,
                       void* stream);
 
-/* Bytes of workspace sp_linear_ce (grad = 0) or sp_linear_ce_grad (grad != 0) needs; -1 on sizes that those refuse.  Host only. */
+/* Bytes of workspace sp_linear_ce (grad = 0) or sp_linear_ce_grad (grad != 0) needs; -1 on sizes that those refuse.  Host only.
+ * Forward: 8 bytes for every token and 128 words, and at most one copy of h.  Gradient: 256 MiB or 2 KiB per token, whichever is more (all of T x V x 2
+ * bytes where that is less), a copy of h, and fp32 sums of dh (one copy, or up to 64 while dh has few tiles). */
 int64_t sp_linear_ce_workspace(int64_t T, int64_t V, int64_t D, int32_t grad);
 
 /* A starting configuration for sp_gemm on this hardware: tile shape, order and its parameters for a given problem.

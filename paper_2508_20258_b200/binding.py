@@ -424,7 +424,7 @@ def linear_ce_workspace(T: int, V: int, D: int, grad: bool = False) -> int:
     """Bytes of workspace linear_ce (or, with ``grad``, linear_ce_grad) needs."""
     n = int(lib().sp_linear_ce_workspace(T, V, D, int(grad)))
     if n < 0:
-        raise SpError(ERR_INVALID_ARG, "sizes must be positive and below 2^31")
+        raise SpError(ERR_INVALID_ARG, "sizes must be positive, below 2^31 each and below about 2^39 in pairs")
     return n
 
 
@@ -437,7 +437,7 @@ def _ce_workspace(workspace, like, sizes, grad: int, stream):
         return workspace, workspace.numel() * workspace.element_size()
     need = lib().sp_linear_ce_workspace(*sizes, grad)
     if need < 0:
-        raise SpError(ERR_INVALID_ARG, "sizes must be positive and below 2^31")
+        raise SpError(ERR_INVALID_ARG, "sizes must be positive, below 2^31 each and below about 2^39 in pairs")
     if stream is not None:
         handle = _stream_handle(stream)
         if handle != _stream_handle(None):

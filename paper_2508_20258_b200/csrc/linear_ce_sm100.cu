@@ -763,7 +763,8 @@ static CePlan ce_plan(int64_t T, int64_t V, int64_t D) {
   p.copy = D % 64 != 0 && T > 128 && (double)T * (double)V * (double)D > 2.5e10;
   p.off_rows = p.off_each + up256(T * 4);
   p.forward_bytes = p.off_rows + (p.copy ? up256(T * p.ld_h * 2) : 0);
-  // g of one piece takes at most 256 MiB: 27 waves of tiles on the whole device, whatever T is
+  // g of one piece takes 256 MiB, 27 waves of tiles on the whole device, or 2 KiB for each token (four tiles in width) where that is more; and the padding of
+  // its rows
   constexpr int64_t kEntries = 128ll << 20;
   p.piece = V;
   if (T * V > kEntries) {
@@ -792,11 +793,18 @@ static CePlan ce_plan(int64_t T, int64_t V, int64_t D) {
   return p;
 }
 
+// Sizes that every grid of tiles of the two calls can hold (kMaxTiles of at least 128 x 160), and below 2^31 each: asked before anything is launched.
+static bool ce_sizes(int64_t T, int64_t V, int64_t D) {
+  if (T <= 0 || V <= 0 || D <= 0 || T >= (1ll << 31) - 512 || V >= (1ll << 31) - 512 || D >= (1ll << 31) - 512) return false;
+  const int64_t rows = div_up(T, ce_rows(T)), width = tile_width(T, V, ce_rows(T) / 128, 32);
+  return rows * div_up(V, width) <= kMaxTiles && rows * div_up(D, 256) <= kMaxTiles && div_up(V, 256) * div_up(D, 256) <= kMaxTiles;
+}
+
 static int check_ce(const void* h, const void* W, const void* target, const void* lse, int64_t T, int64_t V, int64_t D, int32_t dtype, int32_t reduction,
                     const void* workspace) {
   if (!h || !W || !target || !lse || !workspace) { set_error("h, W, target, lse and workspace must not be NULL"); return SP_ERR_INVALID_ARG; }
   if (T <= 0 || V <= 0 || D <= 0) { set_error("T, V, D must be positive"); return SP_ERR_INVALID_ARG; }
-  if (T >= (1ll << 31) - 512 || V >= (1ll << 31) - 512 || D >= (1ll << 31) - 512) { set_error("dimension too large"); return SP_ERR_UNSUPPORTED; }
+  if (!ce_sizes(T, V, D)) { set_error("sizes too large"); return SP_ERR_UNSUPPORTED; }
   if (dtype != SP_BF16 && dtype != SP_FP16) { set_error("h and W must both be bf16 or both fp16"); return SP_ERR_UNSUPPORTED; }
   if (reduction != SP_REDUCE_NONE && reduction != SP_REDUCE_MEAN && reduction != SP_REDUCE_SUM) { set_error("unknown reduction %d", reduction); return SP_ERR_INVALID_ARG; }
   if ((D % 8) != 0) { set_error("D must be a multiple of 8 (16-byte row pitch)"); return SP_ERR_ALIGNMENT; }
@@ -879,7 +887,7 @@ using Bytes = unsigned __int128;
 extern "C" {
 
 int64_t sp_linear_ce_workspace(int64_t T, int64_t V, int64_t D, int32_t grad) {
-  if (T <= 0 || V <= 0 || D <= 0 || T >= (1ll << 31) - 512 || V >= (1ll << 31) - 512 || D >= (1ll << 31) - 512) return -1;
+  if (!ce_sizes(T, V, D)) return -1;
   const CePlan p = ce_plan(T, V, D);
   return grad ? p.grad_bytes : p.forward_bytes;
 }

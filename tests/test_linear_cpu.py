@@ -263,3 +263,14 @@ def test_arguments_side_by_side_are_accepted():
     for size in (T * D * 2, V * D * 2, T * 8, T * 4, T * 4):
         at.append(at[-1] + size)
     assert L.sp_linear_ce(at[0], at[1], at[2], at[3], at[4], T, V, D, sp.BF16, -100, sp.REDUCE_NONE, at[5], n, None) not in (sp.OK, sp.ERR_INVALID_ARG)
+
+
+@pytest.mark.parametrize("f", [_ce, _ce_grad])
+def test_sizes_that_no_grid_of_tiles_holds_are_refused_before_anything_is_launched(f):
+    L = sp.lib()
+    for T, V, D in [(1 << 24, 1 << 18, 64), (1 << 30, 1, 1 << 20), (1, 1 << 30, 1 << 20), ((1 << 31) - 1024, (1 << 31) - 1024, 8), ((1 << 31) - 1024, 8, (1 << 31) - 1024)]:
+        assert f(T=T, V=V, D=D, n=(1 << 62)) == sp.ERR_UNSUPPORTED
+        assert L.sp_linear_ce_workspace(T, V, D, 0) == L.sp_linear_ce_workspace(T, V, D, 1) == -1
+    for T, V, D in [(1 << 22, 1 << 16, 64), (1 << 20, 1 << 18, 1 << 12), (8, 1 << 24, 1 << 14)]:
+        for grad in (0, 1):
+            assert 0 < L.sp_linear_ce_workspace(T, V, D, grad) < 1 << 46
