@@ -171,7 +171,7 @@ def _pp(params: Optional[SpParams]):
 def _stream_handle(stream) -> int:
     if stream is None:
         import torch
-        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())   # the current stream's handle, without building a Stream
+        return int(torch.cuda.current_stream().cuda_stream)
     if isinstance(stream, int):
         return stream
     return int(stream.cuda_stream)
@@ -357,10 +357,12 @@ def _device_tensors(*tensors) -> int:
 
 
 def _stream_on(here: int, stream) -> int:
-    """_stream_handle for a caller that knows the current device."""
+    """_stream_handle for a caller that knows the current device, without building a Stream where torch can say the handle alone."""
     if stream is None:
         import torch
-        return torch._C._cuda_getCurrentRawStream(here)
+        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)      # not part of torch's public interface
+        if raw is not None:
+            return raw(here)
     return _stream_handle(stream)
 
 

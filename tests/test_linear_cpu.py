@@ -274,3 +274,21 @@ def test_sizes_that_no_grid_of_tiles_holds_are_refused_before_anything_is_launch
     for T, V, D in [(1 << 22, 1 << 16, 64), (1 << 20, 1 << 18, 1 << 12), (8, 1 << 24, 1 << 14)]:
         for grad in (0, 1):
             assert 0 < L.sp_linear_ce_workspace(T, V, D, grad) < 1 << 46
+
+
+def test_the_current_stream_is_found_by_torchs_public_interface(monkeypatch):
+    torch = pytest.importorskip("torch")
+
+    class Stream:
+        cuda_stream = 11
+
+    def private(device):
+        return 12
+
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda *a: Stream())
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", private, raising=False)
+    assert binding._stream_handle(None) == 11 and binding._stream_on(0, None) == 12
+    monkeypatch.delattr(torch._C, "_cuda_getCurrentRawStream")
+    assert binding._stream_handle(None) == binding._stream_on(0, None) == 11
+    assert binding._stream_on(0, 7) == 7 and binding._stream_on(0, Stream()) == 11
