@@ -224,3 +224,47 @@ def test_a_workspace_on_another_stream_is_not_memory_still_in_use():
         torch.cuda.synchronize()
         assert sp.get_status() == 0
         assert all(torch.equal(a, b) for a, b in zip(want, got))
+
+
+# Many pieces of the vocabulary, few rows and many slices, both; the sizes of test_linear_ce_gpu's test of pieces, whose bound is so wide at a D of 1000
+# that it holds without the softmax's part of dh.  Sums: V / 16 + V / 512 additions, fewer than V / 8.
+@pytest.mark.parametrize("T,V,D,dtype", [(600, 45001, 1000, "bf16"), (600, 45001, 1000, "fp16"), (40000, 120001, 16, "bf16"), (3, 300001, 64, "fp16"),
+                                         (16384, 50000, 264, "bf16"), (2048, 200000, 16, "fp16")])
+def test_every_part_of_the_sums_in_pieces_and_slices_is_there(T, V, D, dtype):
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    h = torch.randn(T, D, device="cuda", generator=gen).to(BITS[dtype])
+    W = (torch.randn(V, D, device="cuda", generator=gen) * (2 / D ** 0.5)).to(BITS[dtype])
+    t = torch.randint(0, V, (T,), device="cuda", generator=gen)
+    t[T // 2] = -100
+    c = torch.rand(T, device="cuda", generator=gen) + 0.5
+    e, tiny = float(torch.finfo(BITS[dtype]).eps) / 2, 2.0 ** -25 if dtype == "fp16" else 0.0
+    lse, loss = torch.empty(T, device="cuda"), torch.empty(T, device="cuda")
+    sp.linear_ce(h, W, t, lse, loss, reduction="none")
+    dh, dW = torch.full_like(h, float("nan")), torch.full_like(W, float("nan"))
+    sp.linear_ce_grad(h, W, t, lse, c, dh, dW, reduction="none")
+    assert sp.get_status() == 0
+    kept, Wd, cut = t != -100, W.double(), V - V // 8
+    rW, sW, own = (torch.zeros(V, D, dtype=torch.float64, device="cuda") for _ in range(3))
+    seen = [0, 0]
+    for i in range(0, T, 512):
+        part = slice(i, i + 512)
+        hd, kp = h[part].double(), kept[part]
+        want, want_lse, rest, g, size, zmax, _ = reference(h[part], W, t[part], c[part].double())
+        q = slack(size, zmax, D)
+        assert ((loss[part].double() - want).abs() <= q * (1 - (-want).exp()) + 2 * U * want).all() and ((lse[part].double() - want_lse).abs() <= q + want_lse.abs() * U).all()
+        dg = (e + q + 2.0 ** -13)[:, None] * g.abs() + torch.where(kp, c.max() * tiny / 2.0 ** 14, 0.0)[:, None]
+        rh = g @ Wd
+        tol = dg @ Wd.abs() + (V + 2) * U / 8 * (g.abs() @ Wd.abs()) + (e + 2 * U) * rh.abs() + tiny
+        assert near(dh[part], rh, tol)
+        at = torch.where(kp, t[part], 0)[:, None]
+        mine = g.gather(1, at)                                  # the own words' entries
+        p = g.scatter(1, at, 0.0)
+        # the bound sees a dh without the softmax's part, and one without the last eighth of it
+        for k, gone in enumerate((p @ Wd, p[:, cut:] @ Wd[cut:])):
+            seen[k] += int(((gone.abs() > 2 * tol).any(1) & kp).sum())
+        rW += g.t() @ hd
+        sW += dg.t() @ hd.abs() + (T + 2) * U / 8 * (g.abs().t() @ hd.abs())
+        own.index_add_(0, at[:, 0], mine * hd * kp[:, None])
+    assert near(dW, rW, sW + (e + 2 * U) * rW.abs() + tiny)
+    assert seen[0] > 0.9 * T - 1 and seen[1] > 0.5 * T - 1
+    assert float(((rW - own).abs() > 2 * (sW + (e + 2 * U) * rW.abs() + tiny)).double().mean()) > 0.1
