@@ -69,6 +69,7 @@ constexpr int kCeSum = 8;      // stages of 64 products per accumulator
 struct EpiStats {
   static constexpr uint32_t kBytes = 0;
   static constexpr bool kSums = true;
+  static constexpr bool kLive = false;
   struct Args {
     float2* stats;            // [part of the columns][row]
     float* picked;            // score of the row's target
@@ -455,7 +456,8 @@ __device__ __forceinline__ float ce_probabilities(uint32_t (&v)[COLS], float lse
 }
 
 // While the vocabulary is one piece, the gradient's own tiles add the sums up and this kernel puts them into g, before anything reads g.  (Tokens whose
-// p is at most 1/2 keep p - 1, which does not cancel there.)  Sums and launch cost 2 to 3 us in a short step (60 x 5000 x 304: 39 to 40), 3 % at 777 x 20011 x 1032.
+// p is at most 1/2 keep p - 1, which does not cancel there.)  Sums and launch cost 2 us in a short step (1 x 2000 x 512 from
+// a graph: 26.7 to 28.6), 3 % at 777 x 20011 x 1032.
 struct CeOwn {
   const int64_t* target;
   const float* lse;
@@ -539,6 +541,7 @@ __global__ void __launch_bounds__(256) ce_sure_kernel(const CeSure a) {
 struct EpiRest {
   static constexpr uint32_t kBytes = 0;
   static constexpr bool kSums = true;
+  static constexpr bool kLive = true;
   struct Args {
     const float* lse;
     const int64_t* target;
@@ -581,6 +584,7 @@ __device__ __forceinline__ void store_part(const EpiStage& stage, const CUtensor
 struct EpiG {
   static constexpr uint32_t kBytes = 8 * 4096;
   static constexpr bool kSums = true;       // the scores as the forward product made them: a sum that is cut off all along D is too small, and with it every p
+  static constexpr bool kLive = false;
   struct Args {
     const float* lse;
     const float* coef;
@@ -648,6 +652,7 @@ struct EpiG {
 struct EpiSum {
   static constexpr uint32_t kBytes = 8 * 4096;
   static constexpr bool kSums = true;
+  static constexpr bool kLive = false;
   struct Args { int add; };
   const Args& a;
   const CUtensorMap* map;
@@ -680,6 +685,7 @@ template <bool TOKENS>
 struct EpiOut16 {
   static constexpr uint32_t kBytes = 8 * 4096;
   static constexpr bool kSums = true;
+  static constexpr bool kLive = false;
   struct Args {
     const float* factor;
     const float* coef;       // of the tokens

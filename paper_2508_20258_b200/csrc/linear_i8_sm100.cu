@@ -229,6 +229,7 @@ template <bool OUT_F32, bool PLAIN>
 struct EpiI8 {
   static constexpr uint32_t kBytes = 8 * 4096 + (PLAIN ? 8 * 512 : 0);   // staging, then what rows without bulk stores carry from slice to slice
   static constexpr bool kSums = false;
+  static constexpr bool kLive = false;
   struct Args {
     const float* a_scale;
     const float* b_scale;

@@ -52,7 +52,7 @@ struct ProdCfg {
 
 struct ProdArgs {
   const int32_t* perm;   // tile table (orders that are not arithmetic), else nullptr
-  const int32_t* live;   // on the device: rows of A that are there, if that is known there only (tiles beyond them are passed over), else nullptr
+  const int32_t* live;   // Epi::kLive: on the device, rows of A that are there (an order in bands of tile rows, one slice)
   int32_t* status;
   int M, N;              // rows of A, rows of B
   int bn;                // columns of a tile: BN, or less where that fills the last wave better (a multiple of 32; B k-major)
@@ -235,7 +235,7 @@ product_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t rank = CG == 1 ? 0u : cluster_ctarank();
   const int unit = blockIdx.x / CG;
-  const int T = args.sched.T, Tn = args.sched.Tn, total = T * args.splits;
+  const int T = args.sched.T, Tn = args.sched.Tn;
 
   if (threadIdx.x == 32) { prefetch_tensormap(&tmA); prefetch_tensormap(&tmB); }
   if (threadIdx.x == 0) {
@@ -259,8 +259,14 @@ product_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
     const int t = args.sched.use_table ? __ldg(args.perm + o) : slot_to_tile(args.sched, o);
     tm = t / Tn; tn = t - tm * Tn;
   };
-  const int live = args.live ? *args.live : args.M;
-  auto passed_over = [&](int tm) { return tm * 128 * CG >= live; };
+  // Rows that are known on the device only: tiles beyond them are passed over, and bands beyond them, whose slots are the last, not walked at all.
+  int live = 0, total = T * args.splits;
+  if constexpr (Epi::kLive) {
+    live = *args.live;
+    const int64_t band = 128 * CG * args.sched.group;
+    total = (int)min((int64_t)T, (live + band - 1) / band * args.sched.group * Tn);
+  }
+  auto passed_over = [&](int tm) { return Epi::kLive && tm * 128 * CG >= live; };
   auto stages_of = [&](int z) { return (args.kblocks - z + args.splits - 1) / args.splits; };
 
   if (warp < C::kEpi0) {
