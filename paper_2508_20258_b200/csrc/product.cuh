@@ -157,7 +157,7 @@ __device__ __forceinline__ uint32_t ld_shared_32(uint32_t addr) {
 // The slices of a part come from left to right.  Each row is cut where its own addresses are multiples of 16: a window takes its first
 // bytes from the slice before (its last 16 bytes are carried over) and the rest from this one, so that all but a part's two edges is
 // written 16 bytes at a time, four rows per instruction.  (One element per lane, a row per instruction: 2001 x 4999 fp32 results of a
-// 2048-long product 50 us, this way 31; rows of 5000, by bulk stores, 23.)  `len`: bytes of this slice inside the matrix.
+// 2048-long product 50 us, this way 28.6; rows of 5000, by bulk stores, 23.5.)  `len`: bytes of this slice inside the matrix.
 template <int ELT>
 __device__ __forceinline__ void store_slice_plain(uint32_t carry, uint32_t slice, int lane, char* out, int64_t ld_bytes, int row0, int col, int M, int len,
                                                   bool first, bool last) {
@@ -442,7 +442,7 @@ product_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
 
 // Columns of a tile of 128 * CG rows for M x N results: the width, from 256 down in steps of `step`, with the least waves x (width + 48) (the
 // tensor cores' time goes with the width, the operands' way through L2 with 256 + width), while 256 would make up to three waves.  8-bit
-// 1000 x 3000 x 4000: 13.3 us at 192 columns, 15.4 at 256; 2001 x 4999 x 2048: 28.8 and 30.9.  Beyond three waves the power limit decides, not
+// 1000 x 3000 x 4000: 13.4 us at 192 columns, 16.2 at 256; 2001 x 4999 x 2048: 25.8 and 28.6.  Beyond three waves the power limit decides, not
 // the last wave (4096^3: 54.7 and 52.6), and with one tile row the reading of B does (16 tokens x 65536 x 4096: 101 and 97).
 inline int tile_width(int64_t M, int64_t N, int cg, int step) {
   const int64_t units = 148 / cg, rows = (M + 128 * cg - 1) / (128 * cg);
