@@ -268,3 +268,55 @@ def test_every_part_of_the_sums_in_pieces_and_slices_is_there(T, V, D, dtype):
     assert near(dW, rW, sW + (e + 2 * U) * rW.abs() + tiny)
     assert seen[0] > 0.9 * T - 1 and seen[1] > 0.5 * T - 1
     assert float(((rW - own).abs() > 2 * (sW + (e + 2 * U) * rW.abs() + tiny)).double().mean()) > 0.1
+
+
+def test_many_more_tokens_than_a_piece_holds_words():
+    h, W, t = confident(300000, 1500, 64, "bf16", shift=0.0, sure=0.0)      # pieces of 1024 words
+    t[7::11] = -100
+    h[::5] = 8 * W[t[::5].clamp_min(0)]                                      # some sure, not all to the same degree
+    check_gradients(h, W, t, "none", "bf16", 1.0)
+
+
+@pytest.mark.parametrize("T,V,D", [(60, 1001, 512), (2048, 70001, 256)])
+def test_captured_once_and_replayed_on_tokens_as_sure_as_they_come(T, V, D):
+    h, W, t = confident(T, V, D, "bf16", sure=0.0)
+    lse, loss, dh, dW = torch.empty(T, device="cuda"), torch.empty(1, device="cuda"), torch.empty_like(h), torch.empty_like(W)
+    grad = torch.full((1,), -0.75, device="cuda")
+    spaces = [torch.empty(16 + sp.linear_ce_workspace(T, V, D, g), dtype=torch.uint8, device="cuda")[16:] for g in (False, True)]      # 16-byte aligned, no more
+
+    def step(lse, loss, dh, dW):
+        sp.linear_ce(h, W, t, lse, loss, workspace=spaces[0])
+        sp.linear_ce_grad(h, W, t, lse, grad, dh, dW, workspace=spaces[1])
+
+    step(lse, loss, dh, dW)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(lse, loss, dh, dW)
+    for seed, sure in enumerate((0.5, 1.0, 0.0, 0.02)):
+        h2, W2, t2 = confident(T, V, D, "bf16", seed=seed + 5, sure=sure)
+        h.copy_(h2), W.copy_(W2), t.copy_(t2)
+        for v in (lse, loss, dh, dW):
+            v.fill_(float("nan"))
+        for s in spaces:
+            s.fill_(255)
+        graph.replay()
+        got = [v.clone() for v in (lse, loss, dh, dW)]
+        step(lse, loss, dh, dW)
+        assert sp.get_status() == 0
+        assert all(torch.equal(a, b) for a, b in zip(got, (lse, loss, dh, dW)))
+        kept = t != -100
+        c = torch.full((T,), -0.75, dtype=torch.float64, device="cuda") / kept.sum()
+        _, _, _, g, size, zmax, _ = reference(h, W, t, c)
+        e = 2.0 ** -8
+        dg = (e + slack(size, zmax, D) + 2.0 ** -13)[:, None] * g.abs()
+        rh = g @ W.double()
+        assert near(dh, rh, dg @ W.double().abs() + (V + 2) * U * (g.abs() @ W.double().abs()) + (e + 2 * U) * rh.abs())
+
+
+@pytest.mark.parametrize("T", [1, 5, 300])
+def test_a_vocabulary_of_one_word_leaves_nothing_to_learn(T):
+    h, W, t = torch.randn(T, 64, device="cuda").bfloat16() * 4, torch.randn(1, 64, device="cuda").bfloat16(), torch.zeros(T, dtype=torch.int64, device="cuda")
+    lse, loss, dh, dW = torch.empty(T, device="cuda"), torch.empty(T, device="cuda"), torch.empty_like(h), torch.empty_like(W)
+    sp.linear_ce(h, W, t, lse, loss, reduction="none")
+    sp.linear_ce_grad(h, W, t, lse, None, dh, dW, reduction="none")
+    assert (loss == 0).all() and (dh == 0).all() and (dW == 0).all()
