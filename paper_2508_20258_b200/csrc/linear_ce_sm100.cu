@@ -4,9 +4,10 @@
 //   g_tv = c_t (exp(z_tv - lse_t) - [v = target(t)]),     dh = g . W,   dW = g^T . h
 //
 // Forward: the product runs tile by tile on the tensor cores; the epilogue reduces 128 columns of a row to a
-// (maximum, sum of exponentials) pair, so T x V scores become about T x V / 128 pairs, which a second kernel joins.
+// (maximum, sum of exponentials) pair, the row's target left out, so T x V scores become about T x V / 128 pairs, which a second kernel joins.
 // Gradient: the vocabulary is walked in pieces.  A piece's scores are made again, turned into g in the epilogue and written as 16 bits;
-// two more products read them: dh += g . W_piece (k = the vocabulary) and dW_piece = g^T . h (k = the tokens).
+// two more products read them: dh += g . W_piece (k = the vocabulary) and dW_piece = g^T . h (k = the tokens).  Where a token is nearly
+// certain of its word, its own entry is made from the others' (see kRestStep).
 #include <math_constants.h>
 
 #include <mutex>
