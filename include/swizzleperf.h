@@ -429,6 +429,33 @@ int sp_linear_ce_grad(const void* h, const void* W, const int64_t* target, const
  * bytes where that is less), a copy of h, and fp32 sums of dh (one copy, or up to 64 while dh has few tiles). */
 int64_t sp_linear_ce_workspace(int64_t T, int64_t V, int64_t D, int32_t grad);
 
+/* Layer norm of the rows of x:  y[m][n] = (x[m][n] - mean[m]) * rstd[m] * gamma[n] + beta[n],  mean[m] = sum_n x[m][n] / N,
+ * rstd[m] = 1 / sqrt(sum_n (x[m][n] - mean[m])^2 / N + eps), in fp32, y rounded once.
+ *   x, y        : DEVICE, M x N row-major, SP_BF16, SP_FP16 or SP_FP32 (`dtype`).  Any addresses and N that hold whole elements; rows of whole
+ *                 16-byte units at 16-byte addresses are the faster ones.
+ *   gamma, beta : DEVICE, N, `w_dtype`: `dtype` or SP_FP32; NULL: ones, zeros.
+ *   mean, rstd  : DEVICE, M fp32 (the gradient call reads them), or NULL: not wanted.
+ * y, mean and rstd must not overlap anything else of the call.  N up to SP_LAYERNORM_MAX_N, M below 2^31.  A row that holds an infinity or a NaN becomes NaN; so does, with eps = 0, a row of
+ * equal values.  Sums are taken in a fixed order: the same bits every time.  Asynchronous on `stream`; allocates and synchronises nothing and can be captured.
+ * Errors: SP_ERR_INVALID_ARG (NULL, sizes, eps negative or not finite, overlap), SP_ERR_UNSUPPORTED (types, sizes), SP_ERR_ALIGNMENT (pointers not aligned to
+ * their elements), SP_ERR_DEVICE, SP_ERR_CUDA. */
+#define SP_LAYERNORM_MAX_N 32768
+int sp_layernorm(const void* x, const void* gamma, const void* beta, void* y, float* mean, float* rstd, int64_t M, int64_t N, int32_t dtype, int32_t w_dtype,
+                 float eps, void* stream);
+
+/* Its gradients, with xh = (x - mean) * rstd and u = dy * gamma:  dx = rstd * (u - sum_n u / N - xh * sum_n (u * xh) / N),  dgamma = sum_m dy * xh,
+ * dbeta = sum_m dy, in fp32, each rounded once.
+ *   dy, dx        : DEVICE, M x N like x.   mean, rstd : DEVICE, M fp32, as sp_layernorm left them.
+ *   dgamma, dbeta : DEVICE, N, `w_dtype`.   Of dx, dgamma, dbeta at most two may be NULL: not wanted.
+ *   workspace     : DEVICE, 16-byte aligned, sp_layernorm_workspace(M, N) bytes, the caller's, free again when the call's work on `stream` is done; calls that
+ *                   may overlap need one each.  Not used (may be NULL) when only dx is wanted.
+ * What is written (dx, dgamma, dbeta, workspace) must not overlap anything else of the call.  Otherwise as sp_layernorm. */
+int sp_layernorm_grad(const void* dy, const void* x, const void* gamma, const float* mean, const float* rstd, void* dx, void* dgamma, void* dbeta, int64_t M,
+                      int64_t N, int32_t dtype, int32_t w_dtype, void* workspace, int64_t workspace_bytes, void* stream);
+
+/* Bytes of workspace sp_layernorm_grad needs for dgamma and dbeta (at most 296 rows of 2 N fp32); -1 on sizes that it refuses.  Host only. */
+int64_t sp_layernorm_workspace(int64_t M, int64_t N);
+
 /* A starting configuration for sp_gemm on this hardware: tile shape, order and its parameters for a given problem.
  * The paper arrives at a remap by searching with measurements in the loop; this is the short table that this
  * library's own sweeps on B200 distil to (no counterpart in the paper, and no substitute for measuring: the search

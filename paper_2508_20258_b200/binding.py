@@ -59,6 +59,7 @@ TRACE_DTYPE = np.dtype([("slot", "<i4"), ("tile", "<i4"), ("smid", "<i4"), ("uni
 
 EXPORTS = ["sp_tile_count", "sp_tile_map", "sp_tile_map_device", "sp_gemm", "sp_gemm_trace", "sp_gemm_host",
            "sp_gemm_noalloc", "sp_quantize_i8", "sp_gemm_i8", "sp_linear_i8", "sp_linear_ce", "sp_linear_ce_grad", "sp_linear_ce_workspace",
+           "sp_layernorm", "sp_layernorm_grad", "sp_layernorm_workspace",
            "sp_transpose", "sp_stencil2d", "sp_softmax", "sp_gemm_units", "sp_streamk_plan", "sp_recommend",
            "sp_probe_dispatch", "sp_probe_topology", "sp_probe_l2_capacity", "sp_selftest_timeout", "sp_selftest_pinned_tickets", "sp_get_status", "sp_last_error", "sp_shutdown"]
 
@@ -113,6 +114,12 @@ def lib() -> ctypes.CDLL:
         L.sp_linear_ce_grad.argtypes = [vp, vp, vp, vp, vp, vp, vp, i64, i64, i64, i32, i64, i32, vp, i64, vp]
         L.sp_linear_ce_workspace.restype = i64
         L.sp_linear_ce_workspace.argtypes = [i64, i64, i64, i32]
+        L.sp_layernorm.restype = ctypes.c_int
+        L.sp_layernorm.argtypes = [vp, vp, vp, vp, vp, vp, i64, i64, i32, i32, ctypes.c_float, vp]
+        L.sp_layernorm_grad.restype = ctypes.c_int
+        L.sp_layernorm_grad.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, i64, i64, i32, i32, vp, i64, vp]
+        L.sp_layernorm_workspace.restype = i64
+        L.sp_layernorm_workspace.argtypes = [i64, i64]
         L.sp_gemm_units.restype = ctypes.c_int
         L.sp_gemm_units.argtypes = [i32, i32, i64]
         L.sp_recommend.restype = ctypes.c_int
@@ -431,15 +438,20 @@ def linear_ce_workspace(T: int, V: int, D: int, grad: bool = False) -> int:
 
 
 def _ce_workspace(workspace, like, sizes, grad: int, stream):
-    """The caller's workspace, or one of torch's allocator's, taken for the stream it is used on: memory of another stream's may still be at
+    """The caller's workspace, or one for the sizes of linear_ce."""
+    need = 0 if workspace is not None else lib().sp_linear_ce_workspace(*sizes, grad)
+    if need < 0:
+        raise SpError(ERR_INVALID_ARG, "sizes must be positive, below 2^31 each and below about 2^39 in pairs")
+    return _workspace(workspace, like, need, stream)
+
+
+def _workspace(workspace, like, need: int, stream):
+    """(workspace, bytes): the caller's, or one of torch's allocator's, taken for the stream it is used on: memory of another stream's may still be at
     work in that stream's kernels, which the call would not wait for."""
     import torch
     if workspace is not None:
         _device_tensors(workspace)
         return workspace, workspace.numel() * workspace.element_size()
-    need = lib().sp_linear_ce_workspace(*sizes, grad)
-    if need < 0:
-        raise SpError(ERR_INVALID_ARG, "sizes must be positive, below 2^31 each and below about 2^39 in pairs")
     if stream is not None:
         handle = _stream_handle(stream)
         if handle != _stream_handle(None):
@@ -490,6 +502,68 @@ def linear_ce_grad(h, W, target, lse, grad_loss, dh, dW, reduction: str = "mean"
     _check(lib().sp_linear_ce_grad(h.data_ptr(), W.data_ptr(), target.data_ptr(), lse.data_ptr(), None if grad_loss is None else grad_loss.data_ptr(),
                                    None if dh is None else dh.data_ptr(), None if dW is None else dW.data_ptr(), T, V, D, code, ignore_index,
                                    _REDUCE[reduction], ws.data_ptr(), n, _stream_on(here, stream)))
+
+
+LAYERNORM_MAX_N = 32768
+
+
+def layernorm(x, gamma, beta, y, mean=None, rstd=None, eps: float = 1e-5, stream=None) -> None:
+    """y [M, N] = (x - mean) * rstd * gamma + beta over the rows of x (bf16, fp16 or fp32; asynchronous).  gamma, beta: [N] in x's type or
+    fp32, both alike; None: ones, zeros.  mean, rstd: [M] fp32, filled where given (kept for layernorm_grad)."""
+    M, N = x.shape
+    _expect("shape and type of y", (y.shape, y.dtype), (x.shape, x.dtype))
+    w, tensors = _ln_weights(x, (gamma, beta), N)
+    tensors += [x, y] + _ln_stats(M, (mean, rstd))
+    code = _dtype_code(x, (BF16, FP32, FP16))
+    here = _device_tensors(*tensors)
+    _check(lib().sp_layernorm(x.data_ptr(), _ptr(gamma), _ptr(beta), y.data_ptr(), _ptr(mean), _ptr(rstd), M, N, code, code if w is None else _dtype_code(w, (code, FP32)),
+                              eps, _stream_on(here, stream)))
+
+
+def layernorm_workspace(M: int, N: int) -> int:
+    """Bytes of workspace layernorm_grad needs for dgamma and dbeta."""
+    n = int(lib().sp_layernorm_workspace(M, N))
+    if n < 0:
+        raise SpError(ERR_INVALID_ARG, f"M must be positive and below 2^31, N positive and at most {LAYERNORM_MAX_N}")
+    return n
+
+
+def layernorm_grad(dy, x, gamma, mean, rstd, dx, dgamma, dbeta, workspace=None, stream=None) -> None:
+    """Gradients of layernorm for the gradient ``dy`` of y: dx [M, N], dgamma and dbeta [N] (any two of them may be None; asynchronous).  ``mean``
+    and ``rstd`` as layernorm left them; ``workspace``: layernorm_workspace(M, N) bytes, allocated here when not given."""
+    M, N = x.shape
+    _expect("shape and type of dy", (dy.shape, dy.dtype), (x.shape, x.dtype))
+    if dx is not None:
+        _expect("shape and type of dx", (dx.shape, dx.dtype), (x.shape, x.dtype))
+    w, tensors = _ln_weights(x, (gamma, dgamma, dbeta), N)
+    tensors += [x, dy] + _ln_stats(M, (mean, rstd)) + ([dx] if dx is not None else [])
+    code = _dtype_code(x, (BF16, FP32, FP16))
+    here = _device_tensors(*tensors)
+    ws, n = None, 0
+    if dgamma is not None or dbeta is not None:
+        ws, n = _workspace(workspace, x, 0 if workspace is not None else layernorm_workspace(M, N), stream)
+    _check(lib().sp_layernorm_grad(dy.data_ptr(), x.data_ptr(), _ptr(gamma), _ptr(mean), _ptr(rstd), _ptr(dx), _ptr(dgamma), _ptr(dbeta), M, N, code,
+                                   code if w is None else _dtype_code(w, (code, FP32)), _ptr(ws), n, _stream_on(here, stream)))
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
+def _ln_weights(x, weights, N: int):
+    """(one of the vectors that are given or None, all that are given): [N] each, of one type."""
+    given = [w for w in weights if w is not None]
+    for w in given:
+        _expect("shape and type of a weight or its gradient", (w.shape, w.dtype), ((N,), given[0].dtype))
+    return (given[0] if given else None), given
+
+
+def _ln_stats(M: int, stats):
+    import torch
+    given = [s for s in stats if s is not None]
+    for s in given:
+        _expect("shape and type of mean, rstd", (s.shape, s.dtype), ((M,), torch.float32))
+    return given
 
 
 def gemm_units(tile_m: int, tile_n: int, T: int) -> int:
