@@ -4,9 +4,10 @@
 //   xh = (x - mean) rstd,   u = dy gamma,   dx = rstd (u - sum u / N - xh sum (u xh) / N),   dgamma = sum over rows of dy xh,   dbeta = of dy
 //
 // Both are bound by HBM: x is read and y written, or x and dy read and dx written, each once.  A row is held in registers from its one read to its
-// one write, 16 elements per thread, by 1, 2, 4 or 8 warps, beyond 4096 elements by the CTAs of a cluster, which exchange their sums through
-// distributed shared memory.  Each group of warps walks its own rows with the next four on their way through shared memory.
-// Sums are 32-bit and taken in a fixed order: the same bits every time.
+// one write, 32 or (backward, beside the columns' sums) 16 elements per thread, by 1 to 16 warps, beyond a block's width by the CTAs of a cluster, which exchange
+// their sums through distributed shared memory.  Each group of warps walks its own rows with the next ones on their way through shared memory.
+// The issue slots are what comes next (23 bytes a clock and SM leave 8 instructions for an element of 16 bits, read and written), so all arithmetic is on
+// pairs.  Sums are 32-bit and taken in a fixed order: the same bits every time.
 #include <float.h>
 
 #include <mutex>
@@ -15,12 +16,19 @@
 
 namespace sp {
 
-constexpr int kLnThreads = 256, kLnPer = 16;      // threads of a block, elements per thread
-constexpr int kLnDepth = 4;                       // rows on their way per group of warps
-constexpr int kLnSlice = kLnThreads * kLnPer;     // columns of a CTA, at most
-constexpr int kLnMaxCluster = 8;
-constexpr int64_t kLnMaxN = (int64_t)kLnSlice * kLnMaxCluster;
+constexpr int kLnThreads = 512;                   // of a block: 16 warps in groups
+constexpr int kLnMaxCluster = 8;               // portable
+constexpr int kLnSums = 2;                        // of a group of warps at once, at most
+constexpr int64_t kLnMaxN = 32768;
 constexpr int kLnSms = 148;
+constexpr int kLnRing = 192 << 10;                // bytes of rows on their way, at most
+
+// How a row lies in the lanes of its group.
+enum : int {
+  kLnWhole,     // 16-byte units, the rows being whole units at 16-byte addresses
+  kLnEdges,     // 16-byte units of memory, the first and the last of a row shared with its neighbours; a group's rows all begin at the same place in their unit
+  kLnSingle     // single elements: x, dy and the result do not begin at the same place
+};
 
 struct LnArgs {
   const char* x;
@@ -30,7 +38,9 @@ struct LnArgs {
   char* out;                // y, or dx (nullptr: not wanted)
   float* mean;
   float* rstd;
-  float* part;              // backward: sums of a CTA cluster's rows, [cluster][dgamma, dbeta][pitch]; nullptr: not wanted
+  float* part;              // backward: sums of a CTA cluster's rows, [cluster][dgamma, dbeta][pitch]; nullptr: not wanted, or one cluster has them all
+  void* dgamma;             // one cluster: where they go (nullptr: not wanted)
+  void* dbeta;
   int64_t M;
   int N;
   int slice;                // columns of one CTA, a multiple of 16
@@ -52,95 +62,133 @@ __device__ __forceinline__ void ld_shared_16(uint32_t addr, uint32_t (&v)[4]) {
   asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]) : "r"(addr) : "memory");
 }
 
-// Element types: 16 bytes to floats and back.
-struct LnBf16 {
+// Element types: 16 bytes to pairs of floats and back; one element.
+template <bool BF16>
+struct Ln16 {
   static constexpr int kBytes = 2;
-  static __device__ __forceinline__ void unpack(const uint32_t (&v)[4], float* f) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) { f[2 * i] = __uint_as_float(v[i] << 16); f[2 * i + 1] = __uint_as_float(v[i] & 0xffff0000u); }
+  static __device__ __forceinline__ float one(uint32_t bits) {
+    float lo, hi;
+    halves(bits, lo, hi);
+    return lo;
   }
-  static __device__ __forceinline__ void pack(const float* f, uint32_t (&v)[4]) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] = pack_16(f[2 * i], f[2 * i + 1], true);
-  }
-};
-struct LnFp16 {
-  static constexpr int kBytes = 2;
-  static __device__ __forceinline__ void unpack(const uint32_t (&v)[4], float* f) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float2 p = __half22float2(*reinterpret_cast<const __half2*>(&v[i]));
-      f[2 * i] = p.x; f[2 * i + 1] = p.y;
+  static __device__ __forceinline__ void halves(uint32_t v, float& lo, float& hi) {
+    if constexpr (BF16) {
+      lo = __uint_as_float(v << 16); hi = __uint_as_float(v & 0xffff0000u);
+    } else {
+      const float2 p = __half22float2(*reinterpret_cast<const __half2*>(&v));
+      lo = p.x; hi = p.y;
     }
   }
-  static __device__ __forceinline__ void pack(const float* f, uint32_t (&v)[4]) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] = pack_16(f[2 * i], f[2 * i + 1], false);
+  static __device__ __forceinline__ uint32_t twice_from_shared(uint32_t at) {
+    uint16_t b;
+    asm volatile("ld.shared.b16 %0, [%1];" : "=h"(b) : "r"(at) : "memory");
+    return b * 0x10001u;
   }
+  static __device__ __forceinline__ float first(uint32_t v) { return one(v); }
+  static __device__ __forceinline__ float from_shared(uint32_t at) { return one(twice_from_shared(at)); }
+  static __device__ __forceinline__ void unpack(const uint32_t (&v)[4], uint64_t* f) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      float lo, hi;
+      halves(v[i], lo, hi);
+      f[i] = pair_of(lo, hi);
+    }
+  }
+  static __device__ __forceinline__ void pack(const uint64_t* f, uint32_t (&v)[4]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      float lo, hi;
+      halves_of(f[i], lo, hi);
+      v[i] = pack_16(lo, hi, BF16);
+    }
+  }
+  static __device__ __forceinline__ void copy_from_shared(char* to, uint32_t at) { *reinterpret_cast<uint16_t*>(to) = (uint16_t)twice_from_shared(at); }
+  static __device__ __forceinline__ void store_one(char* at, float f) { *reinterpret_cast<uint16_t*>(at) = (uint16_t)pack_16(f, 0.f, BF16); }
 };
-struct LnFp32 {
+struct Ln32 {
   static constexpr int kBytes = 4;
-  static __device__ __forceinline__ void unpack(const uint32_t (&v)[4], float* f) {
+  static __device__ __forceinline__ uint32_t twice_from_shared(uint32_t at) { return ld_shared_32(at); }
+  static __device__ __forceinline__ float first(uint32_t v) { return __uint_as_float(v); }
+  static __device__ __forceinline__ float from_shared(uint32_t at) { return __uint_as_float(ld_shared_32(at)); }
+  static __device__ __forceinline__ void unpack(const uint32_t (&v)[4], uint64_t* f) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) f[i] = __uint_as_float(v[i]);
+    for (int i = 0; i < 2; ++i) f[i] = pair_of(__uint_as_float(v[2 * i]), __uint_as_float(v[2 * i + 1]));
   }
-  static __device__ __forceinline__ void pack(const float* f, uint32_t (&v)[4]) {
+  static __device__ __forceinline__ void pack(const uint64_t* f, uint32_t (&v)[4]) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] = __float_as_uint(f[i]);
+    for (int i = 0; i < 2; ++i) {
+      float lo, hi;
+      halves_of(f[i], lo, hi);
+      v[2 * i] = __float_as_uint(lo); v[2 * i + 1] = __float_as_uint(hi);
+    }
   }
+  static __device__ __forceinline__ void copy_from_shared(char* to, uint32_t at) { *reinterpret_cast<uint32_t*>(to) = ld_shared_32(at); }
+  static __device__ __forceinline__ void store_one(char* at, float f) { *reinterpret_cast<float*>(at) = f; }
 };
 
-// Bytes s .. s + 15 of a and b one behind the other; s from 0 to 15, a multiple of the element size.
-template <int ELT>
-__device__ __forceinline__ void shift_16(const uint32_t (&a)[4], const uint32_t (&b)[4], int s, uint32_t (&o)[4]) {
-  const uint32_t v[8] = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
-  uint32_t t[6], q[5];
-#pragma unroll
-  for (int i = 0; i < 6; ++i) t[i] = s & 8 ? v[i + 2] : v[i];
-#pragma unroll
-  for (int i = 0; i < 5; ++i) q[i] = s & 4 ? t[i + 1] : t[i];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) o[i] = ELT == 2 && (s & 2) ? __funnelshift_r(q[i], q[i + 1], 16) : q[i];
-}
-
-// Element i of 16 bytes to global memory.
-template <int ELT>
-__device__ __forceinline__ void store_element(char* at, const uint32_t (&v)[4], int i) {
-  if constexpr (ELT == 4) *reinterpret_cast<uint32_t*>(at) = v[i];
-  else *reinterpret_cast<uint16_t*>(at) = (uint16_t)(i & 1 ? v[i >> 1] >> 16 : v[i >> 1]);
-}
-
-__device__ __forceinline__ float ln_weight(const void* w, int dtype, int col) {
-  if (dtype == SP_FP32) return __ldg((const float*)w + col);
-  const uint16_t b = __ldg((const uint16_t*)w + col);
-  if (dtype == SP_BF16) return __uint_as_float((uint32_t)b << 16);
-  __half_raw r;
-  r.x = b;
-  return __half2float(__half(r));
-}
-
-// A group of W warps and its part of a row: 16-byte units of the slice, unit (wg U + u) 32 + lane the u-th of a lane, so that a warp's units are one stretch.
-template <class E, int W, bool ALIGNED>
+// A group of W warps and its part of a row, PER elements per thread as PER / 2 pairs.
+//   Units: a lane's u-th is unit (u W + warp) 32 + lane.  With edges the slice begins `lead` elements inside its first unit; what the first and the last
+//   unit hold beside it counts as zeros and is not written.
+//   Single elements: a lane's i-th is column (i W + warp) 32 + lane.
+template <class E, int W, int PER, int MODE>
 struct LnGroup {
-  static constexpr int kGroups = kLnThreads / 32 / W, kGroupThreads = 32 * W;
-  static constexpr int kElems = 16 / E::kBytes, kUnits = kLnPer / kElems;
+  static constexpr int kGroups = kLnThreads / 32 / W, kGroupThreads = 32 * W, kPairs = PER / 2;
+  static constexpr bool kUnits = MODE != kLnSingle;
+  static constexpr int kElems = kUnits ? 16 / E::kBytes : 1;           // next to each other
+  static constexpr int kChunks = PER / kElems;                         // such stretches
+  static constexpr int kStep = kUnits ? 1 : 2;                         // chunks that are done together, kWide pairs
+  static constexpr int kWide = kStep * kElems / 2;
   int lane, wg, group, tid;
   int rank, ranks;             // of the CTA in its cluster
-  int cols;                    // of the slice
+  int cols, lead;              // of the slice
+  // Rows with edges: which of the warp's units the slice has in part only (bit i: among the i-th ones); shared memory of the warp: what of its first and last such unit is
+  // the slice's (all bits of an element set), and the two on their way out; the element of them that this lane writes, its place in the slice's row or -1.
+  uint32_t edges, rim;
+  int rim_at;
   uint32_t red, far;           // shared memory: sums of warps, sums of CTAs (two of each, used in turn)
   uint32_t parity;
 
-  __device__ __forceinline__ LnGroup(const LnArgs& a, uint32_t red_) : red(red_), parity(0) {
+  __device__ __forceinline__ LnGroup(const LnArgs& a, uint32_t red_) : lead(0), edges(0), rim_at(-1), red(red_), parity(0) {
     const int warp = threadIdx.x >> 5;
     lane = threadIdx.x & 31;
     wg = warp % W; group = warp / W; tid = threadIdx.x % kGroupThreads;
-    ranks = W == 8 ? (int)cluster_nctarank() : 1;
-    rank = W == 8 ? (int)cluster_ctarank() : 0;
+    ranks = W == 16 ? (int)cluster_nctarank() : 1;
+    rank = W == 16 ? (int)cluster_ctarank() : 0;
     cols = max(0, min(a.slice, a.N - rank * a.slice));
-    far = red + 2 * 8 * 8;
-    if (W == 8 && ranks > 1) unit_sync<2>();      // every CTA of the cluster is there before one writes to its shared memory
+    far = red + 2 * 16 * 4 * kLnSums;
+    rim = far + 2 * kLnMaxCluster * 4 * kLnSums + warp * 64;
+    if (W == 16 && ranks > 1) unit_sync<2>();      // every CTA of the cluster is there before one writes to its shared memory
   }
-  __device__ __forceinline__ int unit(int u) const { return (wg * kUnits + u) * 32 + lane; }
+  // `m`: address modulo 16 of the group's rows
+  __device__ __forceinline__ void begin_at(int m) {
+    if constexpr (MODE == kLnEdges) {
+      lead = m / E::kBytes;
+#pragma unroll
+      for (int i = 0; i < kChunks; ++i)
+        if (__any_sync(0xffffffffu, has(i) && !full(i))) edges |= 1u << i;
+      const int last = (lead + cols - 1) / kElems, e = lane & 7;      // lanes 0 to 7: the elements of unit 0, 8 to 15: of the last one
+      const int unit = lane < 8 ? 0 : last, c = unit * kElems - lead + e;
+      const bool mine = wg == unit / 32 % W && (lane < 8 || last > 0) && c >= 0 && c < cols;
+      if (lane < 16 && e < kElems) {
+        if constexpr (E::kBytes == 2) asm volatile("st.shared.b16 [%0], %1;" ::"r"(rim + lane * 2), "h"((uint16_t)(mine ? 0xffff : 0)) : "memory");
+        else asm volatile("st.shared.b32 [%0], %1;" ::"r"(rim + (lane < 8 ? 0 : 16) + e * 4), "r"(mine ? 0xffffffffu : 0u) : "memory");
+        if (mine && (unit * kElems - lead < 0 || unit * kElems - lead + kElems > cols)) rim_at = c * E::kBytes;      // in a unit that is not whole
+      }
+      __syncwarp();
+    }
+  }
+  // A branch that is taken by few warps and, for the compiler, not to be made part of the straight line.
+  __device__ __forceinline__ bool edge(int i) const {
+    if constexpr (MODE != kLnEdges) return false;
+    if ((edges >> i & 1u) == 0) return false;
+    __syncwarp();
+    return true;
+  }
+  __device__ __forceinline__ int chunk(int i) const { return (i * W + wg) * 32 + lane; }
+  __device__ __forceinline__ int column(int i) const { return MODE == kLnEdges ? chunk(i) * kElems - lead : chunk(i) * kElems; }
+  __device__ __forceinline__ bool any(int i) const { return (i * W + wg) * 32 * kElems < cols + (MODE == kLnEdges ? lead : 0); }      // of the warp's i-th chunks
+  __device__ __forceinline__ bool has(int i) const { return column(i) < cols; }
+  __device__ __forceinline__ bool full(int i) const { return MODE != kLnEdges || (column(i) >= 0 && column(i) + kElems <= cols); }
   __device__ __forceinline__ void sync() const {
     if constexpr (W == 1) __syncwarp();
     else asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "n"(kGroupThreads) : "memory");
@@ -148,14 +196,18 @@ struct LnGroup {
 
   // A row's slice on its way to shared memory, as whole 16-byte units of global memory.  [lo, hi): the matrix, outside of which nothing is read.
   __device__ __forceinline__ void fetch(uint32_t dst, const char* row, const char* lo, const char* hi) const {
-    const int bytes = cols * E::kBytes;
-    if constexpr (ALIGNED) {      // the units a lane will read itself
+    if constexpr (MODE == kLnWhole) {      // the units a lane will read itself
 #pragma unroll
-      for (int u = 0; u < kUnits; ++u)
-        if (unit(u) * 16 < bytes) cp_async_16(dst + unit(u) * 16, row + unit(u) * 16, 16);
+      for (int u = 0; u < kChunks; ++u)
+        if (has(u)) cp_async_16(dst + chunk(u) * 16, row + chunk(u) * 16, 16);
+    } else if (MODE == kLnEdges && row - lead * E::kBytes >= lo && row + cols * E::kBytes + 15 <= hi) {
+      row -= lead * E::kBytes;
+#pragma unroll
+      for (int u = 0; u < kChunks; ++u)
+        if (has(u)) cp_async_16(dst + chunk(u) * 16, row + chunk(u) * 16, 16);
     } else {
-      const int m = (int)((uintptr_t)row & 15u), n = (m + bytes + 15) >> 4;
-      for (int j = tid; j < n; j += kGroupThreads) {
+      const int m = (int)((uintptr_t)row & 15u), n = (m + cols * E::kBytes + 15) >> 4;
+      const auto unit = [&](int j) {
         const char* p = row - m + 16 * j;
         if (p >= lo) cp_async_16(dst + 16 * j, p, (int)min((int64_t)16, (int64_t)(hi - p)));
         else      // the matrix starts inside this unit
@@ -164,113 +216,194 @@ struct LnGroup {
               if constexpr (E::kBytes == 4) asm volatile("st.shared.b32 [%0], %1;" ::"r"(dst + 16 * j + b), "r"(*reinterpret_cast<const uint32_t*>(p + b)) : "memory");
               else asm volatile("st.shared.b16 [%0], %1;" ::"r"(dst + 16 * j + b), "h"(*reinterpret_cast<const uint16_t*>(p + b)) : "memory");
             }
+      };
+      if constexpr (kUnits) {
+        for (int u = 0; u < kChunks; ++u)
+          if (chunk(u) < n) unit(chunk(u));
+      } else {
+        for (int j = tid; j < n; j += kGroupThreads) unit(j);
       }
     }
   }
-  // Unit k of the slice from shared memory, `m`: its row's address modulo 16.  Columns beyond the slice become zeros.
-  __device__ __forceinline__ void take(uint32_t src, int k, int m, float* f) const {
-    uint32_t v[4] = {0u, 0u, 0u, 0u};
-    const int left = cols - k * kElems;
-    if (left > 0) {
-      ld_shared_16(src + 16 * k, v);
-      if constexpr (!ALIGNED) {
-        if (m) {
-          uint32_t w[4], o[4];
-          ld_shared_16(src + 16 * k + 16, w);
-          shift_16<E::kBytes>(v, w, m, o);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) v[i] = o[i];
+  // A lane's pairs of chunk i from shared memory, `m`: the row's address modulo 16.  Columns outside the slice become zeros.
+  __device__ __forceinline__ void take(uint32_t src, int i, int m, uint64_t* f) const {
+    int none;
+    float filler;
+    take<false>(src, i, m, f, none, filler);
+  }
+  // FILL: what an edge holds beside the slice becomes the slice's own first element there, `extra` times `filler`, which the sums are relieved of again.  (It
+  // is an element of the row, at most sqrt(N) deviations from the mean, so at most 15 rows' worth of squares are added and taken away.)
+  template <bool FILL>
+  __device__ __forceinline__ void take(uint32_t src, int i, int m, uint64_t* f, int& extra, float& filler) const {
+    if constexpr (kUnits) {
+      uint32_t v[4] = {0u, 0u, 0u, 0u};
+      if (has(i)) ld_shared_16(src + 16 * chunk(i), v);
+      if (edge(i) && has(i) && !full(i)) {
+        const bool begin = chunk(i) == 0;
+        uint32_t k[4], fill = 0;
+        ld_shared_16(rim + (begin ? 0 : 16), k);
+        if constexpr (FILL) {
+          fill = E::twice_from_shared(src + 16 * chunk(i) + (begin ? lead * E::kBytes : 0));
+          filler = E::first(fill);
+          extra = kElems - min(kElems, cols - column(i)) + max(0, -column(i));
         }
-      }
-    }
-    E::unpack(v, f);
-    if constexpr (!ALIGNED)
-      if (left < kElems) {
 #pragma unroll
-        for (int i = 0; i < kElems; ++i)
-          if (i >= left) f[i] = 0.f;
+        for (int w = 0; w < 4; ++w) v[w] = (v[w] & k[w]) | (fill & ~k[w]);
       }
-  }
-  // A lane's units to the row's slice.  Unaligned rows: a lane writes the 16-byte unit of global memory in which its own begins, the first part of it
-  // from the lane before; element by element where a stretch of the warp or the slice begins or ends.
-  __device__ __forceinline__ void put(char* row, const float* f) const {
-    const int bytes = cols * E::kBytes;
-    if constexpr (ALIGNED) {
-#pragma unroll
-      for (int u = 0; u < kUnits; ++u) {
-        uint32_t v[4];
-        E::pack(f + u * kElems, v);
-        if (unit(u) * 16 < bytes) *reinterpret_cast<uint4*>(row + unit(u) * 16) = make_uint4(v[0], v[1], v[2], v[3]);
-      }
+      E::unpack(v, f);
     } else {
-      const int m = (int)((uintptr_t)row & 15u);
-      if (wg * kUnits * 512 >= bytes + 16) return;      // a warp with no part of the row
-      uint32_t before[4] = {0u, 0u, 0u, 0u};
+      const uint32_t at = src + m + column(i) * E::kBytes;
+      f[0] = pair_of(has(i) ? E::from_shared(at) : 0.f, has(i + 1) ? E::from_shared(at + 32 * W * E::kBytes) : 0.f);
+    }
+  }
+  // f - v in the columns that the lane holds, else 0 as before
+  __device__ __forceinline__ void subtract(int i, float v, uint64_t* f) const {
+    if constexpr (kUnits) {
+      const float m = has(i) ? -v : 0.f;
 #pragma unroll
-      for (int u = 0; u < kUnits; ++u) {
-        uint32_t v[4], p[4], o[4];
-        E::pack(f + u * kElems, v);
+      for (int k = 0; k < kWide; ++k) f[k] = add_pair(f[k], pair_of(m, m));
+    } else {
+      f[0] = add_pair(f[0], pair_of(has(i) ? -v : 0.f, has(i + 1) ? -v : 0.f));
+    }
+  }
+  __device__ __forceinline__ void put(char* row, int i, const uint64_t* f) const {
+    if constexpr (kUnits) {
+      char* at = row + column(i) * E::kBytes;
+      uint32_t v[4];
+      E::pack(f, v);
+      if (has(i) && full(i)) *reinterpret_cast<uint4*>(at) = make_uint4(v[0], v[1], v[2], v[3]);
+      if (edge(i) && has(i) && !full(i)) st_shared_16(rim + (chunk(i) == 0 ? 32 : 48), v[0], v[1], v[2], v[3]);
+    } else {
+      float lo, hi;
+      halves_of(f[0], lo, hi);
+      char* at = row + column(i) * E::kBytes;
+      if (has(i)) E::store_one(at, lo);
+      if (has(i + 1)) E::store_one(at + 32 * W * E::kBytes, hi);
+    }
+  }
+  // After the row's put: what the edges have of it, an element per lane.
+  __device__ __forceinline__ void put_rim(char* row) const {
+    if constexpr (MODE == kLnEdges) {
+      if (edges == 0) return;
+      __syncwarp();
+      if (rim_at >= 0) E::copy_from_shared(row + rim_at, rim + 32 + (lane < 8 ? 0 : 16) + (lane & 7) * E::kBytes);
+      __syncwarp();
+    }
+  }
+  // gamma or beta of this lane's columns.  All of a kind of loads are in flight together, 16 bytes each where they can be: a block starts with them.
+  __device__ __forceinline__ void weights(const void* w, int dtype, int col0, float none, uint64_t* f) const {
+    if (w == nullptr) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const uint32_t r = __shfl_sync(0xffffffffu, v[i], (lane + 31) & 31);
-          p[i] = lane == 0 ? before[i] : r;
-          before[i] = r;
-          o[i] = v[i];
-        }
-        if (m) shift_16<E::kBytes>(p, v, 16 - m, o);
-        const int at = unit(u) * 16 - m;                                             // of the row: where this unit of global memory begins
-        const int first = u == 0 && lane == 0 ? at + m : at, end = min(at + 16, bytes);
-        if (first == at && end == at + 16) *reinterpret_cast<uint4*>(row + at) = make_uint4(o[0], o[1], o[2], o[3]);
-        else if (first < end) {
+      for (int k = 0; k < kPairs; ++k) f[k] = pair_of(none, none);
+    } else if (dtype == SP_FP32) {
+      const float* p = (const float*)w + col0;
+      if (MODE == kLnWhole && ((uintptr_t)w & 15u) == 0) {
 #pragma unroll
-          for (int i = 0; i < kElems; ++i)
-            if (at + i * E::kBytes >= first && at + i * E::kBytes < end) store_element<E::kBytes>(row + at + i * E::kBytes, o, i);
-        }
-        if (u == kUnits - 1 && lane == 31 && m) {      // the end of the warp's stretch
+        for (int i = 0; i < kChunks; ++i)
 #pragma unroll
-          for (int i = 0; i < kElems; ++i)
-            if (i * E::kBytes >= 16 - m && at + m + i * E::kBytes < bytes) store_element<E::kBytes>(row + at + m + i * E::kBytes, v, i);
+          for (int q = 0; q < kElems / 4; ++q) {
+            const float4 v = has(i) ? __ldg(reinterpret_cast<const float4*>(p + column(i)) + q) : make_float4(none, none, none, none);
+            f[i * kElems / 2 + 2 * q] = pair_of(v.x, v.y);
+            f[i * kElems / 2 + 2 * q + 1] = pair_of(v.z, v.w);
+          }
+      } else {
+        one_by_one(f, none, [&](int c) { return __ldg(p + c); });
+      }
+    } else {      // the rows' type
+      if constexpr (E::kBytes == 2) {
+        const uint16_t* p = (const uint16_t*)w + col0;
+        if (MODE == kLnWhole && ((uintptr_t)w & 15u) == 0) {
+#pragma unroll
+          for (int i = 0; i < kChunks; ++i) {
+            const uint4 q = has(i) ? __ldg(reinterpret_cast<const uint4*>(p + column(i))) : make_uint4(0u, 0u, 0u, 0u);
+            const uint32_t v[4] = {q.x, q.y, q.z, q.w};
+            if constexpr (kUnits) E::unpack(v, f + i * kElems / 2);
+          }
+        } else {
+          one_by_one(f, none, [&](int c) { return E::one(__ldg(p + c)); });
         }
       }
     }
   }
-  // Sums of a and b over the row: lanes, warps, CTAs, in this order.
-  __device__ __forceinline__ void sum(float& a, float& b) {
+  template <class Load>
+  __device__ __forceinline__ void one_by_one(uint64_t* f, float none, const Load& load) const {
 #pragma unroll
-    for (int o = 16; o; o >>= 1) {
-      a += __shfl_xor_sync(0xffffffffu, a, o);
-      b += __shfl_xor_sync(0xffffffffu, b, o);
+    for (int k = 0; k < kPairs; ++k) {
+      float v[2];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int e = 2 * k + h, c = column(e / kElems) + e % kElems;
+        v[h] = c >= 0 && c < cols ? load(c) : none;
+      }
+      f[k] = pair_of(v[0], v[1]);
     }
-    if constexpr (W > 1) {
-      const uint32_t at = red + (parity * 8 + group * W) * 8;
-      if (lane == 0) asm volatile("st.shared.v2.f32 [%0], {%1, %2};" ::"r"(at + wg * 8), "f"(a), "f"(b) : "memory");
-      sync();
-      a = b = 0.f;
+  }
+
+  // n sums over the row (n: a power of two): lanes, warps, CTAs, in this order.  Of several sums every step of the lanes' leaves half to each half of the lanes.
+  template <int n>
+  __device__ __forceinline__ void sum(float* s) {
+    int o = 16;
 #pragma unroll
-      for (int i = 0; i < W; ++i) {
-        float p, q;
-        asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(p), "=f"(q) : "r"(at + i * 8) : "memory");
-        a += p; b += q;
+    for (int left = n / 2; left; left /= 2, o /= 2) {
+      const bool upper = lane & o;
+#pragma unroll
+      for (int j = 0; j < left; ++j) {
+        const float give = upper ? s[j] : s[j + left], keep = upper ? s[j + left] : s[j];
+        s[j] = keep + __shfl_xor_sync(0xffffffffu, give, o);
       }
     }
-    if constexpr (W == 8)
-      if (ranks > 1) {
-        const uint32_t at = far + parity * kLnMaxCluster * 8;
-        if (tid < ranks) asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(mapa(at + rank * 8, tid)), "f"(a), "f"(b) : "memory");
-        unit_sync<2>();      // all threads of the cluster
-        a = b = 0.f;
-        for (int i = 0; i < ranks; ++i) {
+#pragma unroll
+    for (; o; o /= 2) s[0] += __shfl_xor_sync(0xffffffffu, s[0], o);
+    constexpr int kLanes = 32 / n;      // lanes [j kLanes, (j + 1) kLanes) have sum j
+    if constexpr (W == 1) {
+      const float all = s[0];
+#pragma unroll
+      for (int j = 0; j < n; ++j) s[j] = n == 1 ? all : __shfl_sync(0xffffffffu, all, j * kLanes);
+    } else {
+      const uint32_t at = red + (parity * 16 + group * W) * (4 * kLnSums);      // [sum][warp]
+      if (lane % kLanes == 0) asm volatile("st.shared.f32 [%0], %1;" ::"r"(at + (lane / kLanes * W + wg) * 4), "f"(s[0]) : "memory");
+      sync();
+#pragma unroll
+      for (int j = 0; j < n; ++j) {
+        if constexpr (W == 2) {
           float p, q;
-          asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(p), "=f"(q) : "r"(at + i * 8) : "memory");
-          a += p; b += q;
+          asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(p), "=f"(q) : "r"(at + j * 8) : "memory");
+          s[j] = p + q;
+        } else {
+          s[j] = 0.f;
+#pragma unroll
+          for (int i = 0; i < W / 4; ++i) {
+            uint32_t v[4];
+            ld_shared_16(at + j * W * 4 + i * 16, v);
+            s[j] += (__uint_as_float(v[0]) + __uint_as_float(v[1])) + (__uint_as_float(v[2]) + __uint_as_float(v[3]));
+          }
         }
       }
-    parity ^= 1u;
+      if constexpr (W == 16)
+        if (ranks > 1) {
+          const uint32_t here = far + parity * kLnMaxCluster * 4 * kLnSums;      // [CTA][sum]
+          if (tid < ranks) {
+#pragma unroll
+            for (int j = 0; j < n; ++j) asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(mapa(here + (rank * kLnSums + j) * 4, tid)), "f"(s[j]) : "memory");
+          }
+          unit_sync<2>();      // all threads of the cluster
+#pragma unroll
+          for (int j = 0; j < n; ++j) s[j] = 0.f;
+          for (int i = 0; i < ranks; ++i)
+#pragma unroll
+            for (int j = 0; j < n; ++j) s[j] += __uint_as_float(ld_shared_32(here + (i * kLnSums + j) * 4));
+        }
+      parity ^= 1u;
+    }
   }
 };
 
-// Bytes of shared memory beside the rows: sums of warps and of CTAs, two of each.
-constexpr uint32_t kLnRedBytes = 2 * 8 * 8 + 2 * kLnMaxCluster * 8;
+// Bytes of shared memory beside the rows: sums of warps and of CTAs, two of each, and the warps' rims.
+constexpr uint32_t kLnRedBytes = 2 * (16 + kLnMaxCluster) * 4 * kLnSums + 16 * 64;
+
+// Batches of `rows` rows' slices on their way.
+template <class E, int PER, int ROWS>
+constexpr int kLnDepth = kLnRing / (kLnThreads * PER * E::kBytes * ROWS) < 4 ? kLnRing / (kLnThreads * PER * E::kBytes * ROWS) : 4;
 
 // 1 / sqrt(v): the hardware's, which is good to two steps, and one step of Newton's method.
 __device__ __forceinline__ float ln_rsqrt(float v) {
@@ -278,175 +411,215 @@ __device__ __forceinline__ float ln_rsqrt(float v) {
   return s == s ? s : r;      // 0 and infinity
 }
 
-template <class E, int W, bool ALIGNED>
-__global__ void __launch_bounds__(kLnThreads, 3) layernorm_kernel(const LnArgs a) {
+__device__ __forceinline__ float halves_sum(uint64_t s) {
+  float lo, hi;
+  halves_of(s, lo, hi);
+  return lo + hi;
+}
+
+template <class E, int W, int PER, int MODE>
+__global__ void __launch_bounds__(kLnThreads, 1) layernorm_kernel(const LnArgs a) {
   extern __shared__ __align__(16) uint8_t ln_smem[];
-  using G = LnGroup<E, W, ALIGNED>;
-  constexpr int U = G::kUnits, K = G::kElems;
+  using G = LnGroup<E, W, PER, MODE>;
+  constexpr int D = kLnDepth<E, PER, 1>, P = G::kWide;
   const uint32_t base = smem_u32(ln_smem);
   G g(a, base);
-  const uint32_t ring = base + kLnRedBytes + g.group * kLnDepth * a.slot;
-  const int64_t first = (int64_t)(blockIdx.x / g.ranks) * G::kGroups + g.group, step = (int64_t)a.clusters * G::kGroups;
-  const int col0 = g.rank * a.slice;
-  const int64_t pitch = (int64_t)a.N * E::kBytes, from = (int64_t)col0 * E::kBytes;
-  const char* end = a.x + a.M * pitch;
+  const uint32_t ring = base + kLnRedBytes + g.group * D * a.slot;
+  const uint32_t total = a.clusters * G::kGroups, last = (uint32_t)a.M - 1;      // unsigned: beyond the last row they may pass 2^31
+  const int64_t pitch = (int64_t)a.N * E::kBytes, hop = (int64_t)total * pitch, all = a.M * pitch;
+  uint32_t row = blockIdx.x / g.ranks * G::kGroups + g.group;
+  int64_t here = (int64_t)row * pitch + (int64_t)g.rank * a.slice * E::kBytes, next = here;
+  g.begin_at((int)((uintptr_t)(a.x + here) & 15u));
   pdl_begin();
-#pragma unroll
-  for (int i = 0; i < kLnDepth; ++i) {
-    if (first + i * step < a.M) g.fetch(ring + i * a.slot, a.x + (first + i * step) * pitch + from, a.x, end);
+  const auto fetch = [&](uint32_t at, uint32_t r) {
+    if (r <= last) g.fetch(at, a.x + next, a.x, a.x + all);
+    next += hop;
     cp_async_commit();
-  }
-  float gamma[kLnPer], beta[kLnPer];
+  };
+  uint32_t ahead = row;
 #pragma unroll
-  for (int u = 0; u < U; ++u)
-#pragma unroll
-    for (int i = 0; i < K; ++i) {
-      const int c = g.unit(u) * K + i;
-      gamma[u * K + i] = a.gamma != nullptr && c < g.cols ? ln_weight(a.gamma, a.w_dtype, col0 + c) : 1.f;
-      beta[u * K + i] = a.beta != nullptr && c < g.cols ? ln_weight(a.beta, a.w_dtype, col0 + c) : 0.f;
-    }
+  for (int i = 0; i < D; ++i, ahead += total) fetch(ring + i * a.slot, ahead);
+  uint64_t gamma[G::kPairs], beta[G::kPairs];
+  g.weights(a.gamma, a.w_dtype, g.rank * a.slice, 1.f, gamma);
+  g.weights(a.beta, a.w_dtype, g.rank * a.slice, 0.f, beta);
   const float inv = 1.f / (float)a.N;
-  int slot = 0;
-  for (int64_t row = first; row < a.M; row += step) {
-    cp_async_wait<kLnDepth - 1>();
-    if constexpr (!ALIGNED) g.sync();      // the others' copies
-    const char* src = a.x + row * pitch + from;
-    float x[kLnPer];
+  uint32_t at = ring;
+  for (; row <= last; row += total, here += hop) {
+    cp_async_wait<D - 1>();
+    if constexpr (MODE == kLnSingle) g.sync();      // the others' copies
+    uint64_t x[G::kPairs], s2[2] = {0, 0}, v2[2] = {0, 0};
+    float filler[2] = {0.f, 0.f};
+    int extra[2] = {0, 0};
 #pragma unroll
-    for (int u = 0; u < U; ++u) g.take(ring + slot * a.slot, g.unit(u), (int)((uintptr_t)src & 15u), x + u * K);
-    float s = 0.f, t = 0.f;
+    for (int i = 0; i < G::kChunks; i += G::kStep)
+      if (g.any(i)) {
+        uint64_t* f = x + i * G::kElems / 2;
+        g.template take<true>(at, i, (int)((uintptr_t)(a.x + here) & 15u), f, extra[i > 0], filler[i > 0]);      // at most two units of a lane are edges
 #pragma unroll
-    for (int i = 0; i < kLnPer; i += 2) { s += x[i]; t += x[i + 1]; }
-    s += t; t = 0.f;
-    if constexpr (W == 1 && !ALIGNED) __syncwarp();      // all have read the slot
-    g.sum(s, t);
-    if (row + kLnDepth * step < a.M) g.fetch(ring + slot * a.slot, src + kLnDepth * step * pitch, a.x, end);
-    cp_async_commit();
-    slot = slot + 1 == kLnDepth ? 0 : slot + 1;
+        for (int k = 0; k < P; ++k) s2[k & 1] = add_pair(s2[k & 1], f[k]);
+      }
+    float s = halves_sum(add_pair(s2[0], s2[1]));
+    if constexpr (MODE == kLnEdges) s -= extra[0] * filler[0] + extra[1] * filler[1];
+    g.template sum<1>(&s);
+    fetch(at, ahead);
+    ahead += total;
+    at = at + a.slot == ring + D * a.slot ? ring : at + a.slot;
     // The differences' own sum corrects what the rounded mean leaves: of rows whose mean is a thousand deviations, too, variance and y keep their digits.
     const float about = s * inv;
-    float d = 0.f, v = 0.f;
+    s2[0] = s2[1] = 0;
 #pragma unroll
-    for (int u = 0; u < U; ++u)
+    for (int i = 0; i < G::kChunks; i += G::kStep)
+      if (g.any(i)) {
+        uint64_t* f = x + i * G::kElems / 2;
+        g.subtract(i, about, f);
 #pragma unroll
-      for (int i = 0; i < K; ++i) {
-        float& e = x[u * K + i];
-        e = g.unit(u) * K + (ALIGNED ? 0 : i) < g.cols ? e - about : 0.f;
-        d += e;
-        v = fmaf(e, e, v);
+        for (int k = 0; k < P; ++k) {
+          s2[k & 1] = add_pair(s2[k & 1], f[k]);
+          v2[k & 1] = fma_pair(f[k], f[k], v2[k & 1]);
+        }
       }
-    g.sum(d, v);
-    const float off = d * inv, var = fmaf(-off, off, v * inv), rstd = ln_rsqrt((var < 0.f ? 0.f : var) + a.eps);
+    float sv[2] = {halves_sum(add_pair(s2[0], s2[1])), halves_sum(add_pair(v2[0], v2[1]))};
+    if constexpr (MODE == kLnEdges)
+#pragma unroll
+      for (int q = 0; q < 2; ++q) {
+        const float e = filler[q] - about;
+        sv[0] -= extra[q] * e;
+        sv[1] -= extra[q] * e * e;
+      }
+    g.template sum<2>(sv);
+    const float off = sv[0] * inv, var = fmaf(-off, off, sv[1] * inv), rstd = ln_rsqrt((var < 0.f ? 0.f : var) + a.eps);
     if (g.tid == 0 && g.rank == 0) {
       if (a.mean != nullptr) a.mean[row] = about + off;
       if (a.rstd != nullptr) a.rstd[row] = rstd;
     }
+    const uint64_t scale = pair_of(rstd, rstd), minus = pair_of(-off, -off);
 #pragma unroll
-    for (int i = 0; i < kLnPer; ++i) x[i] = fmaf((x[i] - off) * rstd, gamma[i], beta[i]);
-    g.put(a.out + row * pitch + from, x);
+    for (int i = 0; i < G::kChunks; i += G::kStep)
+      if (g.any(i)) {
+        const int o = i * G::kElems / 2;
+#pragma unroll
+        for (int k = o; k < o + P; ++k) x[k] = fma_pair(mul_pair(add_pair(x[k], minus), scale), gamma[k], beta[k]);
+        g.put(a.out + here, i, x + o);
+      }
+    g.put_rim(a.out + here);
   }
 }
 
-template <class E, int W, bool ALIGNED>
-__global__ void __launch_bounds__(kLnThreads, 2) layernorm_grad_kernel(const LnArgs a) {
+__device__ __forceinline__ void store_weight(void* out, int dtype, int col, float s) {
+  if (out == nullptr) return;
+  if (dtype == SP_FP32) ((float*)out)[col] = s;
+  else ((uint16_t*)out)[col] = (uint16_t)pack_16(s, 0.f, dtype == SP_BF16);
+}
+
+// (A row finished beside the sums of the next, between the same two barriers, its x and dy read twice from shared memory: 16384 x 4096 86 us, so 75. Instructions bound it.)
+template <class E, int W, int PER, int MODE>
+__global__ void __launch_bounds__(kLnThreads, 1) layernorm_grad_kernel(const LnArgs a) {
   extern __shared__ __align__(16) uint8_t ln_smem[];
-  using G = LnGroup<E, W, ALIGNED>;
-  constexpr int U = G::kUnits, K = G::kElems;
+  using G = LnGroup<E, W, PER, MODE>;
+  constexpr int D = kLnDepth<E, PER, 2>, P = G::kWide;
   const uint32_t base = smem_u32(ln_smem);
   G g(a, base);
-  const uint32_t ring = base + kLnRedBytes + g.group * kLnDepth * 2 * a.slot;
-  const int64_t first = (int64_t)(blockIdx.x / g.ranks) * G::kGroups + g.group, step = (int64_t)a.clusters * G::kGroups;
+  const uint32_t ring = base + kLnRedBytes + g.group * D * 2 * a.slot, batch = 2 * a.slot;
+  const uint32_t total = a.clusters * G::kGroups, last = (uint32_t)a.M - 1;
   const int col0 = g.rank * a.slice;
-  const int64_t pitch = (int64_t)a.N * E::kBytes, from = (int64_t)col0 * E::kBytes, all = a.M * pitch;
+  const int64_t pitch = (int64_t)a.N * E::kBytes, hop = (int64_t)total * pitch, all = a.M * pitch;
+  uint32_t row = blockIdx.x / g.ranks * G::kGroups + g.group;
+  int64_t here = (int64_t)row * pitch + (int64_t)col0 * E::kBytes, next = here;
+  g.begin_at((int)((uintptr_t)(a.x + here) & 15u));
   pdl_begin();
-  const auto fetch = [&](int slot, int64_t row) {
-    const uint32_t at = ring + slot * 2 * a.slot;
-    g.fetch(at, a.x + row * pitch + from, a.x, a.x + all);
-    g.fetch(at + a.slot, a.dy + row * pitch + from, a.dy, a.dy + all);
-  };
-#pragma unroll
-  for (int i = 0; i < kLnDepth; ++i) {
-    if (first + i * step < a.M) fetch(i, first + i * step);
-    cp_async_commit();
-  }
-  float gamma[kLnPer], dg[kLnPer], db[kLnPer];
-#pragma unroll
-  for (int u = 0; u < U; ++u)
-#pragma unroll
-    for (int i = 0; i < K; ++i) {
-      const int c = g.unit(u) * K + i;
-      gamma[u * K + i] = a.gamma != nullptr && c < g.cols ? ln_weight(a.gamma, a.w_dtype, col0 + c) : 1.f;
-      dg[u * K + i] = db[u * K + i] = 0.f;
+  const auto fetch = [&](uint32_t at, uint32_t r) {
+    if (r <= last) {
+      g.fetch(at, a.x + next, a.x, a.x + all);
+      g.fetch(at + a.slot, a.dy + next, a.dy, a.dy + all);
     }
+    next += hop;
+    cp_async_commit();
+  };
+  uint32_t ahead = row;
+#pragma unroll
+  for (int i = 0; i < D; ++i, ahead += total) fetch(ring + i * batch, ahead);
+  uint64_t gamma[G::kPairs], dg[G::kPairs], db[G::kPairs];
+  g.weights(a.gamma, a.w_dtype, col0, 1.f, gamma);
+#pragma unroll
+  for (int k = 0; k < G::kPairs; ++k) dg[k] = db[k] = 0;
   const float inv = 1.f / (float)a.N;
   float mean = 0.f, rstd = 0.f;
-  if (first < a.M) { mean = __ldg(a.mean + first); rstd = __ldg(a.rstd + first); }
-  int slot = 0;
-  for (int64_t row = first; row < a.M; row += step) {
+  if (row <= last) { mean = __ldg(a.mean + row); rstd = __ldg(a.rstd + row); }
+  uint32_t at = ring;
+  for (; row <= last; row += total, here += hop) {
     float next_mean = 0.f, next_rstd = 0.f;
-    if (row + step < a.M) { next_mean = __ldg(a.mean + row + step); next_rstd = __ldg(a.rstd + row + step); }
-    cp_async_wait<kLnDepth - 1>();
-    if constexpr (!ALIGNED) g.sync();
-    const char *src = a.x + row * pitch + from, *src_dy = a.dy + row * pitch + from;
-    const uint32_t at = ring + slot * 2 * a.slot;
-    float x[kLnPer], y[kLnPer];      // xh and u
-    float s = 0.f, t = 0.f;
+    if (row + total <= last) { next_mean = __ldg(a.mean + row + total); next_rstd = __ldg(a.rstd + row + total); }
+    cp_async_wait<D - 1>();
+    if constexpr (MODE == kLnSingle) g.sync();
+    uint64_t x[G::kPairs], y[G::kPairs], s2[2] = {0, 0}, t2[2] = {0, 0};      // xh and u
+    const uint64_t minus = pair_of(-mean, -mean), scale = pair_of(rstd, rstd);
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      g.take(at, g.unit(u), (int)((uintptr_t)src & 15u), x + u * K);
-      g.take(at + a.slot, g.unit(u), (int)((uintptr_t)src_dy & 15u), y + u * K);
+    for (int i = 0; i < G::kChunks; i += G::kStep)
+      if (g.any(i)) {
+        const int o = i * G::kElems / 2;
+        g.take(at, i, (int)((uintptr_t)(a.x + here) & 15u), x + o);
+        g.take(at + a.slot, i, (int)((uintptr_t)(a.dy + here) & 15u), y + o);      // 0 outside the slice, and with it all that x adds there
 #pragma unroll
-      for (int i = u * K; i < u * K + K; ++i) {
-        x[i] = (x[i] - mean) * rstd;
-        dg[i] = fmaf(y[i], x[i], dg[i]);
-        db[i] += y[i];
-        y[i] *= gamma[i];
-        s += y[i];
-        t = fmaf(y[i], x[i], t);
+        for (int k = o; k < o + P; ++k) {
+          x[k] = mul_pair(add_pair(x[k], minus), scale);
+          dg[k] = fma_pair(y[k], x[k], dg[k]);
+          db[k] = add_pair(db[k], y[k]);
+          y[k] = mul_pair(y[k], gamma[k]);
+          s2[k & 1] = add_pair(s2[k & 1], y[k]);
+          t2[k & 1] = fma_pair(y[k], x[k], t2[k & 1]);
+        }
       }
-    }
-    if constexpr (W == 1 && !ALIGNED) __syncwarp();      // all have read the slot
-    if (a.out != nullptr || W > 1) g.sum(s, t);
-    if (row + kLnDepth * step < a.M) fetch(slot, row + kLnDepth * step);
-    cp_async_commit();
-    slot = slot + 1 == kLnDepth ? 0 : slot + 1;
+    float st[2] = {halves_sum(add_pair(s2[0], s2[1])), halves_sum(add_pair(t2[0], t2[1]))};
+    g.template sum<2>(st);
+    fetch(at, ahead);
+    ahead += total;
+    at = at + batch == ring + D * batch ? ring : at + batch;
     if (a.out != nullptr) {
-      s *= inv; t *= inv;
+      const uint64_t c1 = pair_of(-st[0] * inv, -st[0] * inv), c2 = pair_of(-st[1] * inv, -st[1] * inv);
 #pragma unroll
-      for (int i = 0; i < kLnPer; ++i) x[i] = rstd * fmaf(-t, x[i], y[i] - s);
-      g.put(a.out + row * pitch + from, x);
+      for (int i = 0; i < G::kChunks; i += G::kStep)
+        if (g.any(i)) {
+          uint64_t* f = x + i * G::kElems / 2;
+#pragma unroll
+          for (int k = 0; k < P; ++k) f[k] = mul_pair(scale, fma_pair(c2, f[k], add_pair(y[i * G::kElems / 2 + k], c1)));
+          g.put(a.out + here, i, f);
+        }
+      g.put_rim(a.out + here);
     }
     mean = next_mean; rstd = next_rstd;
   }
-  if (a.part == nullptr) return;
+  if (a.part == nullptr && a.dgamma == nullptr && a.dbeta == nullptr) return;
   // the groups' sums to one, in their order
-  float* part = a.part + (int64_t)(blockIdx.x / g.ranks) * 2 * a.pitch + col0;
+  float* all_groups = reinterpret_cast<float*>(ln_smem + kLnRedBytes);
   cp_async_wait<0>();
 #pragma unroll
   for (int w = 0; w < 2; ++w) {
-    float* v = w == 0 ? dg : db;
+    const auto out = [&](int c, float s) {
+      if (a.part != nullptr) a.part[((int64_t)(blockIdx.x / g.ranks) * 2 + w) * a.pitch + col0 + c] = s;
+      else store_weight(w == 0 ? a.dgamma : a.dbeta, a.w_dtype, col0 + c, s);
+    };
+    if constexpr (G::kGroups > 1) __syncthreads();
+#pragma unroll
+    for (int k = 0; k < G::kPairs; ++k) {
+      float v[2];
+      halves_of(w == 0 ? dg[k] : db[k], v[0], v[1]);
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int e = 2 * k + h, c = g.column(e / G::kElems) + e % G::kElems;
+        if (c >= 0 && c < g.cols) {
+          if constexpr (G::kGroups > 1) all_groups[g.group * a.pitch + c] = v[h];
+          else out(c, v[h]);
+        }
+      }
+    }
     if constexpr (G::kGroups > 1) {
-      float* all_groups = reinterpret_cast<float*>(ln_smem + kLnRedBytes);
-      const int width = (a.N + 15) & ~15;
-      __syncthreads();
-#pragma unroll
-      for (int u = 0; u < U; ++u)
-#pragma unroll
-        for (int i = 0; i < K; ++i)
-          if (g.unit(u) * K + i < width) all_groups[g.group * width + g.unit(u) * K + i] = v[u * K + i];
       __syncthreads();
       for (int c = threadIdx.x; c < a.N; c += kLnThreads) {
         float s = 0.f;
 #pragma unroll
-        for (int i = 0; i < G::kGroups; ++i) s += all_groups[i * width + c];
-        part[w * a.pitch + c] = s;
+        for (int i = 0; i < G::kGroups; ++i) s += all_groups[i * a.pitch + c];
+        out(c, s);
       }
-    } else {
-#pragma unroll
-      for (int u = 0; u < U; ++u)
-#pragma unroll
-        for (int i = 0; i < K; i += 4)
-          if (g.unit(u) * K + i < g.cols) *reinterpret_cast<float4*>(part + w * a.pitch + g.unit(u) * K + i) = make_float4(v[u * K + i], v[u * K + i + 1], v[u * K + i + 2], v[u * K + i + 3]);
     }
   }
 }
@@ -469,8 +642,7 @@ __global__ void __launch_bounds__(512) layernorm_weights_kernel(const float* par
   if (w != 0 || col >= N) return;
 #pragma unroll
   for (int i = 1; i < 16; ++i) s += sums[i][lane];
-  if (dtype == SP_FP32) ((float*)out)[col] = s;
-  else ((uint16_t*)out)[col] = (uint16_t)pack_16(s, 0.f, dtype == SP_BF16);
+  store_weight(out, dtype, col, s);
 }
 
 // ------------------------------------------------------------------ host side
@@ -478,30 +650,53 @@ static std::mutex g_ln_mu;   // per-kernel set-up is done under it
 
 static int ln_bytes(int32_t dtype) { return dtype == SP_FP32 ? 4 : 2; }
 
-// What follows from the sizes: how many CTAs share a row, how many warps a group has, how many clusters run.
+// What follows from the sizes and from how rows lie in the lanes.
 struct LnPlan {
-  int ranks, warps, slice, clusters, pitch;
+  int mode, per;            // elements per thread
+  int ranks, slice;         // CTAs that share a row, columns of one
+  int warps, clusters;      // of a group; launched
+  int pitch;
 };
 
-static LnPlan ln_plan(int64_t M, int64_t N, bool grad) {
+static LnPlan ln_plan(int64_t M, int64_t N, int elt, bool grad, int mode) {
   LnPlan p = {};
-  p.ranks = 1;
-  while ((int64_t)p.ranks * kLnSlice < N) p.ranks *= 2;
-  p.slice = (int)(((N + p.ranks - 1) / p.ranks + 15) / 16 * 16);
-  p.warps = 1;
-  while (p.warps * 32 * kLnPer < p.slice) p.warps *= 2;
+  p.mode = mode;
+  const int edge = mode == kLnEdges ? 16 / elt : 0;      // of elements before the slice, at most one unit less
+  // Forward 32 elements per thread: per row half the warps, with what a warp costs beside its elements (8192 x 4096 bf16: 25.9 us, with 16: 31.9).  Rows with edges, whose bookkeeping wants
+  // registers, 16 where these are well filled: 5001 x 2035 fp16 16.4 us, with 32: 20.3; 16384 x 1031, half filled, 41.4 and 33.7.
+  const auto width = [&](int per) {
+    for (p.ranks = 1;; p.ranks *= 2) {
+      p.slice = (int)(((N + p.ranks - 1) / p.ranks + 15) / 16 * 16);
+      if ((N < p.slice ? N : p.slice) + edge <= kLnThreads * per) break;
+    }
+    p.per = per;
+    const int w = (int)(N < p.slice ? N : p.slice) + edge;
+    for (p.warps = 1; p.warps * 32 * per < w; p.warps *= 2) {}
+    return 4 * w > 3 * p.warps * 32 * per;      // more than three quarters used
+  };
+  if (grad) width(16);
+  else if (mode != kLnEdges || !width(16) || p.ranks > 1) width(32);
+  if (mode == kLnSingle || p.ranks > 1) p.warps = 16;
   const int groups = kLnThreads / 32 / p.warps;
-  // Two (backward) or three blocks per SM; and backward, whose blocks each leave a row of sums, at least four rows for every group.
-  const int64_t most = (grad ? 2 : 3) * kLnSms / p.ranks, per = grad ? 4 : 1, want = (M + groups * per - 1) / (groups * per);
+  // One block per SM; backward, whose blocks each leave a row of sums, at least two rows for every group, and one block for up to four.
+  const int64_t most = kLnSms / p.ranks, rows = grad ? (M <= 4 * groups ? 4 : 2) : 1, want = (M + groups * rows - 1) / (groups * rows);
   p.clusters = (int)(want < most ? want : most);
+  if (mode == kLnEdges && (int64_t)p.clusters * groups < M) {      // a group's rows are a multiple of 16 bytes apart
+    int apart = 1;
+    while (((int64_t)apart * groups * N * elt) % 16) apart *= 2;
+    p.clusters = p.clusters < apart ? apart : p.clusters / apart * apart;
+  }
   p.pitch = (int)((N + 15) / 16 * 16);
   return p;
 }
 
-template <class E, int W, bool ALIGNED>
+template <class E, int W, int PER, int MODE>
 static int ln_launch(bool grad, const LnArgs& a, const LnPlan& p, cudaStream_t stream) {
-  const uint32_t smem = kLnRedBytes + (uint32_t)(kLnThreads / 32 / W) * kLnDepth * (grad ? 2 : 1) * a.slot;
-  auto kern = grad ? layernorm_grad_kernel<E, W, ALIGNED> : layernorm_kernel<E, W, ALIGNED>;
+  const int slots = grad ? 2 * kLnDepth<E, PER, 2> : kLnDepth<E, PER, 1>;
+  const uint32_t smem = kLnRedBytes + (uint32_t)(kLnThreads / 32 / W * slots) * a.slot;
+  void (*kern)(LnArgs) = layernorm_kernel<E, W, PER, MODE>;
+  if constexpr (PER == 16)
+    if (grad) kern = layernorm_grad_kernel<E, W, PER, MODE>;
   static uint64_t configured[2] = {0, 0};
   if (first_use_on_this_device(configured[grad])) {
     const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kProdSmemLimit);
@@ -510,27 +705,42 @@ static int ln_launch(bool grad, const LnArgs& a, const LnPlan& p, cudaStream_t s
   return launch_pdl(grad ? "layer norm gradient" : "layer norm", kern, dim3((unsigned)(p.clusters * p.ranks)), kLnThreads, smem, p.ranks, stream, a);
 }
 
+template <class E, int PER, int MODE>
+static int ln_warps(bool grad, const LnArgs& a, const LnPlan& p, cudaStream_t stream) {
+  if constexpr (MODE != kLnSingle) {
+    switch (p.warps) {
+      case 1: return ln_launch<E, 1, PER, MODE>(grad, a, p, stream);
+      case 2: return ln_launch<E, 2, PER, MODE>(grad, a, p, stream);
+      case 4: return ln_launch<E, 4, PER, MODE>(grad, a, p, stream);
+      case 8: return ln_launch<E, 8, PER, MODE>(grad, a, p, stream);
+    }
+  }
+  return ln_launch<E, 16, PER, MODE>(grad, a, p, stream);
+}
+
 template <class E>
-static int ln_run(bool grad, const LnArgs& a, const LnPlan& p, bool aligned, cudaStream_t stream) {
-  switch (p.warps) {
-    case 1: return aligned ? ln_launch<E, 1, true>(grad, a, p, stream) : ln_launch<E, 1, false>(grad, a, p, stream);
-    case 2: return aligned ? ln_launch<E, 2, true>(grad, a, p, stream) : ln_launch<E, 2, false>(grad, a, p, stream);
-    case 4: return aligned ? ln_launch<E, 4, true>(grad, a, p, stream) : ln_launch<E, 4, false>(grad, a, p, stream);
-    default: return aligned ? ln_launch<E, 8, true>(grad, a, p, stream) : ln_launch<E, 8, false>(grad, a, p, stream);
+static int ln_run(bool grad, const LnArgs& a, const LnPlan& p, cudaStream_t stream) {
+  switch (p.mode) {
+    case kLnWhole: return p.per == 16 ? ln_warps<E, 16, kLnWhole>(grad, a, p, stream) : ln_warps<E, 32, kLnWhole>(grad, a, p, stream);
+    case kLnEdges: return p.per == 16 ? ln_warps<E, 16, kLnEdges>(grad, a, p, stream) : ln_warps<E, 32, kLnEdges>(grad, a, p, stream);
+    default: return p.per == 16 ? ln_warps<E, 16, kLnSingle>(grad, a, p, stream) : ln_warps<E, 32, kLnSingle>(grad, a, p, stream);
   }
 }
 
-static int ln_any(bool grad, LnArgs& a, int32_t dtype, cudaStream_t stream, LnPlan* plan) {
-  const LnPlan p = ln_plan(a.M, a.N, grad);
+// How the rows lie.
+static int ln_mode(const LnArgs& a, int elt) {
+  const uintptr_t x = (uintptr_t)a.x, dy = a.dy ? (uintptr_t)a.dy : x, out = a.out ? (uintptr_t)a.out : x;
+  if (((x ^ dy) | (x ^ out)) & 15u) return kLnSingle;
+  return (x & 15u) == 0 && (int64_t)a.N * elt % 16 == 0 ? kLnWhole : kLnEdges;
+}
+
+static int ln_any(bool grad, LnArgs& a, int32_t dtype, cudaStream_t stream, const LnPlan& p) {
   a.slice = p.slice; a.clusters = p.clusters; a.pitch = p.pitch;
   a.slot = (uint32_t)p.slice * ln_bytes(dtype) + 16;
-  // rows of whole 16-byte units at 16-byte addresses
-  const bool aligned = ((int64_t)a.N * ln_bytes(dtype)) % 16 == 0 && (((uintptr_t)a.x | (uintptr_t)a.dy | (uintptr_t)a.out) & 15u) == 0;
-  *plan = p;
   std::lock_guard<std::mutex> lock(g_ln_mu);
-  if (dtype == SP_BF16) return ln_run<LnBf16>(grad, a, p, aligned, stream);
-  if (dtype == SP_FP16) return ln_run<LnFp16>(grad, a, p, aligned, stream);
-  return ln_run<LnFp32>(grad, a, p, aligned, stream);
+  if (dtype == SP_BF16) return ln_run<Ln16<true>>(grad, a, p, stream);
+  if (dtype == SP_FP16) return ln_run<Ln16<false>>(grad, a, p, stream);
+  return ln_run<Ln32>(grad, a, p, stream);
 }
 
 static int check_ln(int64_t M, int64_t N, int32_t dtype, int32_t w_dtype) {
@@ -570,14 +780,18 @@ int sp_layernorm(const void* x, const void* gamma, const void* beta, void* y, fl
   LnArgs a = {};
   a.x = (const char*)x; a.gamma = gamma; a.beta = beta; a.out = (char*)y; a.mean = mean; a.rstd = rstd;
   a.M = M; a.N = (int)N; a.w_dtype = w_dtype; a.eps = eps;
-  LnPlan p;
-  return ln_any(false, a, dtype, (cudaStream_t)stream, &p);
+  return ln_any(false, a, dtype, (cudaStream_t)stream, ln_plan(M, N, ln_bytes(dtype), false, ln_mode(a, ln_bytes(dtype))));
 }
 
 int64_t sp_layernorm_workspace(int64_t M, int64_t N) {
   if (M <= 0 || N <= 0 || M >= (1ll << 31) || N > kLnMaxN) return -1;
-  const LnPlan p = ln_plan(M, N, true);
-  return (int64_t)p.clusters * 2 * p.pitch * 4;
+  int64_t most = 0;      // whatever the type and the addresses are
+  for (int mode : {kLnWhole, kLnEdges, kLnSingle})
+    for (int elt : {2, 4}) {
+      const LnPlan p = ln_plan(M, N, elt, true, mode);
+      if ((int64_t)p.clusters * 2 * p.pitch * 4 > most) most = (int64_t)p.clusters * 2 * p.pitch * 4;
+    }
+  return most;
 }
 
 int sp_layernorm_grad(const void* dy, const void* x, const void* gamma, const float* mean, const float* rstd, void* dx, void* dgamma, void* dbeta,
@@ -608,11 +822,12 @@ int sp_layernorm_grad(const void* dy, const void* x, const void* gamma, const fl
   if (rc != SP_OK) return rc;
   LnArgs a = {};
   a.x = (const char*)x; a.dy = (const char*)dy; a.gamma = gamma; a.out = (char*)dx; a.mean = const_cast<float*>(mean); a.rstd = const_cast<float*>(rstd);
-  a.part = weights ? (float*)workspace : nullptr;
   a.M = M; a.N = (int)N; a.w_dtype = w_dtype;
-  LnPlan p;
-  rc = ln_any(true, a, dtype, (cudaStream_t)stream, &p);
-  if (rc == SP_OK && weights)
+  const LnPlan p = ln_plan(M, N, ln_bytes(dtype), true, ln_mode(a, ln_bytes(dtype)));
+  if (p.clusters > 1) a.part = weights ? (float*)workspace : nullptr;
+  else { a.dgamma = dgamma; a.dbeta = dbeta; }
+  rc = ln_any(true, a, dtype, (cudaStream_t)stream, p);
+  if (rc == SP_OK && a.part)
     rc = launch_pdl("layer norm gradient of the weights", layernorm_weights_kernel, dim3((unsigned)((N + 31) / 32), 2), 512, 0, 1, (cudaStream_t)stream,
                     (const float*)a.part, p.clusters, p.pitch, (int)N, w_dtype, dgamma, dbeta);
   return rc;
