@@ -429,6 +429,43 @@ int sp_linear_ce_grad(const void* h, const void* W, const int64_t* target, const
  * bytes where that is less), a copy of h, and fp32 sums of dh (one copy, or up to 64 while dh has few tiles). */
 int64_t sp_linear_ce_workspace(int64_t T, int64_t V, int64_t D, int32_t grad);
 
+/* Distillation from a teacher's top logits: the divergence of a student's vocabulary distribution from the teacher's, of which K words per token are known.
+ *   z = h . W^T / temperature in fp32,  lse[t] = log sum_v exp z[t][v],  p = exp(z - lse);
+ *   q[t][v]: softmax of the token's top_logit / temperature over its words, 0 for every other word (of a word that stands twice the sum);
+ *   loss[t] = temperature^2 * sum_v q[t][v] * (log q[t][v] - log p[t][v]).
+ * As in sp_linear_ce the T x V scores are never stored.
+ *   h, W      : DEVICE, T x D and V x D row-major, SP_BF16 or SP_FP16 (`dtype`), read-only.
+ *   top_index : DEVICE, T x K int64: the teacher's words, in any order.  A negative one is not used (a token may have fewer than K); one of V and beyond makes
+ *               the token's loss, lse and diff NaN.
+ *   top_logit : DEVICE, T x K, `top_dtype` SP_BF16, SP_FP16 or SP_FP32.  Minus infinity: q is 0 there.  A NaN or plus infinity makes the token's loss NaN.
+ *   A token without a word, or without one whose logit is above minus infinity, does not count: loss 0, lse plus infinity, diff 0.
+ *   lse       : DEVICE, T fp32;  diff : DEVICE, T x K fp32: p - q at the words of top_index (0 where not used).  The gradient call reads both.
+ *   loss      : DEVICE, fp32: T values (SP_REDUCE_NONE), or one: their sum (SP_REDUCE_SUM) or the sum over the number of tokens that count (SP_REDUCE_MEAN; 0 / 0 =
+ *               NaN when none does).
+ *   temperature : from SP_DISTILL_MIN_TEMPERATURE to SP_DISTILL_MAX_TEMPERATURE.
+ *   workspace : DEVICE, 16-byte aligned, sp_linear_distill_workspace(T, V, D, K, 0) bytes, the caller's, as for sp_linear_ce.
+ * Small losses and differences keep their digits (none is a difference of nearly equal numbers).  K up to SP_DISTILL_MAX_TOP; sizes, overlaps, order of sums, capture and
+ * errors as sp_linear_ce (temperature out of range: SP_ERR_INVALID_ARG). */
+#define SP_DISTILL_MAX_TOP 1024
+#define SP_DISTILL_MIN_TEMPERATURE 1e-4f
+#define SP_DISTILL_MAX_TEMPERATURE 1e4f
+int sp_linear_distill(const void* h, const void* W, const int64_t* top_index, const void* top_logit, int32_t top_dtype, float* lse, float* diff, float* loss,
+                      int64_t T, int64_t V, int64_t D, int64_t K, int32_t dtype, float temperature, int32_t reduction, void* workspace, int64_t workspace_bytes,
+                      void* stream);
+
+/* Its gradients:  g[t][v] = c[t] * temperature * (p[t][v] - q[t][v]),  dh = g . W,  dW = g^T . h,  c as in sp_linear_ce_grad (0 for a token that does not count).
+ * The scores are made again, the vocabulary in pieces; g is held in h's type, sums in fp32.  A token that does not count adds exactly nothing, whatever its row of h
+ * holds, and its row of dh is zero.
+ *   top_index, lse, diff : as given to and left by sp_linear_distill.   grad_loss, dh, dW : as in sp_linear_ce_grad.
+ *   workspace : sp_linear_distill_workspace(T, V, D, K, 1) bytes.   Otherwise as sp_linear_ce_grad. */
+int sp_linear_distill_grad(const void* h, const void* W, const int64_t* top_index, const float* lse, const float* diff, const float* grad_loss, void* dh, void* dW,
+                           int64_t T, int64_t V, int64_t D, int64_t K, int32_t dtype, float temperature, int32_t reduction, void* workspace, int64_t workspace_bytes,
+                           void* stream);
+
+/* Bytes of workspace sp_linear_distill (grad = 0) or sp_linear_distill_grad (grad != 0) needs; -1 on sizes that those refuse.  Host only.
+ * Forward: 10 bytes for every token and 128 words, 20 for each of the teacher's, and at most one copy of h.  Gradient: as sp_linear_ce_workspace. */
+int64_t sp_linear_distill_workspace(int64_t T, int64_t V, int64_t D, int64_t K, int32_t grad);
+
 /* Layer norm of the rows of x:  y[m][n] = (x[m][n] - mean[m]) * rstd[m] * gamma[n] + beta[n],  mean[m] = sum_n x[m][n] / N,
  * rstd[m] = 1 / sqrt(sum_n (x[m][n] - mean[m])^2 / N + eps), in fp32, y rounded once.
  *   x, y        : DEVICE, M x N row-major, SP_BF16, SP_FP16 or SP_FP32 (`dtype`).  Any addresses and N that hold whole elements; rows of whole

@@ -59,7 +59,7 @@ TRACE_DTYPE = np.dtype([("slot", "<i4"), ("tile", "<i4"), ("smid", "<i4"), ("uni
 
 EXPORTS = ["sp_tile_count", "sp_tile_map", "sp_tile_map_device", "sp_gemm", "sp_gemm_trace", "sp_gemm_host",
            "sp_gemm_noalloc", "sp_quantize_i8", "sp_gemm_i8", "sp_linear_i8", "sp_linear_ce", "sp_linear_ce_grad", "sp_linear_ce_workspace",
-           "sp_layernorm", "sp_layernorm_grad", "sp_layernorm_workspace",
+           "sp_linear_distill", "sp_linear_distill_grad", "sp_linear_distill_workspace", "sp_layernorm", "sp_layernorm_grad", "sp_layernorm_workspace",
            "sp_transpose", "sp_stencil2d", "sp_softmax", "sp_gemm_units", "sp_streamk_plan", "sp_recommend",
            "sp_probe_dispatch", "sp_probe_topology", "sp_probe_l2_capacity", "sp_selftest_timeout", "sp_selftest_pinned_tickets", "sp_get_status", "sp_last_error", "sp_shutdown"]
 
@@ -114,6 +114,12 @@ def lib() -> ctypes.CDLL:
         L.sp_linear_ce_grad.argtypes = [vp, vp, vp, vp, vp, vp, vp, i64, i64, i64, i32, i64, i32, vp, i64, vp]
         L.sp_linear_ce_workspace.restype = i64
         L.sp_linear_ce_workspace.argtypes = [i64, i64, i64, i32]
+        L.sp_linear_distill.restype = ctypes.c_int
+        L.sp_linear_distill.argtypes = [vp, vp, vp, vp, i32, vp, vp, vp, i64, i64, i64, i64, i32, ctypes.c_float, i32, vp, i64, vp]
+        L.sp_linear_distill_grad.restype = ctypes.c_int
+        L.sp_linear_distill_grad.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, i64, i64, i64, i64, i32, ctypes.c_float, i32, vp, i64, vp]
+        L.sp_linear_distill_workspace.restype = i64
+        L.sp_linear_distill_workspace.argtypes = [i64, i64, i64, i64, i32]
         L.sp_layernorm.restype = ctypes.c_int
         L.sp_layernorm.argtypes = [vp, vp, vp, vp, vp, vp, i64, i64, i32, i32, ctypes.c_float, vp]
         L.sp_layernorm_grad.restype = ctypes.c_int
@@ -502,6 +508,63 @@ def linear_ce_grad(h, W, target, lse, grad_loss, dh, dW, reduction: str = "mean"
     _check(lib().sp_linear_ce_grad(h.data_ptr(), W.data_ptr(), target.data_ptr(), lse.data_ptr(), None if grad_loss is None else grad_loss.data_ptr(),
                                    None if dh is None else dh.data_ptr(), None if dW is None else dW.data_ptr(), T, V, D, code, ignore_index,
                                    _REDUCE[reduction], ws.data_ptr(), n, _stream_on(here, stream)))
+
+
+DISTILL_MAX_TOP = 1024
+DISTILL_MIN_TEMPERATURE, DISTILL_MAX_TEMPERATURE = 1e-4, 1e4
+
+
+def linear_distill_workspace(T: int, V: int, D: int, K: int, grad: bool = False) -> int:
+    """Bytes of workspace linear_distill (or, with ``grad``, linear_distill_grad) needs."""
+    n = int(lib().sp_linear_distill_workspace(T, V, D, K, int(grad)))
+    if n < 0:
+        raise SpError(ERR_INVALID_ARG, f"sizes must be positive, K at most {DISTILL_MAX_TOP}, the others below 2^31 each and below about 2^39 in pairs")
+    return n
+
+
+def linear_distill(h, W, top_index, top_logit, lse, diff, loss, temperature: float = 1.0, reduction: str = "mean", workspace=None, stream=None) -> None:
+    """Distillation of the scores h [T, D] . W [V, D]^T from a teacher's top logits, without storing the scores (asynchronous): temperature^2 times the divergence of
+    softmax(scores / temperature) from the softmax of top_logit [T, K] / temperature at the words top_index [T, K] (int64; negative: not used).
+    Fills lse [T] and diff [T, K] (kept for linear_distill_grad) and loss: [T] for reduction "none", [1] for "mean" (over the tokens that have a word) and
+    "sum".  ``workspace``: a CUDA tensor of linear_distill_workspace(T, V, D, K) bytes, allocated here when not given."""
+    import torch
+    if reduction not in _REDUCE:
+        raise ValueError(f"unknown reduction {reduction!r}")
+    (T, D), V, K = h.shape, W.shape[0], top_index.shape[-1]
+    _expect("shapes of W, top_index, top_logit, lse, diff, loss", (W.shape, top_index.shape, top_logit.shape, lse.shape, diff.shape, loss.shape),
+            ((V, D), (T, K), (T, K), (T,), (T, K), (T if reduction == "none" else 1,)))
+    _expect("types of W, top_index, lse, diff, loss", (W.dtype, top_index.dtype, lse.dtype, diff.dtype, loss.dtype),
+            (h.dtype, torch.int64, torch.float32, torch.float32, torch.float32))
+    code, top_code = _dtype_code(h, (BF16, FP16)), _dtype_code(top_logit, (BF16, FP32, FP16))
+    here = _device_tensors(h, W, top_index, top_logit, lse, diff, loss)
+    ws, n = _workspace(workspace, h, 0 if workspace is not None else linear_distill_workspace(T, V, D, K), stream)
+    _check(lib().sp_linear_distill(h.data_ptr(), W.data_ptr(), top_index.data_ptr(), top_logit.data_ptr(), top_code, lse.data_ptr(), diff.data_ptr(), loss.data_ptr(),
+                                   T, V, D, K, code, temperature, _REDUCE[reduction], ws.data_ptr(), n, _stream_on(here, stream)))
+
+
+def linear_distill_grad(h, W, top_index, lse, diff, grad_loss, dh, dW, temperature: float = 1.0, reduction: str = "mean", workspace=None, stream=None) -> None:
+    """Gradients of linear_distill: dh [T, D] and dW [V, D] (either may be None) for the gradient ``grad_loss`` of the loss ([T] or [1] fp32; None: ones).
+    ``top_index``, ``temperature`` and ``reduction`` as given to linear_distill, ``lse`` and ``diff`` as it left them; ``workspace``:
+    linear_distill_workspace(T, V, D, K, grad=True) bytes (asynchronous)."""
+    import torch
+    if reduction not in _REDUCE:
+        raise ValueError(f"unknown reduction {reduction!r}")
+    (T, D), V, K = h.shape, W.shape[0], top_index.shape[-1]
+    _expect("shapes of W, top_index, lse, diff", (W.shape, top_index.shape, lse.shape, diff.shape), ((V, D), (T, K), (T,), (T, K)))
+    _expect("types of W, top_index, lse, diff", (W.dtype, top_index.dtype, lse.dtype, diff.dtype), (h.dtype, torch.int64, torch.float32, torch.float32))
+    tensors = [h, W, top_index, lse, diff]
+    if grad_loss is not None:
+        _expect("shape and type of grad_loss", (grad_loss.shape, grad_loss.dtype), ((T if reduction == "none" else 1,), torch.float32))
+        tensors.append(grad_loss)
+    for g, like in ((dh, h), (dW, W)):
+        if g is not None:
+            _expect("shape and type of a gradient", (g.shape, g.dtype), (like.shape, like.dtype))
+            tensors.append(g)
+    code = _dtype_code(h, (BF16, FP16))
+    here = _device_tensors(*tensors)
+    ws, n = _workspace(workspace, h, 0 if workspace is not None else linear_distill_workspace(T, V, D, K, grad=True), stream)
+    _check(lib().sp_linear_distill_grad(h.data_ptr(), W.data_ptr(), top_index.data_ptr(), lse.data_ptr(), diff.data_ptr(), _ptr(grad_loss), _ptr(dh), _ptr(dW), T, V, D, K,
+                                        code, temperature, _REDUCE[reduction], ws.data_ptr(), n, _stream_on(here, stream)))
 
 
 LAYERNORM_MAX_N = 32768

@@ -8,27 +8,12 @@
 // Gradient: the vocabulary is walked in pieces.  A piece's scores are made again, turned into g in the epilogue and written as 16 bits;
 // two more products read them: dh += g . W_piece (k = the vocabulary) and dW_piece = g^T . h (k = the tokens).  Where a token is nearly
 // certain of its word, its own entry is made from the others' (see kRestStep).
-#include <math_constants.h>
-
-#include <mutex>
 #include <new>
 #include <vector>
 
-#include "product.cuh"
+#include "linear_ce.cuh"
 
 namespace sp {
-
-constexpr float kLog2e = 1.4426950408889634f;
-constexpr float kLn2 = 0.6931471805599453f;
-constexpr int kCeTile = 256;     // vocabulary columns of one tile, at most
-constexpr int kCePart = 128;     // and of one epilogue warp, at most
-constexpr int kMaxSplits = 64;   // slices of the vocabulary in the product for dh
-
-__device__ __forceinline__ float ex2(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
 
 __device__ __forceinline__ void tma_store_3d(const CUtensorMap* map, uint32_t src, int x, int y, int z) {
   asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.tile.bulk_group [%0, {%1, %2, %3}], [%4];"
@@ -48,7 +33,6 @@ __device__ __forceinline__ void tma_add_3d(const CUtensorMap* map, uint32_t src,
 // came out 1.8e-6 too small, over 8192 4e-6.  So an accumulator takes 512 products only and the epilogue adds such sums, rounded to
 // nearest: 2e-7, in the same time (256 products: 1e-7, and 11 % more time at D = 1024).
 // What bounds it: 128 x 256 exponentials per CTA and tile at 16 a clock, 2048 cycles beside 512 for every 64 of D.
-constexpr int kCeSum = 8;      // stages of 64 products per accumulator
 struct EpiStats {
   static constexpr uint32_t kBytes = 0;
   static constexpr bool kSums = true;
@@ -124,20 +108,6 @@ struct RowArgs {
   int V, D;
   int bf16;
 };
-
-__device__ __forceinline__ void row_values(uint32_t u, int bf16, float& lo, float& hi) {
-  if (bf16) {
-    lo = __uint_as_float(u << 16); hi = __uint_as_float(u & 0xffff0000u);
-  } else {
-    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&u));
-    lo = f.x; hi = f.y;
-  }
-}
-
-__device__ __forceinline__ void join_pair(float2& a, float2 p) {
-  const float m = fmaxf(a.x, p.x), ref = m == -CUDART_INF_F ? 0.f : m;      // nothing finite yet: every term is exp2(-inf) = 0
-  a = make_float2(m, a.y * ex2(a.x - ref) + p.y * ex2(p.x - ref));
-}
 
 __global__ void __launch_bounds__(kRowThreads, 2) row_stats_kernel(const RowArgs a) {
   extern __shared__ __align__(16) float row_token[];      // D
@@ -217,72 +187,19 @@ struct CeJoin {
   int mean;
 };
 
-// Mean or sum of the per-token losses in a fixed order, in fp64.  One block.
-__device__ void reduce_losses(const CeJoin& a) {
-  __shared__ double part_s[32];
-  __shared__ int part_n[32];
-  double s = 0;
-  int n = 0;
-  for (int64_t t = threadIdx.x; t < a.T; t += blockDim.x) {
-    s += a.each[t];
-    n += a.target[t] != a.ignore;
-  }
-  for (int o = 16; o; o >>= 1) {
-    s += __shfl_xor_sync(0xffffffffu, s, o);
-    n += __shfl_xor_sync(0xffffffffu, n, o);
-  }
-  if ((threadIdx.x & 31) == 0) { part_s[threadIdx.x >> 5] = s; part_n[threadIdx.x >> 5] = n; }
-  __syncthreads();
-  if (threadIdx.x == 0) {
-    for (int i = 1; i < (int)blockDim.x / 32; ++i) { s += part_s[i]; n += part_n[i]; }
-    a.loss[0] = (float)(a.mean ? s / n : s);     // no token left by the mask: 0 / 0
-  }
-}
-
-// 2^shift rows per block (32, or 4 when no more tokens are there); blockDim >> shift threads share a row's pairs, whose reads do not wait
-// for one another.  (Eight threads per row, joining pair after pair, took 6 us for one token's 296 pairs: a chain of trips to L2.)
+// 2^shift rows per block.
 __global__ void __launch_bounds__(1024) ce_join_kernel(const CeJoin a, int shift) {
   pdl_begin();
   __shared__ float2 part[1024];
-  const int rows = 1 << shift, groups = (int)blockDim.x >> shift;
-  const int r = threadIdx.x & (rows - 1), g = threadIdx.x >> shift, lane = threadIdx.x & 31;
+  const int rows = 1 << shift, r = threadIdx.x & (rows - 1);
   for (int64_t first = (int64_t)blockIdx.x << shift; first < a.T; first += (int64_t)gridDim.x << shift) {
     const bool ends = (int)threadIdx.x < rows && first + r < a.T;      // this thread finishes a row
     const int64_t y = ends ? __ldg(a.target + first + r) : -1;
     const bool hit = ends && y >= 0 && y < a.V;
     const float picked = hit ? a.picked[first + r] : -CUDART_INF_F;      // no word of the vocabulary: no term of its own
-    float2 pair = make_float2(-CUDART_INF_F, 0.f);
-    if (first + r < a.T) {
-      const float2* at = a.stats + first + r;
-      for (int i = g; i < a.tiles; i += 8 * groups) {
-        float2 p[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) p[j] = i + j * groups < a.tiles ? __ldg(at + (int64_t)(i + j * groups) * a.T) : make_float2(-CUDART_INF_F, 0.f);
-        float m = pair.x;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) m = fmaxf(m, p[j].x);
-        const float ref = m == -CUDART_INF_F ? 0.f : m;
-        float s = pair.y * ex2(pair.x - ref);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) s = fmaf(p[j].y, ex2(p[j].x - ref), s);
-        pair = make_float2(m, s);
-      }
-    }
-    part[threadIdx.x] = pair;
-    __syncthreads();
-    if (groups > 8) {      // a warp per row first
-      for (int row = threadIdx.x >> 5; row < rows; row += blockDim.x >> 5) {
-        pair = make_float2(-CUDART_INF_F, 0.f);
-        for (int i = lane; i < groups; i += 32) join_pair(pair, part[i * rows + row]);
-#pragma unroll
-        for (int o = 16; o; o >>= 1) join_pair(pair, make_float2(__shfl_xor_sync(0xffffffffu, pair.x, o), __shfl_xor_sync(0xffffffffu, pair.y, o)));
-        if (lane == 0) part[row] = pair;      // slot `row` is group 0's of this row: read above by this warp only
-      }
-      __syncthreads();
-    }
+    join_rows(a.stats, a.T, a.tiles, first, shift, part);
     if (ends) {
-      pair = part[r];
-      for (int i = 1; i < groups && groups <= 8; ++i) join_pair(pair, part[i * rows + r]);
+      const float2 pair = joined_row(part, r, shift);
       // With `own` the target's exponent against the larger maximum, its product not rounded, and `rest` the sum of the others: lse = ref + log2(rest +
       // 2^own), and the loss is log(1 + rest / 2^own), whose digits do not depend on the size of the scores.  (lse - picked, in scores of 30:
       // losses below 1e-5 were noise of +-4e-6.)
@@ -296,33 +213,16 @@ __global__ void __launch_bounds__(1024) ce_join_kernel(const CeJoin a, int shift
   }
   if (a.loss != nullptr && gridDim.x == 1) {
     __syncthreads();
-    reduce_losses(a);
+    reduce_losses(a.each, a.T, a.mean, a.loss, [&](int64_t t) { return a.target[t] != a.ignore; });
   }
 }
 
 __global__ void __launch_bounds__(1024) ce_reduce_kernel(const CeJoin a) {
   pdl_begin();
-  reduce_losses(a);
+  reduce_losses(a.each, a.T, a.mean, a.loss, [&](int64_t t) { return a.target[t] != a.ignore; });
 }
 
 // ------------------------------------------------------------------ gradient
-struct CePrep {
-  const int64_t* target;
-  const float* grad;     // per token (none) or one number; nullptr: 1
-  float* coef;           // per token
-  float* factor;         // one number
-  const uint4* h;        // rows of `vecs` vectors of 8 elements ...
-  uint4* rows;           // ... copied to rows of `ld` vectors
-  int64_t T;
-  int vecs, ld;
-  int V;
-  int64_t ignore;
-  int reduction, fp16;
-  int masked;            // 1: rows of ignored tokens become zeros
-  unsigned long long* rest;   // per token: set to 0 ...
-  int32_t* count;             // ... and this one number too
-};
-
 // The tokens' rows once more, each on a cache line of its own (a row of a tile's 128 bytes then takes one line of L2, not two: 1001 x 50001 x
 // 1032 forward 123 us without, 116 with) and, for the gradient, zeros where a token does not count: dW adds 0 x h for those, and what an
 // ignored row holds need not be finite.
@@ -331,7 +231,7 @@ __device__ __forceinline__ void ce_copy_rows(const CePrep& a, int block, int blo
   for (int64_t i = (int64_t)block * blockDim.x + threadIdx.x; i < n; i += (int64_t)blocks * blockDim.x) {
     const int64_t t = i / a.vecs;
     const uint4 v = __ldg(a.h + i);
-    a.rows[t * a.ld + (i - t * a.vecs)] = a.masked && __ldg(a.target + t) == a.ignore ? make_uint4(0u, 0u, 0u, 0u) : v;
+    a.rows[t * a.ld + (i - t * a.vecs)] = a.masked && !a.kept(t) ? make_uint4(0u, 0u, 0u, 0u) : v;
   }
 }
 
@@ -358,7 +258,7 @@ __global__ void __launch_bounds__(1024) ce_prep_kernel(const CePrep a) {
   int n = 0;
   float top = 0.f;
   for (int64_t t = threadIdx.x; t < a.T; t += 1024) {
-    const bool kept = a.target[t] != a.ignore;
+    const bool kept = a.kept(t);
     n += kept;
     if (kept && a.reduction == SP_REDUCE_NONE && a.grad) top = fmaxf(top, fabsf(a.grad[t]));
   }
@@ -388,13 +288,12 @@ __global__ void __launch_bounds__(1024) ce_prep_kernel(const CePrep a) {
   }
   const float scale = exp2f((float)up);
   for (int64_t t = threadIdx.x; t < a.T; t += 1024) {
-    const int64_t y = a.target[t];
     float c = 0.f;
-    if (y != a.ignore) c = y < 0 || y >= a.V ? CUDART_NAN_F : (each ? a.grad[t] : wild) * scale;
+    if (a.kept(t)) c = a.lse == nullptr && (a.target[t] < 0 || a.target[t] >= a.V) ? CUDART_NAN_F : (each ? a.grad[t] : wild) * scale;
     a.coef[t] = c;
     a.rest[t] = 0;
   }
-  if (threadIdx.x == 0) { *a.factor = factor * exp2f((float)-up); *a.count = 0; }
+  if (threadIdx.x == 0) { *a.factor = factor * a.times * exp2f((float)-up); *a.count = 0; }
 }
 
 // The entry of a token's own word, p - 1, is the one that cancels: lse is a 32-bit number of the size of the scores, so p is off by |lse| 2^-23 or so,
@@ -550,18 +449,6 @@ struct EpiRest {
   }
 };
 
-// One staged slice of 64 16-bit columns to a matrix.
-__device__ __forceinline__ void store_part(const EpiStage& stage, const CUtensorMap* map, int lane, const uint32_t (&p)[32], bool inside, int col, int row) {
-  const uint32_t slice = stage.free();
-  stage_row(slice, lane, p);
-  fence_async_smem();
-  __syncwarp();
-  if (lane == 0 && inside) {
-    tma_store_2d(map, slice, col, row);
-    bulk_commit();
-  }
-}
-
 // g of a tile, to 16 bits: its rounding (at most half a step, 2^-8 of bf16 or 2^-11 of fp16 relative) is independent from entry to entry and
 // enters sums over the vocabulary or the tokens, so it moves a gradient by less than the gradient's own rounding to the same type.
 struct EpiG {
@@ -715,31 +602,9 @@ __global__ void __launch_bounds__(256) ce_finish_kernel(const float4* acc, int64
 }
 
 // ------------------------------------------------------------------ host side
-static std::mutex g_ce_mu;   // per-kernel set-up is done under it
+std::mutex g_ce_mu;
 
-static int64_t up256(int64_t b) { return (b + 255) & ~255ll; }
-static int64_t div_up(int64_t a, int64_t b) { return (a + b - 1) / b; }
-
-// Everything that follows from the sizes alone.
-struct CePlan {
-  int64_t T, V, D;
-  bool row;                   // forward: the form for one token
-  int64_t tiles;              // pairs per token that the forward product leaves: two per vocabulary tile, or one per block
-  int64_t piece, ld_g;        // gradient: vocabulary rows of a piece, row pitch of g
-  int pieces;
-  int slices;                 // of the vocabulary in the product for dh
-  bool copy;                  // forward: the tokens' rows are copied to cache lines of their own
-  int64_t ld_h;               // row pitch of such copies
-  int64_t off_picked, off_each, off_rows, forward_bytes;
-  int64_t off_factor, off_rest, off_list, off_grad_rows, off_g, off_acc, off_sure, grad_bytes;
-};
-
-// Rows of a token tile: a CTA pair's 256, or one CTA's 128 where no more tokens are there.  (Also for token counts that fill their last tile
-// badly the smaller one does not pay: it moves half as much again through L2 per product.  777 x 20011 x 1032: forward 54 us on
-// 4 x 256 rows, 58 on 7 x 128; dh 51 and 55.)
-static int ce_rows(int64_t T) { return T <= 128 ? 128 : 256; }
-
-static CePlan ce_plan(int64_t T, int64_t V, int64_t D) {
+CePlan ce_plan(int64_t T, int64_t V, int64_t D) {
   CePlan p = {};
   p.T = T; p.V = V; p.D = D;
   p.row = T == 1 && D <= kRowMaxD;
@@ -783,7 +648,7 @@ static CePlan ce_plan(int64_t T, int64_t V, int64_t D) {
 }
 
 // Sizes that every grid of tiles of the two calls can hold (kMaxTiles of at least 128 x 160), and below 2^31 each: asked before anything is launched.
-static bool ce_sizes(int64_t T, int64_t V, int64_t D) {
+bool ce_sizes(int64_t T, int64_t V, int64_t D) {
   if (T <= 0 || V <= 0 || D <= 0 || T >= (1ll << 31) - 512 || V >= (1ll << 31) - 512 || D >= (1ll << 31) - 512) return false;
   const int64_t rows = div_up(T, ce_rows(T)), width = tile_width(T, V, ce_rows(T) / 128, 32);
   return rows * div_up(V, width) <= kMaxTiles && rows * div_up(D, 256) <= kMaxTiles && div_up(V, 256) * div_up(D, 256) <= kMaxTiles;
@@ -807,7 +672,7 @@ static int check_ce(const void* h, const void* W, const void* target, const void
 // The tile grid of one product in bands of eight tile rows, walked serpentine-wise: a wave of tiles is then about as
 // tall as it is wide, so it needs few operand panels, and a band starts on the panels the last one used last.  `rows`: row-major, for an
 // output whose writing is what bounds the product: a wave then writes whole rows (dW of 16 tokens, 65536 x 4096: 106 us, in bands 114).
-static int ce_sched(int64_t M, int64_t N, int tile_m, int tile_n, Sched* out, bool rows = false) {
+int ce_sched(int64_t M, int64_t N, int tile_m, int tile_n, Sched* out, bool rows) {
   if (rows) return resolve_sched(M, N, tile_m, tile_n, SP_ROW_MAJOR, nullptr, out);
   sp_params p = {};
   p.struct_size = sizeof p;
@@ -816,7 +681,7 @@ static int ce_sched(int64_t M, int64_t N, int tile_m, int tile_n, Sched* out, bo
   return resolve_sched(M, N, tile_m, tile_n, SP_GROUP_M, &p, out);
 }
 
-static ProdArgs ce_args(const Sched& sched, int32_t* status, int64_t M, int64_t N, int64_t K, int slices) {
+ProdArgs ce_args(const Sched& sched, int32_t* status, int64_t M, int64_t N, int64_t K, int slices) {
   ProdArgs a = {};
   a.status = status;
   a.M = (int)M; a.N = (int)N; a.bn = 256;
@@ -827,35 +692,78 @@ static ProdArgs ce_args(const Sched& sched, int32_t* status, int64_t M, int64_t 
   return a;
 }
 
-// h . W_piece^T with an epilogue of scores.
-template <class Epi>
-static int ce_scores(const char* what, const CePlan& p, const void* h, int64_t ld_h, const void* W, int64_t cols, int32_t* status, bool bf16, const CUtensorMap* tmC,
-                     const typename Epi::Args& ea, cudaStream_t stream, const int32_t* live = nullptr) {
-  CUtensorMap tmA, tmB;
-  Sched sched;
-  const int rows = ce_rows(p.T), width = tile_width(p.T, cols, rows / 128, tmC ? 64 : 32);      // g is stored 64 columns at a time
-  int rc = ce_sched(p.T, cols, rows, width, &sched);
-  if (rc == SP_OK) rc = make_map_any(&tmA, h, 2, p.T, p.D, ld_h, 128, 64);
-  if (rc == SP_OK) rc = make_map_any(&tmB, W, 2, cols, p.D, p.D, width / (rows / 128), 64);
-  if (rc != SP_OK) return rc;
-  ProdArgs a = ce_args(sched, status, p.T, cols, p.D, 1);
-  a.turn = sched.Tm == 1;
-  a.live = live;
-  a.bn = width;
-  if (rows == 256) return launch_product<2, 256, kElem16, false, false, Epi>(what, tmA, tmB, tmC ? *tmC : tmA, a, bf16, ea, stream);
-  return launch_product<1, 256, kElem16, false, false, Epi>(what, tmA, tmB, tmC ? *tmC : tmA, a, bf16, ea, stream);
-}
-
-static CePrep ce_rows_args(const CePlan& p, const void* h, void* rows, const int64_t* target, int64_t ignore, bool masked) {
+CePrep ce_rows_args(const CePlan& p, const void* h, void* rows, const int64_t* target, int64_t ignore, bool masked) {
   CePrep a = {};
   a.target = target; a.h = (const uint4*)h; a.rows = (uint4*)rows; a.T = p.T; a.vecs = (int)(p.D / 8); a.ld = (int)(p.ld_h / 8);
-  a.ignore = ignore; a.masked = masked;
+  a.ignore = ignore; a.masked = masked; a.times = 1.f;
   return a;
 }
 
-static unsigned ce_copy_blocks(const CePlan& p) {      // four vectors per thread, at most two blocks per SM
+unsigned ce_copy_blocks(const CePlan& p) {      // four vectors per thread, at most two blocks per SM
   const int64_t b = div_up(p.T * (p.D / 8), 4096);
   return (unsigned)(b < 296 ? b : 296);
+}
+
+// The two products of a piece of the vocabulary, [v0, v0 + cols): dh (its first piece if v0 = 0) and dW's rows.
+int ce_products(const CePlan& p, const void* Wp, char* ws, void* dh, void* dW, int64_t v0, int64_t cols, bool bf16, int32_t* status, cudaStream_t stream) {
+  const int64_t T = p.T, D = p.D;
+  const float *coef = (const float*)ws, *factor = (const float*)(ws + p.off_factor);
+  char *g = ws + p.off_g, *rows = ws + p.off_grad_rows, *acc = ws + p.off_acc;
+  const bool summed = p.pieces > 1 || p.slices > 1;     // dh passes through fp32 sums
+  CUtensorMap tmA, tmB, tmC;
+  int rc = SP_OK;
+  if (dh) {
+    Sched sched;
+    rc = ce_sched(T, D, ce_rows(T), 256, &sched);
+    if (rc == SP_OK) rc = make_map_any(&tmA, g, 2, T, cols, p.ld_g, 128, 64);
+    if (rc == SP_OK) rc = make_map_any(&tmB, Wp, 2, cols, D, D, 64, 64);
+    if (rc != SP_OK) return rc;
+    ProdArgs a = ce_args(sched, status, T, D, cols, p.slices);
+    if (summed) {
+      rc = make_map_3d_f32(&tmC, acc, p.slices, T, D, 32, 32);
+      if (rc != SP_OK) return rc;
+      const EpiSum::Args es = {v0 > 0};
+      rc = ce_rows(T) == 256 ? launch_product<2, 256, kElem16, false, true, EpiSum>("gradient of h", tmA, tmB, tmC, a, bf16, es, stream)
+                           : launch_product<1, 256, kElem16, false, true, EpiSum>("gradient of h", tmA, tmB, tmC, a, bf16, es, stream);
+    } else {
+      rc = make_map_any(&tmC, dh, 2, T, D, D, 32, 64);
+      if (rc != SP_OK) return rc;
+      const EpiOut16<true>::Args eo = {factor, coef, bf16};
+      rc = ce_rows(T) == 256 ? launch_product<2, 256, kElem16, false, true, EpiOut16<true>>("gradient of h", tmA, tmB, tmC, a, bf16, eo, stream)
+                           : launch_product<1, 256, kElem16, false, true, EpiOut16<true>>("gradient of h", tmA, tmB, tmC, a, bf16, eo, stream);
+    }
+    if (rc != SP_OK) return rc;
+  }
+  if (dW) {
+    Sched sched;
+    rc = ce_sched(cols, D, 256, 256, &sched, T * D <= (8ll << 20));
+    if (rc == SP_OK) rc = make_map_any(&tmA, g, 2, T, cols, p.ld_g, 64, 64);
+    if (rc == SP_OK) rc = make_map_any(&tmB, rows, 2, T, D, p.ld_h, 64, 64);
+    if (rc == SP_OK) rc = make_map_any(&tmC, (char*)dW + v0 * D * 2, 2, cols, D, D, 32, 64);
+    if (rc != SP_OK) return rc;
+    ProdArgs a = ce_args(sched, status, cols, D, T, 1);
+    a.overlap = dh != nullptr;      // it reads g and h only: its CTAs take the SMs that dh leaves free
+    const EpiOut16<false>::Args eo = {factor, nullptr, bf16};
+    rc = launch_product<2, 256, kElem16, true, true, EpiOut16<false>>("gradient of W", tmA, tmB, tmC, a, bf16, eo, stream);
+    if (rc != SP_OK) return rc;
+  }
+  return rc;
+}
+
+// dh from its sums, where it has passed through them.
+int ce_finish(const CePlan& p, char* ws, void* dh, bool bf16, cudaStream_t stream) {
+  if (p.pieces == 1 && p.slices == 1) return SP_OK;
+  const int64_t n4 = p.T * p.D / 4;
+  return launch_pdl("sum of the slices", ce_finish_kernel, dim3((unsigned)div_up(n4, 256)), 256, 0, 1, stream, (const float4*)(ws + p.off_acc), n4, (int)(p.D / 4), p.slices,
+                    (const float*)(ws + p.off_factor), (const float*)ws, (int)bf16, (uint2*)dh);
+}
+
+int launch_ce_rows(const CePlan& p, const CePrep& a, cudaStream_t stream) {
+  return launch_pdl("copy of the tokens", ce_rows_kernel, dim3(ce_copy_blocks(p)), 1024, 0, 1, stream, a);
+}
+
+int launch_ce_prep(const CePlan& p, const CePrep& a, cudaStream_t stream) {
+  return launch_pdl("coefficients and rows of the tokens", ce_prep_kernel, dim3(1 + ce_copy_blocks(p)), 1024, 0, 1, stream, a);
 }
 
 static int launch_row(const RowArgs& a, int blocks, cudaStream_t stream) {
@@ -908,7 +816,7 @@ int sp_linear_ce(const void* h, const void* W, const int64_t* target, float* lse
   } else {
     if (p.copy) {
       CePrep prep = ce_rows_args(p, h, ws + p.off_rows, target, ignore_index, false);
-      rc = launch_pdl("copy of the tokens", ce_rows_kernel, dim3(ce_copy_blocks(p)), 1024, 0, 1, (cudaStream_t)stream, prep);
+      rc = launch_ce_rows(p, prep, (cudaStream_t)stream);
       if (rc != SP_OK) return rc;
     }
     rc = ce_scores<EpiStats>("vocabulary product", p, p.copy ? ws + p.off_rows : h, p.copy ? p.ld_h : D, W, V, st.status, dtype == SP_BF16, nullptr, ea, (cudaStream_t)stream);
@@ -955,7 +863,7 @@ int sp_linear_ce_grad(const void* h, const void* W, const int64_t* target, const
   if (rc != SP_OK) return rc;
   const bool bf16 = dtype == SP_BF16;
   char* ws = (char*)workspace;
-  float *coef = (float*)ws, *factor = (float*)(ws + p.off_factor), *acc = (float*)(ws + p.off_acc);
+  float *coef = (float*)ws, *factor = (float*)(ws + p.off_factor);
   char* g = ws + p.off_g;
   char* rows = ws + p.off_grad_rows;
   auto* rest = (unsigned long long*)(ws + p.off_rest);
@@ -963,7 +871,7 @@ int sp_linear_ce_grad(const void* h, const void* W, const int64_t* target, const
   CePrep prep = ce_rows_args(p, h, rows, target, ignore_index, true);
   prep.rest = rest; prep.count = count;
   prep.grad = grad_loss; prep.coef = coef; prep.factor = factor; prep.V = (int)V; prep.reduction = reduction; prep.fp16 = !bf16;
-  rc = launch_pdl("coefficients and rows of the tokens", ce_prep_kernel, dim3(1 + ce_copy_blocks(p)), 1024, 0, 1, stream, prep);
+  rc = launch_ce_prep(p, prep, stream);
   if (rc != SP_OK) return rc;
   if (p.pieces > 1) {
     uint4* sure = (uint4*)(ws + p.off_sure);
@@ -975,62 +883,16 @@ int sp_linear_ce_grad(const void* h, const void* W, const int64_t* target, const
     rc = ce_scores<EpiRest>("sums of the others", p, sure, p.ld_h, W, V, st.status, bf16, nullptr, er, stream, count);
     if (rc != SP_OK) return rc;
   }
-  const bool summed = p.pieces > 1 || p.slices > 1;     // dh passes through fp32 sums
-  for (int i = 0; i < p.pieces; ++i) {
-    const int64_t v0 = i * p.piece, cols = V - v0 < p.piece ? V - v0 : p.piece;
-    const char* Wp = (const char*)W + v0 * D * 2;
-    CUtensorMap tmG, tmA, tmB, tmC;
-    rc = make_map_any(&tmG, g, 2, T, cols, p.ld_g, 32, 64);
-    if (rc != SP_OK) return rc;
+  const auto scores = [&](int64_t v0, int64_t cols, const void* Wp, const CUtensorMap& tmG) {
     const EpiG::Args ea = {lse, coef, target, v0, rest, p.pieces > 1, bf16};
-    rc = ce_scores<EpiG>("gradient of the scores", p, rows, p.ld_h, Wp, cols, st.status, bf16, &tmG, ea, stream);
-    if (rc != SP_OK) return rc;
-    if (p.pieces == 1) {
+    int rc = ce_scores<EpiG>("gradient of the scores", p, rows, p.ld_h, Wp, cols, st.status, bf16, &tmG, ea, stream);
+    if (rc == SP_OK && p.pieces == 1) {
       const CeOwn co = {target, lse, coef, rest, (uint16_t*)g, p.ld_g, (int)T, (int)V, bf16};
       rc = launch_pdl("own words", ce_own_kernel, dim3((unsigned)div_up(T, 256)), 256, 0, 1, stream, co);
-      if (rc != SP_OK) return rc;
     }
-    if (dh) {
-      Sched sched;
-      rc = ce_sched(T, D, ce_rows(T), 256, &sched);
-      if (rc == SP_OK) rc = make_map_any(&tmA, g, 2, T, cols, p.ld_g, 128, 64);
-      if (rc == SP_OK) rc = make_map_any(&tmB, Wp, 2, cols, D, D, 64, 64);
-      if (rc != SP_OK) return rc;
-      ProdArgs a = ce_args(sched, st.status, T, D, cols, p.slices);
-      if (summed) {
-        rc = make_map_3d_f32(&tmC, acc, p.slices, T, D, 32, 32);
-        if (rc != SP_OK) return rc;
-        const EpiSum::Args es = {i > 0};
-        rc = ce_rows(T) == 256 ? launch_product<2, 256, kElem16, false, true, EpiSum>("gradient of h", tmA, tmB, tmC, a, bf16, es, stream)
-                             : launch_product<1, 256, kElem16, false, true, EpiSum>("gradient of h", tmA, tmB, tmC, a, bf16, es, stream);
-      } else {
-        rc = make_map_any(&tmC, dh, 2, T, D, D, 32, 64);
-        if (rc != SP_OK) return rc;
-        const EpiOut16<true>::Args eo = {factor, coef, bf16};
-        rc = ce_rows(T) == 256 ? launch_product<2, 256, kElem16, false, true, EpiOut16<true>>("gradient of h", tmA, tmB, tmC, a, bf16, eo, stream)
-                             : launch_product<1, 256, kElem16, false, true, EpiOut16<true>>("gradient of h", tmA, tmB, tmC, a, bf16, eo, stream);
-      }
-      if (rc != SP_OK) return rc;
-    }
-    if (dW) {
-      Sched sched;
-      rc = ce_sched(cols, D, 256, 256, &sched, T * D <= (8ll << 20));
-      if (rc == SP_OK) rc = make_map_any(&tmA, g, 2, T, cols, p.ld_g, 64, 64);
-      if (rc == SP_OK) rc = make_map_any(&tmB, rows, 2, T, D, p.ld_h, 64, 64);
-      if (rc == SP_OK) rc = make_map_any(&tmC, (char*)dW + v0 * D * 2, 2, cols, D, D, 32, 64);
-      if (rc != SP_OK) return rc;
-      ProdArgs a = ce_args(sched, st.status, cols, D, T, 1);
-      a.overlap = dh != nullptr;      // it reads g and h only: its CTAs take the SMs that dh leaves free
-      const EpiOut16<false>::Args eo = {factor, nullptr, bf16};
-      rc = launch_product<2, 256, kElem16, true, true, EpiOut16<false>>("gradient of W", tmA, tmB, tmC, a, bf16, eo, stream);
-      if (rc != SP_OK) return rc;
-    }
-  }
-  if (dh && summed) {
-    const int64_t n4 = T * D / 4;
-    rc = launch_pdl("sum of the slices", ce_finish_kernel, dim3((unsigned)div_up(n4, 256)), 256, 0, 1, stream, (const float4*)acc, n4, (int)(D / 4), p.slices,
-                    (const float*)factor, (const float*)coef, (int)bf16, (uint2*)dh);
-  }
+    return rc;
+  };
+  rc = ce_gradients(p, W, ws, dh, dW, bf16, st.status, stream, scores);
   return rc;
 } catch (const std::exception& e) {
   set_error("sp_linear_ce_grad: %s", e.what());
