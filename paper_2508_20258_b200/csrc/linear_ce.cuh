@@ -174,7 +174,7 @@ int ce_finish(const CePlan& p, char* ws, void* dh, bool bf16, cudaStream_t strea
 // h . W_piece^T with an epilogue of scores.
 template <class Epi>
 int ce_scores(const char* what, const CePlan& p, const void* h, int64_t ld_h, const void* W, int64_t cols, int32_t* status, bool bf16, const CUtensorMap* tmC,
-                     const typename Epi::Args& ea, cudaStream_t stream, const int32_t* live = nullptr) {
+                     const typename Epi::Args& ea, cudaStream_t stream, const int32_t* live = nullptr, int overlap = 0) {
   CUtensorMap tmA, tmB;
   Sched sched;
   const int rows = ce_rows(p.T), width = tile_width(p.T, cols, rows / 128, tmC ? 64 : 32);      // g is stored 64 columns at a time
@@ -185,6 +185,7 @@ int ce_scores(const char* what, const CePlan& p, const void* h, int64_t ld_h, co
   ProdArgs a = ce_args(sched, status, p.T, cols, p.D, 1);
   a.turn = sched.Tm == 1;
   a.live = live;
+  a.overlap = overlap;
   a.bn = width;
   if (rows == 256) return launch_product<2, 256, kElem16, false, false, Epi>(what, tmA, tmB, tmC ? *tmC : tmA, a, bf16, ea, stream);
   return launch_product<1, 256, kElem16, false, false, Epi>(what, tmA, tmB, tmC ? *tmC : tmA, a, bf16, ea, stream);

@@ -37,9 +37,6 @@ struct TeacherArgs {
 };
 enum : int { kIgnored = 0, kKept = 1, kInvalid = 2 };      // no word, or none with a logit above minus infinity; a word outside the vocabulary
 
-// The i-th of a token's sorted words is the first of its equals.
-__device__ __forceinline__ bool first_of(const int32_t* word, int i) { return word[i] != kNoWord && (i == 0 || word[i - 1] != word[i]); }
-
 // GROUP threads per token: a warp while its keys are few, else the block.
 template <int GROUP>
 __global__ void __launch_bounds__(256) teacher_kernel(const TeacherArgs a) {
@@ -121,15 +118,23 @@ __global__ void __launch_bounds__(256) teacher_kernel(const TeacherArgs a) {
       }
       a.word[t * a.K + i] = word; a.slot[t * a.K + i] = j; a.q[t * a.K + i] = q; a.lq[t * a.K + i] = lq;
     }
-    for (int p = i0; p <= a.parts; p += GROUP) {
-      const int64_t first = (int64_t)(p >> 1) * a.bn + (p & 1) * kCePart;      // a tile's two parts
-      int lo = 0, hi = a.K;
-      while (lo < hi) {
-        const int mid = (lo + hi) >> 1;
-        if ((int64_t)(key[mid] >> 32) < first) lo = mid + 1;
-        else hi = mid;
+    // words before each part's first column, four parts at a time: the steps of a search wait for one another
+    for (int p0 = i0; p0 <= a.parts; p0 += 4 * GROUP) {
+      uint64_t first[4];
+      int n[4];
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        const int p = p0 + c * GROUP;
+        first[c] = (uint64_t)((int64_t)(p >> 1) * a.bn + (p & 1) * kCePart) << 32;      // a tile's two parts
+        n[c] = 0;
       }
-      a.start[t * (a.parts + 1) + p] = (uint16_t)lo;
+      for (int step = a.size / 2; step; step /= 2)
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+          if (key[n[c] + step - 1] < first[c]) n[c] += step;
+#pragma unroll
+      for (int c = 0; c < 4; ++c)
+        if (p0 + c * GROUP <= a.parts) a.start[t * (a.parts + 1) + p0 + c * GROUP] = (uint16_t)(n[c] + (key[n[c]] < first[c]));
     }
     if (i0 == 0) a.state[t] = (int)state;
     sync();
@@ -161,8 +166,8 @@ struct EpiDistill {
     next = kNoWord;
     if (row < M) {
       const uint16_t* s = a.start + row * (a.parts + 1) + e.part;
-      at = __ldg(s); end = __ldg(s + 1);
-      if (at < end) next = __ldg(a.word + row * a.K + at) - e.col0;
+      at = s[0]; end = s[1];      // written while this kernel was running: not by way of the read-only cache
+      if (at < end) next = a.word[row * a.K + at] - e.col0;
     }
   }
   template <int COLS>
@@ -180,7 +185,7 @@ struct EpiDistill {
         const bool mine = next < q + 32;
         const int rel = mine ? next : -1;
         if (mine) {      // on its way while the columns are looked at
-          next = at + 1 < end ? __ldg(a.word + row * a.K + at + 1) - e.col0 : kNoWord;
+          next = at + 1 < end ? a.word[row * a.K + at + 1] - e.col0 : kNoWord;
         }
         float hit = -CUDART_INF_F;      // the second of two equal words finds its column empty
 #pragma unroll
@@ -246,7 +251,9 @@ __device__ __forceinline__ float divergence(float q, float p, float d) {
   return fmaf(q, d, p - q);
 }
 
-// 2^shift rows per block: their pairs are joined as the cross entropy's, then a warp takes a row's words.
+// 2^shift rows per block: their pairs are joined as the cross entropy's, a warp takes a row's words.  Up to 32 WORDS of them per row are in registers, asked for before
+// the pairs are joined; more are read where they are needed (WORDS 0).
+template <int WORDS>
 __global__ void __launch_bounds__(1024) distill_join_kernel(const DistillJoin a, int shift) {
   pdl_begin();
   __shared__ float2 part[1024];
@@ -257,22 +264,54 @@ __global__ void __launch_bounds__(1024) distill_join_kernel(const DistillJoin a,
     for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
     return v;
   };
+  struct Word {
+    int word, slot;
+    bool first;      // of equals
+    float z, q, lq;
+  };
   for (int64_t first = (int64_t)blockIdx.x << shift; first < a.T; first += (int64_t)gridDim.x << shift) {
+    Word held[WORDS ? WORDS : 1];
+    const auto word_at = [&](int64_t base, int i) {
+      Word w = {kNoWord, 0, false, 0.f, 0.f, 0.f};
+      if (i < a.K) {
+        w.word = a.word[base + i];
+        w.slot = a.slot[base + i];
+        w.first = w.word != kNoWord && (i == 0 || a.word[base + i - 1] != w.word);
+        w.z = a.picked[base + i];
+        w.q = a.q[base + i];
+        w.lq = a.lq[base + i];
+      }
+      return w;
+    };
+    const auto hold = [&](int w) {
+#pragma unroll
+      for (int c = 0; c < WORDS; ++c) held[c] = word_at((first + w) * a.K, c * 32 + lane);
+    };
+    const int w0 = threadIdx.x >> 5;
+    if (w0 < rows && first + w0 < a.T) hold(w0);
     join_rows(a.stats, a.T, a.tiles, first, shift, part);
     if ((int)threadIdx.x < rows) joined[r] = joined_row(part, r, shift);
     __syncthreads();
-    for (int w = threadIdx.x >> 5; w < rows && first + w < a.T; w += blockDim.x >> 5) {
+    for (int w = w0; w < rows && first + w < a.T; w += blockDim.x >> 5) {
+      if (w != w0) hold(w);
       const int64_t t = first + w, base = t * a.K;
+      const auto each_word = [&](const auto& f) {
+        if constexpr (WORDS > 0) {
+#pragma unroll
+          for (int c = 0; c < WORDS; ++c)
+            if (c * 32 + lane < a.K) f(c * 32 + lane, held[c]);
+        } else {
+          for (int i = lane; i < a.K; i += 32) f(i, word_at(base, i));
+        }
+      };
       const float2 pair = joined[w];
       const int state = a.state[t];
       // the largest score, and which of the teacher's words has it (the first of them)
       float own_top = -CUDART_INF_F;
       int own_at = 0;
-      for (int i = lane; i < a.K; i += 32)
-        if (first_of(a.word + base, i)) {
-          const float z = a.picked[base + i];
-          if (z > own_top) { own_top = z; own_at = i; }
-        }
+      each_word([&](int i, const Word& x) {
+        if (x.first && x.z > own_top) { own_top = x.z; own_at = i; }
+      });
 #pragma unroll
       for (int o = 16; o; o >>= 1) {
         const float z = __shfl_xor_sync(0xffffffffu, own_top, o);
@@ -281,32 +320,33 @@ __global__ void __launch_bounds__(1024) distill_join_kernel(const DistillJoin a,
       }
       const float top = fmaxf(pair.x, own_top * a.scale), ref = top == -CUDART_INF_F ? 0.f : top;
       const float others = pair.y * ex2(pair.x - ref);      // the words that are not the teacher's
-      const auto exponent = [&](int i) { return fmaf(a.picked[base + i], a.scale, -ref); };
-      float mine = 0.f, q_rest = 0.f;                        // all of the teacher's but the largest
-      for (int i = lane; i < a.K; i += 32)
-        if (first_of(a.word + base, i) && i != own_at) {
-          mine += ex2(exponent(i));
-          q_rest += a.q[base + i];
-        }
+      const auto exponent = [&](float z) { return fmaf(z, a.scale, -ref); };
+      float mine = 0.f, q_rest = 0.f, largest = 0.f;         // all of the teacher's but the largest, and that one
+      each_word([&](int i, const Word& x) {
+        if (!x.first) return;
+        const float e = ex2(exponent(x.z));
+        if (i == own_at) largest = e;
+        else { mine += e; q_rest += x.q; }
+      });
       mine = total_of(mine);
       q_rest = total_of(q_rest);
+      largest = total_of(largest);
       const bool kept = state == kKept;
-      const float largest = kept ? ex2(exponent(own_at)) : 0.f, rest = others + mine, total = rest + largest;
+      const float rest = others + mine, total = rest + largest;
       const float bits = log2f(total);
       float sum = 0.f;
-      for (int i = lane; i < a.K; i += 32) {
-        const int word = a.word[base + i];
+      each_word([&](int i, const Word& x) {
         float diff = state == kInvalid ? CUDART_NAN_F : 0.f;
-        if (kept && word != kNoWord) {
-          if (!first_of(a.word + base, i)) continue;      // the first of its equals writes
-          const float e = exponent(i), p = ex2(e) / total, q = a.q[base + i];
+        if (kept && x.word != kNoWord) {
+          if (!x.first) return;      // the first of its equals writes
+          const float e = exponent(x.z), p = ex2(e) / total;
           const bool most = i == own_at && p > 0.5f;      // of it 1 - p is better known than p, and 1 - q than q
-          sum += divergence(q, p, most && q > 0.5f ? log1pf(-q_rest) + log1pf(rest / largest) : (a.lq[base + i] - (e - bits)) * kLn2);
-          diff = most ? q_rest - rest / total : p - q;
-          for (int n = i + 1; n < a.K && a.word[base + n] == word; ++n) a.diff[base + a.slot[base + n]] = diff;
+          sum += divergence(x.q, p, most && x.q > 0.5f ? log1pf(-q_rest) + log1pf(rest / largest) : (x.lq - (e - bits)) * kLn2);
+          diff = most ? q_rest - rest / total : p - x.q;
+          for (int n = i + 1; n < a.K && a.word[base + n] == x.word; ++n) a.diff[base + a.slot[base + n]] = diff;
         }
-        a.diff[base + a.slot[base + i]] = diff;
-      }
+        a.diff[base + x.slot] = diff;
+      });
       sum = total_of(sum);
       if (lane == 0) {
         a.lse[t] = state == kIgnored ? CUDART_INF_F : state == kInvalid ? CUDART_NAN_F : (ref + bits) * kLn2;
@@ -487,15 +527,16 @@ int sp_linear_distill(const void* h, const void* W, const int64_t* top_index, co
   const float scale = kLog2e / temperature;
   TeacherArgs ta = {top_index, top_logit, top_dtype, scale, (int32_t*)(ws + p.off_word), (int32_t*)(ws + p.off_slot), (float*)(ws + p.off_q), (float*)(ws + p.off_lq),
                     (uint16_t*)(ws + p.off_start), (int32_t*)(ws + p.off_state), T, (int)V, (int)K, 0, p.parts, p.width};
-  rc = launch_teacher(ta, stream);
-  if (rc != SP_OK) return rc;
   if (p.ce.copy) {
     CePrep prep = ce_rows_args(p.ce, h, ws + p.off_rows, nullptr, 0, false);
     rc = launch_ce_rows(p.ce, prep, stream);
     if (rc != SP_OK) return rc;
   }
+  rc = launch_teacher(ta, stream);
+  if (rc != SP_OK) return rc;
   const EpiDistill::Args ea = {(float2*)ws, (float*)(ws + p.off_picked), ta.word, ta.start, scale, (int)K, p.parts};
-  rc = ce_scores<EpiDistill>("vocabulary product", p.ce, p.ce.copy ? ws + p.off_rows : h, p.ce.copy ? p.ce.ld_h : D, W, V, st.status, dtype == SP_BF16, nullptr, ea, stream);
+  rc = ce_scores<EpiDistill>("vocabulary product", p.ce, p.ce.copy ? ws + p.off_rows : h, p.ce.copy ? p.ce.ld_h : D, W, V, st.status, dtype == SP_BF16, nullptr, ea, stream,
+                             nullptr, 2);
   if (rc != SP_OK) return rc;
   DistillJoin j = {};
   j.stats = ea.stats; j.picked = ea.picked; j.word = ta.word; j.slot = ta.slot; j.q = ta.q; j.lq = ta.lq; j.state = ta.state; j.lse = lse; j.diff = diff;
@@ -505,7 +546,7 @@ int sp_linear_distill(const void* h, const void* W, const int64_t* top_index, co
   // As the cross entropy's: 256 threads while a row's pairs are one batch of reads, one block for up to 64 tokens of few pairs, and the sum of their losses with them.
   const int shift = T <= 4 ? 2 : 5, threads = p.parts <= 8 * (256 >> shift) ? 256 : 1024;
   const unsigned blocks = j.loss && T <= 64 && p.parts <= 256 ? 1u : (unsigned)div_up(T, 1 << shift);
-  rc = launch_pdl("join of the row statistics", distill_join_kernel, dim3(blocks), threads, 0, 1, stream, j, shift);
+  rc = launch_pdl("join of the row statistics", K <= 32 ? distill_join_kernel<1> : K <= 128 ? distill_join_kernel<4> : distill_join_kernel<0>, dim3(blocks), threads, 0, 1, stream, j, shift);
   if (rc == SP_OK && j.loss && blocks > 1) rc = launch_pdl("sum of the losses", distill_reduce_kernel, dim3(1), 1024, 0, 1, stream, j);
   return rc;
 } catch (const std::exception& e) {

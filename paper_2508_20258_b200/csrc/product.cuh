@@ -63,6 +63,7 @@ struct ProdArgs {
                          //    in step they would queue for them in one L2 slice: one token's scores, 131072 x 4096, 219 us in step, 191 so)
   // A product that reads nothing of the kernel before it may run beside it: it goes straight to work (everything before that kernel is
   // complete, see pdl_begin) and waits before it ends instead, so that whatever follows it follows both.
+  // 2: what it multiplies was there before that kernel, but the epilogue reads what that kernel writes: the epilogue warps wait first.
   int overlap;
   int units;             // CTAs or CTA pairs launched
   uint32_t idesc;        // instruction descriptor
@@ -376,6 +377,7 @@ product_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
     const int quarter = warp & 3, half = (warp - C::kEpi0) >> 2;   // TMEM lanes [32 * quarter, 32 * quarter + 32)
     const uint32_t taddr = tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(half * kCols);
     Epi epi(eargs, &tmC, epi_base, warp - C::kEpi0, lane);
+    if (args.overlap == 2) pdl_wait();
     int it = 0;
     bool ok = true;
     for (int s = unit; s < total && ok; s += args.units) {
