@@ -117,6 +117,7 @@ struct CePrep {
   int reduction, fp16;
   float times;           // of `factor`
   int masked;            // 1: rows of ignored tokens become zeros
+  int twice;             // 1: all rows once more behind the first T
   unsigned long long* rest;   // per token: set to 0 ...
   int32_t* count;             // ... and this one number too
 
@@ -149,10 +150,12 @@ struct CePlan {
   int64_t piece, ld_g;        // gradient: vocabulary rows of a piece, row pitch of g
   int pieces;
   int slices;                 // of the vocabulary in the product for dh
+  int halves;                 // 2: the second half of the T rows of h and g repeats the first, g as the rounding errors of the first half's: both add up to one row of dh
   bool copy;                  // forward: the tokens' rows are copied to cache lines of their own
   int64_t ld_h;               // row pitch of such copies
   int64_t off_picked, off_each, off_rows, forward_bytes;
   int64_t off_factor, off_rest, off_list, off_grad_rows, off_g, off_acc, off_sure, grad_bytes;
+  bool summed() const { return pieces > 1 || slices > 1 || halves > 1; }      // dh passes through fp32 sums
 };
 
 // Rows of a token tile: a CTA pair's 256, or one CTA's 128 where no more tokens are there.  (Also for token counts that fill their last tile
@@ -160,7 +163,7 @@ struct CePlan {
 // 4 x 256 rows, 58 on 7 x 128; dh 51 and 55.)
 inline int ce_rows(int64_t T) { return T <= 128 ? 128 : 256; }
 
-CePlan ce_plan(int64_t T, int64_t V, int64_t D);
+CePlan ce_plan(int64_t T, int64_t V, int64_t D, int halves = 1);
 bool ce_sizes(int64_t T, int64_t V, int64_t D);      // whether the calls take them
 int ce_sched(int64_t M, int64_t N, int tile_m, int tile_n, Sched* out, bool rows = false);
 ProdArgs ce_args(const Sched& sched, int32_t* status, int64_t M, int64_t N, int64_t K, int slices);

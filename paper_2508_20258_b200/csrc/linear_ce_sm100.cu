@@ -231,7 +231,9 @@ __device__ __forceinline__ void ce_copy_rows(const CePrep& a, int block, int blo
   for (int64_t i = (int64_t)block * blockDim.x + threadIdx.x; i < n; i += (int64_t)blocks * blockDim.x) {
     const int64_t t = i / a.vecs;
     const uint4 v = __ldg(a.h + i);
-    a.rows[t * a.ld + (i - t * a.vecs)] = a.masked && !a.kept(t) ? make_uint4(0u, 0u, 0u, 0u) : v;
+    const uint4 w = a.masked && !a.kept(t) ? make_uint4(0u, 0u, 0u, 0u) : v;
+    a.rows[t * a.ld + (i - t * a.vecs)] = w;
+    if (a.twice) a.rows[(t + a.T) * a.ld + (i - t * a.vecs)] = w;
   }
 }
 
@@ -604,9 +606,10 @@ __global__ void __launch_bounds__(256) ce_finish_kernel(const float4* acc, int64
 // ------------------------------------------------------------------ host side
 std::mutex g_ce_mu;
 
-CePlan ce_plan(int64_t T, int64_t V, int64_t D) {
+CePlan ce_plan(int64_t T, int64_t V, int64_t D, int halves) {
   CePlan p = {};
-  p.T = T; p.V = V; p.D = D;
+  T *= halves;
+  p.T = T; p.V = V; p.D = D; p.halves = halves;
   p.row = T == 1 && D <= kRowMaxD;
   p.tiles = 2 * div_up(V, tile_width(T, V, ce_rows(T) / 128, 32));
   if (p.row) p.tiles = div_up(V, 2 * kRowThreads / 32) < 2 * 148 ? div_up(V, 2 * kRowThreads / 32) : 2 * 148;   // blocks: two per SM
@@ -641,7 +644,7 @@ CePlan ce_plan(int64_t T, int64_t V, int64_t D) {
   p.off_grad_rows = p.off_list + (p.pieces > 1 ? up256(T * 4) : 0);
   p.off_g = p.off_grad_rows + up256(T * p.ld_h * 2);
   p.off_acc = p.off_g + up256(T * p.ld_g * 2);
-  p.grad_bytes = p.off_acc + ((p.pieces > 1 || p.slices > 1) ? up256(p.slices * T * D * 4) : 0);
+  p.grad_bytes = p.off_acc + (p.summed() ? up256(p.slices * T * D * 4) : 0);
   // With pieces, rows of the tokens that are sure lie where g or the sums of dh come later: a row of g has at least 1024 entries of 2 bytes, one of dh's sums D of 4.
   p.off_sure = p.ld_h <= p.ld_g ? p.off_g : p.off_acc;
   return p;
@@ -694,7 +697,7 @@ ProdArgs ce_args(const Sched& sched, int32_t* status, int64_t M, int64_t N, int6
 
 CePrep ce_rows_args(const CePlan& p, const void* h, void* rows, const int64_t* target, int64_t ignore, bool masked) {
   CePrep a = {};
-  a.target = target; a.h = (const uint4*)h; a.rows = (uint4*)rows; a.T = p.T; a.vecs = (int)(p.D / 8); a.ld = (int)(p.ld_h / 8);
+  a.target = target; a.h = (const uint4*)h; a.rows = (uint4*)rows; a.T = p.T / p.halves; a.twice = p.halves > 1; a.vecs = (int)(p.D / 8); a.ld = (int)(p.ld_h / 8);
   a.ignore = ignore; a.masked = masked; a.times = 1.f;
   return a;
 }
@@ -709,7 +712,7 @@ int ce_products(const CePlan& p, const void* Wp, char* ws, void* dh, void* dW, i
   const int64_t T = p.T, D = p.D;
   const float *coef = (const float*)ws, *factor = (const float*)(ws + p.off_factor);
   char *g = ws + p.off_g, *rows = ws + p.off_grad_rows, *acc = ws + p.off_acc;
-  const bool summed = p.pieces > 1 || p.slices > 1;     // dh passes through fp32 sums
+  const bool summed = p.summed();
   CUtensorMap tmA, tmB, tmC;
   int rc = SP_OK;
   if (dh) {
@@ -752,9 +755,9 @@ int ce_products(const CePlan& p, const void* Wp, char* ws, void* dh, void* dW, i
 
 // dh from its sums, where it has passed through them.
 int ce_finish(const CePlan& p, char* ws, void* dh, bool bf16, cudaStream_t stream) {
-  if (p.pieces == 1 && p.slices == 1) return SP_OK;
-  const int64_t n4 = p.T * p.D / 4;
-  return launch_pdl("sum of the slices", ce_finish_kernel, dim3((unsigned)div_up(n4, 256)), 256, 0, 1, stream, (const float4*)(ws + p.off_acc), n4, (int)(p.D / 4), p.slices,
+  if (!p.summed()) return SP_OK;
+  const int64_t n4 = p.T / p.halves * p.D / 4;
+  return launch_pdl("sum of the slices", ce_finish_kernel, dim3((unsigned)div_up(n4, 256)), 256, 0, 1, stream, (const float4*)(ws + p.off_acc), n4, (int)(p.D / 4), p.slices * p.halves,
                     (const float*)(ws + p.off_factor), (const float*)ws, (int)bf16, (uint2*)dh);
 }
 

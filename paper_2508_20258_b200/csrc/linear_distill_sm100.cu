@@ -367,7 +367,10 @@ __global__ void __launch_bounds__(1024) distill_reduce_kernel(const DistillJoin 
 }
 
 // ------------------------------------------------------------------ gradient
-// c p of a tile, to 16 bits (what that rounding does: see the cross entropy's).
+// c p of a tile, to 16 bits: its rounding (at most half a step, 2^-8 of bf16 or 2^-11 of fp16 relative) is independent from entry to entry and adds up to less than the gradients' own
+// rounding to the same type where many entries make a gradient.  With few tokens a word's row of dW is one or two entries' product.  So up to kSplitTokens tokens
+// have two rows of g, the second one for what the first one's rounding has left: the products, bound by W, take no longer (16 x 65536 x 4096: ..., errors of dW ...).
+constexpr int kSplitTokens = 64;      // two rows of each fill a tile of 128
 struct EpiProb {
   static constexpr uint32_t kBytes = 8 * 4096;
   static constexpr bool kSums = true;       // the scores as the forward product made them
@@ -376,19 +379,22 @@ struct EpiProb {
     const float* lse;
     const float* coef;
     float scale;
-    int bf16;
+    int T, bf16;             // rows of T and beyond: the rounding errors of those before
   };
   const Args& a;
   const CUtensorMap* map;
   EpiStage stage;
   int lane;
+  bool errors;
   float lse2, c;
   __device__ EpiProb(const Args& args, const CUtensorMap* m, uint32_t base, int w, int l) : a(args), map(m), stage{base + (uint32_t)w * 4096u, l}, lane(l) {}
   __device__ __forceinline__ void before(const EpiTile& e, int M, int) {
     const int row = e.row0 + lane;
     const bool in = row < M;
-    c = in ? __ldg(a.coef + row) : 0.f;
-    lse2 = in ? __ldg(a.lse + row) * kLog2e : 0.f;
+    errors = row >= a.T;
+    const int token = errors ? row - a.T : row;
+    c = in ? __ldg(a.coef + token) : 0.f;
+    lse2 = in ? __ldg(a.lse + token) * kLog2e : 0.f;
   }
   template <int COLS>
   __device__ __forceinline__ void finish(uint32_t (&v)[COLS], const EpiTile& e, int M, int N) {
@@ -400,7 +406,14 @@ struct EpiProb {
       for (int j = 0; j < 32; ++j) {
         float lo, hi;
         halves_of(fma_pair(pair_of(__uint_as_float(v[q * 64 + 2 * j]), __uint_as_float(v[q * 64 + 2 * j + 1])), scale, off), lo, hi);
-        p[j] = pack_16(ex2(lo) * c, ex2(hi) * c, a.bf16);
+        lo = ex2(lo) * c;
+        hi = ex2(hi) * c;
+        p[j] = pack_16(lo, hi, a.bf16);
+        if (errors) {
+          float near_lo, near_hi;
+          row_values(p[j], a.bf16, near_lo, near_hi);
+          p[j] = pack_16(lo - near_lo, hi - near_hi, a.bf16);
+        }
         if (c == 0.f) p[j] = 0;     // a token that does not count: exactly nothing, whatever its scores are
       }
       store_part(stage, map, lane, p, e.row0 < M && e.col0 + q * 64 < N, e.col0 + q * 64, e.row0);
@@ -416,6 +429,7 @@ struct PlaceArgs {
   uint16_t* g;
   int64_t n, ld;        // T x K
   int64_t v0, cols;
+  int64_t errors;       // entries of g from a token's row to the one for its rounding errors, or 0
   int K, bf16;
 };
 
@@ -426,7 +440,14 @@ __global__ void __launch_bounds__(256) distill_place_kernel(const PlaceArgs a) {
     if (v < 0 || v >= a.cols) continue;
     const int64_t t = i / a.K;
     const float c = __ldg(a.coef + t), d = __ldg(a.diff + i);
-    if (c != 0.f) a.g[t * a.ld + v] = (uint16_t)pack_16(d * c, 0.f, a.bf16);
+    if (c == 0.f) continue;
+    const uint32_t near = pack_16(d * c, 0.f, a.bf16);
+    a.g[t * a.ld + v] = (uint16_t)near;
+    if (a.errors) {
+      float lo, hi;
+      row_values(near, a.bf16, lo, hi);
+      a.g[a.errors + t * a.ld + v] = (uint16_t)pack_16(d * c - lo, 0.f, a.bf16);
+    }
   }
 }
 
@@ -456,6 +477,8 @@ static DistillPlan distill_plan(int64_t T, int64_t V, int64_t D, int64_t K) {
   p.forward_bytes = p.off_rows + (p.ce.copy ? up256(T * p.ce.ld_h * 2) : 0);
   return p;
 }
+
+static CePlan distill_grad_plan(int64_t T, int64_t V, int64_t D) { return ce_plan(T, V, D, T <= kSplitTokens ? 2 : 1); }
 
 static bool distill_sizes(int64_t T, int64_t V, int64_t D, int64_t K) { return K > 0 && K <= kMaxTop && ce_sizes(T, V, D); }
 
@@ -496,8 +519,7 @@ extern "C" {
 
 int64_t sp_linear_distill_workspace(int64_t T, int64_t V, int64_t D, int64_t K, int32_t grad) {
   if (!distill_sizes(T, V, D, K)) return -1;
-  const DistillPlan p = distill_plan(T, V, D, K);
-  return grad ? p.ce.grad_bytes : p.forward_bytes;
+  return grad ? distill_grad_plan(T, V, D).grad_bytes : distill_plan(T, V, D, K).forward_bytes;
 }
 
 int sp_linear_distill(const void* h, const void* W, const int64_t* top_index, const void* top_logit, int32_t top_dtype, float* lse, float* diff, float* loss, int64_t T,
@@ -560,7 +582,7 @@ int sp_linear_distill_grad(const void* h, const void* W, const int64_t* top_inde
   if (rc != SP_OK) return rc;
   if (!dh && !dW) { set_error("dh and dW must not both be NULL"); return SP_ERR_INVALID_ARG; }
   if ((((uintptr_t)dh | (uintptr_t)dW) & 15u) || ((uintptr_t)grad_loss & 3u)) { set_error("dh and dW must be 16-byte aligned, grad_loss aligned to its elements"); return SP_ERR_ALIGNMENT; }
-  const CePlan p = ce_plan(T, V, D);
+  const CePlan p = distill_grad_plan(T, V, D);
   if (workspace_bytes < p.grad_bytes) { set_error("workspace of %lld bytes, %lld needed", (long long)workspace_bytes, (long long)p.grad_bytes); return SP_ERR_INVALID_ARG; }
   const Span spans[] = {{"dh", dh, (Bytes)T * D * 2}, {"dW", dW, (Bytes)V * D * 2}, {"workspace", workspace, (Bytes)p.grad_bytes}, {"h", h, (Bytes)T * D * 2},
                         {"W", W, (Bytes)V * D * 2}, {"top_index", top_index, (Bytes)T * K * 8}, {"lse", lse, (Bytes)T * 4}, {"diff", diff, (Bytes)T * K * 4},
@@ -587,10 +609,10 @@ int sp_linear_distill_grad(const void* h, const void* W, const int64_t* top_inde
   if (rc != SP_OK) return rc;
   const int64_t n = T * K, blocks = div_up(n, 256);
   const auto scores = [&](int64_t v0, int64_t cols, const void* Wp, const CUtensorMap& tmG) {
-    const EpiProb::Args ea = {lse, coef, kLog2e / temperature, bf16};
+    const EpiProb::Args ea = {lse, coef, kLog2e / temperature, (int)T, bf16};
     int rc = ce_scores<EpiProb>("gradient of the scores", p, rows, p.ld_h, Wp, cols, st.status, bf16, &tmG, ea, stream);
     if (rc != SP_OK) return rc;
-    const PlaceArgs pa = {top_index, diff, coef, (uint16_t*)g, n, p.ld_g, v0, cols, (int)K, bf16};
+    const PlaceArgs pa = {top_index, diff, coef, (uint16_t*)g, n, p.ld_g, v0, cols, p.halves > 1 ? T * p.ld_g : 0, (int)K, bf16};
     return launch_pdl("teacher's words", distill_place_kernel, dim3((unsigned)(blocks < 148 * 16 ? blocks : 148 * 16)), 256, 0, 1, stream, pa);
   };
   return ce_gradients(p, W, ws, dh, dW, bf16, st.status, stream, scores);
