@@ -575,12 +575,9 @@ def layernorm(x, gamma, beta, y, mean=None, rstd=None, eps: float = 1e-5, stream
     fp32, both alike; None: ones, zeros.  mean, rstd: [M] fp32, filled where given (kept for layernorm_grad)."""
     M, N = x.shape
     _expect("shape and type of y", (y.shape, y.dtype), (x.shape, x.dtype))
-    w, tensors = _ln_weights(x, (gamma, beta), N)
-    tensors += [x, y] + _ln_stats(M, (mean, rstd))
-    code = _dtype_code(x, (BF16, FP32, FP16))
+    code, w_code, tensors = _ln_arguments(x, [x, y], (gamma, beta), (mean, rstd))
     here = _device_tensors(*tensors)
-    _check(lib().sp_layernorm(x.data_ptr(), _ptr(gamma), _ptr(beta), y.data_ptr(), _ptr(mean), _ptr(rstd), M, N, code, code if w is None else _dtype_code(w, (code, FP32)),
-                              eps, _stream_on(here, stream)))
+    _check(lib().sp_layernorm(x.data_ptr(), _ptr(gamma), _ptr(beta), y.data_ptr(), _ptr(mean), _ptr(rstd), M, N, code, w_code, eps, _stream_on(here, stream)))
 
 
 def layernorm_workspace(M: int, N: int) -> int:
@@ -596,37 +593,40 @@ def layernorm_grad(dy, x, gamma, mean, rstd, dx, dgamma, dbeta, workspace=None, 
     and ``rstd`` as layernorm left them; ``workspace``: layernorm_workspace(M, N) bytes, allocated here when not given."""
     M, N = x.shape
     _expect("shape and type of dy", (dy.shape, dy.dtype), (x.shape, x.dtype))
+    rows = [x, dy]
     if dx is not None:
         _expect("shape and type of dx", (dx.shape, dx.dtype), (x.shape, x.dtype))
-    w, tensors = _ln_weights(x, (gamma, dgamma, dbeta), N)
-    tensors += [x, dy] + _ln_stats(M, (mean, rstd)) + ([dx] if dx is not None else [])
-    code = _dtype_code(x, (BF16, FP32, FP16))
+        rows.append(dx)
+    code, w_code, tensors = _ln_arguments(x, rows, (gamma, dgamma, dbeta), (mean, rstd))
     here = _device_tensors(*tensors)
     ws, n = None, 0
     if dgamma is not None or dbeta is not None:
         ws, n = _workspace(workspace, x, 0 if workspace is not None else layernorm_workspace(M, N), stream)
-    _check(lib().sp_layernorm_grad(dy.data_ptr(), x.data_ptr(), _ptr(gamma), _ptr(mean), _ptr(rstd), _ptr(dx), _ptr(dgamma), _ptr(dbeta), M, N, code,
-                                   code if w is None else _dtype_code(w, (code, FP32)), _ptr(ws), n, _stream_on(here, stream)))
+    _check(lib().sp_layernorm_grad(dy.data_ptr(), x.data_ptr(), _ptr(gamma), _ptr(mean), _ptr(rstd), _ptr(dx), _ptr(dgamma), _ptr(dbeta), M, N, code, w_code,
+                                   _ptr(ws), n, _stream_on(here, stream)))
 
 
 def _ptr(t):
     return None if t is None else t.data_ptr()
 
 
-def _ln_weights(x, weights, N: int):
-    """(one of the vectors that are given or None, all that are given): [N] each, of one type."""
-    given = [w for w in weights if w is not None]
-    for w in given:
-        _expect("shape and type of a weight or its gradient", (w.shape, w.dtype), ((N,), given[0].dtype))
-    return (given[0] if given else None), given
-
-
-def _ln_stats(M: int, stats):
-    import torch
-    given = [s for s in stats if s is not None]
-    for s in given:
-        _expect("shape and type of mean, rstd", (s.shape, s.dtype), ((M,), torch.float32))
-    return given
+def _ln_arguments(x, tensors, weights, stats):
+    """(the rows' type, the weights', all tensors that are given): of the vectors that are given, weights [N] of one type, statistics [M] fp32."""
+    code = w_code = _dtype_code(x, (BF16, FP32, FP16))
+    (M, N), kind = x.shape, None
+    for w in weights:
+        if w is not None:
+            if kind is None:
+                kind, w_code = w.dtype, _dtype_code(w, (code, FP32))
+            if w.dtype != kind or w.dim() != 1 or w.shape[0] != N:
+                raise ValueError(f"shape and type of a weight or its gradient: got {tuple(w.shape)} {w.dtype}, expected {(N,)} {kind}")
+            tensors.append(w)
+    for s in stats:
+        if s is not None:
+            if _DTYPE_CODES.get(s.dtype) != FP32 or s.dim() != 1 or s.shape[0] != M:
+                raise ValueError(f"shape and type of mean, rstd: got {tuple(s.shape)} {s.dtype}, expected {(M,)} torch.float32")
+            tensors.append(s)
+    return code, w_code, tensors
 
 
 def gemm_units(tile_m: int, tile_n: int, T: int) -> int:
