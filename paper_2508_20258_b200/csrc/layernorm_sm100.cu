@@ -17,16 +17,17 @@
 namespace sp {
 
 constexpr int kLnThreads = 512;                   // of a block: 16 warps in groups
-constexpr int kLnMaxCluster = 8;               // portable
+constexpr int kLnMaxCluster = 4;
 constexpr int kLnSums = 2;                        // of a group of warps at once, at most
 constexpr int64_t kLnMaxN = 32768;
 constexpr int kLnSms = 148;
+constexpr uint32_t kLnSumBytes = 2 * (16 + kLnMaxCluster) * 4 * kLnSums;      // of shared memory: sums of warps and of CTAs, two of each
 constexpr int kLnRing = 192 << 10;                // bytes of rows on their way, at most
 
 // How a row lies in the lanes of its group.
 enum : int {
   kLnWhole,     // 16-byte units, the rows being whole units at 16-byte addresses
-  kLnEdges,     // 16-byte units of memory, the first and the last of a row shared with its neighbours; a group's rows all begin at the same place in their unit
+  kLnEdges,     // whole 16-byte units of memory, and the few elements before the first and behind the last; a group's rows all begin at the same place in a unit
   kLnSingle     // single elements: x, dy and the result do not begin at the same place
 };
 
@@ -79,13 +80,13 @@ struct Ln16 {
       lo = p.x; hi = p.y;
     }
   }
-  static __device__ __forceinline__ uint32_t twice_from_shared(uint32_t at) {
+  static __device__ __forceinline__ float from_shared(uint32_t at) {
     uint16_t b;
     asm volatile("ld.shared.b16 %0, [%1];" : "=h"(b) : "r"(at) : "memory");
-    return b * 0x10001u;
+    return one(b);
   }
-  static __device__ __forceinline__ float first(uint32_t v) { return one(v); }
-  static __device__ __forceinline__ float from_shared(uint32_t at) { return one(twice_from_shared(at)); }
+  static __device__ __forceinline__ float load(const char* at) { return one(__ldg(reinterpret_cast<const uint16_t*>(at))); }
+  static __device__ __forceinline__ void store(char* at, float f) { *reinterpret_cast<uint16_t*>(at) = (uint16_t)pack_16(f, 0.f, BF16); }
   static __device__ __forceinline__ void unpack(const uint32_t (&v)[4], uint64_t* f) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -102,14 +103,12 @@ struct Ln16 {
       v[i] = pack_16(lo, hi, BF16);
     }
   }
-  static __device__ __forceinline__ void copy_from_shared(char* to, uint32_t at) { *reinterpret_cast<uint16_t*>(to) = (uint16_t)twice_from_shared(at); }
-  static __device__ __forceinline__ void store_one(char* at, float f) { *reinterpret_cast<uint16_t*>(at) = (uint16_t)pack_16(f, 0.f, BF16); }
 };
 struct Ln32 {
   static constexpr int kBytes = 4;
-  static __device__ __forceinline__ uint32_t twice_from_shared(uint32_t at) { return ld_shared_32(at); }
-  static __device__ __forceinline__ float first(uint32_t v) { return __uint_as_float(v); }
   static __device__ __forceinline__ float from_shared(uint32_t at) { return __uint_as_float(ld_shared_32(at)); }
+  static __device__ __forceinline__ float load(const char* at) { return __ldg(reinterpret_cast<const float*>(at)); }
+  static __device__ __forceinline__ void store(char* at, float f) { *reinterpret_cast<float*>(at) = f; }
   static __device__ __forceinline__ void unpack(const uint32_t (&v)[4], uint64_t* f) {
 #pragma unroll
     for (int i = 0; i < 2; ++i) f[i] = pair_of(__uint_as_float(v[2 * i]), __uint_as_float(v[2 * i + 1]));
@@ -122,13 +121,11 @@ struct Ln32 {
       v[2 * i] = __float_as_uint(lo); v[2 * i + 1] = __float_as_uint(hi);
     }
   }
-  static __device__ __forceinline__ void copy_from_shared(char* to, uint32_t at) { *reinterpret_cast<uint32_t*>(to) = ld_shared_32(at); }
-  static __device__ __forceinline__ void store_one(char* at, float f) { *reinterpret_cast<float*>(at) = f; }
 };
 
 // A group of W warps and its part of a row, PER elements per thread as PER / 2 pairs.
-//   Units: a lane's u-th is unit (u W + warp) 32 + lane.  With edges the slice begins `lead` elements inside its first unit; what the first and the last
-//   unit hold beside it counts as zeros and is not written.
+//   Units: a lane's u-th is unit (u W + warp) 32 + lane.  With edges, `head` elements come before the first unit and at most as many behind the last: lanes 0 to 7 and 8 to 15
+//   of the first warp have one each, beside their units.
 //   Single elements: a lane's i-th is column (i W + warp) 32 + lane.
 template <class E, int W, int PER, int MODE>
 struct LnGroup {
@@ -140,74 +137,56 @@ struct LnGroup {
   static constexpr int kWide = kStep * kElems / 2;
   int lane, wg, group, tid;
   int rank, ranks;             // of the CTA in its cluster
-  int cols, lead;              // of the slice
-  // Rows with edges: which of the warp's units the slice has in part only (bit i: among the i-th ones); shared memory of the warp: what of its first and last such unit is
-  // the slice's (all bits of an element set), and the two on their way out; the element of them that this lane writes, its place in the slice's row or -1.
-  uint32_t edges, rim;
-  int rim_at;
+  int cols;                    // of the slice
+  int head, chunks;            // elements before the first unit; units (or single elements)
+  int edge;                    // column of the lane's edge element, -1: none
   uint32_t red, far;           // shared memory: sums of warps, sums of CTAs (two of each, used in turn)
+  uint32_t scratch;            // with edges: a warp's chunk of weights for each warp
   uint32_t parity;
 
-  __device__ __forceinline__ LnGroup(const LnArgs& a, uint32_t red_) : lead(0), edges(0), rim_at(-1), red(red_), parity(0) {
+  __device__ __forceinline__ LnGroup(const LnArgs& a, uint32_t red_) : head(0), edge(-1), red(red_), parity(0) {
     const int warp = threadIdx.x >> 5;
     lane = threadIdx.x & 31;
     wg = warp % W; group = warp / W; tid = threadIdx.x % kGroupThreads;
     ranks = W == 16 ? (int)cluster_nctarank() : 1;
     rank = W == 16 ? (int)cluster_ctarank() : 0;
     cols = max(0, min(a.slice, a.N - rank * a.slice));
+    chunks = cols / kElems;
     far = red + 2 * 16 * 4 * kLnSums;
-    rim = far + 2 * kLnMaxCluster * 4 * kLnSums + warp * 64;
+    scratch = red + kLnSumBytes;
     if (W == 16 && ranks > 1) unit_sync<2>();      // every CTA of the cluster is there before one writes to its shared memory
   }
   // `m`: address modulo 16 of the group's rows
   __device__ __forceinline__ void begin_at(int m) {
     if constexpr (MODE == kLnEdges) {
-      lead = m / E::kBytes;
-#pragma unroll
-      for (int i = 0; i < kChunks; ++i)
-        if (__any_sync(0xffffffffu, has(i) && !full(i))) edges |= 1u << i;
-      const int last = (lead + cols - 1) / kElems, e = lane & 7;      // lanes 0 to 7: the elements of unit 0, 8 to 15: of the last one
-      const int unit = lane < 8 ? 0 : last, c = unit * kElems - lead + e;
-      const bool mine = wg == unit / 32 % W && (lane < 8 || last > 0) && c >= 0 && c < cols;
-      if (lane < 16 && e < kElems) {
-        if constexpr (E::kBytes == 2) asm volatile("st.shared.b16 [%0], %1;" ::"r"(rim + lane * 2), "h"((uint16_t)(mine ? 0xffff : 0)) : "memory");
-        else asm volatile("st.shared.b32 [%0], %1;" ::"r"(rim + (lane < 8 ? 0 : 16) + e * 4), "r"(mine ? 0xffffffffu : 0u) : "memory");
-        if (mine && (unit * kElems - lead < 0 || unit * kElems - lead + kElems > cols)) rim_at = c * E::kBytes;      // in a unit that is not whole
-      }
-      __syncwarp();
+      head = min(((16 - m) & 15) / E::kBytes, cols);
+      chunks = (cols - head) / kElems;
+      const int e = lane < 8 ? lane : head + chunks * kElems + lane - 8;
+      if (wg == 0 && lane < 16 && e < (lane < 8 ? head : cols)) edge = e;
     }
   }
-  // A branch that is taken by few warps and, for the compiler, not to be made part of the straight line.
-  __device__ __forceinline__ bool edge(int i) const {
-    if constexpr (MODE != kLnEdges) return false;
-    if ((edges >> i & 1u) == 0) return false;
-    __syncwarp();
-    return true;
-  }
   __device__ __forceinline__ int chunk(int i) const { return (i * W + wg) * 32 + lane; }
-  __device__ __forceinline__ int column(int i) const { return MODE == kLnEdges ? chunk(i) * kElems - lead : chunk(i) * kElems; }
-  __device__ __forceinline__ bool any(int i) const { return (i * W + wg) * 32 * kElems < cols + (MODE == kLnEdges ? lead : 0); }      // of the warp's i-th chunks
-  __device__ __forceinline__ bool has(int i) const { return column(i) < cols; }
-  __device__ __forceinline__ bool full(int i) const { return MODE != kLnEdges || (column(i) >= 0 && column(i) + kElems <= cols); }
+  __device__ __forceinline__ int column(int i) const { return head + chunk(i) * kElems; }
+  __device__ __forceinline__ bool any(int i) const { return (i * W + wg) * 32 < chunks; }      // of the warp's i-th chunks
+  __device__ __forceinline__ bool has(int i) const { return chunk(i) < chunks; }
+  __device__ __forceinline__ bool edges() const { return MODE == kLnEdges && wg == 0; }        // the warp that has them
+  __device__ __forceinline__ float edge_of(const char* row) const { return edge >= 0 ? E::load(row + edge * E::kBytes) : 0.f; }
   __device__ __forceinline__ void sync() const {
     if constexpr (W == 1) __syncwarp();
     else asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "n"(kGroupThreads) : "memory");
   }
 
-  // A row's slice on its way to shared memory, as whole 16-byte units of global memory.  [lo, hi): the matrix, outside of which nothing is read.
+  // A row's slice on its way to shared memory: the units that a lane will read itself, or all whole 16-byte units of global memory that hold it.  [lo, hi): the matrix, outside of
+  // which nothing is read.
   __device__ __forceinline__ void fetch(uint32_t dst, const char* row, const char* lo, const char* hi) const {
-    if constexpr (MODE == kLnWhole) {      // the units a lane will read itself
-#pragma unroll
-      for (int u = 0; u < kChunks; ++u)
-        if (has(u)) cp_async_16(dst + chunk(u) * 16, row + chunk(u) * 16, 16);
-    } else if (MODE == kLnEdges && row - lead * E::kBytes >= lo && row + cols * E::kBytes + 15 <= hi) {
-      row -= lead * E::kBytes;
+    if constexpr (kUnits) {
+      row += head * E::kBytes;
 #pragma unroll
       for (int u = 0; u < kChunks; ++u)
         if (has(u)) cp_async_16(dst + chunk(u) * 16, row + chunk(u) * 16, 16);
     } else {
       const int m = (int)((uintptr_t)row & 15u), n = (m + cols * E::kBytes + 15) >> 4;
-      const auto unit = [&](int j) {
+      for (int j = tid; j < n; j += kGroupThreads) {
         const char* p = row - m + 16 * j;
         if (p >= lo) cp_async_16(dst + 16 * j, p, (int)min((int64_t)16, (int64_t)(hi - p)));
         else      // the matrix starts inside this unit
@@ -216,47 +195,21 @@ struct LnGroup {
               if constexpr (E::kBytes == 4) asm volatile("st.shared.b32 [%0], %1;" ::"r"(dst + 16 * j + b), "r"(*reinterpret_cast<const uint32_t*>(p + b)) : "memory");
               else asm volatile("st.shared.b16 [%0], %1;" ::"r"(dst + 16 * j + b), "h"(*reinterpret_cast<const uint16_t*>(p + b)) : "memory");
             }
-      };
-      if constexpr (kUnits) {
-        for (int u = 0; u < kChunks; ++u)
-          if (chunk(u) < n) unit(chunk(u));
-      } else {
-        for (int j = tid; j < n; j += kGroupThreads) unit(j);
       }
     }
   }
-  // A lane's pairs of chunk i from shared memory, `m`: the row's address modulo 16.  Columns outside the slice become zeros.
+  // A lane's pairs of chunk i from shared memory, `m`: the row's address modulo 16.  Zeros where it has none.
   __device__ __forceinline__ void take(uint32_t src, int i, int m, uint64_t* f) const {
-    int none;
-    float filler;
-    take<false>(src, i, m, f, none, filler);
-  }
-  // FILL: what an edge holds beside the slice becomes the slice's own first element there, `extra` times `filler`, which the sums are relieved of again.  (It
-  // is an element of the row, at most sqrt(N) deviations from the mean, so at most 15 rows' worth of squares are added and taken away.)
-  template <bool FILL>
-  __device__ __forceinline__ void take(uint32_t src, int i, int m, uint64_t* f, int& extra, float& filler) const {
     if constexpr (kUnits) {
       uint32_t v[4] = {0u, 0u, 0u, 0u};
       if (has(i)) ld_shared_16(src + 16 * chunk(i), v);
-      if (edge(i) && has(i) && !full(i)) {
-        const bool begin = chunk(i) == 0;
-        uint32_t k[4], fill = 0;
-        ld_shared_16(rim + (begin ? 0 : 16), k);
-        if constexpr (FILL) {
-          fill = E::twice_from_shared(src + 16 * chunk(i) + (begin ? lead * E::kBytes : 0));
-          filler = E::first(fill);
-          extra = kElems - min(kElems, cols - column(i)) + max(0, -column(i));
-        }
-#pragma unroll
-        for (int w = 0; w < 4; ++w) v[w] = (v[w] & k[w]) | (fill & ~k[w]);
-      }
       E::unpack(v, f);
     } else {
       const uint32_t at = src + m + column(i) * E::kBytes;
       f[0] = pair_of(has(i) ? E::from_shared(at) : 0.f, has(i + 1) ? E::from_shared(at + 32 * W * E::kBytes) : 0.f);
     }
   }
-  // f - v in the columns that the lane holds, else 0 as before
+  // f - v where the lane has something, else 0 as before
   __device__ __forceinline__ void subtract(int i, float v, uint64_t* f) const {
     if constexpr (kUnits) {
       const float m = has(i) ? -v : 0.f;
@@ -267,28 +220,23 @@ struct LnGroup {
     }
   }
   __device__ __forceinline__ void put(char* row, int i, const uint64_t* f) const {
+    char* at = row + column(i) * E::kBytes;
     if constexpr (kUnits) {
-      char* at = row + column(i) * E::kBytes;
       uint32_t v[4];
       E::pack(f, v);
-      if (has(i) && full(i)) *reinterpret_cast<uint4*>(at) = make_uint4(v[0], v[1], v[2], v[3]);
-      if (edge(i) && has(i) && !full(i)) st_shared_16(rim + (chunk(i) == 0 ? 32 : 48), v[0], v[1], v[2], v[3]);
+      if (has(i)) *reinterpret_cast<uint4*>(at) = make_uint4(v[0], v[1], v[2], v[3]);
     } else {
       float lo, hi;
       halves_of(f[0], lo, hi);
-      char* at = row + column(i) * E::kBytes;
-      if (has(i)) E::store_one(at, lo);
-      if (has(i + 1)) E::store_one(at + 32 * W * E::kBytes, hi);
+      if (has(i)) E::store(at, lo);
+      if (has(i + 1)) E::store(at + 32 * W * E::kBytes, hi);
     }
   }
-  // After the row's put: what the edges have of it, an element per lane.
-  __device__ __forceinline__ void put_rim(char* row) const {
-    if constexpr (MODE == kLnEdges) {
-      if (edges == 0) return;
-      __syncwarp();
-      if (rim_at >= 0) E::copy_from_shared(row + rim_at, rim + 32 + (lane < 8 ? 0 : 16) + (lane & 7) * E::kBytes);
-      __syncwarp();
-    }
+  // gamma or beta in one column of the slice
+  __device__ __forceinline__ float weight(const void* w, int dtype, int col0, int c, float none) const {
+    if (w == nullptr || c < 0) return none;
+    if (dtype == SP_FP32) return __ldg((const float*)w + col0 + c);
+    return E::load((const char*)w + (int64_t)(col0 + c) * E::kBytes);
   }
   // gamma or beta of this lane's columns.  All of a kind of loads are in flight together, 16 bytes each where they can be: a block starts with them.
   __device__ __forceinline__ void weights(const void* w, int dtype, int col0, float none, uint64_t* f) const {
@@ -307,7 +255,7 @@ struct LnGroup {
             f[i * kElems / 2 + 2 * q + 1] = pair_of(v.z, v.w);
           }
       } else {
-        one_by_one(f, none, [&](int c) { return __ldg(p + c); });
+        one_by_one<kSpread>(f, none, [&](int c) { return __ldg(p + c); });
       }
     } else {      // the rows' type
       if constexpr (E::kBytes == 2) {
@@ -320,22 +268,49 @@ struct LnGroup {
             if constexpr (kUnits) E::unpack(v, f + i * kElems / 2);
           }
         } else {
-          one_by_one(f, none, [&](int c) { return E::one(__ldg(p + c)); });
+          one_by_one<false>(f, none, [&](int c) { return E::one(__ldg(p + c)); });
         }
       }
     }
   }
-  template <class Load>
+  // SPREAD: the lanes' loads next to each other, and through shared memory to those that want them.  32-bit weights of 16-bit rows lie 32 bytes apart from lane to lane otherwise (5001 x
+  // 2035 19.8 us, so 17.9; 16-bit ones 16 bytes, where it costs 1.7 us more than it saves).
+  static constexpr bool kSpread = MODE == kLnEdges && E::kBytes == 2;
+  template <bool SPREAD, class Load>
   __device__ __forceinline__ void one_by_one(uint64_t* f, float none, const Load& load) const {
+    if constexpr (SPREAD) {
+      float v[PER];
 #pragma unroll
-    for (int k = 0; k < kPairs; ++k) {
-      float v[2];
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const int e = 2 * k + h, c = column(e / kElems) + e % kElems;
-        v[h] = c >= 0 && c < cols ? load(c) : none;
+      for (int e = 0; e < PER; ++e) {
+        const int c = ((e / kElems * W + wg) * 32) * kElems + e % kElems * 32 + lane;
+        v[e] = c < chunks * kElems ? load(head + c) : none;
       }
-      f[k] = pair_of(v[0], v[1]);
+      const uint32_t mine = scratch + (threadIdx.x >> 5) * 32 * kElems * 4;
+#pragma unroll
+      for (int i = 0; i < kChunks; ++i) {
+#pragma unroll
+        for (int k = 0; k < kElems; ++k) asm volatile("st.shared.f32 [%0], %1;" ::"r"(mine + (k * 32 + lane) * 4), "f"(v[i * kElems + k]) : "memory");
+        __syncwarp();
+#pragma unroll
+        for (int k = 0; k < kElems; k += 4) {
+          uint32_t q[4];
+          ld_shared_16(mine + (lane * kElems + k) * 4, q);
+          f[(i * kElems + k) / 2] = pair_of(__uint_as_float(q[0]), __uint_as_float(q[1]));
+          f[(i * kElems + k) / 2 + 1] = pair_of(__uint_as_float(q[2]), __uint_as_float(q[3]));
+        }
+        __syncwarp();
+      }
+    } else {
+#pragma unroll
+      for (int k = 0; k < kPairs; ++k) {
+        float v[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int e = 2 * k + h;
+          v[h] = has(e / kElems) ? load(column(e / kElems) + e % kElems) : none;
+        }
+        f[k] = pair_of(v[0], v[1]);
+      }
     }
   }
 
@@ -407,8 +382,9 @@ struct LnGroup {
   }
 };
 
-// Bytes of shared memory beside the rows: sums of warps and of CTAs, two of each, and the warps' rims.
-constexpr uint32_t kLnRedBytes = 2 * (16 + kLnMaxCluster) * 4 * kLnSums + 16 * 64;
+// Bytes of shared memory before the rows.
+template <class E, int MODE>
+constexpr uint32_t kLnBefore = kLnSumBytes + (MODE == kLnEdges && E::kBytes == 2 ? kLnThreads * 8 * 4 : 0);
 
 // Batches of `rows` rows' slices on their way.
 template <class E, int PER, int ROWS>
@@ -433,7 +409,7 @@ __global__ void __launch_bounds__(kLnThreads, 1) layernorm_kernel(const LnArgs a
   constexpr int D = kLnDepth<E, PER, 1>, P = G::kWide;
   const uint32_t base = smem_u32(ln_smem);
   G g(a, base);
-  const uint32_t ring = base + kLnRedBytes + g.group * D * a.slot;
+  const uint32_t ring = base + kLnBefore<E, MODE> + g.group * D * a.slot;
   const uint32_t total = a.clusters * G::kGroups, last = (uint32_t)a.M - 1;      // unsigned: beyond the last row they may pass 2^31
   const int64_t pitch = (int64_t)a.N * E::kBytes, hop = (int64_t)total * pitch, all = a.M * pitch;
   uint32_t row = blockIdx.x / g.ranks * G::kGroups + g.group;
@@ -451,24 +427,28 @@ __global__ void __launch_bounds__(kLnThreads, 1) layernorm_kernel(const LnArgs a
   uint64_t gamma[G::kPairs], beta[G::kPairs];
   g.weights(a.gamma, a.w_dtype, g.rank * a.slice, 1.f, gamma);
   g.weights(a.beta, a.w_dtype, g.rank * a.slice, 0.f, beta);
+  const float edge_gamma = g.weight(a.gamma, a.w_dtype, g.rank * a.slice, g.edge, 1.f), edge_beta = g.weight(a.beta, a.w_dtype, g.rank * a.slice, g.edge, 0.f);
+  float edge = row <= last ? g.edge_of(a.x + here) : 0.f;      // of the row to come
   const float inv = 1.f / (float)a.N;
   uint32_t at = ring;
   for (; row <= last; row += total, here += hop) {
     cp_async_wait<D - 1>();
     if constexpr (MODE == kLnSingle) g.sync();      // the others' copies
     uint64_t x[G::kPairs], s2[2] = {0, 0}, v2[2] = {0, 0};
-    float filler[2] = {0.f, 0.f};
-    int extra[2] = {0, 0};
 #pragma unroll
     for (int i = 0; i < G::kChunks; i += G::kStep)
       if (g.any(i)) {
         uint64_t* f = x + i * G::kElems / 2;
-        g.template take<true>(at, i, (int)((uintptr_t)(a.x + here) & 15u), f, extra[i > 0], filler[i > 0]);      // at most two units of a lane are edges
+        g.take(at, i, (int)((uintptr_t)(a.x + here) & 15u), f);
 #pragma unroll
         for (int k = 0; k < P; ++k) s2[k & 1] = add_pair(s2[k & 1], f[k]);
       }
     float s = halves_sum(add_pair(s2[0], s2[1]));
-    if constexpr (MODE == kLnEdges) s -= extra[0] * filler[0] + extra[1] * filler[1];
+    const float xe = edge;
+    if (g.edges()) {
+      s += xe;
+      if (row + total <= last) edge = g.edge_of(a.x + here + hop);
+    }
     g.template sum<1>(&s);
     fetch(at, ahead);
     ahead += total;
@@ -488,13 +468,11 @@ __global__ void __launch_bounds__(kLnThreads, 1) layernorm_kernel(const LnArgs a
         }
       }
     float sv[2] = {halves_sum(add_pair(s2[0], s2[1])), halves_sum(add_pair(v2[0], v2[1]))};
-    if constexpr (MODE == kLnEdges)
-#pragma unroll
-      for (int q = 0; q < 2; ++q) {
-        const float e = filler[q] - about;
-        sv[0] -= extra[q] * e;
-        sv[1] -= extra[q] * e * e;
-      }
+    const float de = g.edge >= 0 ? xe - about : 0.f;
+    if (g.edges()) {
+      sv[0] += de;
+      sv[1] = fmaf(de, de, sv[1]);
+    }
     g.template sum<2>(sv);
     const float off = sv[0] * inv, var = fmaf(-off, off, sv[1] * inv), rstd = ln_rsqrt((var < 0.f ? 0.f : var) + a.eps);
     if (g.tid == 0 && g.rank == 0) {
@@ -510,7 +488,7 @@ __global__ void __launch_bounds__(kLnThreads, 1) layernorm_kernel(const LnArgs a
         for (int k = o; k < o + P; ++k) x[k] = fma_pair(mul_pair(add_pair(x[k], minus), scale), gamma[k], beta[k]);
         g.put(a.out + here, i, x + o);
       }
-    g.put_rim(a.out + here);
+    if (g.edges() && g.edge >= 0) E::store(a.out + here + g.edge * E::kBytes, fmaf((de - off) * rstd, edge_gamma, edge_beta));
   }
 }
 
@@ -528,7 +506,7 @@ __global__ void __launch_bounds__(kLnThreads, 1) layernorm_grad_kernel(const LnA
   constexpr int D = kLnDepth<E, PER, 2>, P = G::kWide;
   const uint32_t base = smem_u32(ln_smem);
   G g(a, base);
-  const uint32_t ring = base + kLnRedBytes + g.group * D * 2 * a.slot, batch = 2 * a.slot;
+  const uint32_t ring = base + kLnBefore<E, MODE> + g.group * D * 2 * a.slot, batch = 2 * a.slot;
   const uint32_t total = a.clusters * G::kGroups, last = (uint32_t)a.M - 1;
   const int col0 = g.rank * a.slice;
   const int64_t pitch = (int64_t)a.N * E::kBytes, hop = (int64_t)total * pitch, all = a.M * pitch;
@@ -552,7 +530,13 @@ __global__ void __launch_bounds__(kLnThreads, 1) layernorm_grad_kernel(const LnA
 #pragma unroll
   for (int k = 0; k < G::kPairs; ++k) dg[k] = db[k] = 0;
   const float inv = 1.f / (float)a.N;
+  const float edge_gamma = g.weight(a.gamma, a.w_dtype, col0, g.edge, 1.f);
+  float edge_x = 0.f, edge_dy = 0.f, edge_dg = 0.f, edge_db = 0.f;      // of the row to come; sums
   float mean = 0.f, rstd = 0.f;
+  if (row <= last) {
+    edge_x = g.edge_of(a.x + here);
+    edge_dy = g.edge_of(a.dy + here);
+  }
   if (row <= last) { mean = __ldg(a.mean + row); rstd = __ldg(a.rstd + row); }
   uint32_t at = ring;
   for (; row <= last; row += total, here += hop) {
@@ -579,6 +563,21 @@ __global__ void __launch_bounds__(kLnThreads, 1) layernorm_grad_kernel(const LnA
         }
       }
     float st[2] = {halves_sum(add_pair(s2[0], s2[1])), halves_sum(add_pair(t2[0], t2[1]))};
+    float xe = 0.f, ue = 0.f;
+    if (g.edges()) {
+      if (g.edge >= 0) {
+        xe = (edge_x - mean) * rstd;
+        edge_dg = fmaf(edge_dy, xe, edge_dg);
+        edge_db += edge_dy;
+        ue = edge_dy * edge_gamma;
+        st[0] += ue;
+        st[1] = fmaf(ue, xe, st[1]);
+      }
+      if (row + total <= last) {
+        edge_x = g.edge_of(a.x + here + hop);
+        edge_dy = g.edge_of(a.dy + here + hop);
+      }
+    }
     g.template sum<2>(st);
     fetch(at, ahead);
     ahead += total;
@@ -593,13 +592,13 @@ __global__ void __launch_bounds__(kLnThreads, 1) layernorm_grad_kernel(const LnA
           for (int k = 0; k < P; ++k) f[k] = mul_pair(scale, fma_pair(c2, f[k], add_pair(y[i * G::kElems / 2 + k], c1)));
           g.put(a.out + here, i, f);
         }
-      g.put_rim(a.out + here);
+      if (g.edges() && g.edge >= 0) E::store(a.out + here + g.edge * E::kBytes, rstd * fmaf(-st[1] * inv, xe, ue - st[0] * inv));
     }
     mean = next_mean; rstd = next_rstd;
   }
   if (a.part == nullptr && a.dgamma == nullptr && a.dbeta == nullptr) return;
   // the groups' sums to one, in their order
-  float* all_groups = reinterpret_cast<float*>(ln_smem + kLnRedBytes);
+  float* all_groups = reinterpret_cast<float*>(ln_smem + kLnBefore<E, MODE>);
   cp_async_wait<0>();
 #pragma unroll
   for (int w = 0; w < 2; ++w) {
@@ -608,19 +607,21 @@ __global__ void __launch_bounds__(kLnThreads, 1) layernorm_grad_kernel(const LnA
       else store_weight(w == 0 ? a.dgamma : a.dbeta, a.w_dtype, col0 + c, s);
     };
     if constexpr (G::kGroups > 1) __syncthreads();
+    const auto give = [&](int c, float v) {
+      if constexpr (G::kGroups > 1) all_groups[g.group * a.pitch + c] = v;
+      else out(c, v);
+    };
 #pragma unroll
     for (int k = 0; k < G::kPairs; ++k) {
       float v[2];
       halves_of(w == 0 ? dg[k] : db[k], v[0], v[1]);
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        const int e = 2 * k + h, c = g.column(e / G::kElems) + e % G::kElems;
-        if (c >= 0 && c < g.cols) {
-          if constexpr (G::kGroups > 1) all_groups[g.group * a.pitch + c] = v[h];
-          else out(c, v[h]);
-        }
+        const int e = 2 * k + h;
+        if (g.has(e / G::kElems)) give(g.column(e / G::kElems) + e % G::kElems, v[h]);
       }
     }
+    if (g.edge >= 0) give(g.edge, w == 0 ? edge_dg : edge_db);
     if constexpr (G::kGroups > 1) {
       __syncthreads();
       for (int c = threadIdx.x; c < a.N; c += kLnThreads) {
@@ -670,21 +671,15 @@ struct LnPlan {
 static LnPlan ln_plan(int64_t M, int64_t N, int elt, bool grad, int mode) {
   LnPlan p = {};
   p.mode = mode;
-  const int edge = mode == kLnEdges ? 16 / elt : 0;      // of elements before the slice, at most one unit less
-  // Forward 32 elements per thread: per row half the warps, with what a warp costs beside its elements (8192 x 4096 bf16: 25.9 us, with 16: 31.9).  Rows with edges, whose bookkeeping wants
-  // registers, 16 where these are well filled: 5001 x 2035 fp16 16.4 us, with 32: 20.3; 16384 x 1031, half filled, 41.4 and 33.7.
-  const auto width = [&](int per) {
-    for (p.ranks = 1;; p.ranks *= 2) {
-      p.slice = (int)(((N + p.ranks - 1) / p.ranks + 15) / 16 * 16);
-      if ((N < p.slice ? N : p.slice) + edge <= kLnThreads * per) break;
-    }
-    p.per = per;
-    const int w = (int)(N < p.slice ? N : p.slice) + edge;
-    for (p.warps = 1; p.warps * 32 * per < w; p.warps *= 2) {}
-    return 4 * w > 3 * p.warps * 32 * per;      // more than three quarters used
-  };
-  if (grad) width(16);
-  else if (mode != kLnEdges || !width(16) || p.ranks > 1) width(32);
+  // Forward 32 elements per thread: per row half the warps, with what a warp costs beside its elements (8192 x 4096 bf16: 25.9 us, with 16: 31.9).  Backward 16, beside the columns' sums.
+  p.per = grad ? 16 : 32;
+  for (p.ranks = 1;; p.ranks *= 2) {
+    p.slice = (int)(((N + p.ranks - 1) / p.ranks + 15) / 16 * 16);
+    if ((N < p.slice ? N : p.slice) <= kLnThreads * p.per) break;
+  }
+  // With edges only whole units count: 1031 elements of 16 bits have at most 128.
+  const int cols = (int)(N < p.slice ? N : p.slice), width = mode == kLnEdges ? cols / (16 / elt) * (16 / elt) : cols;
+  for (p.warps = 1; p.warps * 32 * p.per < width; p.warps *= 2) {}
   if (mode == kLnSingle || p.ranks > 1) p.warps = 16;
   const int groups = kLnThreads / 32 / p.warps;
   // One block per SM; backward, whose blocks each leave a row of sums, at least two rows for every group, and one block for up to four.
@@ -702,7 +697,7 @@ static LnPlan ln_plan(int64_t M, int64_t N, int elt, bool grad, int mode) {
 template <class E, int W, int PER, int MODE>
 static int ln_launch(bool grad, const LnArgs& a, const LnPlan& p, cudaStream_t stream) {
   const int slots = grad ? 2 * kLnDepth<E, PER, 2> : kLnDepth<E, PER, 1>;
-  const uint32_t smem = kLnRedBytes + (uint32_t)(kLnThreads / 32 / W * slots) * a.slot;
+  const uint32_t smem = kLnBefore<E, MODE> + (uint32_t)(kLnThreads / 32 / W * slots) * a.slot;
   void (*kern)(LnArgs) = layernorm_kernel<E, W, PER, MODE>;
   if constexpr (PER == 16)
     if (grad) kern = layernorm_grad_kernel<E, W, PER, MODE>;

@@ -143,7 +143,7 @@ __global__ void __launch_bounds__(256) teacher_kernel(const TeacherArgs a) {
 
 // ------------------------------------------------------------------ forward: statistics of a tile's rows
 // As the cross entropy's: per row and part the maximum (in powers of two) and the sum, all of the teacher's words left out and their scores handed on.  A warp looks at 32
-// columns at a time as long as one of its rows has a word there: 64 words per token cost 4096 x 32768 x 2048 under 1 %.
+// columns at a time as long as one of its rows has a word there: 64 words per token cost 4096 x 32768 x 2048 3 % (327 to 339 us).
 struct EpiDistill {
   static constexpr uint32_t kBytes = 0;
   static constexpr bool kSums = true;
@@ -367,9 +367,11 @@ __global__ void __launch_bounds__(1024) distill_reduce_kernel(const DistillJoin 
 }
 
 // ------------------------------------------------------------------ gradient
-// c p of a tile, to 16 bits: its rounding (at most half a step, 2^-8 of bf16 or 2^-11 of fp16 relative) is independent from entry to entry and adds up to less than the gradients' own
-// rounding to the same type where many entries make a gradient.  With few tokens a word's row of dW is one or two entries' product.  So up to kSplitTokens tokens
-// have two rows of g, the second one for what the first one's rounding has left: the products, bound by W, take no longer (16 x 65536 x 4096: ..., errors of dW ...).
+// c p of a tile, to 16 bits: its rounding (at most half a step, 2^-8 of bf16 or 2^-11 of fp16 relative) is independent from entry to entry and moves a gradient about as much as the
+// gradient's own rounding to the same type does.  With few tokens, though, a word's row of dW is one or two entries' product and may have all of it.  So up to kSplitTokens
+// tokens have two rows of g, the second one for what the first one's rounding has left: the products, bound by W, take 2 to 7 % longer (16 x 65536 x 4096 290 to 296 us, 64 x
+// 32768 x 512 51 to 66), and the errors of dh and dW go from 1.4 to 1.0 times those of their own rounding.  (Up to 128 tokens, in a tile of 256 rows: 568 to 693 us at 65 x
+// 131072 x 4096.)
 constexpr int kSplitTokens = 64;      // two rows of each fill a tile of 128
 struct EpiProb {
   static constexpr uint32_t kBytes = 8 * 4096;
@@ -436,9 +438,9 @@ struct PlaceArgs {
 __global__ void __launch_bounds__(256) distill_place_kernel(const PlaceArgs a) {
   pdl_begin();
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < a.n; i += (int64_t)gridDim.x * 256) {
-    const int64_t v = __ldg(a.index + i) - a.v0;
-    if (v < 0 || v >= a.cols) continue;
-    const int64_t t = i / a.K;
+    const int64_t word = __ldg(a.index + i);
+    if (word < a.v0 || word >= a.v0 + a.cols) continue;
+    const int64_t t = i / a.K, v = word - a.v0;
     const float c = __ldg(a.coef + t), d = __ldg(a.diff + i);
     if (c == 0.f) continue;
     const uint32_t near = pack_16(d * c, 0.f, a.bf16);
