@@ -63,6 +63,15 @@ __device__ __forceinline__ void ld_shared_16(uint32_t addr, uint32_t (&v)[4]) {
   asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]) : "r"(addr) : "memory");
 }
 
+// The same where reads may be moved beside each other and beside arithmetic: of a row that has arrived, at an address that came through `arrived`.
+__device__ __forceinline__ void ld_row_16(uint32_t addr, uint32_t (&v)[4]) {
+  asm("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]) : "r"(addr));
+}
+__device__ __forceinline__ uint32_t arrived(uint32_t at) {
+  asm volatile("" : "+r"(at)::"memory");
+  return at;
+}
+
 // Element types: 16 bytes to pairs of floats and back; one element.
 template <bool BF16>
 struct Ln16 {
@@ -167,8 +176,11 @@ struct LnGroup {
   }
   __device__ __forceinline__ int chunk(int i) const { return (i * W + wg) * 32 + lane; }
   __device__ __forceinline__ int column(int i) const { return head + chunk(i) * kElems; }
-  __device__ __forceinline__ bool any(int i) const { return (i * W + wg) * 32 < chunks; }      // of the warp's i-th chunks
-  __device__ __forceinline__ bool has(int i) const { return chunk(i) < chunks; }
+  // PER is the least number of elements, in steps of 8, that holds the row: only the last 8 may be missing, and no warp passes any over.  (Blocks' and clusters' groups, whose CTAs have
+  // unequal slices, ask.)
+  static constexpr int kSure = kUnits && W < 16 ? (PER - 8) / kElems : 0;
+  __device__ __forceinline__ bool any(int i) const { return kUnits || (i * W + wg) * 32 < chunks; }
+  __device__ __forceinline__ bool has(int i) const { return i < kSure || chunk(i) < chunks; }
   __device__ __forceinline__ bool edges() const { return MODE == kLnEdges && wg == 0; }        // the warp that has them
   __device__ __forceinline__ float edge_of(const char* row) const { return edge >= 0 ? E::load(row + edge * E::kBytes) : 0.f; }
   __device__ __forceinline__ void sync() const {
@@ -202,7 +214,7 @@ struct LnGroup {
   __device__ __forceinline__ void take(uint32_t src, int i, int m, uint64_t* f) const {
     if constexpr (kUnits) {
       uint32_t v[4] = {0u, 0u, 0u, 0u};
-      if (has(i)) ld_shared_16(src + 16 * chunk(i), v);
+      if (has(i)) ld_row_16(src + 16 * chunk(i), v);
       E::unpack(v, f);
     } else {
       const uint32_t at = src + m + column(i) * E::kBytes;
@@ -434,12 +446,13 @@ __global__ void __launch_bounds__(kLnThreads, 1) layernorm_kernel(const LnArgs a
   for (; row <= last; row += total, here += hop) {
     cp_async_wait<D - 1>();
     if constexpr (MODE == kLnSingle) g.sync();      // the others' copies
+    const uint32_t here_at = arrived(at);
     uint64_t x[G::kPairs], s2[2] = {0, 0}, v2[2] = {0, 0};
 #pragma unroll
     for (int i = 0; i < G::kChunks; i += G::kStep)
       if (g.any(i)) {
         uint64_t* f = x + i * G::kElems / 2;
-        g.take(at, i, (int)((uintptr_t)(a.x + here) & 15u), f);
+        g.take(here_at, i, (int)((uintptr_t)(a.x + here) & 15u), f);
 #pragma unroll
         for (int k = 0; k < P; ++k) s2[k & 1] = add_pair(s2[k & 1], f[k]);
       }
@@ -544,14 +557,15 @@ __global__ void __launch_bounds__(kLnThreads, 1) layernorm_grad_kernel(const LnA
     if (row + total <= last) { next_mean = __ldg(a.mean + row + total); next_rstd = __ldg(a.rstd + row + total); }
     cp_async_wait<D - 1>();
     if constexpr (MODE == kLnSingle) g.sync();
+    const uint32_t here_at = arrived(at);
     uint64_t x[G::kPairs], y[G::kPairs], s2[2] = {0, 0}, t2[2] = {0, 0};      // xh and u
     const uint64_t minus = pair_of(-mean, -mean), scale = pair_of(rstd, rstd);
 #pragma unroll
     for (int i = 0; i < G::kChunks; i += G::kStep)
       if (g.any(i)) {
         const int o = i * G::kElems / 2;
-        g.take(at, i, (int)((uintptr_t)(a.x + here) & 15u), x + o);
-        g.take(at + a.slot, i, (int)((uintptr_t)(a.dy + here) & 15u), y + o);      // 0 outside the slice, and with it all that x adds there
+        g.take(here_at, i, (int)((uintptr_t)(a.x + here) & 15u), x + o);
+        g.take(here_at + a.slot, i, (int)((uintptr_t)(a.dy + here) & 15u), y + o);      // 0 outside the slice, and with it all that x adds there
 #pragma unroll
         for (int k = o; k < o + P; ++k) {
           x[k] = mul_pair(add_pair(x[k], minus), scale);
@@ -671,16 +685,18 @@ struct LnPlan {
 static LnPlan ln_plan(int64_t M, int64_t N, int elt, bool grad, int mode) {
   LnPlan p = {};
   p.mode = mode;
-  // Forward 32 elements per thread: per row half the warps, with what a warp costs beside its elements (8192 x 4096 bf16: 25.9 us, with 16: 31.9).  Backward 16, beside the columns' sums.
-  p.per = grad ? 16 : 32;
+  // Forward up to 32 elements per thread: per row half the warps, with what a warp costs beside its elements, that up to 16 take (8192 x 4096 bf16: 25.9 us, with 16: 31.9).  Backward up to
+  // 16, beside the columns' sums.
+  const int most_per = grad ? 16 : 32;
   for (p.ranks = 1;; p.ranks *= 2) {
     p.slice = (int)(((N + p.ranks - 1) / p.ranks + 15) / 16 * 16);
-    if ((N < p.slice ? N : p.slice) <= kLnThreads * p.per) break;
+    if ((N < p.slice ? N : p.slice) <= kLnThreads * most_per) break;
   }
   // With edges only whole units count: 1031 elements of 16 bits have at most 128.
   const int cols = (int)(N < p.slice ? N : p.slice), width = mode == kLnEdges ? cols / (16 / elt) * (16 / elt) : cols;
-  for (p.warps = 1; p.warps * 32 * p.per < width; p.warps *= 2) {}
+  for (p.warps = 1; p.warps * 32 * most_per < width; p.warps *= 2) {}
   if (mode == kLnSingle || p.ranks > 1) p.warps = 16;
+  for (p.per = 8; p.per < most_per && (p.warps * 32 * p.per < width || mode == kLnSingle); p.per += 8) {}
   const int groups = kLnThreads / 32 / p.warps;
   // One block per SM; backward, whose blocks each leave a row of sums, at least two rows for every group, and one block for up to four.
   const int64_t most = kLnSms / p.ranks, rows = grad ? (M <= 4 * groups ? 4 : 2) : 1, want = (M + groups * rows - 1) / (groups * rows);
@@ -698,9 +714,11 @@ template <class E, int W, int PER, int MODE>
 static int ln_launch(bool grad, const LnArgs& a, const LnPlan& p, cudaStream_t stream) {
   const int slots = grad ? 2 * kLnDepth<E, PER, 2> : kLnDepth<E, PER, 1>;
   const uint32_t smem = kLnBefore<E, MODE> + (uint32_t)(kLnThreads / 32 / W * slots) * a.slot;
-  void (*kern)(LnArgs) = layernorm_kernel<E, W, PER, MODE>;
-  if constexpr (PER == 16)
-    if (grad) kern = layernorm_grad_kernel<E, W, PER, MODE>;
+  void (*kern)(LnArgs);
+  // of 16 warps with 16 elements each 8 would do, forward; beyond 16 there is no backward
+  if constexpr (PER > 16) kern = layernorm_kernel<E, W, PER, MODE>;
+  else if constexpr (W > 1) kern = layernorm_grad_kernel<E, W, PER, MODE>;
+  else kern = grad ? layernorm_grad_kernel<E, W, PER, MODE> : layernorm_kernel<E, W, PER, MODE>;
   static uint64_t configured[2] = {0, 0};
   if (first_use_on_this_device(configured[grad])) {
     const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kProdSmemLimit);
@@ -709,25 +727,34 @@ static int ln_launch(bool grad, const LnArgs& a, const LnPlan& p, cudaStream_t s
   return launch_pdl(grad ? "layer norm gradient" : "layer norm", kern, dim3((unsigned)(p.clusters * p.ranks)), kLnThreads, smem, p.ranks, stream, a);
 }
 
-template <class E, int PER, int MODE>
-static int ln_warps(bool grad, const LnArgs& a, const LnPlan& p, cudaStream_t stream) {
-  if constexpr (MODE != kLnSingle) {
-    switch (p.warps) {
-      case 1: return ln_launch<E, 1, PER, MODE>(grad, a, p, stream);
-      case 2: return ln_launch<E, 2, PER, MODE>(grad, a, p, stream);
-      case 4: return ln_launch<E, 4, PER, MODE>(grad, a, p, stream);
-      case 8: return ln_launch<E, 8, PER, MODE>(grad, a, p, stream);
-    }
+// W warps are taken where half of them would not do: with more than half of the largest PER each.
+template <class E, int W, int MODE>
+static int ln_width(bool grad, const LnArgs& a, const LnPlan& p, cudaStream_t stream) {
+  if constexpr (W == 1) {
+    if (p.per == 8) return ln_launch<E, 1, 8, MODE>(grad, a, p, stream);
   }
-  return ln_launch<E, 16, PER, MODE>(grad, a, p, stream);
+  if (grad || p.per == 16) return ln_launch<E, W, 16, MODE>(grad, a, p, stream);
+  if (p.per == 24) return ln_launch<E, W, 24, MODE>(grad, a, p, stream);
+  return ln_launch<E, W, 32, MODE>(grad, a, p, stream);
+}
+
+template <class E, int MODE>
+static int ln_warps(bool grad, const LnArgs& a, const LnPlan& p, cudaStream_t stream) {
+  switch (p.warps) {
+    case 1: return ln_width<E, 1, MODE>(grad, a, p, stream);
+    case 2: return ln_width<E, 2, MODE>(grad, a, p, stream);
+    case 4: return ln_width<E, 4, MODE>(grad, a, p, stream);
+    case 8: return ln_width<E, 8, MODE>(grad, a, p, stream);
+    default: return ln_width<E, 16, MODE>(grad, a, p, stream);
+  }
 }
 
 template <class E>
 static int ln_run(bool grad, const LnArgs& a, const LnPlan& p, cudaStream_t stream) {
   switch (p.mode) {
-    case kLnWhole: return p.per == 16 ? ln_warps<E, 16, kLnWhole>(grad, a, p, stream) : ln_warps<E, 32, kLnWhole>(grad, a, p, stream);
-    case kLnEdges: return p.per == 16 ? ln_warps<E, 16, kLnEdges>(grad, a, p, stream) : ln_warps<E, 32, kLnEdges>(grad, a, p, stream);
-    default: return p.per == 16 ? ln_warps<E, 16, kLnSingle>(grad, a, p, stream) : ln_warps<E, 32, kLnSingle>(grad, a, p, stream);
+    case kLnWhole: return ln_warps<E, kLnWhole>(grad, a, p, stream);
+    case kLnEdges: return ln_warps<E, kLnEdges>(grad, a, p, stream);
+    default: return grad ? ln_launch<E, 16, 16, kLnSingle>(grad, a, p, stream) : ln_launch<E, 16, 32, kLnSingle>(grad, a, p, stream);
   }
 }
 
