@@ -588,6 +588,9 @@ def layernorm_workspace(M: int, N: int) -> int:
     return n
 
 
+_LN_SIZES: dict = {}      # (M, N) -> layernorm_workspace(M, N)
+
+
 def layernorm_grad(dy, x, gamma, mean, rstd, dx, dgamma, dbeta, workspace=None, stream=None) -> None:
     """Gradients of layernorm for the gradient ``dy`` of y: dx [M, N], dgamma and dbeta [N] (any two of them may be None; asynchronous).  ``mean``
     and ``rstd`` as layernorm left them; ``workspace``: layernorm_workspace(M, N) bytes, allocated here when not given."""
@@ -601,7 +604,11 @@ def layernorm_grad(dy, x, gamma, mean, rstd, dx, dgamma, dbeta, workspace=None, 
     here = _device_tensors(*tensors)
     ws, n = None, 0
     if dgamma is not None or dbeta is not None:
-        ws, n = _workspace(workspace, x, 0 if workspace is not None else layernorm_workspace(M, N), stream)
+        if workspace is None and (M, N) not in _LN_SIZES:
+            if len(_LN_SIZES) > 1000:
+                _LN_SIZES.clear()
+            _LN_SIZES[M, N] = layernorm_workspace(M, N)
+        ws, n = _workspace(workspace, x, _LN_SIZES.get((M, N), 0), stream)
     _check(lib().sp_layernorm_grad(dy.data_ptr(), x.data_ptr(), _ptr(gamma), _ptr(mean), _ptr(rstd), _ptr(dx), _ptr(dgamma), _ptr(dbeta), M, N, code, w_code,
                                    _ptr(ws), n, _stream_on(here, stream)))
 
