@@ -189,8 +189,8 @@ struct LnGroup {
   }
   __device__ __forceinline__ int chunk(int i) const { return (i * W + wg) * 32 + lane; }
   __device__ __forceinline__ int column(int i) const { return head + chunk(i) * kElems; }
-  // PER is the least number of elements, in steps of 8, that holds the row: only the last 8 may be missing, and no warp passes any over.  (Blocks' and clusters' groups, whose CTAs have
-  // unequal slices, ask.)
+  // PER is the least number of elements, in steps of 8, that holds the row: only the last 8 may be missing, and no warp passes any over.  (Groups of 16 warps ask, as the CTAs of a cluster have
+  // unequal slices.)
   static constexpr int kSure = kUnits && W < 16 ? (PER - 8) / kElems : 0;
   __device__ __forceinline__ bool any(int i) const { return kUnits || (i * W + wg) * 32 < chunks; }
   __device__ __forceinline__ bool has(int i) const { return i < kSure || chunk(i) < chunks; }
@@ -389,7 +389,8 @@ struct LnGroup {
         }
       }
       if constexpr (W == 16)
-        if (ranks > 1) {      // (Every warp's sums straight to all CTAs behind one barrier: gradient of 2048 x 16384 fp32 97.8 us, so 91.9.)
+        if (ranks > 1) {      // (Every warp's sums straight to all CTAs behind one barrier: gradient of 2048 x 16384 fp32 97.8 us, so 91.9.  Groups of 8 warps in twice the CTAs, whose sums complete on
+                              // barriers of their own by st.async, so that a CTA's two groups need not wait for each other: 137.)
           const uint32_t here = far + parity * kLnMaxCluster * 4 * kLnSums;      // [CTA][sum]
           if (tid < ranks) {
 #pragma unroll
@@ -630,7 +631,7 @@ __global__ void __launch_bounds__(kLnThreads, 1) layernorm_grad_kernel(const LnA
 #pragma unroll
   for (int w = 0; w < 2; ++w) {
     __syncthreads();      // all rows, and the sums before these, have been read
-    float* mine = all_groups + g.group * a.pitch;
+    float* mine = all_groups + g.group * a.slice;
 #pragma unroll
     for (int i = 0; i < G::kChunks; i += G::kStep)
       if (g.any(i)) {
@@ -663,7 +664,7 @@ __global__ void __launch_bounds__(kLnThreads, 1) layernorm_grad_kernel(const LnA
     for (int c = threadIdx.x; c < g.cols; c += kLnThreads) {
       float s = 0.f;
 #pragma unroll
-      for (int i = 0; i < G::kGroups; ++i) s += all_groups[i * a.pitch + c];
+      for (int i = 0; i < G::kGroups; ++i) s += all_groups[i * a.slice + c];
       if (a.part != nullptr) a.part[((int64_t)(blockIdx.x / g.ranks) * 2 + w) * a.pitch + col0 + c] = s;
       else store_weight(w == 0 ? a.dgamma : a.dbeta, a.w_dtype, col0 + c, s);
     }
@@ -730,51 +731,50 @@ static LnPlan ln_plan(int64_t M, int64_t N, int elt, bool grad, int mode) {
   return p;
 }
 
-template <class E, int W, int PER, int MODE>
-static int ln_launch(bool grad, const LnArgs& a, const LnPlan& p, cudaStream_t stream) {
-  const int slots = grad ? 2 * kLnDepth<E, PER, 2> : kLnDepth<E, PER, 1>;
+template <bool GRAD, class E, int W, int PER, int MODE>
+static int ln_launch(const LnArgs& a, const LnPlan& p, cudaStream_t stream) {
+  const int slots = GRAD ? 2 * kLnDepth<E, PER, 2> : kLnDepth<E, PER, 1>;
   const uint32_t smem = kLnBefore<E, MODE> + (uint32_t)(kLnThreads / 32 / W * slots) * a.slot;
   void (*kern)(LnArgs);
-  // of 16 warps with 16 elements each 8 would do, forward; beyond 16 there is no backward
-  if constexpr (PER > 16) kern = layernorm_kernel<E, W, PER, MODE>;
-  else if constexpr (W > 1) kern = layernorm_grad_kernel<E, W, PER, MODE>;
-  else kern = grad ? layernorm_grad_kernel<E, W, PER, MODE> : layernorm_kernel<E, W, PER, MODE>;
-  static uint64_t configured[2] = {0, 0};
-  if (first_use_on_this_device(configured[grad])) {
+  if constexpr (GRAD) kern = layernorm_grad_kernel<E, W, PER, MODE>;
+  else kern = layernorm_kernel<E, W, PER, MODE>;
+  static uint64_t configured = 0;
+  if (first_use_on_this_device(configured)) {
     const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kProdSmemLimit);
-    if (e != cudaSuccess) { configured[grad] = 0; set_error("cudaFuncSetAttribute failed: %s", cudaGetErrorString(e)); return SP_ERR_CUDA; }
+    if (e != cudaSuccess) { configured = 0; set_error("cudaFuncSetAttribute failed: %s", cudaGetErrorString(e)); return SP_ERR_CUDA; }
   }
-  return launch_pdl(grad ? "layer norm gradient" : "layer norm", kern, dim3((unsigned)(p.clusters * p.ranks)), kLnThreads, smem, p.ranks, stream, a);
+  return launch_pdl(GRAD ? "layer norm gradient" : "layer norm", kern, dim3((unsigned)(p.clusters * p.ranks)), kLnThreads, smem, p.ranks, stream, a);
 }
 
-// W warps are taken where half of them would not do: with more than half of the largest PER each.
-template <class E, int W, int MODE>
-static int ln_width(bool grad, const LnArgs& a, const LnPlan& p, cudaStream_t stream) {
+// More than one warp is taken where half as many would not do, clusters where one CTA would not: each thread then has more than half of the most.
+template <bool GRAD, class E, int W, int MODE>
+static int ln_width(const LnArgs& a, const LnPlan& p, cudaStream_t stream) {
   if constexpr (W == 1) {
-    if (p.per == 8) return ln_launch<E, 1, 8, MODE>(grad, a, p, stream);
+    if (p.per == 8) return ln_launch<GRAD, E, W, 8, MODE>(a, p, stream);
+    if (!GRAD && p.per == 16) return ln_launch<false, E, W, 16, MODE>(a, p, stream);
   }
-  if (grad || p.per == 16) return ln_launch<E, W, 16, MODE>(grad, a, p, stream);
-  if (p.per == 24) return ln_launch<E, W, 24, MODE>(grad, a, p, stream);
-  return ln_launch<E, W, 32, MODE>(grad, a, p, stream);
+  if constexpr (GRAD) return ln_launch<true, E, W, 16, MODE>(a, p, stream);
+  else if (p.per == 24) return ln_launch<false, E, W, 24, MODE>(a, p, stream);
+  else return ln_launch<false, E, W, 32, MODE>(a, p, stream);
 }
 
-template <class E, int MODE>
-static int ln_warps(bool grad, const LnArgs& a, const LnPlan& p, cudaStream_t stream) {
+template <bool GRAD, class E, int MODE>
+static int ln_warps(const LnArgs& a, const LnPlan& p, cudaStream_t stream) {
   switch (p.warps) {
-    case 1: return ln_width<E, 1, MODE>(grad, a, p, stream);
-    case 2: return ln_width<E, 2, MODE>(grad, a, p, stream);
-    case 4: return ln_width<E, 4, MODE>(grad, a, p, stream);
-    case 8: return ln_width<E, 8, MODE>(grad, a, p, stream);
-    default: return ln_width<E, 16, MODE>(grad, a, p, stream);
+    case 1: return ln_width<GRAD, E, 1, MODE>(a, p, stream);
+    case 2: return ln_width<GRAD, E, 2, MODE>(a, p, stream);
+    case 4: return ln_width<GRAD, E, 4, MODE>(a, p, stream);
+    case 8: return ln_width<GRAD, E, 8, MODE>(a, p, stream);
+    default: return ln_width<GRAD, E, 16, MODE>(a, p, stream);
   }
 }
 
-template <class E>
-static int ln_run(bool grad, const LnArgs& a, const LnPlan& p, cudaStream_t stream) {
+template <bool GRAD, class E>
+static int ln_run(const LnArgs& a, const LnPlan& p, cudaStream_t stream) {
   switch (p.mode) {
-    case kLnWhole: return ln_warps<E, kLnWhole>(grad, a, p, stream);
-    case kLnEdges: return ln_warps<E, kLnEdges>(grad, a, p, stream);
-    default: return grad ? ln_launch<E, 16, 16, kLnSingle>(grad, a, p, stream) : ln_launch<E, 16, 32, kLnSingle>(grad, a, p, stream);
+    case kLnWhole: return ln_warps<GRAD, E, kLnWhole>(a, p, stream);
+    case kLnEdges: return ln_warps<GRAD, E, kLnEdges>(a, p, stream);
+    default: return ln_launch<GRAD, E, 16, GRAD ? 16 : 32, kLnSingle>(a, p, stream);
   }
 }
 
@@ -785,13 +785,14 @@ static int ln_mode(const LnArgs& a, int elt) {
   return (x & 15u) == 0 && (int64_t)a.N * elt % 16 == 0 ? kLnWhole : kLnEdges;
 }
 
-static int ln_any(bool grad, LnArgs& a, int32_t dtype, cudaStream_t stream, const LnPlan& p) {
+template <bool GRAD>
+static int ln_any(LnArgs& a, int32_t dtype, cudaStream_t stream, const LnPlan& p) {
   a.slice = p.slice; a.clusters = p.clusters; a.pitch = p.pitch;
   a.slot = (uint32_t)p.slice * ln_bytes(dtype) + 16;
   std::lock_guard<std::mutex> lock(g_ln_mu);
-  if (dtype == SP_BF16) return ln_run<Ln16<true>>(grad, a, p, stream);
-  if (dtype == SP_FP16) return ln_run<Ln16<false>>(grad, a, p, stream);
-  return ln_run<Ln32>(grad, a, p, stream);
+  if (dtype == SP_BF16) return ln_run<GRAD, Ln16<true>>(a, p, stream);
+  if (dtype == SP_FP16) return ln_run<GRAD, Ln16<false>>(a, p, stream);
+  return ln_run<GRAD, Ln32>(a, p, stream);
 }
 
 static int check_ln(int64_t M, int64_t N, int32_t dtype, int32_t w_dtype) {
@@ -831,7 +832,7 @@ int sp_layernorm(const void* x, const void* gamma, const void* beta, void* y, fl
   LnArgs a = {};
   a.x = (const char*)x; a.gamma = gamma; a.beta = beta; a.out = (char*)y; a.mean = mean; a.rstd = rstd;
   a.M = M; a.N = (int)N; a.w_dtype = w_dtype; a.eps = eps;
-  return ln_any(false, a, dtype, (cudaStream_t)stream, ln_plan(M, N, ln_bytes(dtype), false, ln_mode(a, ln_bytes(dtype))));
+  return ln_any<false>(a, dtype, (cudaStream_t)stream, ln_plan(M, N, ln_bytes(dtype), false, ln_mode(a, ln_bytes(dtype))));
 }
 
 int64_t sp_layernorm_workspace(int64_t M, int64_t N) {
@@ -877,7 +878,7 @@ int sp_layernorm_grad(const void* dy, const void* x, const void* gamma, const fl
   const LnPlan p = ln_plan(M, N, ln_bytes(dtype), true, ln_mode(a, ln_bytes(dtype)));
   if (p.clusters > 1) a.part = weights ? (float*)workspace : nullptr;
   else { a.dgamma = dgamma; a.dbeta = dbeta; }
-  rc = ln_any(true, a, dtype, (cudaStream_t)stream, p);
+  rc = ln_any<true>(a, dtype, (cudaStream_t)stream, p);
   if (rc == SP_OK && a.part)
     rc = launch_pdl("layer norm gradient of the weights", layernorm_weights_kernel, dim3((unsigned)((N + 31) / 32), 2), 1024, 0, 1, (cudaStream_t)stream,
                     (const float*)a.part, p.clusters, p.pitch, (int)N, w_dtype, dgamma, dbeta);
