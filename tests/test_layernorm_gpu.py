@@ -37,18 +37,18 @@ def within(got, want, tol, what):
 
 
 class Case:
-    """Inputs `off` elements behind an allocation, outputs between guards."""
+    """Inputs `off` elements behind an allocation (or, unless `alike`, a multiple of them), outputs between guards."""
 
-    def __init__(self, M, N, x="bf16", w="bf16", off=0, scale=1.0, shift=0.3, seed=0, weights=True):
+    def __init__(self, M, N, x="bf16", w="bf16", off=0, scale=1.0, shift=0.3, seed=0, weights=True, alike=False):
         g = torch.Generator().manual_seed(seed * 100003 + M * 7 + N)
         self.M, self.N, self.xt, self.wt = M, N, x, w
         self.guards = []
         self.x = self.place(torch.randn(M, N, generator=g) * scale + shift, x, off)
-        self.dy = self.place(torch.randn(M, N, generator=g), x, off * 3)
+        self.dy = self.place(torch.randn(M, N, generator=g), x, off * (1 if alike else 3))
         self.gamma = self.place(1 + 0.3 * torch.randn(N, generator=g), w, off) if weights else None
         self.beta = self.place(torch.randn(N, generator=g), w, off) if weights else None
         nan = float("nan")
-        self.y = self.place(torch.full((M, N), nan), x, off * 2, guard=True)
+        self.y = self.place(torch.full((M, N), nan), x, off * (1 if alike else 2), guard=True)
         self.dx = self.place(torch.full((M, N), nan), x, off, guard=True)
         self.dgamma, self.dbeta = (self.place(torch.full((N,), nan), w, off, guard=True) for _ in range(2))
         self.mean, self.rstd = (self.place(torch.full((M,), nan), "fp32", off, guard=True) for _ in range(2))
@@ -114,11 +114,12 @@ def test_widths(N, types):
         c.check_guards()
 
 
+@pytest.mark.parametrize("alike", [False, True])
 @pytest.mark.parametrize("off", [1, 3, 4, 7, 8])
-@pytest.mark.parametrize("M,N", [(1, 5), (9, 1031), (5, 1032), (3, 4095), (3, 4104), (2, 9001), (40, 96)])
+@pytest.mark.parametrize("M,N", [(1, 5), (300, 3), (9, 1031), (5, 1032), (3, 4095), (3, 4104), (2, 9001), (3, 17001), (40, 96)])
 @pytest.mark.parametrize("types", [("bf16", "fp32"), ("fp16", "fp16"), ("fp32", "fp32")], ids="-".join)
-def test_any_address(M, N, types, off):
-    c = Case(M, N, *types, off=off)
+def test_any_address(M, N, types, off, alike):
+    c = Case(M, N, *types, off=off, alike=alike)
     c.forward()
     c.check_forward()
     c.backward()
