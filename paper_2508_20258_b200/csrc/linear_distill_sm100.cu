@@ -37,13 +37,42 @@ struct TeacherArgs {
 };
 enum : int { kIgnored = 0, kKept = 1, kInvalid = 2 };      // no word, or none with a logit above minus infinity; a word outside the vocabulary
 
-// GROUP threads per token: a warp while its keys are few, else the block.
-template <int GROUP>
+// Sorts 32 KEYS keys, the c-th of a lane being element 32 c + lane, in registers (4096 tokens of 64 words by way of shared memory 15.6 us, so 10.4).
+template <int KEYS>
+__device__ __forceinline__ void sort_keys(uint64_t (&key)[KEYS], int lane) {
+#pragma unroll
+  for (int k = 2; k <= 32 * KEYS; k *= 2)
+#pragma unroll
+    for (int o = k / 2; o; o /= 2) {
+      if (o >= 32) {
+#pragma unroll
+        for (int c = 0; c < KEYS; ++c)
+          if ((c & (o / 32)) == 0) {
+            uint64_t &u = key[c], &w = key[c | (o / 32)];
+            if ((u > w) == ((c * 32 & k) == 0)) {
+              const uint64_t t = u;
+              u = w; w = t;
+            }
+          }
+      } else {
+#pragma unroll
+        for (int c = 0; c < KEYS; ++c) {
+          const uint64_t w = __shfl_xor_sync(0xffffffffu, key[c], o);
+          const bool low = ((c * 32 + lane) & k) == 0 == ((lane & o) == 0);      // this one keeps the smaller
+          if ((w < key[c]) == low) key[c] = w;
+        }
+      }
+    }
+}
+
+// GROUP threads per token, 32 KEYS keys: a warp, sorting in registers, or (KEYS 0: `size` of them) the block, in shared memory.
+template <int GROUP, int KEYS>
 __global__ void __launch_bounds__(256) teacher_kernel(const TeacherArgs a) {
   extern __shared__ uint64_t teacher_keys[];
   __shared__ float part[8];
   const int group = threadIdx.x / GROUP, i0 = threadIdx.x % GROUP, lane = threadIdx.x & 31;
-  uint64_t* key = teacher_keys + group * a.size;
+  uint64_t* key = teacher_keys + group * a.size;                                               // word, and where it stood
+  float* value = reinterpret_cast<float*>(teacher_keys + 256 / GROUP * a.size) + group * a.size;      // logits as they stood
   const auto sync = [] {
     if constexpr (GROUP == 32) __syncwarp();
     else __syncthreads();
@@ -73,11 +102,14 @@ __global__ void __launch_bounds__(256) teacher_kernel(const TeacherArgs a) {
       return lo;
     };
     float state = kIgnored, top = -CUDART_INF_F;
-    for (int j = i0; j < a.size; j += GROUP) {
+    uint64_t mine[KEYS ? KEYS : 1];
+#pragma unroll
+    for (int j = i0, c = 0; KEYS ? c < KEYS : j < a.size; j += GROUP, ++c) {
       int word = kNoWord;
       if (j < a.K) {
         const int64_t v = __ldg(a.index + t * a.K + j);
         const float l = logit(j);
+        value[j] = l;
         if (v >= a.V) state = kInvalid;
         else if (v >= 0) {
           word = (int)v;
@@ -85,22 +117,31 @@ __global__ void __launch_bounds__(256) teacher_kernel(const TeacherArgs a) {
           if (l != -CUDART_INF_F) state = fmaxf(state, kKept);
         }
       }
-      key[j] = (uint64_t)word << 32 | (uint32_t)j;
+      const uint64_t k = (uint64_t)word << 32 | (uint32_t)j;
+      if constexpr (KEYS > 0) mine[c] = k;
+      else key[j] = k;
     }
     state = over_group(state, true);
     top = over_group(top, true);
-    sync();
-    for (int k = 2; k <= a.size; k *= 2)      // bitonic sort
-      for (int o = k / 2; o; o /= 2) {
-        for (int i = i0; i < a.size / 2; i += GROUP) {
-          const int x = (i & ~(o - 1)) * 2 + (i & (o - 1)), y = x + o;
-          const uint64_t u = key[x], w = key[y];
-          if ((u > w) == ((x & k) == 0)) { key[x] = w; key[y] = u; }
+    if constexpr (KEYS > 0) {
+      sort_keys<KEYS>(mine, lane);
+#pragma unroll
+      for (int c = 0; c < KEYS; ++c) key[c * 32 + lane] = mine[c];
+      sync();
+    } else {
+      sync();
+      for (int k = 2; k <= a.size; k *= 2)      // bitonic, as in registers
+        for (int o = k / 2; o; o /= 2) {
+          for (int i = i0; i < a.size / 2; i += GROUP) {
+            const int x = (i & ~(o - 1)) * 2 + (i & (o - 1)), y = x + o;
+            const uint64_t u = key[x], w = key[y];
+            if ((u > w) == ((x & k) == 0)) { key[x] = w; key[y] = u; }
+          }
+          sync();
         }
-        sync();
-      }
+    }
     float sum = 0.f;
-    const auto term = [&](int i) { return ex2((logit((int)(uint32_t)key[i]) - top) * a.scale); };      // a NaN, an infinity: all NaN
+    const auto term = [&](int i) { return ex2((value[(uint32_t)key[i]] - top) * a.scale); };      // a NaN, an infinity: all NaN
     for (int i = i0; i < a.K; i += GROUP)
       if ((int)(key[i] >> 32) != kNoWord) sum += term(i);
     sum = over_group(sum, false);
@@ -110,7 +151,7 @@ __global__ void __launch_bounds__(256) teacher_kernel(const TeacherArgs a) {
       float q = 0.f, lq = -CUDART_INF_F;
       if (word != kNoWord && (i == 0 || (int)(key[i - 1] >> 32) != word)) {
         q = term(i);
-        lq = fmaf(logit(j) - top, a.scale, -log_sum);
+        lq = fmaf(value[j] - top, a.scale, -log_sum);
         int n = i + 1;
         for (; n < a.K && (int)(key[n] >> 32) == word; ++n) q += term(n);
         if (n > i + 1) lq = log2f(q) - log_sum;
@@ -118,24 +159,22 @@ __global__ void __launch_bounds__(256) teacher_kernel(const TeacherArgs a) {
       }
       a.word[t * a.K + i] = word; a.slot[t * a.K + i] = j; a.q[t * a.K + i] = q; a.lq[t * a.K + i] = lq;
     }
-    // words before each part's first column, four parts at a time: the steps of a search wait for one another
-    for (int p0 = i0; p0 <= a.parts; p0 += 4 * GROUP) {
-      uint64_t first[4];
-      int n[4];
-#pragma unroll
-      for (int c = 0; c < 4; ++c) {
-        const int p = p0 + c * GROUP;
-        first[c] = (uint64_t)((int64_t)(p >> 1) * a.bn + (p & 1) * kCePart) << 32;      // a tile's two parts
-        n[c] = 0;
-      }
-      for (int step = a.size / 2; step; step /= 2)
-#pragma unroll
-        for (int c = 0; c < 4; ++c)
-          if (key[n[c] + step - 1] < first[c]) n[c] += step;
-#pragma unroll
-      for (int c = 0; c < 4; ++c)
-        if (p0 + c * GROUP <= a.parts) a.start[t * (a.parts + 1) + p0 + c * GROUP] = (uint16_t)(n[c] + (key[n[c]] < first[c]));
+    // Words before each part's first column: the i-th word makes that i from the part behind the word's before on, up to its own.  Before the first and behind the last all
+    // threads write; `used` words are in a part.
+    const auto part_of = [&](uint32_t word) { return (int)(word / a.bn * 2 + (word % a.bn >= (uint32_t)kCePart)); };
+    uint16_t* start = a.start + t * (a.parts + 1);
+    int used = 0;
+    for (int i = i0; i < a.K; i += GROUP) {
+      const uint32_t word = (uint32_t)(key[i] >> 32);
+      if (word == kNoWord) break;
+      used = i + 1;
+      if (i > 0)
+        for (int p = part_of((uint32_t)(key[i - 1] >> 32)) + 1, end = part_of(word); p <= end; ++p) start[p] = (uint16_t)i;
     }
+    used = (int)over_group((float)used, true);
+    const int first = used ? part_of((uint32_t)(key[0] >> 32)) : a.parts, last = used ? part_of((uint32_t)(key[used - 1] >> 32)) : a.parts;
+    for (int p = i0; p <= first; p += GROUP) start[p] = 0;
+    for (int p = last + 1 + i0; p <= a.parts; p += GROUP) start[p] = (uint16_t)used;
     if (i0 == 0) a.state[t] = (int)state;
     sync();
   }
@@ -506,9 +545,13 @@ static int launch_teacher(TeacherArgs& a, cudaStream_t stream) {
   const int per_block = a.size <= 256 ? 8 : 1;      // tokens
   const int64_t blocks = div_up(a.T, per_block);
   const unsigned grid = (unsigned)(blocks < 148 * 8 ? blocks : 148 * 8);
-  const size_t smem = (size_t)per_block * a.size * 8;
-  if (per_block == 8) return launch_pdl("teacher's words", teacher_kernel<32>, dim3(grid), 256, smem, 1, stream, a);
-  return launch_pdl("teacher's words", teacher_kernel<256>, dim3(grid), 256, smem, 1, stream, a);
+  const size_t smem = (size_t)per_block * a.size * 12;
+  void (*kern)(TeacherArgs) = teacher_kernel<256, 0>;
+  if (a.size == 32) kern = teacher_kernel<32, 1>;
+  else if (a.size == 64) kern = teacher_kernel<32, 2>;
+  else if (a.size == 128) kern = teacher_kernel<32, 4>;
+  else if (a.size == 256) kern = teacher_kernel<32, 8>;
+  return launch_pdl("teacher's words", kern, dim3(grid), 256, smem, 1, stream, a);
 }
 
 }  // namespace sp
