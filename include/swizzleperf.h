@@ -463,7 +463,8 @@ int sp_linear_distill_grad(const void* h, const void* W, const int64_t* top_inde
                            void* stream);
 
 /* Bytes of workspace sp_linear_distill (grad = 0) or sp_linear_distill_grad (grad != 0) needs; -1 on sizes that those refuse.  Host only.
- * Forward: 10 bytes for every token and 128 words, 20 for each of the teacher's, and at most one copy of h.  Gradient: as sp_linear_ce_workspace. */
+ * Forward: 10 bytes for every token and 128 words, 20 for each of the teacher's, and at most one copy of h.  Gradient: as sp_linear_ce_workspace,
+ * for up to 64 tokens as for twice as many: these keep the rounding errors of g beside it. */
 int64_t sp_linear_distill_workspace(int64_t T, int64_t V, int64_t D, int64_t K, int32_t grad);
 
 /* Layer norm of the rows of x:  y[m][n] = (x[m][n] - mean[m]) * rstd[m] * gamma[n] + beta[n],  mean[m] = sum_n x[m][n] / N,

@@ -366,6 +366,7 @@ def test_end_of_a_students_training_step():
     each = tau ** 2 * (torch.special.entr(q).neg() - q * logp).sum(1)
     total = torch.where(kept, each, 0.0).sum() / kept.sum()
     total.backward()
+    total = total.detach()
     # norms: half a step of rounding in h moves the scores by 2^-9 of their size (random signs), p and with it g by as much relative
     far = lambda got, want: float((got.double() - want).norm() / want.norm())  # noqa: E731
     assert abs(float(loss) - float(total)) <= 2.0 ** -7 * float(total)
