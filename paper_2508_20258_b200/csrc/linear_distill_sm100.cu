@@ -266,6 +266,9 @@ struct DistillJoin {
   float* diff;        // [T][K], in the caller's order
   float* each;        // loss per token
   float* loss;        // the reduced loss (mean, sum), else nullptr
+  const uint4* h;     // rows of `vecs` vectors of 8 elements
+  const uint4* W;
+  int vecs, bf16;
   int T, K, tiles;
   float scale, tau;
   int mean;
@@ -302,6 +305,28 @@ __global__ void __launch_bounds__(1024) distill_join_kernel(const DistillJoin a,
 #pragma unroll
     for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
     return v;
+  };
+  // A word's score once more, by a warp.  The tensor cores cut sums off towards zero, of products that are all positive, as where a state lies along its word's row of W, a little each time,
+  // and more where products are long: of tokens that have settled on a word the score of fp16 was 2e-7 of itself too small and p - q of a batch with them off by 2 to 4e-6 (24 x 32768 x 1024), so
+  // 1e-7.  It takes the reading of a row of h and one of W, 1 to 2 us.  (bf16, whose products have 16 bits for 22: 0.3 to 1.7e-6, left so.)
+  const auto score_of = [&](int64_t t, int word) {
+    const uint4 *u = a.h + t * a.vecs, *w = a.W + (int64_t)word * a.vecs;
+    float z = 0.f;
+#pragma unroll 4
+    for (int i = lane; i < a.vecs; i += 32) {
+      const uint4 p = __ldg(u + i), q = __ldg(w + i);
+      const uint32_t pu[4] = {p.x, p.y, p.z, p.w}, qu[4] = {q.x, q.y, q.z, q.w};
+      float s[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        float ul, uh, wl, wh;
+        row_values(pu[k], a.bf16, ul, uh);
+        row_values(qu[k], a.bf16, wl, wh);
+        s[k] = fmaf(uh, wh, ul * wl);
+      }
+      z += (s[0] + s[1]) + (s[2] + s[3]);
+    }
+    return total_of(z);
   };
   struct Word {
     int word, slot;
@@ -347,30 +372,34 @@ __global__ void __launch_bounds__(1024) distill_join_kernel(const DistillJoin a,
       const int state = a.state[t];
       // the largest score, and which of the teacher's words has it (the first of them)
       float own_top = -CUDART_INF_F;
-      int own_at = 0;
+      int own_at = 0, own_word = kNoWord;
       each_word([&](int i, const Word& x) {
-        if (x.first && x.z > own_top) { own_top = x.z; own_at = i; }
+        if (x.first && (x.z > own_top || i == 0)) { own_top = x.z; own_at = i; own_word = x.word; }
       });
 #pragma unroll
       for (int o = 16; o; o >>= 1) {
         const float z = __shfl_xor_sync(0xffffffffu, own_top, o);
-        const int at = __shfl_xor_sync(0xffffffffu, own_at, o);
-        if (z > own_top || (z == own_top && at < own_at)) { own_top = z; own_at = at; }
+        const int at = __shfl_xor_sync(0xffffffffu, own_at, o), word = __shfl_xor_sync(0xffffffffu, own_word, o);
+        if (word != kNoWord && (own_word == kNoWord || z > own_top || (z == own_top && at < own_at))) { own_top = z; own_at = at; own_word = word; }
+      }
+      const bool kept = state == kKept;
+      if (kept && !a.bf16) {      // p is at most this, without the teacher's other words; of p below 1/64 the error does not count
+        const float top = fmaxf(pair.x, own_top * a.scale), own = ex2(fmaf(own_top, a.scale, -top));
+        if (own > (own + pair.y * ex2(pair.x - top)) * 0x1p-6f) own_top = score_of(t, own_word);
       }
       const float top = fmaxf(pair.x, own_top * a.scale), ref = top == -CUDART_INF_F ? 0.f : top;
       const float others = pair.y * ex2(pair.x - ref);      // the words that are not the teacher's
-      const auto exponent = [&](float z) { return fmaf(z, a.scale, -ref); };
+      const auto exponent = [&](int i, const Word& x) { return fmaf(i == own_at ? own_top : x.z, a.scale, -ref); };
       float mine = 0.f, q_rest = 0.f, largest = 0.f;         // all of the teacher's but the largest, and that one
       each_word([&](int i, const Word& x) {
         if (!x.first) return;
-        const float e = ex2(exponent(x.z));
+        const float e = ex2(exponent(i, x));
         if (i == own_at) largest = e;
         else { mine += e; q_rest += x.q; }
       });
       mine = total_of(mine);
       q_rest = total_of(q_rest);
       largest = total_of(largest);
-      const bool kept = state == kKept;
       const float rest = others + mine, total = rest + largest;
       const float bits = log2f(total);
       float sum = 0.f;
@@ -378,7 +407,7 @@ __global__ void __launch_bounds__(1024) distill_join_kernel(const DistillJoin a,
         float diff = state == kInvalid ? CUDART_NAN_F : 0.f;
         if (kept && x.word != kNoWord) {
           if (!x.first) return;      // the first of its equals writes
-          const float e = exponent(x.z), p = ex2(e) / total;
+          const float e = exponent(i, x), p = ex2(e) / total;
           const bool most = i == own_at && p > 0.5f;      // of it 1 - p is better known than p, and 1 - q than q
           sum += divergence(x.q, p, most && x.q > 0.5f ? log1pf(-q_rest) + log1pf(rest / largest) : (x.lq - (e - bits)) * kLn2);
           diff = most ? q_rest - rest / total : p - x.q;
@@ -609,10 +638,13 @@ int sp_linear_distill(const void* h, const void* W, const int64_t* top_index, co
   j.stats = ea.stats; j.picked = ea.picked; j.word = ta.word; j.slot = ta.slot; j.q = ta.q; j.lq = ta.lq; j.state = ta.state; j.lse = lse; j.diff = diff;
   j.each = reduction == SP_REDUCE_NONE ? loss : (float*)(ws + p.off_each);
   j.loss = reduction == SP_REDUCE_NONE ? nullptr : loss;
+  j.h = (const uint4*)h; j.W = (const uint4*)W; j.vecs = (int)(D / 8); j.bf16 = dtype == SP_BF16;
   j.T = (int)T; j.K = (int)K; j.tiles = p.parts; j.scale = scale; j.tau = temperature; j.mean = reduction == SP_REDUCE_MEAN;
-  // As the cross entropy's: 256 threads while a row's pairs are one batch of reads, one block for up to 64 tokens of few pairs, and the sum of their losses with them.
-  const int shift = T <= 4 ? 2 : 5, threads = p.parts <= 8 * (256 >> shift) ? 256 : 1024;
-  const unsigned blocks = j.loss && T <= 64 && p.parts <= 256 ? 1u : (unsigned)div_up(T, 1 << shift);
+  // A warp per token: eight to a block, or all in one block, with the sum of their losses, while 32 warps suffice.  (32 to a block of 8 warps, as the cross entropy has them: 110 x 1216 x 688, 75
+  // words, 27 us in this kernel alone, so 10.)
+  const bool one = j.loss && T <= 32;
+  const int shift = one ? 5 : 3, threads = 32 << shift;
+  const unsigned blocks = (unsigned)div_up(T, 1 << shift);
   rc = launch_pdl("join of the row statistics", K <= 32 ? distill_join_kernel<1> : K <= 128 ? distill_join_kernel<4> : distill_join_kernel<0>, dim3(blocks), threads, 0, 1, stream, j, shift);
   if (rc == SP_OK && j.loss && blocks > 1) rc = launch_pdl("sum of the losses", distill_reduce_kernel, dim3(1), 1024, 0, 1, stream, j);
   return rc;
