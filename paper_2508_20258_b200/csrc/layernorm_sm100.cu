@@ -707,17 +707,18 @@ static LnPlan ln_plan(int64_t M, int64_t N, int elt, bool grad, int mode) {
   LnPlan p = {};
   p.mode = mode;
   // Forward up to 32 elements per thread: per row half the warps, with what a warp costs beside its elements, that up to 16 take (8192 x 4096 bf16: 25.9 us, with 16: 31.9).  Backward up to
-  // 16, beside the columns' sums.
-  const int most_per = grad ? 16 : 32;
+  // 16, beside the columns' sums; with 24 some of it leaves the registers (4096 x 5120 44 us, with 16: 36), but 16 warps of 24 save a cluster CTAs (4096 x 12288 in one CTA 96 us, in two
+  // 105; 2000 x 20000 fp32 in two 156, in four 247).
+  const int most_per = grad ? 16 : 32, widest = grad && mode != kLnSingle ? 24 : most_per;
   for (p.ranks = 1;; p.ranks *= 2) {
     p.slice = (int)(((N + p.ranks - 1) / p.ranks + 15) / 16 * 16);
-    if ((N < p.slice ? N : p.slice) <= kLnThreads * most_per) break;
+    if ((N < p.slice ? N : p.slice) <= kLnThreads * widest) break;
   }
   // With edges only whole units count: 1031 elements of 16 bits have at most 128.
   const int cols = (int)(N < p.slice ? N : p.slice), width = mode == kLnEdges ? cols / (16 / elt) * (16 / elt) : cols;
-  for (p.warps = 1; p.warps * 32 * most_per < width; p.warps *= 2) {}
+  for (p.warps = 1; p.warps < 16 && p.warps * 32 * most_per < width; p.warps *= 2) {}
   if (mode == kLnSingle || p.ranks > 1) p.warps = 16;
-  for (p.per = 8; p.per < most_per && (p.warps * 32 * p.per < width || mode == kLnSingle); p.per += 8) {}
+  for (p.per = 8; p.per < widest && (p.warps * 32 * p.per < width || mode == kLnSingle); p.per += 8) {}
   const int groups = kLnThreads / 32 / p.warps;
   // One block per SM; backward, whose blocks each leave a row of sums, at least two rows for every group, and one block for up to four.
   const int64_t most = kLnSms / p.ranks, rows = grad ? (M <= 4 * groups ? 4 : 2) : 1, want = (M + groups * rows - 1) / (groups * rows);
@@ -746,12 +747,16 @@ static int ln_launch(const LnArgs& a, const LnPlan& p, cudaStream_t stream) {
   return launch_pdl(GRAD ? "layer norm gradient" : "layer norm", kern, dim3((unsigned)(p.clusters * p.ranks)), kLnThreads, smem, p.ranks, stream, a);
 }
 
-// More than one warp is taken where half as many would not do, clusters where one CTA would not: each thread then has more than half of the most.
+// More than one warp is taken where half as many would not do, clusters where one CTA would not: each thread then has more than half of the most (backward in clusters, of 12288 columns and
+// more, 16 or 24 all the same).
 template <bool GRAD, class E, int W, int MODE>
 static int ln_width(const LnArgs& a, const LnPlan& p, cudaStream_t stream) {
   if constexpr (W == 1) {
     if (p.per == 8) return ln_launch<GRAD, E, W, 8, MODE>(a, p, stream);
     if (!GRAD && p.per == 16) return ln_launch<false, E, W, 16, MODE>(a, p, stream);
+  }
+  if constexpr (GRAD && W == 16) {
+    if (p.per == 24) return ln_launch<true, E, W, 24, MODE>(a, p, stream);
   }
   if constexpr (GRAD) return ln_launch<true, E, W, 16, MODE>(a, p, stream);
   else if (p.per == 24) return ln_launch<false, E, W, 24, MODE>(a, p, stream);

@@ -127,7 +127,7 @@ def test_any_address(M, N, types, off, alike):
     c.check_guards()
 
 
-@pytest.mark.parametrize("M,N", [(2, 4096), (4095, 64), (700, 1031), (1500, 2048), (900, 5000), (20011, 40), (3000, 512), (1300, 4104)])
+@pytest.mark.parametrize("M,N", [(2, 4096), (4095, 64), (700, 1031), (1500, 2048), (900, 5000), (20011, 40), (3000, 512), (1300, 4104), (700, 12288), (800, 9001), (400, 20008)])
 def test_many_rows(M, N):
     c = Case(M, N, "bf16", "fp32")
     c.forward()
