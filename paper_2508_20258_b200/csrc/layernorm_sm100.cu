@@ -412,6 +412,11 @@ struct LnGroup {
 template <class E, int MODE>
 constexpr uint32_t kLnBefore = kLnSumBytes + (MODE == kLnEdges && E::kBytes == 2 ? kLnThreads * 8 * 4 : 0);
 
+// Backward with 24 elements per thread, gamma waits in shared memory, where the rows' ring leaves room for it (16 bits): 4096 x 12288 78 us, in registers, which it overfills, 96.  Every
+// thread keeps its own, 16 bytes of each side by side.
+template <class E, int PER>
+constexpr bool kLnFarGamma = PER == 24 && E::kBytes == 2;
+
 // Batches of `rows` rows' slices on their way.
 template <class E, int PER, int ROWS>
 constexpr int kLnDepth = kLnRing / (kLnThreads * PER * E::kBytes * ROWS) < 3 ? kLnRing / (kLnThreads * PER * E::kBytes * ROWS) : 3;
@@ -533,7 +538,9 @@ __global__ void __launch_bounds__(kLnThreads, 1) layernorm_grad_kernel(const LnA
   constexpr int D = kLnDepth<E, PER, 2>, P = G::kWide;
   const uint32_t base = smem_u32(ln_smem);
   G g(a, base);
-  const uint32_t ring = base + kLnBefore<E, MODE> + g.group * D * 2 * a.slot, batch = 2 * a.slot;
+  constexpr bool kFar = kLnFarGamma<E, PER>;
+  const uint32_t gammas = base + kLnBefore<E, MODE> + threadIdx.x * 16;
+  const uint32_t ring = base + kLnBefore<E, MODE> + (kFar ? kLnThreads * PER * 4 : 0) + g.group * D * 2 * a.slot, batch = 2 * a.slot;
   const uint32_t total = a.clusters * G::kGroups, last = (uint32_t)a.M - 1;
   const int col0 = g.rank * a.slice;
   const int64_t pitch = (int64_t)a.N * E::kBytes, hop = (int64_t)total * pitch, all = a.M * pitch;
@@ -554,6 +561,10 @@ __global__ void __launch_bounds__(kLnThreads, 1) layernorm_grad_kernel(const LnA
   for (int i = 0; i < D; ++i, ahead += total) fetch(ring + i * batch, ahead);
   uint64_t gamma[G::kPairs], dg[G::kPairs], db[G::kPairs];
   g.weights(a.gamma, a.w_dtype, col0, 1.f, gamma);
+  if constexpr (kFar) {
+#pragma unroll
+    for (int k = 0; k < G::kPairs; k += 2) asm volatile("st.shared.v2.b64 [%0], {%1, %2};" :: "r"(gammas + k * 8 * kLnThreads), "l"(gamma[k]), "l"(gamma[k + 1]) : "memory");
+  }
 #pragma unroll
   for (int k = 0; k < G::kPairs; ++k) dg[k] = db[k] = 0;
   const float inv = 1.f / (float)a.N;
@@ -579,6 +590,10 @@ __global__ void __launch_bounds__(kLnThreads, 1) layernorm_grad_kernel(const LnA
       if (g.any(i)) {
         const int o = i * G::kElems / 2;
         g.take(here_at, i, (int)((uintptr_t)(a.x + here) & 15u), x + o);
+        if constexpr (kFar) {
+#pragma unroll
+          for (int k = o; k < o + P; k += 2) asm volatile("ld.shared.v2.b64 {%0, %1}, [%2];" : "=l"(gamma[k]), "=l"(gamma[k + 1]) : "r"(gammas + k * 8 * kLnThreads) : "memory");
+        }
         g.take(here_at + a.slot, i, (int)((uintptr_t)(a.dy + here) & 15u), y + o);      // 0 outside the slice, and with it all that x adds there
 #pragma unroll
         for (int k = o; k < o + P; ++k) {
@@ -707,8 +722,8 @@ static LnPlan ln_plan(int64_t M, int64_t N, int elt, bool grad, int mode) {
   LnPlan p = {};
   p.mode = mode;
   // Forward up to 32 elements per thread: per row half the warps, with what a warp costs beside its elements, that up to 16 take (8192 x 4096 bf16: 25.9 us, with 16: 31.9).  Backward up to
-  // 16, beside the columns' sums; with 24 some of it leaves the registers (4096 x 5120 44 us, with 16: 36), but 16 warps of 24 save a cluster CTAs (4096 x 12288 in one CTA 96 us, in two
-  // 105; 2000 x 20000 fp32 in two 156, in four 247).
+  // 16, beside the columns' sums; 24 in half the warps are slower (16 bits: 8192 x 3000 42 us, with 16: 35; fp32, where some of it leaves the registers: 4096 x 5120 70, with 16: 49),
+  // but 16 warps of 24 save a cluster CTAs (4096 x 12288 in one CTA 78 us, in two 105; 2000 x 20000 fp32 in two 156, in four 247).
   const int most_per = grad ? 16 : 32, widest = grad && mode != kLnSingle ? 24 : most_per;
   for (p.ranks = 1;; p.ranks *= 2) {
     p.slice = (int)(((N + p.ranks - 1) / p.ranks + 15) / 16 * 16);
@@ -735,7 +750,7 @@ static LnPlan ln_plan(int64_t M, int64_t N, int elt, bool grad, int mode) {
 template <bool GRAD, class E, int W, int PER, int MODE>
 static int ln_launch(const LnArgs& a, const LnPlan& p, cudaStream_t stream) {
   const int slots = GRAD ? 2 * kLnDepth<E, PER, 2> : kLnDepth<E, PER, 1>;
-  const uint32_t smem = kLnBefore<E, MODE> + (uint32_t)(kLnThreads / 32 / W * slots) * a.slot;
+  const uint32_t smem = kLnBefore<E, MODE> + (uint32_t)(kLnThreads / 32 / W * slots) * a.slot + (GRAD && kLnFarGamma<E, PER> ? kLnThreads * PER * 4 : 0);
   void (*kern)(LnArgs);
   if constexpr (GRAD) kern = layernorm_grad_kernel<E, W, PER, MODE>;
   else kern = layernorm_kernel<E, W, PER, MODE>;
