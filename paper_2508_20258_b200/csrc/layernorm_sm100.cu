@@ -4,12 +4,12 @@
 //   xh = (x - mean) rstd,   u = dy gamma,   dx = rstd (u - sum u / N - xh sum (u xh) / N),   dgamma = sum over rows of dy xh,   dbeta = of dy
 //
 // Both are bound by HBM: x is read and y written, or x and dy read and dx written, each once (16384 x 4096 bf16: 45 us, 5.9 TB/s, and 70 us, 5.8 TB/s; a copy of as many bytes 43 and 64).
-// A row is held in registers from its one read to its one write, up to 32 or (backward, beside the columns' sums) 16 elements per thread, by 1 to 16 warps, beyond a
-// block's width by the CTAs of a cluster, which exchange their sums through distributed shared memory.  Each group of warps walks its own rows with the next ones on their
+// A row is held in registers from its one read to its one write, up to 32 or (backward, beside the columns' sums) 16 or 24 elements per thread, by 1 to 16 warps, beyond a
+// block's width by the CTAs of a cluster, which exchange their sums through distributed shared memory (backward such rows stay in shared memory, and sums cross beside another row's work).  Each group of warps walks its own rows with the next ones on their
 // way through shared memory.
 // What comes next are issue slots and the chain of a row, read, sums, barriers, write, with 16 warps on an SM to hide it (half of the slots are used): so all arithmetic is on pairs, kernels have no
 // branch among a thread's elements, and rows wider than 4096 (backward) or 8192, whose one group per SM has nothing beside it, are slower: 4096 x 8192 27.7 and 44.5 us, 2048 x 16384 fp32
-// 53 and 94 (copies 22.6 and 33, 43 and 64).
+// 53 and 87 (copies 22.6 and 33, 43 and 64).
 // Sums are 32-bit and taken in a fixed order: the same bits every time.
 #include <float.h>
 
@@ -24,6 +24,7 @@ constexpr int kLnMaxCluster = 4;
 constexpr int kLnSums = 2;                        // of a group of warps at once, at most
 constexpr int64_t kLnMaxN = 32768;
 constexpr int kLnSms = 148;
+constexpr int kLnFours = 33;                      // clusters of four that find room at once: with 37 a second wave (1000 x 32768 fp32 164 us, with 33: 101)
 constexpr uint32_t kLnSumBytes = 2 * (16 + kLnMaxCluster) * 4 * kLnSums;      // of shared memory: sums of warps and of CTAs, two of each
 constexpr int kLnRing = 192 << 10;                // bytes of rows on their way, at most
 
@@ -421,6 +422,9 @@ constexpr bool kLnFarGamma = PER == 24 && E::kBytes == 2;
 template <class E, int PER, int ROWS>
 constexpr int kLnDepth = kLnRing / (kLnThreads * PER * E::kBytes * ROWS) < 3 ? kLnRing / (kLnThreads * PER * E::kBytes * ROWS) : 3;
 
+// Of the kernel that finishes a row beside the sums of the next: sums of all warps of a cluster, [turn][CTA][sum][warp].
+constexpr uint32_t kLnTurnSums = kLnMaxCluster * 2 * 16 * 4;
+
 // 1 / sqrt(v): the hardware's, which is good to two steps, and one step of Newton's method.
 __device__ __forceinline__ float ln_rsqrt(float v) {
   const float r = rsqrtf(v), s = r * fmaf(-0.5f * v * r, r, 1.5f);
@@ -530,7 +534,56 @@ __device__ __forceinline__ void store_weight(void* out, int dtype, int col, floa
   else ((uint16_t*)out)[col] = (uint16_t)pack_16(s, 0.f, dtype == SP_BF16);
 }
 
-// (A row finished beside the sums of the next, between the same two barriers, its x and dy read twice from shared memory: 16384 x 4096 86 us, so 75. Instructions bound it.)
+// The block's sums of columns, to its row of the workspace or to dgamma and dbeta.
+template <class E, int MODE, class G>
+__device__ __forceinline__ void ln_column_sums(const G& g, const LnArgs& a, const uint64_t* dg, const uint64_t* db, float edge_dg, float edge_db, float* all_groups) {
+  constexpr int P = G::kWide;
+  if (a.part == nullptr && a.dgamma == nullptr && a.dbeta == nullptr) return;
+  // The groups' sums to one, in their order, by way of shared memory: written to global memory as the lanes hold them, 32 bytes apart, they took 4 us longer.
+  cp_async_wait<0>();
+#pragma unroll
+  for (int w = 0; w < 2; ++w) {
+    __syncthreads();      // all rows, and the sums before these, have been read
+    float* mine = all_groups + g.group * a.slice;
+#pragma unroll
+    for (int i = 0; i < G::kChunks; i += G::kStep)
+      if (g.any(i)) {
+        const uint64_t* f = (w == 0 ? dg : db) + i * G::kElems / 2;
+        if constexpr (MODE == kLnWhole) {
+          if (g.has(i)) {
+#pragma unroll
+            for (int k = 0; k < P; k += 2) {
+              float4 v;
+              halves_of(f[k], v.x, v.y);
+              halves_of(f[k + 1], v.z, v.w);
+              *reinterpret_cast<float4*>(mine + g.column(i) + 2 * k) = v;
+            }
+          }
+        } else {
+#pragma unroll
+          for (int k = 0; k < P; ++k) {
+            float v[2];
+            halves_of(f[k], v[0], v[1]);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              const int e = 2 * k + h;
+              if (g.has(i + e / G::kElems)) mine[g.column(i + e / G::kElems) + e % G::kElems] = v[h];
+            }
+          }
+        }
+      }
+    if (g.edge >= 0) mine[g.edge] = w == 0 ? edge_dg : edge_db;
+    __syncthreads();
+    for (int c = threadIdx.x; c < g.cols; c += kLnThreads) {
+      float s = 0.f;
+#pragma unroll
+      for (int i = 0; i < G::kGroups; ++i) s += all_groups[i * a.slice + c];
+      if (a.part != nullptr) a.part[((int64_t)(blockIdx.x / g.ranks) * 2 + w) * a.pitch + g.rank * a.slice + c] = s;
+      else store_weight(w == 0 ? a.dgamma : a.dbeta, a.w_dtype, g.rank * a.slice + c, s);
+    }
+  }
+}
+
 template <class E, int W, int PER, int MODE>
 __global__ void __launch_bounds__(kLnThreads, 1) layernorm_grad_kernel(const LnArgs a) {
   extern __shared__ __align__(16) uint8_t ln_smem[];
@@ -639,53 +692,152 @@ __global__ void __launch_bounds__(kLnThreads, 1) layernorm_grad_kernel(const LnA
     }
     mean = next_mean; rstd = next_rstd;
   }
-  if (a.part == nullptr && a.dgamma == nullptr && a.dbeta == nullptr) return;
-  // The groups' sums to one, in their order, by way of shared memory: written to global memory as the lanes hold them, 32 bytes apart, they took 4 us longer.
-  float* all_groups = reinterpret_cast<float*>(ln_smem + kLnBefore<E, MODE>);
-  cp_async_wait<0>();
-#pragma unroll
-  for (int w = 0; w < 2; ++w) {
-    __syncthreads();      // all rows, and the sums before these, have been read
-    float* mine = all_groups + g.group * a.slice;
-#pragma unroll
-    for (int i = 0; i < G::kChunks; i += G::kStep)
-      if (g.any(i)) {
-        const uint64_t* f = (w == 0 ? dg : db) + i * G::kElems / 2;
-        if constexpr (MODE == kLnWhole) {
-          if (g.has(i)) {
-#pragma unroll
-            for (int k = 0; k < P; k += 2) {
-              float4 v;
-              halves_of(f[k], v.x, v.y);
-              halves_of(f[k + 1], v.z, v.w);
-              *reinterpret_cast<float4*>(mine + g.column(i) + 2 * k) = v;
-            }
-          }
-        } else {
-#pragma unroll
-          for (int k = 0; k < P; ++k) {
-            float v[2];
-            halves_of(f[k], v[0], v[1]);
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-              const int e = 2 * k + h;
-              if (g.has(i + e / G::kElems)) mine[g.column(i + e / G::kElems) + e % G::kElems] = v[h];
-            }
-          }
-        }
-      }
-    if (g.edge >= 0) mine[g.edge] = w == 0 ? edge_dg : edge_db;
-    __syncthreads();
-    for (int c = threadIdx.x; c < g.cols; c += kLnThreads) {
-      float s = 0.f;
-#pragma unroll
-      for (int i = 0; i < G::kGroups; ++i) s += all_groups[i * a.slice + c];
-      if (a.part != nullptr) a.part[((int64_t)(blockIdx.x / g.ranks) * 2 + w) * a.pitch + col0 + c] = s;
-      else store_weight(w == 0 ? a.dgamma : a.dbeta, a.w_dtype, col0 + c, s);
-    }
-  }
+  ln_column_sums<E, MODE>(g, a, dg, db, edge_dg, edge_db, reinterpret_cast<float*>(ln_smem + kLnBefore<E, MODE>));
 }
 
+// The same by groups of 16 warps that finish a row beside the sums of the next, which cross the cluster (or the block) meanwhile: for rows that clusters share, whose barrier had nothing beside it,
+// and those that only fit one CTA this way, since x and dy are read from shared memory twice and the registers hold gamma and the columns' sums alone (gradients of 2048 x 16384 fp32 92 to 87 us,
+// 3000 x 16384 bf16 in one CTA instead of two 89 to 80, 1000 x 24576 fp32 96 to 84).  Narrower rows lose more by the second reading and conversion (4096 x 5120 36 to 45 us, 4096 x 12288 78 to 82,
+// 16384 x 4096 75 to 86).
+template <class E, int PER, int MODE>
+__global__ void __launch_bounds__(kLnThreads, 1) layernorm_grad_ahead_kernel(const LnArgs a) {
+  extern __shared__ __align__(16) uint8_t ln_smem[];
+  using G = LnGroup<E, 16, PER, MODE>;
+  constexpr int D = kLnDepth<E, PER, 2>, P = G::kWide;
+  static_assert(D == 3, "a row to finish, one to sum, one on its way");
+  const uint32_t base = smem_u32(ln_smem);
+  G g(a, base);
+  const uint32_t sums = base + kLnBefore<E, MODE>;
+  const uint32_t ring = sums + 2 * kLnTurnSums, batch = 2 * a.slot;
+  const uint32_t total = a.clusters, last = (uint32_t)a.M - 1;
+  const int col0 = g.rank * a.slice;
+  const int64_t pitch = (int64_t)a.N * E::kBytes, hop = (int64_t)total * pitch, all = a.M * pitch;
+  uint32_t row = blockIdx.x / g.ranks;
+  int64_t here = (int64_t)row * pitch + (int64_t)col0 * E::kBytes, next = here;
+  g.begin_at((int)((uintptr_t)(a.x + here) & 15u));
+  pdl_begin();
+  const auto fetch = [&](uint32_t at, uint32_t r) {
+    if (r <= last) {
+      g.fetch(at, a.x + next, a.x, a.x + all);
+      g.fetch(at + a.slot, a.dy + next, a.dy, a.dy + all);
+    }
+    next += hop;
+    cp_async_commit();
+  };
+  uint32_t ahead = row;
+#pragma unroll
+  for (int i = 0; i < D; ++i, ahead += total) fetch(ring + i * batch, ahead);
+  uint64_t gamma[G::kPairs], dg[G::kPairs], db[G::kPairs];
+  g.weights(a.gamma, a.w_dtype, col0, 1.f, gamma);
+#pragma unroll
+  for (int k = 0; k < G::kPairs; ++k) dg[k] = db[k] = 0;
+  const float inv = 1.f / (float)a.N;
+  const float edge_gamma = g.weight(a.gamma, a.w_dtype, col0, g.edge, 1.f);
+  float edge_x = 0.f, edge_dy = 0.f, edge_dg = 0.f, edge_db = 0.f;      // of the row to come; sums
+  float mean = 0.f, rstd = 0.f, mean_before = 0.f, rstd_before = 0.f, xe_before = 0.f, ue_before = 0.f;
+  if (row <= last) {
+    edge_x = g.edge_of(a.x + here);
+    edge_dy = g.edge_of(a.dy + here);
+    mean = __ldg(a.mean + row); rstd = __ldg(a.rstd + row);
+  }
+  uint32_t at = ring, at_before = ring, turn = 0;
+  for (bool first = true;; first = false) {
+    const bool more = row <= last;
+    float next_mean = 0.f, next_rstd = 0.f, st[2], xe = 0.f, ue = 0.f;
+    if (more) {
+      if (row + total <= last) { next_mean = ask_for(a.mean + row + total); next_rstd = ask_for(a.rstd + row + total); }
+      cp_async_wait<D - 2>();
+      const uint32_t here_at = arrived(at);
+      uint64_t s2[2] = {0, 0}, t2[2] = {0, 0};
+      const uint64_t minus = pair_of(-mean, -mean), scale = pair_of(rstd, rstd);
+#pragma unroll
+      for (int i = 0; i < G::kChunks; ++i) {
+        const int o = i * G::kElems / 2;
+        uint64_t x[P], y[P];
+        g.take(here_at, i, 0, x);
+        g.take(here_at + a.slot, i, 0, y);
+#pragma unroll
+        for (int k = 0; k < P; ++k) {
+          x[k] = mul_pair(add_pair(x[k], minus), scale);
+          dg[o + k] = fma_pair(y[k], x[k], dg[o + k]);
+          db[o + k] = add_pair(db[o + k], y[k]);
+          y[k] = mul_pair(y[k], gamma[o + k]);
+          s2[k & 1] = add_pair(s2[k & 1], y[k]);
+          t2[k & 1] = fma_pair(y[k], x[k], t2[k & 1]);
+        }
+      }
+      st[0] = halves_sum(add_pair(s2[0], s2[1]));
+      st[1] = halves_sum(add_pair(t2[0], t2[1]));
+      if (g.edges()) {
+        if (g.edge >= 0) {
+          xe = (edge_x - mean) * rstd;
+          edge_dg = fmaf(edge_dy, xe, edge_dg);
+          edge_db += edge_dy;
+          ue = edge_dy * edge_gamma;
+          st[0] += ue;
+          st[1] = fmaf(ue, xe, st[1]);
+        }
+        if (row + total <= last) {
+          edge_x = g.edge_of(a.x + here + hop);
+          edge_dy = g.edge_of(a.dy + here + hop);
+        }
+      }
+      // lanes 0-15 keep the first sum, 16-31 the second
+      const bool upper = g.lane & 16;
+      float v = (upper ? st[1] : st[0]) + __shfl_xor_sync(0xffffffffu, upper ? st[0] : st[1], 16);
+#pragma unroll
+      for (int o = 8; o; o /= 2) v += __shfl_xor_sync(0xffffffffu, v, o);
+      st[0] = v;
+    }
+    float c1 = 0.f, c2 = 0.f;
+    if (!first) {      // all CTAs' sums of the row before; they have read those of the row before that, whose place is free
+      asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+      const uint32_t from = sums + ((turn & 1u) ^ 1u) * (kLnTurnSums) + g.lane * 4;
+      float v = 0.f;
+      for (int i = 0; i < g.ranks; ++i) v += __uint_as_float(ld_shared_32(from + i * 128));
+#pragma unroll
+      for (int o = 8; o; o /= 2) v += __shfl_xor_sync(0xffffffffu, v, o);
+      c1 = -__shfl_sync(0xffffffffu, v, 0) * inv;
+      c2 = -__shfl_sync(0xffffffffu, v, 16) * inv;
+    }
+    if (more) {
+      if ((g.lane & 15) < g.ranks)
+        asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(mapa(sums + (turn & 1u) * (kLnTurnSums) + g.rank * 128 + (g.lane >> 4) * 64 + g.wg * 4, g.lane & 15)), "f"(st[0]) : "memory");
+      asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+      ++turn;
+    }
+    if (!first) {
+      if (a.out != nullptr) {
+        const uint32_t here_at = arrived(at_before);
+        char* out = a.out + here - hop;
+        const uint64_t minus = pair_of(-mean_before, -mean_before), scale = pair_of(rstd_before, rstd_before), p1 = pair_of(c1, c1), p2 = pair_of(c2, c2);
+#pragma unroll
+        for (int i = 0; i < G::kChunks; ++i) {
+          const int o = i * G::kElems / 2;
+          uint64_t x[P], y[P];
+          g.take(here_at, i, 0, x);
+          g.take(here_at + a.slot, i, 0, y);
+#pragma unroll
+          for (int k = 0; k < P; ++k) {
+            x[k] = mul_pair(add_pair(x[k], minus), scale);
+            x[k] = mul_pair(scale, fma_pair(p2, x[k], fma_pair(y[k], gamma[o + k], p1)));
+          }
+          g.put(out, i, x);
+        }
+        if (g.edges() && g.edge >= 0) E::store(out + g.edge * E::kBytes, rstd_before * fmaf(c2, xe_before, ue_before + c1));
+      }
+      fetch(at_before, ahead);
+      ahead += total;
+    }
+    if (!more) break;
+    mean_before = mean; rstd_before = rstd; xe_before = xe; ue_before = ue; at_before = at;
+    mean = next_mean; rstd = next_rstd;
+    at = at + batch == ring + D * batch ? ring : at + batch;
+    row += total; here += hop;
+  }
+  cp_async_wait<0>();
+  ln_column_sums<E, MODE>(g, a, dg, db, edge_dg, edge_db, reinterpret_cast<float*>(ln_smem + kLnBefore<E, MODE> + 2 * kLnTurnSums));
+}
 // dgamma (blockIdx.y 0) and dbeta (1) from the clusters' sums, in a fixed order: 32 rows of 32 columns side by side, up to five of them for a thread, asked for at once.
 __global__ void __launch_bounds__(1024) layernorm_weights_kernel(const float* part, int rows, int pitch, int N, int dtype, void* dgamma, void* dbeta) {
   pdl_begin();
@@ -722,9 +874,9 @@ static LnPlan ln_plan(int64_t M, int64_t N, int elt, bool grad, int mode) {
   LnPlan p = {};
   p.mode = mode;
   // Forward up to 32 elements per thread: per row half the warps, with what a warp costs beside its elements, that up to 16 take (8192 x 4096 bf16: 25.9 us, with 16: 31.9).  Backward up to
-  // 16, beside the columns' sums; 24 in half the warps are slower (16 bits: 8192 x 3000 42 us, with 16: 35; fp32, where some of it leaves the registers: 4096 x 5120 70, with 16: 49),
-  // but 16 warps of 24 save a cluster CTAs (4096 x 12288 in one CTA 78 us, in two 105; 2000 x 20000 fp32 in two 156, in four 247).
-  const int most_per = grad ? 16 : 32, widest = grad && mode != kLnSingle ? 24 : most_per;
+  // 16, beside the columns' sums: 24 in half the warps are slower (16 bits: 8192 x 3000 42 us, with 16: 35; fp32, where some of it leaves the registers: 4096 x 5120 70, with 16: 49).  But in 16
+  // bits 16 warps of 24, and of 32 with the rows in shared memory alone, save a cluster CTAs (4096 x 12288 in one CTA 78 us, in two 105).
+  const int most_per = grad ? 16 : 32, widest = grad && elt == 2 && mode != kLnSingle ? 32 : most_per;
   for (p.ranks = 1;; p.ranks *= 2) {
     p.slice = (int)(((N + p.ranks - 1) / p.ranks + 15) / 16 * 16);
     if ((N < p.slice ? N : p.slice) <= kLnThreads * widest) break;
@@ -736,7 +888,7 @@ static LnPlan ln_plan(int64_t M, int64_t N, int elt, bool grad, int mode) {
   for (p.per = 8; p.per < widest && (p.warps * 32 * p.per < width || mode == kLnSingle); p.per += 8) {}
   const int groups = kLnThreads / 32 / p.warps;
   // One block per SM; backward, whose blocks each leave a row of sums, at least two rows for every group, and one block for up to four.
-  const int64_t most = kLnSms / p.ranks, rows = grad ? (M <= 4 * groups ? 4 : 2) : 1, want = (M + groups * rows - 1) / (groups * rows);
+  const int64_t most = p.ranks < 4 ? kLnSms / p.ranks : kLnFours, rows = grad ? (M <= 4 * groups ? 4 : 2) : 1, want = (M + groups * rows - 1) / (groups * rows);
   p.clusters = (int)(want < most ? want : most);
   if (mode == kLnEdges && (int64_t)p.clusters * groups < M) {      // a group's rows are a multiple of 16 bytes apart
     int apart = 1;
@@ -747,12 +899,13 @@ static LnPlan ln_plan(int64_t M, int64_t N, int elt, bool grad, int mode) {
   return p;
 }
 
-template <bool GRAD, class E, int W, int PER, int MODE>
+template <bool GRAD, class E, int W, int PER, int MODE, bool AHEAD = false>
 static int ln_launch(const LnArgs& a, const LnPlan& p, cudaStream_t stream) {
   const int slots = GRAD ? 2 * kLnDepth<E, PER, 2> : kLnDepth<E, PER, 1>;
-  const uint32_t smem = kLnBefore<E, MODE> + (uint32_t)(kLnThreads / 32 / W * slots) * a.slot + (GRAD && kLnFarGamma<E, PER> ? kLnThreads * PER * 4 : 0);
+  const uint32_t smem = kLnBefore<E, MODE> + (uint32_t)(kLnThreads / 32 / W * slots) * a.slot + (AHEAD ? 2 * kLnTurnSums : GRAD && kLnFarGamma<E, PER> ? kLnThreads * PER * 4 : 0);
   void (*kern)(LnArgs);
-  if constexpr (GRAD) kern = layernorm_grad_kernel<E, W, PER, MODE>;
+  if constexpr (AHEAD) kern = layernorm_grad_ahead_kernel<E, PER, MODE>;
+  else if constexpr (GRAD) kern = layernorm_grad_kernel<E, W, PER, MODE>;
   else kern = layernorm_kernel<E, W, PER, MODE>;
   static uint64_t configured = 0;
   if (first_use_on_this_device(configured)) {
@@ -762,16 +915,21 @@ static int ln_launch(const LnArgs& a, const LnPlan& p, cudaStream_t stream) {
   return launch_pdl(GRAD ? "layer norm gradient" : "layer norm", kern, dim3((unsigned)(p.clusters * p.ranks)), kLnThreads, smem, p.ranks, stream, a);
 }
 
-// More than one warp is taken where half as many would not do, clusters where one CTA would not: each thread then has more than half of the most (backward in clusters, of 12288 columns and
-// more, 16 or 24 all the same).
+// More than one warp is taken where half as many would not do, clusters where one CTA would not: each thread then has more than half of the most (backward, 16 warps of
+// 16 bits have up to 32).
 template <bool GRAD, class E, int W, int MODE>
 static int ln_width(const LnArgs& a, const LnPlan& p, cudaStream_t stream) {
   if constexpr (W == 1) {
     if (p.per == 8) return ln_launch<GRAD, E, W, 8, MODE>(a, p, stream);
     if (!GRAD && p.per == 16) return ln_launch<false, E, W, 16, MODE>(a, p, stream);
   }
-  if constexpr (GRAD && W == 16) {
-    if (p.per == 24) return ln_launch<true, E, W, 24, MODE>(a, p, stream);
+  if constexpr (GRAD && W == 16 && E::kBytes == 2) {
+    if (p.per == 24 && p.ranks == 1) return ln_launch<true, E, W, 24, MODE>(a, p, stream);
+    if (p.per == 24) return ln_launch<true, E, W, 24, MODE, true>(a, p, stream);
+    if (p.per == 32) return ln_launch<true, E, W, 32, MODE, true>(a, p, stream);
+  }
+  if constexpr (GRAD && W == 16 && E::kBytes == 4) {
+    if (p.ranks > 1) return ln_launch<true, E, W, 16, MODE, true>(a, p, stream);
   }
   if constexpr (GRAD) return ln_launch<true, E, W, 16, MODE>(a, p, stream);
   else if (p.per == 24) return ln_launch<false, E, W, 24, MODE>(a, p, stream);

@@ -137,6 +137,19 @@ def test_many_rows(M, N):
     c.check_guards()
 
 
+@pytest.mark.parametrize("M,N", [(300, 10008), (310, 12291), (300, 16384), (160, 24583), (170, 32768)])
+@pytest.mark.parametrize("types", [("bf16", "bf16"), ("fp16", "fp32"), ("fp32", "fp32")], ids="-".join)
+def test_many_wide_rows(M, N, types):
+    c = Case(M, N, *types)
+    c.forward()
+    c.backward()
+    c.check_backward()
+    c.check_guards()
+    first = [t.clone() for t in (c.dx, c.dgamma, c.dbeta)]
+    c.backward()
+    assert all(torch.equal(a, b) for a, b in zip(first, (c.dx, c.dgamma, c.dbeta)))
+
+
 @pytest.mark.parametrize("N", [300, 4096, 9001])
 def test_rows_far_from_zero_and_of_small_and_large_scale(N):
     for scale, shift in ((1.0, 1000.0), (1e-3, 0.0), (1e15, 0.0), (1.0, -30000.0)):
