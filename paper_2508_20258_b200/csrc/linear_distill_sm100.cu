@@ -370,22 +370,24 @@ __global__ void __launch_bounds__(1024) distill_join_kernel(const DistillJoin a,
       };
       const float2 pair = joined[w];
       const int state = a.state[t];
-      // the largest score, and which of the teacher's words has it (the first of them)
+      // The largest score, and which of the teacher's words has it (the first of them).  A NaN counts as the largest: the order is total, and all lanes settle on the same word whatever the scores
+      // are.
+      const auto order = [](float z) { return z == z ? z : CUDART_INF_F; };
       float own_top = -CUDART_INF_F;
       int own_at = 0, own_word = kNoWord;
       each_word([&](int i, const Word& x) {
-        if (x.first && (x.z > own_top || i == 0)) { own_top = x.z; own_at = i; own_word = x.word; }
+        if (x.first && (order(x.z) > order(own_top) || i == 0)) { own_top = x.z; own_at = i; own_word = x.word; }
       });
 #pragma unroll
       for (int o = 16; o; o >>= 1) {
         const float z = __shfl_xor_sync(0xffffffffu, own_top, o);
         const int at = __shfl_xor_sync(0xffffffffu, own_at, o), word = __shfl_xor_sync(0xffffffffu, own_word, o);
-        if (word != kNoWord && (own_word == kNoWord || z > own_top || (z == own_top && at < own_at))) { own_top = z; own_at = at; own_word = word; }
+        if (word != kNoWord && (own_word == kNoWord || order(z) > order(own_top) || (order(z) == order(own_top) && at < own_at))) { own_top = z; own_at = at; own_word = word; }
       }
       const bool kept = state == kKept;
       if (kept && !a.bf16) {      // p is at most this, without the teacher's other words; of p below 1/64 the error does not count
         const float top = fmaxf(pair.x, own_top * a.scale), own = ex2(fmaf(own_top, a.scale, -top));
-        if (own > (own + pair.y * ex2(pair.x - top)) * 0x1p-6f) own_top = score_of(t, own_word);
+        if (__any_sync(0xffffffffu, own > (own + pair.y * ex2(pair.x - top)) * 0x1p-6f)) own_top = score_of(t, own_word);      // all lanes or none: it sums over the warp
       }
       const float top = fmaxf(pair.x, own_top * a.scale), ref = top == -CUDART_INF_F ? 0.f : top;
       const float others = pair.y * ex2(pair.x - ref);      // the words that are not the teacher's

@@ -387,3 +387,59 @@ def test_refusals_of_the_binding():
         sp.linear_distill_grad(h, W, index, lse, diff, None, h, torch.empty_like(W))
     assert e.value.status == sp.ERR_INVALID_ARG
     assert sp.get_status() == 0
+
+
+# a word per lane, several, and lists that are read where they are needed; of a warp's lanes some without any
+@pytest.mark.parametrize("K", [1, 2, 20, 40, 200])
+@pytest.mark.parametrize("place", ["lowest", "middle", "highest", "none"])
+@pytest.mark.parametrize("value", [float("nan"), INF, -INF])
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+def test_a_row_of_W_that_is_not_finite(K, place, value, dtype):
+    if K == 1 and place == "middle":
+        pytest.skip("one word is the lowest and the highest")
+    T, V, D, bad, at = 12, 700, 64, 350, 3
+    h, W, _, _ = inputs(T, V, D, K, dtype)
+    g = torch.Generator().manual_seed(K)
+    h[:, at] = torch.where(torch.arange(T, device="cuda") % 2 == 0, 1.0, -1.0)
+    below = {"lowest": 0, "middle": K // 2, "highest": K - 1, "none": K // 2}[place]
+    above = K - below - (place != "none")
+    index = torch.stack([torch.cat([torch.randperm(bad, generator=g)[:below], torch.tensor([bad] if place != "none" else [], dtype=torch.int64),
+                                    bad + 1 + torch.randperm(V - bad - 1, generator=g)[:above]])[torch.randperm(K, generator=g)] for _ in range(T)]).cuda()
+    top = torch.randn(T, K, generator=g).cuda()
+    out = torch.arange(T, device="cuda") % 6 == 5
+    index[out] = -1
+    W[bad, at] = -60000.0      # the words' scores 0 of itself under a softmax, or above all others
+    low = Result(h, W, index, top, 1.0, "none")
+    W[bad, at] = 60000.0
+    high = Result(h, W, index, top, 1.0, "none")
+    W[bad, at] = value
+    r = Result(h, W, index, top, 1.0, "none")
+    assert (r.lse[out] == INF).all() and (r.loss[out] == 0).all() and (r.diff[out] == 0).all() and (r.dh[out] == 0).all()
+    # a score of minus infinity: p is 0 there, as of one of -60000, and only the loss tells them apart, where the teacher has the word
+    gone = ~out & (h[:, at] * value == -INF)
+    finite = low if value < 0 else high
+    assert value != value or gone.sum() >= 4
+    assert torch.equal(r.lse[gone], finite.lse[gone]) and torch.equal(r.diff[gone], finite.diff[gone])
+    assert (r.loss[gone] == INF).all() if place != "none" else torch.equal(r.loss[gone], finite.loss[gone])
+    others = torch.arange(D, device="cuda") != at
+    assert torch.equal(r.dh[gone][:, others], finite.dh[gone][:, others])
+    # a NaN, or plus infinity: all of the token is NaN
+    rest = ~out & ~gone
+    assert rest.sum() >= 4 and all(torch.isnan(x[rest]).all() for x in (r.lse, r.loss, r.diff, r.dh)) and torch.isnan(r.dW).all()
+    for red in ("mean", "sum"):
+        assert torch.isnan(Result(h, W, index, top, 1.0, red, want=None).loss).all()
+
+
+@pytest.mark.parametrize("value", [float("nan"), INF])
+@pytest.mark.parametrize("T,K", [(20, 3), (40, 33), (300, 150)])
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+def test_a_token_that_counts_and_is_not_finite_stays_alone(T, K, dtype, value):
+    h, W, index, top = inputs(T, 700, 64, K, dtype)
+    index[2], top[2] = torch.arange(K, device="cuda"), 0.0
+    good = Result(h, W, index, top, 1.0, "none")
+    h[2, 5] = value
+    r = Result(h, W, index, top, 1.0, "none")
+    assert all(torch.isnan(x[2]).all() for x in (r.lse, r.loss, r.diff, r.dh)) and torch.isnan(r.dW).all()
+    others = torch.arange(T, device="cuda") != 2
+    for name in ("loss", "lse", "diff", "dh"):
+        assert torch.equal(getattr(r, name)[others], getattr(good, name)[others]), name
