@@ -307,8 +307,9 @@ __global__ void __launch_bounds__(1024) distill_join_kernel(const DistillJoin a,
     return v;
   };
   // A word's score once more, by a warp.  The tensor cores cut sums off towards zero, of products that are all positive, as where a state lies along its word's row of W, a little each time,
-  // and more where products are long: of tokens that have settled on a word the score of fp16 was 2e-7 of itself too small and p - q of a batch with them off by 2 to 4e-6 (24 x 32768 x 1024), so
-  // 1e-7.  It takes the reading of a row of h and one of W, 1 to 2 us.  (bf16, whose products have 16 bits for 22: 0.3 to 1.7e-6, left so.)
+  // and more where products are long: of tokens that have settled on a word the score of fp16 was 2.7e-6 of itself too small (512 to 4096 products), so 1e-8 on average and 4e-8 in the root of the
+  // mean square, and p - q of a batch with them off by 2 to 4e-6 (24 x 32768 x 1024), so 1e-7.  It takes the reading of a row of h and one of W, 1 to 2 us.  (bf16, whose products have 16 bits for 22:
+  // scores 4.7e-7 too small, p - q off by 0.3 to 1.7e-6, left so.)
   const auto score_of = [&](int64_t t, int word) {
     const uint4 *u = a.h + t * a.vecs, *w = a.W + (int64_t)word * a.vecs;
     float z = 0.f;

@@ -443,3 +443,41 @@ def test_a_token_that_counts_and_is_not_finite_stays_alone(T, K, dtype, value):
     others = torch.arange(T, device="cuda") != 2
     for name in ("loss", "lse", "diff", "dh"):
         assert torch.equal(getattr(r, name)[others], getattr(good, name)[others]), name
+
+
+@pytest.mark.parametrize("D", [1024, 4096])
+def test_the_score_of_a_settled_word_is_not_cut_off(D):
+    # fp16 states along their word's row of W, all other rows 0: p - q is -(V - 1) / (V - 1 + e^z), and with p next to 1 its relative error that of z itself.  Products of fp16 numbers are exact
+    # in fp32.  Cut off, z is always too small (2e-7 of itself); rounded to nearest its n = 1 + 2 + D / 256 + 5 roundings, each at most u = 2^-24 of z, are as often up as down, and the mean over T
+    # tokens is beyond u sqrt(n) sqrt(2 ln(2e9) / T) of z once in 1e9 (Hoeffding).  log2 e in fp32: 2^-25 of z.  Two exponentials, good to 2^-22, and four roundings, whatever z is.
+    T, V, word = 8192, 512, 300
+    g = torch.Generator(device="cuda").manual_seed(D)
+    W = torch.zeros(V, D, dtype=torch.float16, device="cuda")
+    W[word] = (0.5 + torch.rand(D, device="cuda", generator=g)) * torch.where(torch.rand(D, device="cuda", generator=g) < 0.5, -1.0, 1.0)
+    h = ((0.1 + torch.rand(T, D, device="cuda", generator=g)) * (25 / (0.6 * D)) * W[word].sign()).half()
+    index, top = torch.full((T, 1), word, device="cuda"), torch.zeros(T, 1, device="cuda")
+    r = Result(h, W, index, top, 1.0, "none", want=None)
+    z = h.double() @ W[word].double()
+    assert float(z.min()) > 20 and float(z.max()) < 30
+    odds = (V - 1) * torch.exp(-z)
+    off = ((r.diff[:, 0].double() / (-odds / (1 + odds)) - 1) / z).mean()
+    u, n = 2.0 ** -24, 1 + 2 + D / 256 + 5
+    assert abs(float(off)) <= u * (n * 2 * 21.5 / T) ** 0.5 + 2.0 ** -25 + (2 * 2.0 ** -22 + 4 * u) / 20, float(off)
+
+
+@pytest.mark.parametrize("T,V,D,K", [(1, 4001, 256, 8), (16, 3001, 512, 20), (64, 2001, 256, 32)])
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+def test_gradients_of_few_tokens_are_as_good_as_rounded_once(T, V, D, K, dtype):
+    # Up to 64 tokens g is held with its rounding errors, to e^2 (2^-16, 2^-22) of an entry, and the scores' errors move it by 1e-6 to 1e-5: at most a twentieth of what rounding a gradient once does
+    # (a uniform error of up to e of a value, about e / 2 in the norm: 2^-9, 2^-12), which adds 1 / 800 to the norm.  g rounded without them adds as much as the rounding itself: sqrt 2 where a
+    # gradient is one product.
+    h, W, index, top = inputs(T, V, D, K, dtype)
+    top = top.masked_fill(top == -INF, -1.0)
+    grad = torch.full((T,), 64.0 if dtype == "fp16" else 1.0, device="cuda")
+    r = Result(h, W, index, top, 1.0, "none", grad)
+    kept, (_, _, _, dh, dW), _ = reference(h, W, index, top, 1.0, "none", grad, dtype)
+    listed = torch.zeros(V, dtype=torch.bool, device="cuda")
+    listed[index[kept].clamp(min=0).flatten()] = True
+    for got, want in ((r.dh, dh), (r.dW[listed], dW[listed]), (r.dW[~listed], dW[~listed])):
+        once = (want.to(BITS[dtype]).double() - want).norm()
+        assert float(once) > 0 and float((got.double() - want).norm() / once) <= 1.02
