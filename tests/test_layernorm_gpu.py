@@ -293,3 +293,44 @@ def test_refusals_of_the_binding():
         sp.layernorm(torch.empty(1, sp.LAYERNORM_MAX_N + 8, device="cuda"), None, None, torch.empty(1, sp.LAYERNORM_MAX_N + 8, device="cuda"))
     assert e.value.status == sp.ERR_UNSUPPORTED
     assert sp.get_status() == 0
+
+
+# rows whose places in shared memory are used several times: 148, 74, 33 groups share them
+@pytest.mark.parametrize("M,N", [(1200, 40), (700, 1031), (400, 17001)])
+@pytest.mark.parametrize("types", [("bf16", "fp32"), ("fp16", "fp16"), ("fp32", "fp32")], ids="-".join)
+def test_many_rows_at_unequal_addresses(M, N, types):
+    c = Case(M, N, *types, off=1)
+    c.forward()
+    c.check_forward()
+    c.backward()
+    c.check_backward()
+    c.check_guards()
+
+
+@pytest.mark.parametrize("M,N", [(600, 16384), (400, 17001), (400, 24583), (310, 32768)])
+@pytest.mark.parametrize("types", [("bf16", "bf16"), ("fp16", "fp32"), ("fp32", "fp32")], ids="-".join)
+def test_many_wide_rows_forward(M, N, types):
+    c = Case(M, N, *types)
+    c.forward()
+    c.check_forward()
+    c.check_guards()
+
+
+@pytest.mark.parametrize("M,N", [(400, 9001), (400, 16384), (400, 20001), (150, 32768)])
+@pytest.mark.parametrize("types", [("fp16", "fp32"), ("fp32", "fp32")], ids="-".join)
+def test_each_gradient_of_wide_rows_alone_has_the_same_bits(M, N, types):
+    c = Case(M, N, *types)
+    c.forward()
+    c.backward()
+    c.check_backward()
+    want = [t.clone() for t in (c.dx, c.dgamma, c.dbeta)]
+    for only in range(3):
+        for both in (False, True):
+            outs = [t if (i == only) != both else None for i, t in enumerate((c.dx, c.dgamma, c.dbeta))]
+            for t in outs:
+                if t is not None:
+                    t.fill_(float("nan"))
+            sp.layernorm_grad(c.dy, c.x, c.gamma, c.mean, c.rstd, *outs)
+            for t, w in zip(outs, want):
+                assert t is None or torch.equal(t, w)
+    c.check_guards()
