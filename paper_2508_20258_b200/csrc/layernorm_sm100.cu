@@ -24,7 +24,9 @@ constexpr int kLnMaxCluster = 4;
 constexpr int kLnSums = 2;                        // of a group of warps at once, at most
 constexpr int64_t kLnMaxN = 32768;
 constexpr int kLnSms = 148;
-constexpr int kLnFours = 33;                      // clusters of four that find room at once: with 37 a second wave (1000 x 32768 fp32 164 us, with 33: 101)
+// Clusters of four that find room at once, as the occupancy calculator has it for the devices seen (which SMs share a GPC decides): with 37 a second wave (1000 x 32768 fp32 164 us, with 33: 101).
+// A constant, not asked of each device: it decides in which order dgamma and dbeta are added up.  Where fewer find room, that second wave is what it costs.
+constexpr int kLnFours = 33;
 constexpr uint32_t kLnSumBytes = 2 * (16 + kLnMaxCluster) * 4 * kLnSums;      // of shared memory: sums of warps and of CTAs, two of each
 constexpr int kLnRing = 192 << 10;                // bytes of rows on their way, at most
 

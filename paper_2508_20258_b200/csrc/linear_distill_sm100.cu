@@ -8,8 +8,9 @@
 // lse, the loss and p - q of the token's words.  Gradient: the tiles write c p in 16 bits, and a kernel puts c (p - q) over it where the teacher has words: T x K
 // scattered entries, a fraction of a percent of g.
 //
-// Nothing is a difference of two nearly equal numbers.  The loss is tau^2 (sum of the other words' p + sum over the teacher's words of q d - q + p), d = log q - log p, whose
-// terms are not negative; p - q of a word with p above 1/2 is the sum of all other q less the sum of all other p.
+// The loss is tau^2 (sum of the other words' p + sum over the teacher's words of q d - q + p), d = log q - log p, whose terms are not negative; p - q of a word with p above 1/2 is the
+// sum of all other q less the sum of all other p, and its d (with q above 1/2 too) made from those: a student that is sure and right keeps its digits.  For words below 1/2, p - q and d are
+// differences of fp32 numbers, good to the scores' error and a few 2^-23 of p, q and their logarithms.
 #include <new>
 
 #include "linear_ce.cuh"

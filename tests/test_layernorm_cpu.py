@@ -110,3 +110,12 @@ def test_binding_checks_shapes_and_types_before_the_library():
         sp.layernorm_grad(x[:2], x, g, s, s, x, g, g)
     with pytest.raises(ValueError, match="element type"):
         sp.layernorm(x.double(), g, g, x.double())
+
+
+def test_workspace_is_at_most_148_rows_of_sums():
+    for M in (1, 13, 148, 5000, 1 << 20, (1 << 31) - 1):
+        for N in (1, 8, 17, 304, 1031, 4096, 8193, 12291, 16385, sp.LAYERNORM_MAX_N):
+            row = 2 * ((N + 15) // 16 * 16) * 4
+            n = sp.layernorm_workspace(M, N)
+            assert n % row == 0 and row <= n <= 148 * row
+    assert sp.layernorm_workspace(1 << 20, 1) == 148 * 2 * 16 * 4
