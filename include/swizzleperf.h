@@ -478,7 +478,7 @@ int64_t sp_linear_distill_workspace(int64_t T, int64_t V, int64_t D, int64_t K, 
  *   gamma, beta : DEVICE, N, `w_dtype`: `dtype` or SP_FP32; NULL: ones, zeros.
  *   mean, rstd  : DEVICE, M fp32 (the gradient call reads them), or NULL: not wanted.
  * y, mean and rstd must not overlap anything else of the call.  N up to SP_LAYERNORM_MAX_N, M below 2^31.  A row that holds an infinity or a NaN becomes NaN; so does, with eps = 0, a row of
- * equal values.  fp32 has to hold the squares: of values whose differences from the mean pass 1e19 rstd is 0.  Sums are taken in a fixed order: the same bits every time.  Asynchronous on `stream`; allocates and synchronises nothing and can be captured.
+ * equal values.  The sum of a row's squared differences has to be within fp32: beyond 3.4e38 rstd is 0.  Sums are taken in a fixed order: the same bits every time.  Asynchronous on `stream`; allocates and synchronises nothing and can be captured.
  * Errors: SP_ERR_INVALID_ARG (NULL, sizes, eps negative or not finite, overlap), SP_ERR_UNSUPPORTED (types, sizes), SP_ERR_ALIGNMENT (pointers not aligned to
  * their elements), SP_ERR_DEVICE, SP_ERR_CUDA. */
 #define SP_LAYERNORM_MAX_N 32768

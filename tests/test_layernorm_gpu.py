@@ -334,3 +334,11 @@ def test_each_gradient_of_wide_rows_alone_has_the_same_bits(M, N, types):
             for t, w in zip(outs, want):
                 assert t is None or torch.equal(t, w)
     c.check_guards()
+
+
+@pytest.mark.parametrize("N", [64, 1031, 20001])
+def test_squares_beyond_fp32_leave_beta(N):
+    c = Case(3, N, "fp32", "fp32", scale=1e20, shift=0.0)      # some of them beyond 1.9e19, whose square is beyond 3.4e38
+    c.forward()
+    assert (c.rstd == 0).all() and torch.equal(c.y, c.beta.expand(3, -1))
+    c.check_guards()

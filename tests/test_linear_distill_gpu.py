@@ -481,3 +481,17 @@ def test_gradients_of_few_tokens_are_as_good_as_rounded_once(T, V, D, K, dtype):
     for got, want in ((r.dh, dh), (r.dW[listed], dW[listed]), (r.dW[~listed], dW[~listed])):
         once = (want.to(BITS[dtype]).double() - want).norm()
         assert float(once) > 0 and float((got.double() - want).norm() / once) <= 1.02
+
+
+@pytest.mark.parametrize("tau", [sp.DISTILL_MIN_TEMPERATURE, 0.01, 100.0, sp.DISTILL_MAX_TEMPERATURE])
+@pytest.mark.parametrize("T,V,D", [(5, 1000, 112), (150, 3000, 64)])
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+def test_temperatures_from_end_to_end(T, V, D, dtype, tau):
+    # One word per token, so that no q is too small for float64.  Scores of 1e5: p falls below what fp32 and bf16 hold, 2^-126, which is all that is lost of g there, as held, before its factor.
+    h, W, index, top = inputs(T, V, D, 1, dtype)
+    grad = torch.full((T,), (64.0 if dtype == "fp16" else 1.0) / max(tau, 1.0), device="cuda")
+    ref = reference(h, W, index, top, tau, "none", grad, dtype)
+    r = Result(h, W, index, top, tau, "none", grad)
+    check(r, ref, ("lse", "diff", "loss", "dh"))
+    lost = T * 2.0 ** -126 * float(h.abs().max()) * max(1.0, float(grad.max()) * tau)
+    assert ((r.dW.double() - ref[1][4]).abs() <= ref[2][4] + lost).all()
